@@ -131,7 +131,7 @@ def _hold(x):
     amax = g.abs().amax(-1)
     fine = torch.isfinite(g).all(-1)
     some = fine & (amax >= 2.0 ** -100)
-    inv = torch.where(some, 127.0 / amax, torch.zeros_like(amax))
+    inv = torch.where(some, torch.full_like(amax, 127.0) / amax, torch.zeros_like(amax))
     q = torch.where(some[..., None], torch.round(g * inv[..., None]), torch.zeros_like(g)).to(torch.int8)
     scale = torch.where(some, amax / 127.0, torch.where(fine, torch.zeros_like(amax), torch.full_like(amax, math.nan)))
     held = torch.zeros(M, -(-C // 16) * 16, dtype=torch.int8, device=x.device)
