@@ -202,6 +202,82 @@ o1d_status_t o1d_dsc_bwd(const void* x, const void* z, const void* dy, const voi
                          int W, int K, o1d_dtype_t dtype, void* workspace, size_t workspace_bytes, void* stream);
 size_t o1d_dsc_bwd_workspace_bytes(int N, int C, int Cout, int H, int W, int K, o1d_dtype_t dtype);
 
+/* ---- Row operators: what a block of the network computes around the
+ * convolution, on channels-last activations (an N x H x W x C tensor is M = N H W
+ * rows of C features).
+ *
+ * Matrices have M rows; a row's features are contiguous and rows lie `ld`
+ * elements apart (at least the number of features, below 2^21), so that a slice
+ * of a wider tensor can be given.  Weights are dense and, like the biases,
+ * of the activations' dtype.  Any number of features from 1 to 2^20 and any
+ * element-aligned address is accepted.  Sums, statistics and products
+ * accumulate in float32 and are rounded once when stored, except that the weight
+ * gradient of a checkpointed or activated input rounds that input to dtype
+ * first (the matrix cores' operand).  All sums have a fixed order: results are
+ * bitwise reproducible.  Ownership, asynchrony and error rules are those of the
+ * other entry points; no output may overlap an input, another output or the
+ * workspace, measured over the rows' whole reach.  M = 0 is valid: nothing is
+ * launched, except that weight gradients are set to zeros. */
+typedef enum {
+  O1D_ACT_NONE = 0,
+  O1D_ACT_RELU = 1,
+  O1D_ACT_GELU = 2,      /* x Phi(x) */
+  O1D_ACT_GELU_TANH = 3, /* x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2 */
+  O1D_ACT_SILU = 4       /* x / (1 + exp(-x)) */
+} o1d_act_t;
+
+/* 8-bit checkpoints of a matrix of C features: signed char q[M][ldq] with ldq =
+ * C rounded up to 16 (q 16-byte aligned; the padding is zero) and float
+ * scale[M][ceil(C / 64)].  A group of 64 columns of a row shares a scale:
+ *   amax = max |x|, scale = amax / 127, q = rint(x (127 / amax)), which stands for q scale,
+ * an error of at most amax / 254 (and float32 rounding).  A group that holds a
+ * NaN or an infinity gets the scale NaN: all of it reads NaN.  One whose amax is
+ * below 2^-100 gets scale 0. */
+o1d_status_t o1d_pack(const void* x, long long ldx, signed char* q, float* scale, int M, int C, o1d_dtype_t dtype,
+                      void* stream);
+/* y = act(what the checkpoint stands for). */
+o1d_status_t o1d_unpack(const signed char* q, const float* scale, o1d_act_t act, void* y, long long ldy, int M, int C,
+                        o1d_dtype_t dtype, void* stream);
+
+/* Layer norm over a row's features: mean = sum x / C, var = sum (x - mean)^2 / C,
+ * rstd = (var + eps)^-1/2, y = (x - mean) rstd w + b.  mean and rstd (float32, one
+ * per row, for the backward) are written unless both are NULL. */
+o1d_status_t o1d_ln_fwd(const void* x, long long ldx, const void* w, const void* b, void* y, long long ldy, float* mean,
+                        float* rstd, int M, int C, float eps, o1d_dtype_t dtype, void* stream);
+/* Its gradients: with xh = (x - mean) rstd and g = dy w,
+ *   dx = rstd (g - mean(g) - xh mean(g xh)),  dw = sum_rows dy xh,  db = sum_rows dy.
+ * x is a tensor (x, ldx) or a checkpoint (xq, xscale): exactly one of x and xq is not NULL. */
+o1d_status_t o1d_ln_bwd(const void* x, long long ldx, const signed char* xq, const float* xscale, const void* dy,
+                        long long lddy, const float* mean, const float* rstd, const void* w, void* dx, long long lddx,
+                        void* dw, void* db, int M, int C, o1d_dtype_t dtype, void* workspace, size_t workspace_bytes,
+                        void* stream);
+size_t o1d_ln_bwd_workspace_bytes(int M, int C, o1d_dtype_t dtype);
+
+/* h = x W^T + b,  y = act(h) + residual, with x M x I, W [O][I], b [O] (or NULL),
+ * the residual M x O (or NULL).  For the backward h is stored where asked: as a
+ * tensor (pre, or NULL), as a checkpoint (q, scale, or NULL), or both. */
+o1d_status_t o1d_linear_fwd(const void* x, long long ldx, const void* w, const void* b, o1d_act_t act, const void* res,
+                            long long ldres, void* y, long long ldy, void* pre, long long ldpre, signed char* q,
+                            float* scale, int M, int I, int O, o1d_dtype_t dtype, void* stream);
+/* Gradient in the input, carried through the activation that made the input:
+ *   dx = (dy W) act'(pre),  dy M x O, W [O][I], pre and dx M x I.
+ * With O1D_ACT_NONE pre is not read; else it is a tensor (pre, ldpre) or a
+ * checkpoint (preq, prescale), exactly one. */
+o1d_status_t o1d_linear_bwd_input(const void* dy, long long lddy, const void* w, o1d_act_t act, const void* pre,
+                                  long long ldpre, const signed char* preq, const float* prescale, void* dx,
+                                  long long lddx, int M, int I, int O, o1d_dtype_t dtype, void* stream);
+/* Gradients in the weights: dw = dy^T act(x) ([O][I]), db = sum_rows dy ([O], or
+ * NULL).  x is a tensor or a checkpoint, exactly one; act is the activation
+ * between it and the product's input (O1D_ACT_NONE: x is the input). */
+o1d_status_t o1d_linear_bwd_weight(const void* x, long long ldx, const signed char* xq, const float* xscale, o1d_act_t act,
+                                   const void* dy, long long lddy, void* dw, void* db, int M, int I, int O,
+                                   o1d_dtype_t dtype, void* workspace, size_t workspace_bytes, void* stream);
+size_t o1d_linear_bwd_weight_workspace_bytes(int M, int I, int O, o1d_act_t act, int held, o1d_dtype_t dtype);
+/* dh = dy act'(pre), pre a tensor or a checkpoint, exactly one. */
+o1d_status_t o1d_act_bwd(const void* pre, long long ldpre, const signed char* preq, const float* prescale, o1d_act_t act,
+                         const void* dy, long long lddy, void* dh, long long lddh, int M, int C, o1d_dtype_t dtype,
+                         void* stream);
+
 /* ---- Planning introspection (host only, no device work; for tests and tools).
  *
  * o1d_kernel_name: the kernel(s) a call with these arguments would launch,

@@ -14,11 +14,14 @@ LIB_PATH = os.path.join(PKG, "libo1d.so")
 O1D_F32, O1D_BF16 = 0, 1
 O1D_NCHW, O1D_NHWC = 0, 1
 O1D_FLOOR, O1D_BILINEAR = 0, 1
+ACT = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+GROUP = 64  # columns that share a scale in an 8-bit checkpoint
 STATUS = {0: "O1D_OK", 1: "O1D_ERR_INVALID", 2: "O1D_ERR_UNSUPPORTED", 3: "O1D_ERR_WORKSPACE", 4: "O1D_ERR_HIP"}
 MAX_K = 127
 
 # name -> (restype, argtypes), mirroring include/o1d.h
 _vp, _i, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+_ll, _f = ctypes.c_longlong, ctypes.c_float
 SIGNATURES = {
     "o1d_fwd": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp]),
     "o1d_bwd_input": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp]),
@@ -33,6 +36,16 @@ SIGNATURES = {
     "o1d_dsc_fwd": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp]),
     "o1d_dsc_bwd": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp, _sz, _vp]),
     "o1d_dsc_bwd_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i, _i]),
+    "o1d_pack": (_i, [_vp, _ll, _vp, _vp, _i, _i, _i, _vp]),
+    "o1d_unpack": (_i, [_vp, _vp, _i, _vp, _ll, _i, _i, _i, _vp]),
+    "o1d_ln_fwd": (_i, [_vp, _ll, _vp, _vp, _vp, _ll, _vp, _vp, _i, _i, _f, _i, _vp]),
+    "o1d_ln_bwd": (_i, [_vp, _ll, _vp, _vp, _vp, _ll, _vp, _vp, _vp, _vp, _ll, _vp, _vp, _i, _i, _i, _vp, _sz, _vp]),
+    "o1d_ln_bwd_workspace_bytes": (_sz, [_i, _i, _i]),
+    "o1d_linear_fwd": (_i, [_vp, _ll, _vp, _vp, _i, _vp, _ll, _vp, _ll, _vp, _ll, _vp, _vp, _i, _i, _i, _i, _vp]),
+    "o1d_linear_bwd_input": (_i, [_vp, _ll, _vp, _i, _vp, _ll, _vp, _vp, _vp, _ll, _i, _i, _i, _i, _vp]),
+    "o1d_linear_bwd_weight": (_i, [_vp, _ll, _vp, _vp, _i, _vp, _ll, _vp, _vp, _i, _i, _i, _i, _vp, _sz, _vp]),
+    "o1d_linear_bwd_weight_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
+    "o1d_act_bwd": (_i, [_vp, _ll, _vp, _vp, _i, _vp, _ll, _vp, _ll, _i, _i, _i, _vp]),
     "o1d_kernel_name": (ctypes.c_char_p, [_i, _i, _i, _i, _i, _i, _i, _i, _i, _i, _i]),
     "o1d_kernel_variant": (ctypes.c_char_p, [_i]),
     "o1d_status_str": (ctypes.c_char_p, [_i]),

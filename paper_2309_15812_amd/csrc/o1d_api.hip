@@ -32,6 +32,7 @@
 #include "o1d_launch.h"
 #include "o1d_plane.h"
 #include "o1d_pw.h"
+#include "o1d_status.h"
 #include "o1d_strip.h"
 #include "o1d_walk.h"
 
@@ -39,6 +40,10 @@ namespace {
 
 thread_local char g_last_error[512] = "";
 thread_local char g_name[256] = "";
+
+}  // namespace
+
+namespace o1d {
 
 o1d_status_t fail(o1d_status_t st, const char* fmt, ...) {
   va_list ap;
@@ -53,13 +58,16 @@ o1d_status_t ok() {
   return O1D_OK;
 }
 
-size_t elem_size(o1d_dtype_t dt) { return dt == O1D_BF16 ? 2u : 4u; }
-const char* dt_name(o1d_dtype_t dt) { return dt == O1D_BF16 ? "bf16" : "f32"; }
+}  // namespace o1d
 
-bool overlaps(const void* a, size_t abytes, const void* b, size_t bbytes) {
-  const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
-  return a0 < b0 + bbytes && b0 < a0 + abytes;
-}
+namespace {
+
+using o1d::elem_size;
+using o1d::fail;
+using o1d::ok;
+using o1d::overlaps;
+
+const char* dt_name(o1d_dtype_t dt) { return dt == O1D_BF16 ? "bf16" : "f32"; }
 
 // The options every entry point takes (the plain entry points: stride 1,
 // NCHW, rounding down).

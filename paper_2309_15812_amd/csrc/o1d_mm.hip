@@ -1,0 +1,94 @@
+// Plan of the matrix products of rows, and the sum of the weight gradient's
+// partial results.
+#include <hip/hip_runtime.h>
+
+#include "o1d_device.h"
+#include "o1d_rows.h"
+
+namespace o1d {
+namespace rows {
+
+MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups) {
+  MmPlan pl{};
+  MmParams& p = pl.p;
+  p.M = M;
+  p.N = N;
+  p.K = K;
+  const int bk = kStepBytes / esize;
+  p.steps = (int)cdiv(K, bk);
+  // The shape that computes the least past the output's edge; the small tiles
+  // where the large ones would leave CUs without work.
+  long long best = -1;
+  for (int s = 0; s < kShapeCount; ++s) {
+    const Shape& sh = kShapes[s];
+    if (groups && sh.t < 2) continue;
+    const int bm = 32 * sh.t * sh.wm, bn = 32 * sh.t * sh.wn;
+    const long long tm = cdiv(M, bm), tn = cdiv(N, bn), tiles = tm * tn;
+    long long cost;
+    if (kind == kWgrad) {
+      cost = tiles * bm * bn * (sh.t == 1 ? 3 : 2) * 64 + tiles * (bm + bn);
+    } else {
+      const long long rounds = cdiv(tiles, 512);
+      cost = rounds * bm * bn * (sh.t == 1 ? 3 : 2) * 64 + (bm + bn);
+    }
+    if (best < 0 || cost < best) {
+      best = cost;
+      pl.shape = s;
+      p.tm = (int)tm;
+      p.tn = (int)tn;
+    }
+  }
+  p.nsplit = 1;
+  p.per = p.steps;
+  if (kind == kWgrad) {
+    const long long tiles = (long long)p.tm * p.tn;
+    const long long want = cdiv(512, tiles), most = p.steps / 4;
+    const long long pieces = want < most ? want : most;
+    p.per = (int)cdiv(p.steps, pieces > 1 ? pieces : 1);
+    p.nsplit = (int)cdiv(p.steps, p.per);
+  }
+  p.nblocks = p.tm * p.tn * p.nsplit;
+  return pl;
+}
+
+namespace {
+
+// Four outputs per thread where the partial rows allow it would not matter:
+// the loads of sixteen pieces are in flight together.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void mm_sum(const float* __restrict__ part, int pieces, long long MN, int M,
+                                                   T* __restrict__ dw, T* __restrict__ db) {
+  const long long width = MN + M;
+  const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= (db ? width : MN)) return;
+  constexpr int kBatch = 16;
+  float s = 0.f;
+  for (int j0 = 0; j0 < pieces; j0 += kBatch) {
+    float v[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) v[u] = j0 + u < pieces ? part[(long long)(j0 + u) * width + i] : 0.f;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) s += v[u];
+  }
+  if (i < MN)
+    dw[i] = from_f32<T>(s);
+  else
+    db[i - MN] = from_f32<T>(s);
+}
+
+}  // namespace
+
+hipError_t launch_mm_sum(Dtype dt, const MmPlan& pl, void* dw, void* db, hipStream_t stream) {
+  const long long MN = (long long)pl.p.M * pl.p.N, width = MN + (db ? pl.p.M : 0);
+  const dim3 grid((unsigned)cdiv(width, kThreads)), block(kThreads);
+  if (dt == Dtype::F32)
+    hipLaunchKernelGGL(mm_sum<float>, grid, block, 0, stream, pl.p.part, pl.p.nsplit, MN, pl.p.M, static_cast<float*>(dw),
+                       static_cast<float*>(db));
+  else
+    hipLaunchKernelGGL(mm_sum<uint16_t>, grid, block, 0, stream, pl.p.part, pl.p.nsplit, MN, pl.p.M,
+                       static_cast<uint16_t*>(dw), static_cast<uint16_t*>(db));
+  return hipGetLastError();
+}
+
+}  // namespace rows
+}  // namespace o1d

@@ -1,0 +1,10 @@
+// Matrix products of rows, float32 storage: dgrad.
+#include "o1d_mm_kernels.h"
+
+namespace o1d {
+namespace rows {
+
+hipError_t launch_mm_dgrad_f32(const MmPlan& pl, hipStream_t stream) { return launch_kind<float, kDgrad>(pl, stream); }
+
+}  // namespace rows
+}  // namespace o1d

@@ -1,0 +1,10 @@
+// Matrix products of rows, bfloat16 storage: fwd.
+#include "o1d_mm_kernels.h"
+
+namespace o1d {
+namespace rows {
+
+hipError_t launch_mm_fwd_bf16(const MmPlan& pl, hipStream_t stream) { return launch_kind<uint16_t, kFwd>(pl, stream); }
+
+}  // namespace rows
+}  // namespace o1d

@@ -1,0 +1,418 @@
+// Matrix products of rows with an epilogue, on the matrix cores (included by
+// o1d_mm_*.hip; the host plan is in o1d_mm.hip).
+//
+//   C[m][n] = sum_k A[m][k] B[n][k]
+//   kFwd    A = x  [m][k], B = W  [n][k]   C = y:  + bias, (saved), activation, + residual
+//   kDgrad  A = dy [m][k], B = W  [k][n]   C = dx: * act'(pre)
+//   kWgrad  A = dy [k][m], B = x  [k][n]   C = dW: float32 partials per piece of k; db = sum_k A
+//
+// A workgroup of four waves (WM x WN of them, each 32 T x 32 T) stages 128
+// bytes of k of its rows in LDS per step; the next step's loads are in flight
+// during a step's products.  An operand that is contiguous along k lies in LDS
+// as rows of k (144 bytes apart: 16-byte accesses without conflicts), one
+// that is contiguous along its rows as it is in memory; from the latter float32
+// fragments are read as single words and bfloat16 ones with the transposing
+// 8-byte read.  float32 multiplies on v_mfma_f32_32x32x2_f32, bfloat16 on
+// v_mfma_f32_32x32x16_bf16; both accumulate in float32.
+//
+// B's fragment is the instruction's first operand, so that a lane holds four
+// consecutive columns n of one row m.  They pass through LDS (a region per
+// wave) and the epilogue runs on eight consecutive columns per lane: all its
+// accesses are 16-byte ones along rows, and eight lanes have the 64 columns
+// that share a scale in an 8-bit checkpoint.
+//
+// Widths need not be multiples of anything: a 16-byte run past a row's end is
+// loaded from the row's last 16 bytes and moved to its place, k past the end is
+// cleared in both operands (so that no infinity or NaN of a repeated element
+// meets a zero), and rows past the end repeat the last row and are not stored.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <atomic>
+
+#include "o1d_rows.h"
+#include "o1d_rows_device.h"
+
+namespace o1d {
+namespace rows {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+
+constexpr int kMmThreads = 256;
+constexpr int kPitchK = kStepBytes + 16;  // bytes between LDS rows of k
+
+template <typename T>
+struct Fmt {
+  static constexpr int V = 16 / (int)sizeof(T);
+  static constexpr int BK = kStepBytes / (int)sizeof(T);
+};
+
+// Moves a run down by `shift` elements (0 .. V; zeros come in from above).
+template <typename T>
+__device__ __forceinline__ void move_down(u32x4& w, int shift) {
+  if constexpr (sizeof(T) == 2) {
+    if (shift & 1) {
+      w[0] = (w[0] >> 16) | (w[1] << 16);
+      w[1] = (w[1] >> 16) | (w[2] << 16);
+      w[2] = (w[2] >> 16) | (w[3] << 16);
+      w[3] = w[3] >> 16;
+    }
+  }
+  const int words = shift * (int)sizeof(T) / 4;
+  if (words & 1) w = u32x4{w[1], w[2], w[3], 0u};
+  if (words & 2) w = u32x4{w[2], w[3], 0u, 0u};
+  if (words & 4) w = u32x4{0u, 0u, 0u, 0u};
+}
+
+// One operand's tile: R rows x a step of k.  KC: contiguous along k.
+template <typename T, int R, bool KC>
+struct Tile {
+  static constexpr int V = Fmt<T>::V, BK = Fmt<T>::BK;
+  static constexpr int N = R / 32;                               // runs of a thread
+  static constexpr int kRunsPerRow = R / V;                      // (not KC)
+  static constexpr int kPitch = KC ? kPitchK : R * (int)sizeof(T) + (sizeof(T) == 2 ? 64 : 0);
+  static constexpr int kBytes = KC ? R * kPitchK : BK * kPitch;
+  u32x4 w[N];
+
+  static __device__ __forceinline__ int k_of(int i) { return ((int)threadIdx.x + kMmThreads * i) / kRunsPerRow; }
+  static __device__ __forceinline__ int r_of() { return (int)threadIdx.x % kRunsPerRow * V; }
+
+  // rows r0 .. of `rows`, k from k0 on of K
+  __device__ __forceinline__ void load(const T* p, long long ld, int r0, int rows, int k0, int K) {
+    if constexpr (KC) {
+      const char* base = reinterpret_cast<const char*>(p + (long long)r0 * ld);
+      const int k = k0 + (int)(threadIdx.x % 8) * V;
+      if (K >= V) {
+        const uint32_t from = (uint32_t)min(k, K - V);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const uint32_t r = (uint32_t)min((int)threadIdx.x / 8 + 32 * i, rows - 1 - r0);
+          __builtin_memcpy(&w[i], base + (r * (uint32_t)ld + from) * (uint32_t)sizeof(T), 16);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const uint32_t r = (uint32_t)min((int)threadIdx.x / 8 + 32 * i, rows - 1 - r0);
+          T t[V] = {};
+#pragma unroll
+          for (int e = 0; e < V; ++e)
+            if (k + e < K) t[e] = p[(long long)(r0 + (int)r) * ld + k + e];
+          __builtin_memcpy(&w[i], t, 16);
+        }
+      }
+    } else {
+      const char* base = reinterpret_cast<const char*>(p + (long long)k0 * ld);
+      const int r = r0 + r_of();
+      if (rows >= V) {
+        const uint32_t from = (uint32_t)min(r, rows - V);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const uint32_t k = (uint32_t)min(k_of(i), K - 1 - k0);
+          __builtin_memcpy(&w[i], base + (k * (uint32_t)ld + from) * (uint32_t)sizeof(T), 16);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int k = min(k_of(i), K - 1 - k0);
+          T t[V] = {};
+#pragma unroll
+          for (int e = 0; e < V; ++e)
+            if (r + e < rows) t[e] = p[(long long)(k0 + k) * ld + r + e];
+          __builtin_memcpy(&w[i], t, 16);
+        }
+      }
+    }
+  }
+
+  // Puts runs past the end in their places and clears k past the end.
+  __device__ __forceinline__ void place(int r0, int rows, int k0, int K) {
+    if constexpr (KC) {
+      if (k0 + BK <= K || K < V) return;
+      const int k = k0 + (int)(threadIdx.x % 8) * V, shift = min(V, max(0, k + V - K));
+#pragma unroll
+      for (int i = 0; i < N; ++i) move_down<T>(w[i], shift);
+    } else {
+      if (r0 + R > rows && rows >= V) {
+        const int shift = min(V, max(0, r0 + r_of() + V - rows));
+#pragma unroll
+        for (int i = 0; i < N; ++i) move_down<T>(w[i], shift);
+      }
+      if (k0 + BK > K) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (k0 + k_of(i) >= K) w[i] = u32x4{0u, 0u, 0u, 0u};
+      }
+    }
+  }
+
+  __device__ __forceinline__ void store(char* lds) const {
+    if constexpr (KC) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        *reinterpret_cast<u32x4*>(lds + (threadIdx.x / 8 + 32 * i) * kPitchK + (threadIdx.x % 8) * 16) = w[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        *reinterpret_cast<u32x4*>(lds + k_of(i) * kPitch + r_of() * (int)sizeof(T)) = w[i];
+    }
+  }
+
+  // Fragment j (0 .. 3, a quarter of the step) of the 32 rows from `row` on:
+  // half-wave h has k 4 (2 j + h) + 0 .. 3 (float32) or 8 (2 j + h) + 0 .. 7.
+  static __device__ __forceinline__ u32x4 frag(const char* lds, int row, int j) {
+    const int l = threadIdx.x & 63;
+    if constexpr (KC) {
+      return *reinterpret_cast<const u32x4*>(lds + (row + (l & 31)) * kPitchK + (2 * j + (l >> 5)) * 16);
+    } else if constexpr (sizeof(T) == 4) {
+      const char* at = lds + 4 * (2 * j + (l >> 5)) * kPitch + (row + (l & 31)) * 4;
+      u32x4 f;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) f[s] = *reinterpret_cast<const uint32_t*>(at + s * kPitch);
+      return f;
+    } else {
+      // sixteen lanes read 4 k x 16 rows, four consecutive rows each, and get
+      // one row's four k each
+      const int g = l >> 4, i = l & 15;
+      const char* at = lds + (8 * (2 * j + (g >> 1)) + (i >> 2)) * kPitch + (row + 16 * (g & 1) + 4 * (i & 3)) * 2;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 4 * kPitch));
+      u32x4 f;
+      __builtin_memcpy(&f, &lo, 8);
+      __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
+      return f;
+    }
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void product(const u32x4& n, const u32x4& m, f32x16& acc) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(n[s]), __uint_as_float(m[s]), acc, 0, 0, 0);
+  } else {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, n), __builtin_bit_cast(bf16x8, m), acc, 0, 0,
+                                                  0);
+  }
+}
+
+// Sum of a fragment's elements.
+template <typename T>
+__device__ __forceinline__ float add_frag(const u32x4& f, float s) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      s += __uint_as_float(f[i]);
+    } else {
+      s += __uint_as_float(f[i] << 16);
+      s += __uint_as_float(f[i] & 0xffff0000u);
+    }
+  }
+  return s;
+}
+
+// Eight columns n .. n + 7 of row m.
+template <typename T, int KIND, bool PACK>
+__device__ __forceinline__ void finish(const MmParams& P, int m, int n, float (&v)[8]) {
+  constexpr bool kFast = sizeof(T) == 2;
+  const int left = P.N - n;
+  const bool in = m < P.M && left > 0;
+  if constexpr (KIND == kFwd) {
+    if (in && P.bias) {
+      float b[8];
+      load_some(static_cast<const T*>(P.bias) + n, left, b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += b[e];
+    }
+    if constexpr (PACK) {
+      if (P.q) {  // eight lanes have a group, in range or not
+        float u[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = e < left ? v[e] : 0.f;
+        const Scale s = scale_of(max8(amax_bits(u)));
+        const uint2 w = round8(u, s);
+        if (m < P.M && n < P.ldq) {
+          *reinterpret_cast<uint2*>(P.q + (long long)m * P.ldq + n) = w;
+          if (n % kGroup == 0) P.scale[(long long)m * P.groups + n / kGroup] = s.scale;
+        }
+      }
+    }
+    if (!in) return;
+    if (P.pre) store_some(static_cast<T*>(P.pre) + (long long)m * P.ldpre + n, left, v);
+    act_values<kFast>(v, P.act);
+    if (P.res) {
+      float r[8];
+      load_some(static_cast<const T*>(P.res) + (long long)m * P.ldres + n, left, r);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += r[e];
+    }
+    store_some(static_cast<T*>(P.out) + (long long)m * P.ldo + n, left, v);
+  } else {
+    if (!in) return;
+    if (P.act != kNone) {
+      float x[8];
+      if (P.q)
+        unround8(*reinterpret_cast<const uint2*>(P.q + (long long)m * P.ldq + n),
+                 P.scale[(long long)m * P.groups + n / kGroup], x);
+      else
+        load_some(static_cast<const T*>(P.pre) + (long long)m * P.ldpre + n, left, x);
+      act_slopes<kFast>(v, x, P.act);
+    }
+    store_some(static_cast<T*>(P.out) + (long long)m * P.ldo + n, left, v);
+  }
+}
+
+template <typename T, int KIND, int SHAPE>
+struct Geo {
+  static constexpr Shape S = kShapes[SHAPE];
+  static constexpr int BM = 32 * S.t * S.wm, BN = 32 * S.t * S.wn;
+  using TA = Tile<T, BM, KIND != kWgrad>;
+  using TB = Tile<T, BN, KIND == kFwd>;
+  static constexpr int kOutPitch = 32 * S.t + 4;  // words between rows of a wave's output region
+  static constexpr int kStage = TA::kBytes + TB::kBytes, kOut = 4 * 32 * kOutPitch * 4;
+  static constexpr int kLds = kStage > kOut ? kStage : kOut;
+};
+
+template <typename T, int KIND, int SHAPE>
+__global__ __launch_bounds__(kMmThreads, 2) void mm(MmParams P) {
+  using G = Geo<T, KIND, SHAPE>;
+  constexpr int TT = G::S.t, BK = Fmt<T>::BK;
+  extern __shared__ __align__(16) char lds[];
+  // consecutive tiles, which share rows of A (weight gradient: the piece of
+  // k), on one XCD
+  const int per_xcd = (P.nblocks + 7) / 8, id = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
+  if (id >= P.nblocks) return;
+  const int nt = id % P.tn, rest = id / P.tn, mt = rest % P.tm, split = rest / P.tm;
+  const int m0 = mt * G::BM, n0 = nt * G::BN;
+  const int s0 = split * P.per, s1 = min(P.steps, s0 + P.per);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = wave / G::S.wn * 32 * TT, wn = wave % G::S.wn * 32 * TT;
+  const T *A = static_cast<const T*>(P.a), *B = static_cast<const T*>(P.b);
+  typename G::TA ta;
+  typename G::TB tb;
+  auto load = [&](int s) __attribute__((always_inline)) {
+    ta.load(A, P.lda, m0, P.M, s * BK, P.K);
+    tb.load(B, P.ldb, n0, P.N, s * BK, P.K);
+  };
+  f32x16 acc[TT][TT];
+  float dbs[TT];
+#pragma unroll
+  for (int i = 0; i < TT; ++i) {
+    dbs[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < TT; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  }
+  const bool sum_a = KIND == kWgrad && P.want_db && nt == 0 && wn == 0;
+  load(s0);
+  for (int s = s0; s < s1; ++s) {
+    __syncthreads();  // the previous step's fragments are read
+    ta.place(m0, P.M, s * BK, P.K);
+    tb.place(n0, P.N, s * BK, P.K);
+    ta.store(lds);
+    tb.store(lds + G::TA::kBytes);
+    load(min(s + 1, s1 - 1));
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      u32x4 fm[TT], fn[TT];
+#pragma unroll
+      for (int i = 0; i < TT; ++i) {
+        fm[i] = G::TA::frag(lds, wm + 32 * i, j);
+        fn[i] = G::TB::frag(lds + G::TA::kBytes, wn + 32 * i, j);
+      }
+      if (sum_a) {
+#pragma unroll
+        for (int i = 0; i < TT; ++i) dbs[i] = add_frag<T>(fm[i], dbs[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < TT; ++i)
+#pragma unroll
+        for (int k = 0; k < TT; ++k) product<T>(fn[k], fm[i], acc[i][k]);
+    }
+  }
+  if constexpr (KIND == kWgrad) {
+    if (sum_a) {
+#pragma unroll
+      for (int i = 0; i < TT; ++i) {
+        const float s = dbs[i] + __shfl_xor(dbs[i], 32, 64);
+        const int m = m0 + wm + 32 * i + (lane & 31);
+        if (lane < 32 && m < P.M) P.part[(long long)split * ((long long)P.M * P.N + P.M) + (long long)P.M * P.N + m] = s;
+      }
+    }
+  }
+  // the wave's output, 32 rows at a time through its region of LDS
+  __syncthreads();
+  float* region = reinterpret_cast<float*>(lds) + wave * 32 * G::kOutPitch;
+  constexpr int kLanes = 4 * TT, kRowsPer = 64 / kLanes;  // lanes of a row, rows at a time
+#pragma unroll
+  for (int i = 0; i < TT; ++i) {
+#pragma unroll
+    for (int k = 0; k < TT; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][k][4 * j + e];
+        *reinterpret_cast<f32x4*>(region + (lane & 31) * G::kOutPitch + 32 * k + 8 * j + 4 * (lane >> 5)) = v;
+      }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int r = 0; r < 32; r += kRowsPer) {
+      const int row = r + lane / kLanes, col = lane % kLanes * 8;
+      const int m = m0 + wm + 32 * i + row, n = n0 + wn + col;
+      float v[8];
+      __builtin_memcpy(v, region + row * G::kOutPitch + col, 32);
+      if constexpr (KIND == kWgrad) {
+        if (m < P.M && n < P.N)
+          store_some(P.part + (long long)split * ((long long)P.M * P.N + P.M) + (long long)m * P.N + n, P.N - n, v);
+      } else {
+        finish<T, KIND, TT == 2>(P, m, n, v);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+}
+
+template <typename T, int KIND, int SHAPE>
+hipError_t launch_shape(const MmPlan& pl, hipStream_t stream) {
+  using G = Geo<T, KIND, SHAPE>;
+  static std::atomic<int> allowed{0};
+  if (!allowed.load(std::memory_order_acquire)) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(mm<T, KIND, SHAPE>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, G::kLds);
+    if (e != hipSuccess) return e;
+    allowed.store(1, std::memory_order_release);
+  }
+  hipLaunchKernelGGL((mm<T, KIND, SHAPE>), dim3((unsigned)(pl.p.nblocks + 7) / 8 * 8), dim3(kMmThreads), G::kLds, stream,
+                     pl.p);
+  return hipGetLastError();
+}
+
+template <typename T, int KIND>
+hipError_t launch_kind(const MmPlan& pl, hipStream_t stream) {
+  switch (pl.shape) {
+    case 0: return launch_shape<T, KIND, 0>(pl, stream);
+    case 1: return launch_shape<T, KIND, 1>(pl, stream);
+    case 2: return launch_shape<T, KIND, 2>(pl, stream);
+    default: return launch_shape<T, KIND, 3>(pl, stream);
+  }
+}
+
+}  // namespace
+}  // namespace rows
+}  // namespace o1d

@@ -1,0 +1,136 @@
+// Host-side plans and launchers of the row operators: layer norm, the matrix
+// product with an epilogue and its gradients, and 8-bit checkpoints.  All act on
+// matrices of M rows (pixels or tokens, channels last) whose features are
+// contiguous; rows are `ld` elements apart.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "o1d_launch.h"
+
+namespace o1d {
+namespace rows {
+
+inline long long cdiv(long long a, long long b) { return (a + b - 1) / b; }
+
+// ---- 8-bit checkpoints: groups of 64 columns of a row share a scale; the
+// integers' rows are padded to 16 bytes.
+constexpr int kGroup = 64;
+inline long long held_ld(int C) { return cdiv(C, 16) * 16; }
+inline int held_groups(int C) { return (int)cdiv(C, kGroup); }
+
+struct Held {
+  int8_t* q;
+  float* scale;
+};
+
+// A matrix operand: its elements (rows ld apart), or its 8-bit checkpoint.
+struct Operand {
+  const void* p;
+  long long ld;
+  const int8_t* q;  // not NULL: the checkpoint
+  const float* scale;
+};
+
+enum Act { kNone = 0, kRelu = 1, kGelu = 2, kGeluTanh = 3, kSilu = 4, kActs = 5 };
+
+// ---- layer norm
+
+struct LnParams {
+  int M, C;
+  long long ldx, ldy, lddx;  // ldy: y's (forward) or dy's (backward)
+  float eps;
+  const void *x, *w, *b, *dy;
+  const int8_t* xq;
+  const float* xscale;
+  void *y, *dx;
+  float *mean, *rstd;         // written by the forward, read by the backward
+  float* part;                // backward: partial sums, blocks x 2 x C
+  int blocks;
+};
+
+// Workgroups of the backward, each of which leaves one partial row of dw and db.
+constexpr int kLnMostBlocks = 1024;
+inline int ln_bwd_blocks(int M, int C, int esize) {
+  const long long runs = cdiv(C, 16 / esize);
+  const int lanes = runs <= 16 ? 4 : (runs <= 32 ? 8 : (runs <= 64 ? 16 : (runs <= 128 ? 32 : 64)));
+  const long long blocks = runs > 512 ? (M < 256 ? M : 256) : cdiv(M, 256 / lanes);
+  return (int)(blocks < kLnMostBlocks ? blocks : kLnMostBlocks);
+}
+
+hipError_t launch_ln_fwd_f32(const LnParams& p, hipStream_t stream);
+hipError_t launch_ln_fwd_bf16(const LnParams& p, hipStream_t stream);
+hipError_t launch_ln_bwd_f32(const LnParams& p, hipStream_t stream);
+hipError_t launch_ln_bwd_bf16(const LnParams& p, hipStream_t stream);
+
+// out[c] = sum over j < parts of part[j ld + c], c < C, in a fixed order; two
+// such sums side by side (the second at part + C) where out2 is given.
+hipError_t launch_col_sum(Dtype dt, const float* part, int parts, long long ld, int C, void* out, void* out2,
+                          hipStream_t stream);
+
+// ---- checkpoints
+
+hipError_t launch_pack(Dtype dt, const void* x, long long ldx, int M, int C, const Held& h, hipStream_t stream);
+// y = act(x) (dy NULL) or dy act'(x)
+hipError_t launch_act(Dtype dt, const Operand& x, const void* dy, long long lddy, int M, int C, int act, void* y,
+                      long long ldy, hipStream_t stream);
+
+// ---- products  C[m][n] = sum_k A[m][k] B[n][k]
+//
+//   kFwd    y  = x W^T     m rows of x,  n = output feature, k = input feature
+//   kDgrad  dx = dy W      m rows of dy, n = input feature,  k = output feature
+//   kWgrad  dW = dy^T x    m = output feature, n = input feature, k = row
+enum Kind { kFwd = 0, kDgrad = 1, kWgrad = 2 };
+
+struct MmParams {
+  int M, N, K;
+  const void *a, *b;
+  long long lda, ldb;
+  int tm, tn;           // tiles along m and n
+  int steps, per;       // k steps in all and per piece
+  int nsplit;           // weight gradient: pieces of k
+  int nblocks;
+  // epilogues
+  int act;
+  const void* bias;                     // forward
+  const void* res; long long ldres;     // forward
+  void* out; long long ldo;             // forward, input gradient
+  void* pre; long long ldpre;           // forward: written; input gradient: read
+  int8_t* q; float* scale;              // the same in 8 bits
+  long long ldq; int groups;
+  float* part;                          // weight gradient: nsplit x (M N + M)
+  int want_db;
+};
+
+// Workgroup tiles: waves along m x n, each 32 TM x 32 TN.
+struct Shape {
+  int wm, wn, t;
+};
+
+struct MmPlan {
+  int shape;  // index into kShapes
+  MmParams p;
+};
+
+constexpr Shape kShapes[] = {{2, 2, 2}, {4, 1, 2}, {1, 4, 2}, {2, 2, 1}};
+constexpr int kShapeCount = 4;
+constexpr int kStepBytes = 128;  // k per step: 32 float32 or 64 bfloat16
+
+// `groups`: an 8-bit checkpoint is written (waves with 64 columns).
+MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups = false);
+
+#define O1D_MM_DECL(T)                                                                    \
+  hipError_t launch_mm_fwd_##T(const MmPlan& pl, hipStream_t stream);                     \
+  hipError_t launch_mm_dgrad_##T(const MmPlan& pl, hipStream_t stream);                   \
+  hipError_t launch_mm_wgrad_##T(const MmPlan& pl, hipStream_t stream);
+O1D_MM_DECL(f32)
+O1D_MM_DECL(bf16)
+#undef O1D_MM_DECL
+
+// dw[i] = sum of the pieces' partials (i < M N), db[o] likewise behind them.
+hipError_t launch_mm_sum(Dtype dt, const MmPlan& pl, void* dw, void* db, hipStream_t stream);
+
+}  // namespace rows
+}  // namespace o1d

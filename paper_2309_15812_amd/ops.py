@@ -279,3 +279,242 @@ def dsc_bwd(x: torch.Tensor, z: torch.Tensor, dy: torch.Tensor, w_dw: torch.Tens
                                         dwp.data_ptr(), N, C, Co, H, W, K, _dt(x), workspace.data_ptr(), nbytes,
                                         _stream(x)))
     return dx, dwd, dwp
+
+
+# ---------------------------------------------------------------- row operators (channels last)
+#
+# An activation is any tensor whose last axis holds the features and whose other axes collapse to rows a fixed stride
+# apart: a dense (N, H, W, C) tensor, an (M, C) matrix, or a slice of a wider one.
+
+def _rows(t: torch.Tensor, what: str) -> tuple[torch.Tensor, int, int, int]:
+    """(t as (M, C), M, C, row stride); refuses what the kernels cannot address."""
+    if t.dim() < 1 or t.shape[-1] < 1:
+        raise ValueError(f"{what} must have at least one feature on its last axis, got {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be on the GPU")
+    C = int(t.shape[-1])
+    try:
+        v = t.view(-1, C) if t.numel() else t.reshape(0, C)
+    except RuntimeError:
+        raise ValueError(f"{what} {tuple(t.shape)} with strides {t.stride()} is no matrix of rows") from None
+    M = int(v.shape[0])
+    ld = int(v.stride(0)) if M > 1 else C
+    if (C > 1 and v.stride(1) != 1) or ld < C:
+        raise ValueError(f"{what} {tuple(t.shape)} with strides {t.stride()} needs contiguous features and rows that do "
+                         f"not overlap")
+    return v, M, C, ld
+
+
+def _vector(t: torch.Tensor, what: str, C: int, like: torch.Tensor) -> torch.Tensor:
+    if t.shape != (C,) or t.dtype != like.dtype or t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous ({C},) tensor of {like.dtype} on {like.device}, got "
+                         f"{tuple(t.shape)} {t.dtype} {t.device}")
+    return t
+
+
+def _weight(w: torch.Tensor, like: torch.Tensor) -> tuple[int, int]:
+    if w.dim() != 2 or w.dtype != like.dtype or w.device != like.device or not w.is_contiguous():
+        raise ValueError(f"w must be a contiguous (O, I) tensor of {like.dtype} on {like.device}, got {tuple(w.shape)} "
+                         f"{w.dtype} {w.device}")
+    return int(w.shape[0]), int(w.shape[1])
+
+
+def _act(act: str) -> int:
+    if act not in _lib.ACT:
+        raise ValueError(f"act must be one of {list(_lib.ACT)}, got {act!r}")
+    return _lib.ACT[act]
+
+
+def _same(t: torch.Tensor, what: str, M: int, C: int, like: torch.Tensor) -> tuple[torch.Tensor, int]:
+    """t as rows, checked to be M x C like `like`; (t, row stride)."""
+    if t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{what} must be {like.dtype} on {like.device}, got {t.dtype} on {t.device}")
+    v, m, c, ld = _rows(t, what)
+    if (m, c) != (M, C):
+        raise ValueError(f"{what} has {m} rows of {c} features, expected {M} of {C}")
+    return v, ld
+
+
+class Packed8:
+    """An 8-bit checkpoint of rows of `cols` features: int8 `q` (M, cols rounded up to 16) and float32 `scale`
+    (M, ceil(cols / 64)); group g of a row stands for q[64 g : 64 g + 64] * scale[g]."""
+
+    __slots__ = ("q", "scale", "cols")
+
+    def __init__(self, q: torch.Tensor, scale: torch.Tensor, cols: int):
+        ldq, groups = -(-cols // 16) * 16, -(-cols // _lib.GROUP)
+        if cols < 1 or q.dim() != 2 or q.dtype != torch.int8 or q.shape[1] != ldq or not q.is_contiguous():
+            raise ValueError(f"q must be a contiguous int8 (M, {ldq}) tensor, got {tuple(q.shape)} {q.dtype}")
+        if scale.shape != (q.shape[0], groups) or scale.dtype != torch.float32 or not scale.is_contiguous():
+            raise ValueError(f"scale must be a contiguous float32 ({q.shape[0]}, {groups}) tensor, got "
+                             f"{tuple(scale.shape)} {scale.dtype}")
+        if not q.is_cuda or q.device != scale.device:
+            raise ValueError("a checkpoint's tensors must be on one GPU")
+        self.q, self.scale, self.cols = q, scale, cols
+
+    @staticmethod
+    def empty(M: int, cols: int, device) -> "Packed8":
+        return Packed8(torch.empty(M, -(-cols // 16) * 16, dtype=torch.int8, device=device),
+                       torch.empty(M, -(-cols // _lib.GROUP), dtype=torch.float32, device=device), cols)
+
+    @property
+    def rows(self) -> int:
+        return int(self.q.shape[0])
+
+    @property
+    def nbytes(self) -> int:
+        return self.q.numel() + 4 * self.scale.numel()
+
+
+def _either(t, what: str, M: int, C: int, like: torch.Tensor) -> tuple:
+    """(pointer, row stride, q, scale) of a tensor or a checkpoint of M rows of C features."""
+    if isinstance(t, Packed8):
+        if (t.rows, t.cols) != (M, C) or t.q.device != like.device:
+            raise ValueError(f"{what} is a checkpoint of {t.rows} rows of {t.cols} features on {t.q.device}, expected "
+                             f"{M} of {C} on {like.device}")
+        return None, C, t.q.data_ptr(), t.scale.data_ptr()
+    v, ld = _same(t, what, M, C, like)
+    return v.data_ptr(), ld, None, None
+
+
+def _into(out: torch.Tensor | None, like: torch.Tensor, C: int) -> torch.Tensor:
+    """Output with like's leading axes and C features."""
+    return _out(out, like, (*like.shape[:-1], C))
+
+
+def pack8(x: torch.Tensor) -> Packed8:
+    """The 8-bit checkpoint of x's rows."""
+    dt = _dt(x)
+    v, M, C, ld = _rows(x, "x")
+    held = Packed8.empty(M, C, x.device)
+    _lib.check("o1d_pack", _lib.call("o1d_pack", v.data_ptr(), ld, held.q.data_ptr(), held.scale.data_ptr(), M, C, dt,
+                                     _stream(x)))
+    return held
+
+
+def unpack8(held: Packed8, dtype: torch.dtype, act: str = "none", out: torch.Tensor | None = None) -> torch.Tensor:
+    """act(what a checkpoint stands for), as (M, cols) of dtype."""
+    if dtype not in _DT:
+        raise TypeError(f"unsupported dtype {dtype}; use float32 or bfloat16")
+    y = torch.empty(held.rows, held.cols, dtype=dtype, device=held.q.device) if out is None else out
+    v, ld = _same(y, "out", held.rows, held.cols, y)
+    if y.dtype != dtype or y.device != held.q.device:
+        raise ValueError(f"out must be {dtype} on {held.q.device}")
+    _lib.check("o1d_unpack", _lib.call("o1d_unpack", held.q.data_ptr(), held.scale.data_ptr(), _act(act), v.data_ptr(),
+                                       ld, held.rows, held.cols, _DT[dtype], _stream(held.q)))
+    return y
+
+
+def ln_fwd(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor, eps: float = 1e-6, out: torch.Tensor | None = None
+           ) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(y, mean, rstd): layer norm over the last axis; mean and rstd (M,) float32 are for ln_bwd."""
+    dt = _dt(x)
+    v, M, C, ld = _rows(x, "x")
+    _vector(w, "w", C, x)
+    _vector(b, "b", C, x)
+    y = _into(out, x, C)
+    stats = torch.empty(2, M, dtype=torch.float32, device=x.device)
+    _lib.check("o1d_ln_fwd", _lib.call("o1d_ln_fwd", v.data_ptr(), ld, w.data_ptr(), b.data_ptr(), y.data_ptr(), C,
+                                       stats[0].data_ptr(), stats[1].data_ptr(), M, C, eps, dt, _stream(x)))
+    return y, stats[0], stats[1]
+
+
+def ln_workspace_bytes(M: int, C: int, dtype: torch.dtype) -> int:
+    return int(_lib.lib().o1d_ln_bwd_workspace_bytes(M, C, _DT[dtype]))
+
+
+def ln_bwd(x: torch.Tensor | Packed8, dy: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, w: torch.Tensor,
+           out: tuple[torch.Tensor, torch.Tensor, torch.Tensor] | None = None,
+           workspace: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(dx, dw, db) of ln_fwd given its input (or the input's checkpoint), dy and its mean and rstd."""
+    dt = _dt(dy)
+    g, M, C, lddy = _rows(dy, "dy")
+    px, ldx, q, scale = _either(x, "x", M, C, dy)
+    _vector(w, "w", C, dy)
+    for t, n in ((mean, "mean"), (rstd, "rstd")):
+        if t.shape != (M,) or t.dtype != torch.float32 or t.device != dy.device or not t.is_contiguous():
+            raise ValueError(f"{n} must be a contiguous float32 ({M},) tensor on {dy.device}")
+    dx, dw, db = (None, None, None) if out is None else out
+    dx, dw, db = _into(dx, dy, C), _out(dw, w), _out(db, w)
+    workspace, nbytes = _workspace(workspace, dy, ln_workspace_bytes(M, C, dy.dtype))
+    _lib.check("o1d_ln_bwd", _lib.call("o1d_ln_bwd", px, ldx, q, scale, g.data_ptr(), lddy, mean.data_ptr(),
+                                       rstd.data_ptr(), w.data_ptr(), dx.data_ptr(), C, dw.data_ptr(), db.data_ptr(), M,
+                                       C, dt, workspace.data_ptr(), nbytes, _stream(dy)))
+    return dx, dw, db
+
+
+def linear_fwd(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor | None = None, act: str = "none",
+               residual: torch.Tensor | None = None, save: str | None = None, out: torch.Tensor | None = None):
+    """y = act(x w^T + b) + residual for w (O, I).  save="pre" returns (y, pre) with the pre-activation x w^T + b as a
+    tensor, save="pack8" returns (y, its checkpoint)."""
+    if save not in (None, "pre", "pack8"):
+        raise ValueError(f"save must be None, 'pre' or 'pack8', got {save!r}")
+    dt, a = _dt(x), _act(act)
+    v, M, I, ldx = _rows(x, "x")
+    O, wi = _weight(w, x)
+    if wi != I:
+        raise ValueError(f"w {tuple(w.shape)} does not take {I} features")
+    if b is not None:
+        _vector(b, "b", O, x)
+    res, ldres = (None, O) if residual is None else _same(residual, "residual", M, O, x)
+    y = _into(out, x, O)
+    pre = _into(None, x, O) if save == "pre" else None
+    held = Packed8.empty(M, O, x.device) if save == "pack8" else None
+    _lib.check("o1d_linear_fwd", _lib.call(
+        "o1d_linear_fwd", v.data_ptr(), ldx, w.data_ptr(), None if b is None else b.data_ptr(), a,
+        None if res is None else res.data_ptr(), ldres, y.data_ptr(), O, None if pre is None else pre.data_ptr(), O,
+        None if held is None else held.q.data_ptr(), None if held is None else held.scale.data_ptr(), M, I, O, dt,
+        _stream(x)))
+    return y if save is None else (y, pre if held is None else held)
+
+
+def linear_bwd_input(dy: torch.Tensor, w: torch.Tensor, pre: torch.Tensor | Packed8 | None = None, act: str = "none",
+                     out: torch.Tensor | None = None) -> torch.Tensor:
+    """dx = (dy w) act'(pre): the gradient in a product's input, carried through the activation that made it
+    (pre: that activation's argument, a tensor or a checkpoint)."""
+    dt, a = _dt(dy), _act(act)
+    g, M, O, lddy = _rows(dy, "dy")
+    wo, I = _weight(w, dy)
+    if wo != O:
+        raise ValueError(f"w {tuple(w.shape)} does not give {O} features")
+    if (pre is None) != (act == "none"):
+        raise ValueError("pre and act are given together")
+    p, ldp, q, scale = (None, I, None, None) if pre is None else _either(pre, "pre", M, I, dy)
+    dx = _into(out, dy, I)
+    _lib.check("o1d_linear_bwd_input", _lib.call("o1d_linear_bwd_input", g.data_ptr(), lddy, w.data_ptr(), a, p, ldp, q,
+                                                 scale, dx.data_ptr(), I, M, I, O, dt, _stream(dy)))
+    return dx
+
+
+def linear_workspace_bytes(M: int, I: int, O: int, dtype: torch.dtype, act: str = "none", packed: bool = False) -> int:
+    return int(_lib.lib().o1d_linear_bwd_weight_workspace_bytes(M, I, O, _act(act), int(packed), _DT[dtype]))
+
+
+def linear_bwd_weight(x: torch.Tensor | Packed8, dy: torch.Tensor, act: str = "none", bias: bool = True,
+                      out: tuple[torch.Tensor, torch.Tensor | None] | None = None,
+                      workspace: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor | None]:
+    """(dw, db): dw (O, I) = dy^T act(x), db = dy's sum over rows (None with bias=False).  x is the product's input, or
+    (with act) the pre-activation that it was made from, as a tensor or a checkpoint."""
+    dt, a = _dt(dy), _act(act)
+    g, M, O, lddy = _rows(dy, "dy")
+    I = x.cols if isinstance(x, Packed8) else int(x.shape[-1]) if x.dim() else 0
+    p, ldx, q, scale = _either(x, "x", M, I, dy)
+    dw, db = (None, None) if out is None else out
+    dw = _out(dw, dy, (O, I))
+    db = _out(db, dy, (O,)) if bias else None
+    workspace, nbytes = _workspace(workspace, dy, linear_workspace_bytes(M, I, O, dy.dtype, act, q is not None))
+    _lib.check("o1d_linear_bwd_weight", _lib.call(
+        "o1d_linear_bwd_weight", p, ldx, q, scale, a, g.data_ptr(), lddy, dw.data_ptr(),
+        None if db is None else db.data_ptr(), M, I, O, dt, workspace.data_ptr(), nbytes, _stream(dy)))
+    return dw, db
+
+
+def act_bwd(pre: torch.Tensor | Packed8, dy: torch.Tensor, act: str, out: torch.Tensor | None = None) -> torch.Tensor:
+    """dh = dy act'(pre), pre a tensor or a checkpoint."""
+    dt, a = _dt(dy), _act(act)
+    g, M, C, lddy = _rows(dy, "dy")
+    p, ldp, q, scale = _either(pre, "pre", M, C, dy)
+    dh = _into(out, dy, C)
+    _lib.check("o1d_act_bwd", _lib.call("o1d_act_bwd", p, ldp, q, scale, a, g.data_ptr(), lddy, dh.data_ptr(), C, M, C,
+                                        dt, _stream(dy)))
+    return dh
