@@ -21,15 +21,15 @@ MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups) {
   long long best = -1;
   for (int s = 0; s < kShapeCount; ++s) {
     const Shape& sh = kShapes[s];
-    if (groups && sh.t < 2) continue;
-    const int bm = 32 * sh.t * sh.wm, bn = 32 * sh.t * sh.wn;
+    if (groups && sh.tn % 2) continue;
+    const int bm = 32 * sh.tm * sh.wm, bn = 32 * sh.tn * sh.wn;
     const long long tm = cdiv(M, bm), tn = cdiv(N, bn), tiles = tm * tn;
     long long cost;
     if (kind == kWgrad) {
-      cost = tiles * bm * bn * (sh.t == 1 ? 3 : 2) * 64 + tiles * (bm + bn);
+      cost = tiles * bm * bn * (sh.tm * sh.tn == 1 ? 3 : 2) * 64 + tiles * (bm + bn);
     } else {
       const long long rounds = cdiv(tiles, 512);
-      cost = rounds * bm * bn * (sh.t == 1 ? 3 : 2) * 64 + (bm + bn);
+      cost = rounds * bm * bn * (sh.tm * sh.tn == 1 ? 3 : 2) * 64 + (bm + bn);
     }
     if (best < 0 || cost < best) {
       best = cost;
@@ -52,6 +52,14 @@ MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups) {
 }
 
 namespace {
+
+// Whole 16-byte runs: along k where an operand is contiguous along it, else along its rows.
+bool whole_runs(int kind, const MmParams& p, int esize) {
+  const int v = 16 / esize;
+  auto aligned = [&](const void* t, long long ld) { return (uintptr_t)t % 16 == 0 && ld % v == 0; };
+  const bool a = kind == kWgrad ? p.M % v == 0 : p.K % v == 0, b = kind == kFwd ? p.K % v == 0 : p.N % v == 0;
+  return a && b && aligned(p.a, p.lda) && aligned(p.b, p.ldb);
+}
 
 // Four outputs per thread where the partial rows allow it would not matter:
 // the loads of sixteen pieces are in flight together.
@@ -77,6 +85,18 @@ __global__ __launch_bounds__(kThreads) void mm_sum(const float* __restrict__ par
 }
 
 }  // namespace
+
+hipError_t launch_mm(Dtype dt, int kind, const MmPlan& pl, hipStream_t stream) {
+  if (dt == Dtype::BF16 && whole_runs(kind, pl.p, 2)) {
+    return kind == kFwd ? launch_mmf_fwd_bf16(pl, stream)
+                        : (kind == kDgrad ? launch_mmf_dgrad_bf16(pl, stream) : launch_mmf_wgrad_bf16(pl, stream));
+  }
+  if (dt == Dtype::F32)
+    return kind == kFwd ? launch_mm_fwd_f32(pl, stream)
+                        : (kind == kDgrad ? launch_mm_dgrad_f32(pl, stream) : launch_mm_wgrad_f32(pl, stream));
+  return kind == kFwd ? launch_mm_fwd_bf16(pl, stream)
+                      : (kind == kDgrad ? launch_mm_dgrad_bf16(pl, stream) : launch_mm_wgrad_bf16(pl, stream));
+}
 
 hipError_t launch_mm_sum(Dtype dt, const MmPlan& pl, void* dw, void* db, hipStream_t stream) {
   const long long MN = (long long)pl.p.M * pl.p.N, width = MN + (db ? pl.p.M : 0);

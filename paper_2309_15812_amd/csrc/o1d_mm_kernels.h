@@ -6,7 +6,7 @@
 //   kDgrad  A = dy [m][k], B = W  [k][n]   C = dx: * act'(pre)
 //   kWgrad  A = dy [k][m], B = x  [k][n]   C = dW: float32 partials per piece of k; db = sum_k A
 //
-// A workgroup of four waves (WM x WN of them, each 32 T x 32 T) stages 128
+// A workgroup of four waves (WM x WN of them, each 32 TM x 32 TN) stages 128
 // bytes of k of its rows in LDS per step; the next step's loads are in flight
 // during a step's products.  An operand that is contiguous along k lies in LDS
 // as rows of k (144 bytes apart: 16-byte accesses without conflicts), one
@@ -16,10 +16,12 @@
 // v_mfma_f32_32x32x16_bf16; both accumulate in float32.
 //
 // B's fragment is the instruction's first operand, so that a lane holds four
-// consecutive columns n of one row m.  They pass through LDS (a region per
-// wave) and the epilogue runs on eight consecutive columns per lane: all its
-// accesses are 16-byte ones along rows, and eight lanes have the 64 columns
-// that share a scale in an 8-bit checkpoint.
+// consecutive columns n of one row m, and the other half-wave the next four:
+// one swap between the halves gives every lane runs of eight columns, on which
+// the epilogue works with 16-byte accesses; two lanes have the 64 columns that
+// share a scale in an 8-bit checkpoint.  (Through LDS, with whole lines per
+// store, the epilogue was bound by LDS and the group's maxima: 12544 x 384 -> 1536
+// with GELU and checkpoint 36 us.)
 //
 // Widths need not be multiples of anything: a 16-byte run past a row's end is
 // loaded from the row's last 16 bytes and moved to its place, k past the end is
@@ -40,9 +42,7 @@ namespace rows {
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
@@ -79,12 +79,16 @@ struct Tile {
   static constexpr int V = Fmt<T>::V, BK = Fmt<T>::BK;
   static constexpr int N = R / 32;                               // runs of a thread
   static constexpr int kRunsPerRow = R / V;                      // (not KC)
-  static constexpr int kPitch = KC ? kPitchK : R * (int)sizeof(T) + (sizeof(T) == 2 ? 64 : 0);
+  // (bfloat16: 64 bytes modulo 128 apart, so that the transposing read's four k lie in different banks)
+  static constexpr int kPitch = KC ? kPitchK : R * (int)sizeof(T) + (sizeof(T) == 2 && R * 2 % 128 == 0 ? 64 : 0);
   static constexpr int kBytes = KC ? R * kPitchK : BK * kPitch;
   u32x4 w[N];
 
   static __device__ __forceinline__ int k_of(int i) { return ((int)threadIdx.x + kMmThreads * i) / kRunsPerRow; }
-  static __device__ __forceinline__ int r_of() { return (int)threadIdx.x % kRunsPerRow * V; }
+  static __device__ __forceinline__ int r_of(int i) {
+    if constexpr (kMmThreads % kRunsPerRow == 0) return (int)threadIdx.x % kRunsPerRow * V;
+    return ((int)threadIdx.x + kMmThreads * i) % kRunsPerRow * V;
+  }
 
   // rows r0 .. of `rows`, k from k0 on of K
   __device__ __forceinline__ void load(const T* p, long long ld, int r0, int rows, int k0, int K) {
@@ -111,18 +115,17 @@ struct Tile {
       }
     } else {
       const char* base = reinterpret_cast<const char*>(p + (long long)k0 * ld);
-      const int r = r0 + r_of();
       if (rows >= V) {
-        const uint32_t from = (uint32_t)min(r, rows - V);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
+          const uint32_t from = (uint32_t)min(r0 + r_of(i), rows - V);
           const uint32_t k = (uint32_t)min(k_of(i), K - 1 - k0);
           __builtin_memcpy(&w[i], base + (k * (uint32_t)ld + from) * (uint32_t)sizeof(T), 16);
         }
       } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const int k = min(k_of(i), K - 1 - k0);
+          const int k = min(k_of(i), K - 1 - k0), r = r0 + r_of(i);
           T t[V] = {};
 #pragma unroll
           for (int e = 0; e < V; ++e)
@@ -142,9 +145,8 @@ struct Tile {
       for (int i = 0; i < N; ++i) move_down<T>(w[i], shift);
     } else {
       if (r0 + R > rows && rows >= V) {
-        const int shift = min(V, max(0, r0 + r_of() + V - rows));
 #pragma unroll
-        for (int i = 0; i < N; ++i) move_down<T>(w[i], shift);
+        for (int i = 0; i < N; ++i) move_down<T>(w[i], min(V, max(0, r0 + r_of(i) + V - rows)));
       }
       if (k0 + BK > K) {
 #pragma unroll
@@ -162,7 +164,7 @@ struct Tile {
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i)
-        *reinterpret_cast<u32x4*>(lds + k_of(i) * kPitch + r_of() * (int)sizeof(T)) = w[i];
+        *reinterpret_cast<u32x4*>(lds + k_of(i) * kPitch + r_of(i) * (int)sizeof(T)) = w[i];
     }
   }
 
@@ -220,72 +222,182 @@ __device__ __forceinline__ float add_frag(const u32x4& f, float s) {
   return s;
 }
 
-// Eight columns n .. n + 7 of row m.
-template <typename T, int KIND, bool PACK>
-__device__ __forceinline__ void finish(const MmParams& P, int m, int n, float (&v)[8]) {
-  constexpr bool kFast = sizeof(T) == 2;
-  const int left = P.N - n;
-  const bool in = m < P.M && left > 0;
-  if constexpr (KIND == kFwd) {
-    if (in && P.bias) {
-      float b[8];
-      load_some(static_cast<const T*>(P.bias) + n, left, b);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += b[e];
-    }
-    if constexpr (PACK) {
-      if (P.q) {  // eight lanes have a group, in range or not
-        float u[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = e < left ? v[e] : 0.f;
-        const Scale s = scale_of(max8(amax_bits(u)));
-        const uint2 w = round8(u, s);
-        if (m < P.M && n < P.ldq) {
-          *reinterpret_cast<uint2*>(P.q + (long long)m * P.ldq + n) = w;
-          if (n % kGroup == 0) P.scale[(long long)m * P.groups + n / kGroup] = s.scale;
+// The epilogue of eight columns n .. n + 7 of a row m: what it reads besides the
+// products is loaded ahead of them, for all runs that a lane has in a row
+// (`Ahead`), so that one wait covers them.  WHOLE: the tile lies inside the output.
+template <typename T, int KIND, bool WHOLE>
+struct Ahead {
+  T e[8];      // residual (forward) or pre (input gradient)
+  uint2 q;     // or the latter's checkpoint
+  float scale;
+
+  __device__ __forceinline__ void load(const MmParams& P, int m, int n) {
+    if constexpr (KIND == kFwd) {
+      if (P.res) run(static_cast<const T*>(P.res) + (long long)m * P.ldres + n, P.N - n, m < P.M);
+    } else {
+      if (P.act == kNone) return;
+      if (P.q) {
+        if (WHOLE || (m < P.M && n < P.N)) {
+          q = *reinterpret_cast<const uint2*>(P.q + (long long)m * P.ldq + n);
+          scale = P.scale[(long long)m * P.groups + n / kGroup];
         }
+      } else {
+        run(static_cast<const T*>(P.pre) + (long long)m * P.ldpre + n, P.N - n, m < P.M);
       }
     }
-    if (!in) return;
-    if (P.pre) store_some(static_cast<T*>(P.pre) + (long long)m * P.ldpre + n, left, v);
+  }
+  __device__ __forceinline__ void run(const T* p, int left, bool in) {
+    if (WHOLE || (in && left >= 8)) {
+      __builtin_memcpy(e, p, sizeof(e));
+    } else if (in) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < left) e[k] = p[k];
+    }
+  }
+};
+
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void put(T* p, int left, const float (&v)[8]) {
+  if constexpr (WHOLE)
+    store_run(p, v);
+  else
+    store_some(p, left, v);
+}
+
+template <typename T, int KIND, bool WHOLE>
+__device__ __forceinline__ void finish(const MmParams& P, int m, int n, const Ahead<T, KIND, WHOLE>& a, float (&v)[8]) {
+  constexpr bool kFast = sizeof(T) == 2;
+  const int left = P.N - n;
+  if (!WHOLE && (m >= P.M || left <= 0)) return;
+  if constexpr (KIND == kFwd) {
+    if (P.pre) put<T, WHOLE>(static_cast<T*>(P.pre) + (long long)m * P.ldpre + n, left, v);
     act_values<kFast>(v, P.act);
     if (P.res) {
-      float r[8];
-      load_some(static_cast<const T*>(P.res) + (long long)m * P.ldres + n, left, r);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += r[e];
+      for (int e = 0; e < 8; ++e) v[e] += WHOLE || e < left ? to_f32(a.e[e]) : 0.f;
     }
-    store_some(static_cast<T*>(P.out) + (long long)m * P.ldo + n, left, v);
-  } else {
-    if (!in) return;
+    put<T, WHOLE>(static_cast<T*>(P.out) + (long long)m * P.ldo + n, left, v);
+  } else if constexpr (KIND == kDgrad) {
     if (P.act != kNone) {
       float x[8];
-      if (P.q)
-        unround8(*reinterpret_cast<const uint2*>(P.q + (long long)m * P.ldq + n),
-                 P.scale[(long long)m * P.groups + n / kGroup], x);
-      else
-        load_some(static_cast<const T*>(P.pre) + (long long)m * P.ldpre + n, left, x);
+      if (P.q) {
+        unround8(a.q, a.scale, x);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = WHOLE || e < left ? to_f32(a.e[e]) : 0.f;
+      }
       act_slopes<kFast>(v, x, P.act);
     }
-    store_some(static_cast<T*>(P.out) + (long long)m * P.ldo + n, left, v);
+    put<T, WHOLE>(static_cast<T*>(P.out) + (long long)m * P.ldo + n, left, v);
   }
+}
+
+// a's lanes 32 .. 63 for b's lanes 0 .. 31
+__device__ __forceinline__ void swap_halves(float& a, float& b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  a = __uint_as_float(r[0]);
+  b = __uint_as_float(r[1]);
 }
 
 template <typename T, int KIND, int SHAPE>
 struct Geo {
   static constexpr Shape S = kShapes[SHAPE];
-  static constexpr int BM = 32 * S.t * S.wm, BN = 32 * S.t * S.wn;
+  static constexpr int BM = 32 * S.tm * S.wm, BN = 32 * S.tn * S.wn;
   using TA = Tile<T, BM, KIND != kWgrad>;
   using TB = Tile<T, BN, KIND == kFwd>;
-  static constexpr int kOutPitch = 32 * S.t + 4;  // words between rows of a wave's output region
-  static constexpr int kStage = TA::kBytes + TB::kBytes, kOut = 4 * 32 * kOutPitch * 4;
-  static constexpr int kLds = kStage > kOut ? kStage : kOut;
+  // waves per SIMD that the accumulators leave room for
+  static constexpr int kWaves = S.tm * S.tn <= 1 ? 6 : S.tm * S.tn <= 4 && BM + BN <= 256 ? 3 : 2;
+  static constexpr int kLds = TA::kBytes + TB::kBytes;
 };
 
+// The wave's tile, 32 rows x 32 or (of a 64-column group) 64 columns at a time.
+// first(): called before the first store.
+template <typename T, int KIND, bool WHOLE, int TM, int TN, class F>
+__device__ __forceinline__ void epilogue(const MmParams& P, int m0, int n0, int split, const f32x16 (&acc)[TM][TN],
+                                         F&& first) {
+  constexpr int NB = TN % 2 ? 1 : 2, NR = 2 * NB;  // blocks and (a lane's) runs of eight columns at a time
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+#pragma unroll
+  for (int c = 0; c < TN / NB; ++c) {
+    const int n = n0 + 32 * NB * c + 8 * half;
+    T bias[NR][8];
+    const bool biased = KIND == kFwd && P.bias;
+    if (biased) {
+#pragma unroll
+      for (int q = 0; q < NR; ++q) {
+        const T* p = static_cast<const T*>(P.bias) + n + 16 * q;
+        if (WHOLE || n + 16 * q + 8 <= P.N) {
+          __builtin_memcpy(bias[q], p, sizeof(bias[q]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) bias[q][e] = n + 16 * q + e < P.N ? p[e] : T(0);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int m = m0 + 32 * i + (lane & 31);
+      Ahead<T, KIND, WHOLE> ahead[NR];
+      if constexpr (KIND != kWgrad) {
+#pragma unroll
+        for (int q = 0; q < NR; ++q) ahead[q].load(P, m, n + 16 * q);
+      }
+      float v[NR][8];
+#pragma unroll
+      for (int q = 0; q < NR; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[q][e] = acc[i][NB * c + q / 2][8 * (q % 2) + e];
+          v[q][4 + e] = acc[i][NB * c + q / 2][8 * (q % 2) + 4 + e];
+          swap_halves(v[q][e], v[q][4 + e]);
+        }
+      if (biased) {
+#pragma unroll
+        for (int q = 0; q < NR; ++q)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[q][e] += to_f32(bias[q][e]);
+      }
+      if (c == 0 && i == 0) first();
+      if constexpr (KIND == kFwd && NB == 2) {
+        if (P.q) {  // (all lanes take part, in range or not)
+          uint32_t most = 0;
+          if constexpr (!WHOLE) {
+#pragma unroll
+            for (int q = 0; q < NR; ++q)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[q][e] = n + 16 * q + e < P.N ? v[q][e] : 0.f;
+          }
+#pragma unroll
+          for (int q = 0; q < NR; ++q) most = max(most, amax_bits(v[q]));
+          const auto both = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+          const Scale s = scale_of(max((uint32_t)both[0], (uint32_t)both[1]));
+#pragma unroll
+          for (int q = 0; q < NR; ++q)
+            if (WHOLE || (m < P.M && n + 16 * q < P.ldq))
+              *reinterpret_cast<uint2*>(P.q + (long long)m * P.ldq + n + 16 * q) = round8(v[q], s);
+          if (half == 0 && (WHOLE || (m < P.M && n < P.N))) P.scale[(long long)m * P.groups + n / kGroup] = s.scale;
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < NR; ++q) {
+        if constexpr (KIND == kWgrad) {
+          const int at = n + 16 * q;
+          if (WHOLE || (m < P.M && at < P.N))
+            put<float, WHOLE>(P.part + (long long)split * ((long long)P.M * P.N + P.M) + (long long)m * P.N + at,
+                              P.N - at, v[q]);
+        } else {
+          finish<T, KIND, WHOLE>(P, m, n + 16 * q, ahead[q], v[q]);
+        }
+      }
+    }
+  }
+}
+
 template <typename T, int KIND, int SHAPE>
-__global__ __launch_bounds__(kMmThreads, 2) void mm(MmParams P) {
+__global__ __launch_bounds__(kMmThreads, (Geo<T, KIND, SHAPE>::kWaves)) void mm(MmParams P) {
   using G = Geo<T, KIND, SHAPE>;
-  constexpr int TT = G::S.t, BK = Fmt<T>::BK;
+  constexpr int TM = G::S.tm, TN = G::S.tn, BK = Fmt<T>::BK;
   extern __shared__ __align__(16) char lds[];
   // consecutive tiles, which share rows of A (weight gradient: the piece of
   // k), on one XCD
@@ -295,7 +407,7 @@ __global__ __launch_bounds__(kMmThreads, 2) void mm(MmParams P) {
   const int m0 = mt * G::BM, n0 = nt * G::BN;
   const int s0 = split * P.per, s1 = min(P.steps, s0 + P.per);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wm = wave / G::S.wn * 32 * TT, wn = wave % G::S.wn * 32 * TT;
+  const int wm = wave / G::S.wn * 32 * TM, wn = wave % G::S.wn * 32 * TN;
   const T *A = static_cast<const T*>(P.a), *B = static_cast<const T*>(P.b);
   typename G::TA ta;
   typename G::TB tb;
@@ -303,18 +415,18 @@ __global__ __launch_bounds__(kMmThreads, 2) void mm(MmParams P) {
     ta.load(A, P.lda, m0, P.M, s * BK, P.K);
     tb.load(B, P.ldb, n0, P.N, s * BK, P.K);
   };
-  f32x16 acc[TT][TT];
-  float dbs[TT];
-#pragma unroll
-  for (int i = 0; i < TT; ++i) {
-    dbs[i] = 0.f;
-#pragma unroll
-    for (int j = 0; j < TT; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-  }
-  const bool sum_a = KIND == kWgrad && P.want_db && nt == 0 && wn == 0;
   load(s0);
+  f32x16 acc[TM][TN];
+  float dbs[TM];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) dbs[i] = 0.f;
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int k = 0; k < TN; ++k)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][k][e] = 0.f;
+  const bool sum_a = KIND == kWgrad && P.want_db && nt == 0 && wn == 0;
   for (int s = s0; s < s1; ++s) {
     __syncthreads();  // the previous step's fragments are read
     ta.place(m0, P.M, s * BK, P.K);
@@ -325,67 +437,35 @@ __global__ __launch_bounds__(kMmThreads, 2) void mm(MmParams P) {
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      u32x4 fm[TT], fn[TT];
+      u32x4 fm[TM], fn[TN];
 #pragma unroll
-      for (int i = 0; i < TT; ++i) {
-        fm[i] = G::TA::frag(lds, wm + 32 * i, j);
-        fn[i] = G::TB::frag(lds + G::TA::kBytes, wn + 32 * i, j);
-      }
+      for (int i = 0; i < TM; ++i) fm[i] = G::TA::frag(lds, wm + 32 * i, j);
+#pragma unroll
+      for (int i = 0; i < TN; ++i) fn[i] = G::TB::frag(lds + G::TA::kBytes, wn + 32 * i, j);
       if (sum_a) {
 #pragma unroll
-        for (int i = 0; i < TT; ++i) dbs[i] = add_frag<T>(fm[i], dbs[i]);
+        for (int i = 0; i < TM; ++i) dbs[i] = add_frag<T>(fm[i], dbs[i]);
       }
 #pragma unroll
-      for (int i = 0; i < TT; ++i)
+      for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int k = 0; k < TT; ++k) product<T>(fn[k], fm[i], acc[i][k]);
+        for (int k = 0; k < TN; ++k) product<T>(fn[k], fm[i], acc[i][k]);
     }
   }
   if constexpr (KIND == kWgrad) {
     if (sum_a) {
 #pragma unroll
-      for (int i = 0; i < TT; ++i) {
+      for (int i = 0; i < TM; ++i) {
         const float s = dbs[i] + __shfl_xor(dbs[i], 32, 64);
         const int m = m0 + wm + 32 * i + (lane & 31);
         if (lane < 32 && m < P.M) P.part[(long long)split * ((long long)P.M * P.N + P.M) + (long long)P.M * P.N + m] = s;
       }
     }
   }
-  // the wave's output, 32 rows at a time through its region of LDS
-  __syncthreads();
-  float* region = reinterpret_cast<float*>(lds) + wave * 32 * G::kOutPitch;
-  constexpr int kLanes = 4 * TT, kRowsPer = 64 / kLanes;  // lanes of a row, rows at a time
-#pragma unroll
-  for (int i = 0; i < TT; ++i) {
-#pragma unroll
-    for (int k = 0; k < TT; ++k)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        f32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][k][4 * j + e];
-        *reinterpret_cast<f32x4*>(region + (lane & 31) * G::kOutPitch + 32 * k + 8 * j + 4 * (lane >> 5)) = v;
-      }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll
-    for (int r = 0; r < 32; r += kRowsPer) {
-      const int row = r + lane / kLanes, col = lane % kLanes * 8;
-      const int m = m0 + wm + 32 * i + row, n = n0 + wn + col;
-      float v[8];
-      __builtin_memcpy(v, region + row * G::kOutPitch + col, 32);
-      if constexpr (KIND == kWgrad) {
-        if (m < P.M && n < P.N)
-          store_some(P.part + (long long)split * ((long long)P.M * P.N + P.M) + (long long)m * P.N + n, P.N - n, v);
-      } else {
-        finish<T, KIND, TT == 2>(P, m, n, v);
-      }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  }
+  if (m0 + G::BM <= P.M && n0 + G::BN <= P.N)
+    epilogue<T, KIND, true>(P, m0 + wm, n0 + wn, split, acc, [] {});
+  else
+    epilogue<T, KIND, false>(P, m0 + wm, n0 + wn, split, acc, [] {});
 }
 
 template <typename T, int KIND, int SHAPE>
@@ -409,7 +489,11 @@ hipError_t launch_kind(const MmPlan& pl, hipStream_t stream) {
     case 0: return launch_shape<T, KIND, 0>(pl, stream);
     case 1: return launch_shape<T, KIND, 1>(pl, stream);
     case 2: return launch_shape<T, KIND, 2>(pl, stream);
-    default: return launch_shape<T, KIND, 3>(pl, stream);
+    case 3: return launch_shape<T, KIND, 3>(pl, stream);
+    case 4: return launch_shape<T, KIND, 4>(pl, stream);
+    case 5: return launch_shape<T, KIND, 5>(pl, stream);
+    case 6: return launch_shape<T, KIND, 6>(pl, stream);
+    default: return launch_shape<T, KIND, 7>(pl, stream);
   }
 }
 

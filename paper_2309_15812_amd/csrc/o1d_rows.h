@@ -104,9 +104,9 @@ struct MmParams {
   int want_db;
 };
 
-// Workgroup tiles: waves along m x n, each 32 TM x 32 TN.
+// Workgroup tiles: wm x wn waves, each 32 tm x 32 tn.
 struct Shape {
-  int wm, wn, t;
+  int wm, wn, tm, tn;
 };
 
 struct MmPlan {
@@ -114,8 +114,8 @@ struct MmPlan {
   MmParams p;
 };
 
-constexpr Shape kShapes[] = {{2, 2, 2}, {4, 1, 2}, {1, 4, 2}, {2, 2, 1}};
-constexpr int kShapeCount = 4;
+constexpr Shape kShapes[] = {{2, 2, 2, 2}, {4, 1, 2, 2}, {1, 4, 2, 2}, {2, 2, 1, 1}, {4, 1, 1, 3}, {4, 1, 2, 3}, {2, 2, 1, 2}, {4, 1, 1, 2}};
+constexpr int kShapeCount = 8;
 constexpr int kStepBytes = 128;  // k per step: 32 float32 or 64 bfloat16
 
 // `groups`: an 8-bit checkpoint is written (waves with 64 columns).
@@ -128,6 +128,12 @@ MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups = false);
 O1D_MM_DECL(f32)
 O1D_MM_DECL(bf16)
 #undef O1D_MM_DECL
+hipError_t launch_mmf_fwd_bf16(const MmPlan& pl, hipStream_t stream);
+hipError_t launch_mmf_dgrad_bf16(const MmPlan& pl, hipStream_t stream);
+hipError_t launch_mmf_wgrad_bf16(const MmPlan& pl, hipStream_t stream);
+
+// The product's kernel: of whole aligned runs where the operands have those.
+hipError_t launch_mm(Dtype dt, int kind, const MmPlan& pl, hipStream_t stream);
 
 // dw[i] = sum of the pieces' partials (i < M N), db[o] likewise behind them.
 hipError_t launch_mm_sum(Dtype dt, const MmPlan& pl, void* dw, void* db, hipStream_t stream);

@@ -269,7 +269,7 @@ o1d_status_t o1d_linear_fwd(const void* x, long long ldx, const void* w, const v
   p.ldq = rows::held_ld(O);
   p.groups = rows::held_groups(O);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return hip_status(fn, dtype == O1D_F32 ? rows::launch_mm_fwd_f32(pl, s) : rows::launch_mm_fwd_bf16(pl, s));
+  return hip_status(fn, rows::launch_mm((Dtype)dtype, rows::kFwd, pl, s));
 }
 
 o1d_status_t o1d_linear_bwd_input(const void* dy, long long lddy, const void* w, o1d_act_t act, const void* pre,
@@ -311,7 +311,7 @@ o1d_status_t o1d_linear_bwd_input(const void* dy, long long lddy, const void* w,
   p.ldq = rows::held_ld(I);
   p.groups = rows::held_groups(I);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return hip_status(fn, dtype == O1D_F32 ? rows::launch_mm_dgrad_f32(pl, s) : rows::launch_mm_dgrad_bf16(pl, s));
+  return hip_status(fn, rows::launch_mm((Dtype)dtype, rows::kDgrad, pl, s));
 }
 
 size_t o1d_linear_bwd_weight_workspace_bytes(int M, int I, int O, o1d_act_t act, int held, o1d_dtype_t dtype) {
@@ -366,8 +366,7 @@ o1d_status_t o1d_linear_bwd_weight(const void* x, long long ldx, const signed ch
     p.b = operand;
     p.ldb = space.ldx;
   }
-  O1D_TRY(hip_status(fn, dtype == O1D_F32 ? rows::launch_mm_wgrad_f32(space.plan, s)
-                                          : rows::launch_mm_wgrad_bf16(space.plan, s)));
+  O1D_TRY(hip_status(fn, rows::launch_mm((Dtype)dtype, rows::kWgrad, space.plan, s)));
   return hip_status(fn, rows::launch_mm_sum((Dtype)dtype, space.plan, dw, db, s));
 }
 

@@ -50,34 +50,61 @@ __device__ __forceinline__ void store_some(T* p, int n, const float (&v)[N]) {
   }
 }
 
-// ---- activations.  Fast: for results that are rounded to bfloat16.
+// ---- activations.  FAST: for results that are rounded to bfloat16.
 //
 // gelu(x) = x Phi(x), Phi(x) = (1 + erf(x / sqrt 2)) / 2.  erf: the library's
-// in float32; for bfloat16 results Abramowitz and Stegun 7.1.26, whose error
-// (1.5e-7) is far below their rounding, at a third of the instructions and
-// with the exp(-x^2 / 2) that the derivative needs too.
+// in float32.  For bfloat16 results, whose rounding is four decimal places
+// coarser than either, two formulas of Abramowitz and Stegun: 7.1.28 (error
+// 3e-7, one reciprocal) for the value, 7.1.26 (1.5e-7), which computes the
+// exp(-x^2 / 2) of the derivative on its way, for the slope.  With Q(a) =
+// 1 - Phi(a) for a = |x|, gelu(x) = max(x, 0) - a Q(a): 16 issue slots per value
+// against 40 with the library's function.  The epilogues of the products are bound by these
+// slots: 12544 x 384 -> 1536 with GELU and its checkpoint, 40 -> 31 us.
 template <bool FAST>
 __device__ __forceinline__ float exp_(float x) { return FAST ? __expf(x) : expf(x); }
 template <bool FAST>
 __device__ __forceinline__ float recip(float x) { return FAST ? __builtin_amdgcn_rcpf(x) : 1.f / x; }
 
-// Phi(x) and exp(-x^2 / 2)
+// Q(|x|) by 7.1.28: erf(z) = 1 - 1 / (1 + a1 z + ... + a6 z^6)^16, z = |x| / sqrt 2 taken into the coefficients.
+__device__ __forceinline__ float upper_tail(float x) {
+  constexpr float k = 1.04427378242741384f;  // 2^(1/16): the result's factor 1/2
+  const float a = fabsf(x);
+  float s = fmaf(k * 0.0000430638f * 0.125f, a, k * 0.0002765672f * 0.17677669529663689f);
+  s = fmaf(s, a, k * 0.0001520143f * 0.25f);
+  s = fmaf(s, a, k * 0.0092705272f * 0.35355339059327379f);
+  s = fmaf(s, a, k * 0.0422820123f * 0.5f);
+  s = fmaf(s, a, k * 0.0705230784f * 0.70710678118654752f);
+  s = fmaf(s, a, k);
+  s *= s;
+  s *= s;
+  s *= s;
+  s *= s;
+  return __builtin_amdgcn_rcpf(s);
+}
+
 template <bool FAST>
-__device__ __forceinline__ float normal_cdf(float x, float* density) {
-  const float z = x * 0.70710678118654752f;
+__device__ __forceinline__ float gelu_value(float x) {
+  if constexpr (FAST) return fmaf(-fabsf(x), upper_tail(x), fmaxf(x, 0.f));
+  return x * (0.5f * (1.f + erff(x * 0.70710678118654752f)));
+}
+
+// Phi(x) + x exp(-x^2 / 2) / sqrt(2 pi)
+template <bool FAST>
+__device__ __forceinline__ float gelu_slope(float x) {
+  constexpr float kDensity = 0.39894228040143268f;
   if constexpr (FAST) {
-    const float a = fabsf(z), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.f)), e = __expf(-a * a);
-    float s = fmaf(1.061405429f, t, -1.453152027f);
-    s = fmaf(s, t, 1.421413741f);
-    s = fmaf(s, t, -0.284496736f);
-    s = fmaf(s, t, 0.254829592f);
-    const float half = 0.5f * s * t * e;  // (1 - erf |z|) / 2
-    *density = e;
-    return x < 0.f ? half : 1.f - half;
-  } else {
-    *density = expf(-z * z);
-    return 0.5f * (1.f + erff(z));
+    const float a = fabsf(x), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, a, 1.f));
+    const float e = __builtin_amdgcn_exp2f(x * x * (-0.5f * 1.44269504088896341f));
+    float s = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+    s = fmaf(s, t, 0.5f * 1.421413741f);
+    s = fmaf(s, t, 0.5f * -0.284496736f);
+    s = fmaf(s, t, 0.5f * 0.254829592f);
+    // Q(a) = s t e; the slope is 1 - Q + a e d for x >= 0 and Q - a e d for x < 0
+    const float q = e * fmaf(s, t, -kDensity * a);
+    return x < 0.f ? q : 1.f - q;
   }
+  const float z = x * 0.70710678118654752f;
+  return fmaf(x * kDensity, expf(-z * z), 0.5f * (1.f + erff(z)));
 }
 
 // gelu(x) ~ x sigma(2 u), u = sqrt(2 / pi) (x + 0.044715 x^3)   [(1 + tanh u) / 2 = sigma(2 u)]
@@ -86,10 +113,9 @@ constexpr float kTanhCube = 0.044715f;
 
 template <bool FAST>
 __device__ __forceinline__ float act_value(float x, int act) {
-  float d;
   switch (act) {
     case kRelu: return x < 0.f ? 0.f : x;
-    case kGelu: return x * normal_cdf<FAST>(x, &d);
+    case kGelu: return gelu_value<FAST>(x);
     case kGeluTanh: return x * recip<FAST>(1.f + exp_<FAST>(-kTanhScale * (x + kTanhCube * x * x * x)));
     case kSilu: return x * recip<FAST>(1.f + exp_<FAST>(-x));
     default: return x;
@@ -100,11 +126,7 @@ template <bool FAST>
 __device__ __forceinline__ float act_slope(float x, int act) {
   switch (act) {
     case kRelu: return x <= 0.f ? 0.f : 1.f;
-    case kGelu: {
-      float d;
-      const float phi = normal_cdf<FAST>(x, &d);
-      return fmaf(x * 0.39894228040143268f, d, phi);
-    }
+    case kGelu: return gelu_slope<FAST>(x);
     case kGeluTanh: {
       const float g = recip<FAST>(1.f + exp_<FAST>(-kTanhScale * (x + kTanhCube * x * x * x)));
       return g + x * g * (1.f - g) * kTanhScale * fmaf(3.f * kTanhCube * x, x, 1.f);
@@ -181,17 +203,22 @@ __device__ __forceinline__ Scale scale_of(uint32_t amax_bits) {
   const float amax = __uint_as_float(amax_bits);
   const bool some = amax >= 0x1p-100f && amax_bits < 0x7f800000u;
   s.inv = some ? 127.f / amax : 0.f;
-  s.scale = some ? amax / 127.f : (amax_bits < 0x7f800000u ? 0.f : __uint_as_float(0x7fc00000u));
+  // amax / 127: one correction of the product with the reciprocal rounds it
+  // correctly (checked over all significands)
+  constexpr float kInv = 1.f / 127.f;
+  const float q0 = amax * kInv, q = fmaf(fmaf(-q0, 127.f, amax), kInv, q0);
+  s.scale = some ? q : (amax_bits < 0x7f800000u ? 0.f : __uint_as_float(0x7fc00000u));
   return s;
 }
 
-// |x| as bits: their unsigned order is that of the values, with NaN above infinity above the finite ones.
+// max |x| as bits, a NaN above infinity above the finite values.  (The
+// maximum that passes NaN on is one instruction for two values on gfx950.)
 template <int N>
 __device__ __forceinline__ uint32_t amax_bits(const float (&v)[N]) {
-  uint32_t m = 0;
+  float m = fabsf(v[0]);
 #pragma unroll
-  for (int e = 0; e < N; ++e) m = max(m, __float_as_uint(v[e]) & 0x7fffffffu);
-  return m;
+  for (int e = 1; e < N; ++e) m = __builtin_elementwise_maximum(m, fabsf(v[e]));
+  return __float_as_uint(m) & 0x7fffffffu;
 }
 
 // The largest over eight consecutive lanes (a multiple of eight on), in all of them.
@@ -202,20 +229,31 @@ __device__ __forceinline__ uint32_t max8(uint32_t m) {
   return m;
 }
 
-// Eight integers as two words.  (A group that is not finite has inv 0 and
-// products 0 or NaN: its integers are set to 0.)
+// Eight integers as two words.  Adding 1.5 x 2^23 rounds to the nearest
+// integer, ties to even, and leaves it in the sum's low byte.  (A group that is
+// not finite or is too small has inv 0 and products 0 or NaN: its integers are 0.)
+// The product is rounded before: ties of bfloat16 values depend on it.
 __device__ __forceinline__ uint2 round8(const float (&v)[8], const Scale& s) {
-  uint32_t w[2] = {0u, 0u};
-  if (s.inv != 0.f) {
+#pragma clang fp contract(off)
+  uint32_t b[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e >> 2] |= ((uint32_t)(int)rintf(v[e] * s.inv) & 0xffu) << (8 * (e & 3));
+  for (int e = 0; e < 8; ++e) {
+    const float p = v[e] * s.inv;
+    b[e] = __float_as_uint(p + 12582912.f);
   }
-  return make_uint2(w[0], w[1]);
+  auto four = [&](int e) __attribute__((always_inline)) {
+    const uint32_t lo = __builtin_amdgcn_perm(b[e + 1], b[e], 0x0c0c0400u), hi = __builtin_amdgcn_perm(b[e + 3], b[e + 2], 0x04000c0cu);
+    return s.inv != 0.f ? lo | hi : 0u;
+  };
+  return make_uint2(four(0), four(4));
 }
 
+// q scale: the bytes plus 128 are converted (one instruction each), and
+// (q + 128) scale - 128 scale is rounded once, as q scale is.
 __device__ __forceinline__ void unround8(uint2 w, float scale, float (&v)[8]) {
+  const uint32_t u[2] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u};
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = (float)(int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3))) * scale;
+  for (int e = 0; e < 8; ++e) v[e] = fmaf((float)((u[e >> 2] >> (8 * (e & 3))) & 0xffu), scale, -128.f * scale);
 }
 
 }  // namespace rows
