@@ -12,8 +12,17 @@
 // as rows of k (144 bytes apart: 16-byte accesses without conflicts), one
 // that is contiguous along its rows as it is in memory; from the latter float32
 // fragments are read as single words and bfloat16 ones with the transposing
-// 8-byte read.  float32 multiplies on v_mfma_f32_32x32x2_f32, bfloat16 on
-// v_mfma_f32_32x32x16_bf16; both accumulate in float32.
+// 8-byte read.  Both types multiply on v_mfma_f32_32x32x16_bf16 and accumulate
+// in float32.
+//
+// float32 operands are staged as three bfloat16 pieces, x = x1 + x2 + x3 with
+// x1 the nearest bfloat16 to x, x2 that to x - x1 and x3 the rest: 24 bits, all
+// of a float32's.  x y is summed as x1 y1 + x1 y2 + x2 y1 + x2 y2 + x1 y3 + x3 y1,
+// six exact products; the ones left out are below 2^-25 |x y|, under float32's own
+// rounding (2^-24).  The six take 3/8 of the time of the float32 instruction, and
+// sixteen products enter each rounding of the sum instead of two: measured against
+// 64 bits the results are no further off.  (Values below 2^-110, whose
+// pieces leave bfloat16's range, keep fewer bits.)
 //
 // B's fragment is the instruction's first operand, so that a lane holds four
 // consecutive columns n of one row m, and the other half-wave the next four:
@@ -48,12 +57,65 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 
 constexpr int kMmThreads = 256;
-constexpr int kPitchK = kStepBytes + 16;  // bytes between LDS rows of k
 
 template <typename T>
 struct Fmt {
   static constexpr int V = 16 / (int)sizeof(T);
   static constexpr int BK = kStepBytes / (int)sizeof(T);
+  static constexpr int kPieces = sizeof(T) == 4 ? 3 : 1;  // bfloat16 pieces of an element
+  static constexpr int kFrags = BK / 16;                  // fragments of 16 k in a step
+};
+
+// The three pieces of four float32, two words each.  A value that is not
+// finite is (+-1, 0, itself): only the third piece meets every other operand
+// once (times its first piece, which is 0 only if that operand is), so that the
+// sum is what float32 products give: infinite with its sign, or NaN.
+__device__ __forceinline__ uint32_t pair_bf16(float a, float b) {
+  return (uint32_t)from_f32<uint16_t>(a) | (uint32_t)from_f32<uint16_t>(b) << 16;
+}
+__device__ __forceinline__ void split4(const u32x4& w, uint2 (&p)[3]) {
+  uint32_t words[3][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float a = __uint_as_float(w[2 * i]), b = __uint_as_float(w[2 * i + 1]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      words[k][i] = pair_bf16(a, b);
+      a -= __uint_as_float(words[k][i] << 16);
+      b -= __uint_as_float(words[k][i] & 0xffff0000u);
+    }
+  }
+  const uint32_t most = max(max(w[0] & 0x7fffffffu, w[1] & 0x7fffffffu), max(w[2] & 0x7fffffffu, w[3] & 0x7fffffffu));
+  if (most >= 0x7f7f8000u) {  // not finite, or rounds to infinity
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t bits = w[e];
+      if ((bits & 0x7fffffffu) < 0x7f7f8000u) continue;
+      uint32_t h[3];
+      if ((bits & 0x7fffffffu) >= 0x7f800000u) {
+        h[0] = 0x3f80u | (bits >> 16 & 0x8000u);
+        h[1] = 0u;
+        h[2] = bits >> 16 | ((bits & 0x7fffffffu) > 0x7f800000u ? 0x40u : 0u);
+      } else {
+        float x = __uint_as_float(bits);
+        h[0] = bits >> 16;  // rounded towards zero
+        x -= __uint_as_float(h[0] << 16);
+        h[1] = from_f32<uint16_t>(x);
+        x -= __uint_as_float(h[1] << 16);
+        h[2] = from_f32<uint16_t>(x);
+      }
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        words[k][e / 2] = e % 2 ? (words[k][e / 2] & 0xffffu) | h[k] << 16 : (words[k][e / 2] & 0xffff0000u) | h[k];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) p[k] = make_uint2(words[k][0], words[k][1]);
+}
+
+template <typename T>
+struct Frag {
+  u32x4 p[Fmt<T>::kPieces];
 };
 
 // Moves a run down by `shift` elements (0 .. V; zeros come in from above).
@@ -78,10 +140,14 @@ template <typename T, int R, bool KC>
 struct Tile {
   static constexpr int V = Fmt<T>::V, BK = Fmt<T>::BK;
   static constexpr int N = R / 32;                               // runs of a thread
+  static constexpr int kPieces = Fmt<T>::kPieces;
   static constexpr int kRunsPerRow = R / V;                      // (not KC)
-  // (bfloat16: 64 bytes modulo 128 apart, so that the transposing read's four k lie in different banks)
-  static constexpr int kPitch = KC ? kPitchK : R * (int)sizeof(T) + (sizeof(T) == 2 && R * 2 % 128 == 0 ? 64 : 0);
-  static constexpr int kBytes = KC ? R * kPitchK : BK * kPitch;
+  // LDS, of each piece: KC: rows of k, 16 bytes more apart than they hold (an
+  // odd number of 16 bytes); else rows of R, 64 bytes modulo 128 apart, so that
+  // the transposing read's four k lie in different banks
+  static constexpr int kPitch = KC ? BK * 2 + 16 : R * 2 + (R * 2 % 128 == 0 ? 64 : 0);
+  static constexpr int kPiece = (KC ? R : BK) * kPitch;
+  static constexpr int kBytes = kPieces * kPiece;
   u32x4 w[N];
 
   static __device__ __forceinline__ int k_of(int i) { return ((int)threadIdx.x + kMmThreads * i) / kRunsPerRow; }
@@ -157,66 +223,75 @@ struct Tile {
   }
 
   __device__ __forceinline__ void store(char* lds) const {
-    if constexpr (KC) {
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        *reinterpret_cast<u32x4*>(lds + (threadIdx.x / 8 + 32 * i) * kPitchK + (threadIdx.x % 8) * 16) = w[i];
-    } else {
+    for (int i = 0; i < N; ++i) {
+      char* at = lds + (KC ? ((int)threadIdx.x / 8 + 32 * i) * kPitch + (int)(threadIdx.x % 8) * V * 2
+                           : k_of(i) * kPitch + r_of(i) * 2);
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<u32x4*>(at) = w[i];
+      } else {
+        uint2 p[3];
+        split4(w[i], p);
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        *reinterpret_cast<u32x4*>(lds + k_of(i) * kPitch + r_of(i) * (int)sizeof(T)) = w[i];
+        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(at + k * kPiece) = p[k];
+      }
     }
   }
 
-  // Fragment j (0 .. 3, a quarter of the step) of the 32 rows from `row` on:
-  // half-wave h has k 4 (2 j + h) + 0 .. 3 (float32) or 8 (2 j + h) + 0 .. 7.
-  static __device__ __forceinline__ u32x4 frag(const char* lds, int row, int j) {
+  // Fragment j (16 k of the step) of the 32 rows from `row` on: half-wave h has
+  // k 8 (2 j + h) + 0 .. 7.
+  static __device__ __forceinline__ Frag<T> frag(const char* lds, int row, int j) {
     const int l = threadIdx.x & 63;
-    if constexpr (KC) {
-      return *reinterpret_cast<const u32x4*>(lds + (row + (l & 31)) * kPitchK + (2 * j + (l >> 5)) * 16);
-    } else if constexpr (sizeof(T) == 4) {
-      const char* at = lds + 4 * (2 * j + (l >> 5)) * kPitch + (row + (l & 31)) * 4;
-      u32x4 f;
+    Frag<T> f;
 #pragma unroll
-      for (int s = 0; s < 4; ++s) f[s] = *reinterpret_cast<const uint32_t*>(at + s * kPitch);
-      return f;
-    } else {
-      // sixteen lanes read 4 k x 16 rows, four consecutive rows each, and get
-      // one row's four k each
-      const int g = l >> 4, i = l & 15;
-      const char* at = lds + (8 * (2 * j + (g >> 1)) + (i >> 2)) * kPitch + (row + 16 * (g & 1) + 4 * (i & 3)) * 2;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 4 * kPitch));
-      u32x4 f;
-      __builtin_memcpy(&f, &lo, 8);
-      __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
-      return f;
+    for (int k = 0; k < kPieces; ++k) {
+      if constexpr (KC) {
+        f.p[k] = *reinterpret_cast<const u32x4*>(lds + k * kPiece + (row + (l & 31)) * kPitch + (2 * j + (l >> 5)) * 16);
+      } else {
+        // sixteen lanes read 4 k x 16 rows, four consecutive rows each, and get
+        // one row's four k each
+        const int g = l >> 4, i = l & 15;
+        const char* at =
+            lds + k * kPiece + (8 * (2 * j + (g >> 1)) + (i >> 2)) * kPitch + (row + 16 * (g & 1) + 4 * (i & 3)) * 2;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 4 * kPitch));
+        __builtin_memcpy(&f.p[k], &lo, 8);
+        __builtin_memcpy(reinterpret_cast<char*>(&f.p[k]) + 8, &hi, 8);
+      }
     }
+    return f;
   }
 };
 
 template <typename T>
-__device__ __forceinline__ void product(const u32x4& n, const u32x4& m, f32x16& acc) {
-  if constexpr (sizeof(T) == 4) {
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(n[s]), __uint_as_float(m[s]), acc, 0, 0, 0);
-  } else {
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, n), __builtin_bit_cast(bf16x8, m), acc, 0, 0,
-                                                  0);
+__device__ __forceinline__ void product(const Frag<T>& n, const Frag<T>& m, f32x16& acc) {
+  auto add = [&](int i, int k) __attribute__((always_inline)) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, n.p[i]), __builtin_bit_cast(bf16x8, m.p[k]),
+                                                  acc, 0, 0, 0);
+  };
+  if constexpr (sizeof(T) == 4) {  // the small ones first
+    add(2, 0);
+    add(0, 2);
+    add(1, 1);
+    add(1, 0);
+    add(0, 1);
   }
+  add(0, 0);
 }
 
 // Sum of a fragment's elements.
 template <typename T>
-__device__ __forceinline__ float add_frag(const u32x4& f, float s) {
+__device__ __forceinline__ float add_frag(const Frag<T>& f, float s) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 4) {
-      s += __uint_as_float(f[i]);
+    auto lo = [&](int k) __attribute__((always_inline)) { return __uint_as_float(f.p[k][i] << 16); };
+    auto hi = [&](int k) __attribute__((always_inline)) { return __uint_as_float(f.p[k][i] & 0xffff0000u); };
+    if constexpr (sizeof(T) == 4) {  // (the pieces' sum is the element)
+      s += (lo(0) + lo(1)) + lo(2);
+      s += (hi(0) + hi(1)) + hi(2);
     } else {
-      s += __uint_as_float(f[i] << 16);
-      s += __uint_as_float(f[i] & 0xffff0000u);
+      s += lo(0);
+      s += hi(0);
     }
   }
   return s;
@@ -307,7 +382,7 @@ struct Geo {
   using TA = Tile<T, BM, KIND != kWgrad>;
   using TB = Tile<T, BN, KIND == kFwd>;
   // waves per SIMD that the accumulators leave room for
-  static constexpr int kWaves = S.tm * S.tn <= 1 ? 6 : S.tm * S.tn <= 4 && BM + BN <= 256 ? 3 : 2;
+  static constexpr int kWaves = S.tm * S.tn <= 1 ? 6 : (S.tm * S.tn <= 2 || (S.tm * S.tn <= 4 && BM + BN <= 256 && KIND != kFwd)) && sizeof(T) == 2 ? 3 : 2;
   static constexpr int kLds = TA::kBytes + TB::kBytes;
 };
 
@@ -436,8 +511,8 @@ __global__ __launch_bounds__(kMmThreads, (Geo<T, KIND, SHAPE>::kWaves)) void mm(
     load(min(s + 1, s1 - 1));
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      u32x4 fm[TM], fn[TN];
+    for (int j = 0; j < Fmt<T>::kFrags; ++j) {
+      Frag<T> fm[TM], fn[TN];
 #pragma unroll
       for (int i = 0; i < TM; ++i) fm[i] = G::TA::frag(lds, wm + 32 * i, j);
 #pragma unroll

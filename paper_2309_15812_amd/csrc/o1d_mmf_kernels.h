@@ -56,7 +56,7 @@ struct FastTile {
     // LDS has 64 banks: sixteen 16-byte reads (KC: of consecutive rows) or 32
     // 8-byte ones (the transposing reads: two 32-byte pieces of four k) at a time
     if constexpr (KC) return slot ^ ((row >> 1) & 7);
-    if constexpr (sizeof(T) == 4 || R % 64 != 0) return slot;  // (rows of 96: 192 bytes apart)
+    if constexpr (R % 64 != 0) return slot;  // (rows of 96: 192 bytes apart)
     if constexpr (R == 64) return slot ^ (2 * (row & 2));
     return slot ^ (4 * (row & 3));
   }
@@ -80,17 +80,12 @@ struct FastTile {
   }
 
   // Fragment j (0 .. 3: a quarter of the step) of the 32 rows from `row` on; k as in Tile::frag.
-  static __device__ __forceinline__ u32x4 frag(const char* lds, int row, int j) {
+  static __device__ __forceinline__ Frag<T> frag(const char* lds, int row, int j) {
+    Frag<T> f;
     const int l = threadIdx.x & 63;
     if constexpr (KC) {
       const int r = row + (l & 31);
-      return *reinterpret_cast<const u32x4*>(lds + r * kFastStep + run_at(r, 2 * j + (l >> 5)) * 16);
-    } else if constexpr (sizeof(T) == 4) {
-      const char* at = lds + (4 * (2 * j + (l >> 5)) * R + row + (l & 31)) * 4;
-      u32x4 f;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) f[s] = *reinterpret_cast<const uint32_t*>(at + s * R * 4);
-      return f;
+      f.p[0] = *reinterpret_cast<const u32x4*>(lds + r * kFastStep + run_at(r, 2 * j + (l >> 5)) * 16);
     } else {
       const int g = l >> 4, i = l & 15;
       const int k = 8 * (2 * j + (g >> 1)) + (i >> 2), r = row + 16 * (g & 1) + 4 * (i & 3);
@@ -98,11 +93,10 @@ struct FastTile {
       const char* at = lds + k * R * 2 + run_at(k, r / 8) * 16 + r % 8 * 2;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at));
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 4 * R * 2));
-      u32x4 f;
-      __builtin_memcpy(&f, &lo, 8);
-      __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
-      return f;
+      __builtin_memcpy(&f.p[0], &lo, 8);
+      __builtin_memcpy(reinterpret_cast<char*>(&f.p[0]) + 8, &hi, 8);
     }
+    return f;
   }
 };
 
@@ -237,7 +231,7 @@ __global__ __launch_bounds__(kMmThreads, (FastGeo<T, KIND, SHAPE>::kWaves)) void
       step_barrier();
       const char *la = lds + stage, *lb = la + G::TA::kBytes;
       stage = stage == (S - 1) * G::kStage ? 0 : stage + G::kStage;
-      u32x4 fm[4][TM], fn[4][TN];
+      Frag<T> fm[4][TM], fn[4][TN];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
 #pragma unroll

@@ -13,7 +13,13 @@ from . import _lib
 _DT = {torch.float32: _lib.O1D_F32, torch.bfloat16: _lib.O1D_BF16}
 
 
+# The current stream's handle without a Stream object around it (2 us less per call), where this torch has that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(t: torch.Tensor) -> int:
+    if _raw_stream is not None:
+        return _raw_stream(t.get_device())
     return torch.cuda.current_stream(t.device).cuda_stream
 
 
@@ -287,18 +293,21 @@ def dsc_bwd(x: torch.Tensor, z: torch.Tensor, dy: torch.Tensor, w_dw: torch.Tens
 # apart: a dense (N, H, W, C) tensor, an (M, C) matrix, or a slice of a wider one.
 
 def _rows(t: torch.Tensor, what: str) -> tuple[torch.Tensor, int, int, int]:
-    """(t as (M, C), M, C, row stride); refuses what the kernels cannot address."""
-    if t.dim() < 1 or t.shape[-1] < 1:
+    """(t or a view of it that starts where it does, rows, features, row stride); refuses what the kernels cannot
+    address."""
+    C = t.shape[-1] if t.dim() else 0
+    if C < 1:
         raise ValueError(f"{what} must have at least one feature on its last axis, got {tuple(t.shape)}")
     if not t.is_cuda:
         raise ValueError(f"{what} must be on the GPU")
-    C = int(t.shape[-1])
+    if t.is_contiguous():
+        return t, t.numel() // C, C, C
     try:
         v = t.view(-1, C) if t.numel() else t.reshape(0, C)
     except RuntimeError:
         raise ValueError(f"{what} {tuple(t.shape)} with strides {t.stride()} is no matrix of rows") from None
-    M = int(v.shape[0])
-    ld = int(v.stride(0)) if M > 1 else C
+    M = v.shape[0]
+    ld = v.stride(0) if M > 1 else C
     if (C > 1 and v.stride(1) != 1) or ld < C:
         raise ValueError(f"{what} {tuple(t.shape)} with strides {t.stride()} needs contiguous features and rows that do "
                          f"not overlap")
@@ -354,8 +363,11 @@ class Packed8:
 
     @staticmethod
     def empty(M: int, cols: int, device) -> "Packed8":
-        return Packed8(torch.empty(M, -(-cols // 16) * 16, dtype=torch.int8, device=device),
-                       torch.empty(M, -(-cols // _lib.GROUP), dtype=torch.float32, device=device), cols)
+        held = object.__new__(Packed8)
+        held.q = torch.empty((M, -(-cols // 16) * 16), dtype=torch.int8, device=device)
+        held.scale = torch.empty((M, -(-cols // _lib.GROUP)), dtype=torch.float32, device=device)
+        held.cols = cols
+        return held
 
     @property
     def rows(self) -> int:
@@ -379,7 +391,12 @@ def _either(t, what: str, M: int, C: int, like: torch.Tensor) -> tuple:
 
 def _into(out: torch.Tensor | None, like: torch.Tensor, C: int) -> torch.Tensor:
     """Output with like's leading axes and C features."""
-    return _out(out, like, (*like.shape[:-1], C))
+    return like.new_empty((*like.shape[:-1], C)) if out is None else _out(out, like, (*like.shape[:-1], C))
+
+
+def _scratch(workspace: torch.Tensor | None, like: torch.Tensor, need: int) -> tuple[torch.Tensor, int]:
+    return (like.new_empty((max(need, 1),), dtype=torch.uint8), need) if workspace is None else \
+        _workspace(workspace, like, need)
 
 
 def pack8(x: torch.Tensor) -> Packed8:
@@ -396,10 +413,14 @@ def unpack8(held: Packed8, dtype: torch.dtype, act: str = "none", out: torch.Ten
     """act(what a checkpoint stands for), as (M, cols) of dtype."""
     if dtype not in _DT:
         raise TypeError(f"unsupported dtype {dtype}; use float32 or bfloat16")
-    y = torch.empty(held.rows, held.cols, dtype=dtype, device=held.q.device) if out is None else out
-    v, ld = _same(y, "out", held.rows, held.cols, y)
-    if y.dtype != dtype or y.device != held.q.device:
-        raise ValueError(f"out must be {dtype} on {held.q.device}")
+    if out is None:
+        y = v = torch.empty((held.rows, held.cols), dtype=dtype, device=held.q.device)
+        ld = held.cols
+    else:
+        if out.dtype != dtype or out.device != held.q.device:
+            raise ValueError(f"out must be {dtype} on {held.q.device}")
+        y = out
+        v, ld = _same(out, "out", held.rows, held.cols, out)
     _lib.check("o1d_unpack", _lib.call("o1d_unpack", held.q.data_ptr(), held.scale.data_ptr(), _act(act), v.data_ptr(),
                                        ld, held.rows, held.cols, _DT[dtype], _stream(held.q)))
     return y
@@ -413,10 +434,10 @@ def ln_fwd(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor, eps: float = 1e-6,
     _vector(w, "w", C, x)
     _vector(b, "b", C, x)
     y = _into(out, x, C)
-    stats = torch.empty(2, M, dtype=torch.float32, device=x.device)
+    mean, rstd = x.new_empty((M,), dtype=torch.float32), x.new_empty((M,), dtype=torch.float32)
     _lib.check("o1d_ln_fwd", _lib.call("o1d_ln_fwd", v.data_ptr(), ld, w.data_ptr(), b.data_ptr(), y.data_ptr(), C,
-                                       stats[0].data_ptr(), stats[1].data_ptr(), M, C, eps, dt, _stream(x)))
-    return y, stats[0], stats[1]
+                                       mean.data_ptr(), rstd.data_ptr(), M, C, eps, dt, _stream(x)))
+    return y, mean, rstd
 
 
 def ln_workspace_bytes(M: int, C: int, dtype: torch.dtype) -> int:
@@ -435,8 +456,9 @@ def ln_bwd(x: torch.Tensor | Packed8, dy: torch.Tensor, mean: torch.Tensor, rstd
         if t.shape != (M,) or t.dtype != torch.float32 or t.device != dy.device or not t.is_contiguous():
             raise ValueError(f"{n} must be a contiguous float32 ({M},) tensor on {dy.device}")
     dx, dw, db = (None, None, None) if out is None else out
-    dx, dw, db = _into(dx, dy, C), _out(dw, w), _out(db, w)
-    workspace, nbytes = _workspace(workspace, dy, ln_workspace_bytes(M, C, dy.dtype))
+    dx = _into(dx, dy, C)
+    dw, db = (torch.empty_like(w) if t is None else _out(t, w) for t in (dw, db))
+    workspace, nbytes = _scratch(workspace, dy, ln_workspace_bytes(M, C, dy.dtype))
     _lib.check("o1d_ln_bwd", _lib.call("o1d_ln_bwd", px, ldx, q, scale, g.data_ptr(), lddy, mean.data_ptr(),
                                        rstd.data_ptr(), w.data_ptr(), dx.data_ptr(), C, dw.data_ptr(), db.data_ptr(), M,
                                        C, dt, workspace.data_ptr(), nbytes, _stream(dy)))
@@ -500,9 +522,9 @@ def linear_bwd_weight(x: torch.Tensor | Packed8, dy: torch.Tensor, act: str = "n
     I = x.cols if isinstance(x, Packed8) else int(x.shape[-1]) if x.dim() else 0
     p, ldx, q, scale = _either(x, "x", M, I, dy)
     dw, db = (None, None) if out is None else out
-    dw = _out(dw, dy, (O, I))
-    db = _out(db, dy, (O,)) if bias else None
-    workspace, nbytes = _workspace(workspace, dy, linear_workspace_bytes(M, I, O, dy.dtype, act, q is not None))
+    dw = dy.new_empty((O, I)) if dw is None else _out(dw, dy, (O, I))
+    db = None if not bias else dy.new_empty((O,)) if db is None else _out(db, dy, (O,))
+    workspace, nbytes = _scratch(workspace, dy, linear_workspace_bytes(M, I, O, dy.dtype, act, q is not None))
     _lib.check("o1d_linear_bwd_weight", _lib.call(
         "o1d_linear_bwd_weight", p, ldx, q, scale, a, g.data_ptr(), lddy, dw.data_ptr(),
         None if db is None else db.data_ptr(), M, I, O, dt, workspace.data_ptr(), nbytes, _stream(dy)))

@@ -496,3 +496,29 @@ def test_wrappers_refuse():
         ops.Packed8(held.q[:, :16], held.scale, 24)
     with pytest.raises(ValueError):
         ops.Packed8(held.q, held.scale.double(), 24)
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+def test_products_of_extreme_values(dt):
+    """Infinities keep their sign, infinity times zero is NaN, and the largest finite values stay finite."""
+    M, I, O = 40, 72, 56
+    x, w = torch.zeros(M, I, device=DEV, dtype=dt), torch.zeros(O, I, device=DEV, dtype=dt)
+    w[:] = torch.where(torch.arange(O, device=DEV)[:, None] % 2 == 0, 1.5, -2.25)
+    w[3] = 0
+    w[5, 7] = math.inf
+    x[0, 7], x[1, 71], x[2, 0] = math.inf, -math.inf, math.nan
+    big = float(torch.finfo(dt).max)
+    x[4, 9], x[6, 9] = big, -big
+    w[8] = 0.25
+    y = ops.linear_fwd(x, w).double()
+    want = x.double()[:, :, None] * w.double().t()[None]
+    want = want.sum(1).clamp(-1e300, 1e300).where(~torch.isinf(want.sum(1)), want.sum(1))
+    top = float(torch.finfo(F32).max)
+    want = torch.where(want.abs() > top, torch.sign(want) * math.inf, want)
+    assert torch.equal(torch.isnan(y), torch.isnan(want))
+    assert torch.equal(torch.where(torch.isinf(y), y, torch.zeros_like(y)).nan_to_num(0),
+                       torch.where(torch.isinf(want), want, torch.zeros_like(want)).nan_to_num(0))
+    assert float(y[4, 8]) == pytest.approx(big / 4, rel=2.0 ** -8) and float(y[6, 8]) == pytest.approx(-big / 4, rel=2.0 ** -8)
+    dw, db = ops.linear_bwd_weight(x, torch.ones(M, O, device=DEV, dtype=dt))
+    assert torch.isnan(dw[:, 0]).all() and (dw[:, 7] == math.inf).all() and (dw[:, 71] == -math.inf).all()
+    assert not dw[:, 9].any() and (db == M).all()
