@@ -8,28 +8,49 @@
 namespace o1d {
 namespace rows {
 
+namespace {
+
+// Time of a product as rounds of resident workgroups, each with a time of its
+// own and a time per step of 128 bytes of k (microseconds, measured over
+// 784 .. 200704 rows and 96 .. 2048 features; they fit within about 15%).
+struct Cost {
+  float first, step;
+  int resident;  // workgroups of a CU
+};
+constexpr Cost kCost[2][kShapeCount] = {
+    // float32: 128 x 128, 64 x 256, 64 x 64, 128 x 96, 64 x 128, 128 x 64
+    {{5.f, 3.0f, 2}, {}, {5.f, 1.9f, 4}, {7.f, 1.9f, 2}, {7.f, 1.9f, 3}, {6.f, 1.9f, 3}},
+    // bfloat16
+    {{3.7f, 0.90f, 2}, {}, {2.3f, 0.45f, 3}, {3.0f, 0.72f, 2}, {3.0f, 0.68f, 3}, {3.0f, 0.68f, 3}}};
+
+// Weight gradients run as many pieces as fill the GPU whatever the tile, so
+// the tile that computes least past the output's edge is taken, weighted by
+// the time of its products (float32: smaller tiles make more pieces per product).
+constexpr float kArea[2][kShapeCount] = {{1.f, 1.02f, 1.5f, 1.15f, 1.3f, 1.3f}, {1.05f, 1.f, 1.3f, 1.35f, 1.f, 1.f}};
+constexpr int kWgradBlocks = 512;
+
+}  // namespace
+
 MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups) {
   MmPlan pl{};
   MmParams& p = pl.p;
   p.M = M;
   p.N = N;
   p.K = K;
-  const int bk = kStepBytes / esize;
-  p.steps = (int)cdiv(K, bk);
-  // The shape that computes the least past the output's edge; the small tiles
-  // where the large ones would leave CUs without work.
-  long long best = -1;
+  p.steps = (int)cdiv(K, kStepBytes / esize);
+  const int type = esize == 2 ? 1 : 0;
+  double best = -1.;
   for (int s = 0; s < kShapeCount; ++s) {
     const Shape& sh = kShapes[s];
-    if (groups && sh.tn % 2) continue;
+    if ((groups && sh.tn % 2) || !shape_used(kind, esize, s)) continue;
     const int bm = 32 * sh.tm * sh.wm, bn = 32 * sh.tn * sh.wn;
     const long long tm = cdiv(M, bm), tn = cdiv(N, bn), tiles = tm * tn;
-    long long cost;
+    double cost;
     if (kind == kWgrad) {
-      cost = tiles * bm * bn * (sh.tm * sh.tn == 1 ? 3 : 2) * 64 + tiles * (bm + bn);
+      cost = (double)tiles * bm * bn * kArea[type][s];
     } else {
-      const long long rounds = cdiv(tiles, 512);
-      cost = rounds * bm * bn * (sh.tm * sh.tn == 1 ? 3 : 2) * 64 + (bm + bn);
+      const Cost& c = kCost[type][s];
+      cost = (double)cdiv(tiles, 256 * c.resident) * (c.first + c.step * p.steps);
     }
     if (best < 0 || cost < best) {
       best = cost;
@@ -41,8 +62,8 @@ MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups) {
   p.nsplit = 1;
   p.per = p.steps;
   if (kind == kWgrad) {
-    const long long tiles = (long long)p.tm * p.tn;
-    const long long want = cdiv(512, tiles), most = p.steps / 4;
+    // pieces of at least four steps
+    const long long want = cdiv(kWgradBlocks, (long long)p.tm * p.tn), most = p.steps / 4;
     const long long pieces = want < most ? want : most;
     p.per = (int)cdiv(p.steps, pieces > 1 ? pieces : 1);
     p.nsplit = (int)cdiv(p.steps, p.per);

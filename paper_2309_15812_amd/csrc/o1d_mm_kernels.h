@@ -73,7 +73,9 @@ struct Fmt {
 __device__ __forceinline__ uint32_t pair_bf16(float a, float b) {
   return (uint32_t)from_f32<uint16_t>(a) | (uint32_t)from_f32<uint16_t>(b) << 16;
 }
-__device__ __forceinline__ void split4(const u32x4& w, uint2 (&p)[3]) {
+// (`odd` becomes NaN where a value is not finite or rounds to infinity: then
+// split_any has to make the pieces.)
+__device__ __forceinline__ void split4(const u32x4& w, uint2 (&p)[3], float& odd) {
   uint32_t words[3][2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -81,33 +83,45 @@ __device__ __forceinline__ void split4(const u32x4& w, uint2 (&p)[3]) {
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
       words[k][i] = pair_bf16(a, b);
+      if (k == 2) break;
       a -= __uint_as_float(words[k][i] << 16);
       b -= __uint_as_float(words[k][i] & 0xffff0000u);
     }
+    odd += a;
+    odd += b;
   }
-  const uint32_t most = max(max(w[0] & 0x7fffffffu, w[1] & 0x7fffffffu), max(w[2] & 0x7fffffffu, w[3] & 0x7fffffffu));
-  if (most >= 0x7f7f8000u) {  // not finite, or rounds to infinity
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t bits = w[e];
-      if ((bits & 0x7fffffffu) < 0x7f7f8000u) continue;
-      uint32_t h[3];
-      if ((bits & 0x7fffffffu) >= 0x7f800000u) {
-        h[0] = 0x3f80u | (bits >> 16 & 0x8000u);
-        h[1] = 0u;
-        h[2] = bits >> 16 | ((bits & 0x7fffffffu) > 0x7f800000u ? 0x40u : 0u);
-      } else {
-        float x = __uint_as_float(bits);
-        h[0] = bits >> 16;  // rounded towards zero
-        x -= __uint_as_float(h[0] << 16);
-        h[1] = from_f32<uint16_t>(x);
-        x -= __uint_as_float(h[1] << 16);
-        h[2] = from_f32<uint16_t>(x);
-      }
+  for (int k = 0; k < 3; ++k) p[k] = make_uint2(words[k][0], words[k][1]);
+}
+__device__ __forceinline__ void split_any(const u32x4& w, uint2 (&p)[3]) {
+  float none = 0.f;
+  split4(w, p, none);
+  uint32_t words[3][2];
 #pragma unroll
-      for (int k = 0; k < 3; ++k)
-        words[k][e / 2] = e % 2 ? (words[k][e / 2] & 0xffffu) | h[k] << 16 : (words[k][e / 2] & 0xffff0000u) | h[k];
+  for (int k = 0; k < 3; ++k) {
+    words[k][0] = p[k].x;
+    words[k][1] = p[k].y;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t bits = w[e];
+    if ((bits & 0x7fffffffu) < 0x7f7f8000u) continue;
+    uint32_t h[3];
+    if ((bits & 0x7fffffffu) >= 0x7f800000u) {
+      h[0] = 0x3f80u | (bits >> 16 & 0x8000u);
+      h[1] = 0u;
+      h[2] = bits >> 16 | ((bits & 0x7fffffffu) > 0x7f800000u ? 0x40u : 0u);
+    } else {
+      float x = __uint_as_float(bits);
+      h[0] = bits >> 16;  // rounded towards zero
+      x -= __uint_as_float(h[0] << 16);
+      h[1] = from_f32<uint16_t>(x);
+      x -= __uint_as_float(h[1] << 16);
+      h[2] = from_f32<uint16_t>(x);
     }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      words[k][e / 2] = e % 2 ? (words[k][e / 2] & 0xffffu) | h[k] << 16 : (words[k][e / 2] & 0xffff0000u) | h[k];
   }
 #pragma unroll
   for (int k = 0; k < 3; ++k) p[k] = make_uint2(words[k][0], words[k][1]);
@@ -222,18 +236,29 @@ struct Tile {
     }
   }
 
+  static __device__ __forceinline__ int place_of(int i) {
+    return KC ? ((int)threadIdx.x / 8 + 32 * i) * kPitch + (int)(threadIdx.x % 8) * V * 2 : k_of(i) * kPitch + r_of(i) * 2;
+  }
   __device__ __forceinline__ void store(char* lds) const {
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      char* at = lds + (KC ? ((int)threadIdx.x / 8 + 32 * i) * kPitch + (int)(threadIdx.x % 8) * V * 2
-                           : k_of(i) * kPitch + r_of(i) * 2);
-      if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<u32x4*>(at) = w[i];
-      } else {
-        uint2 p[3];
-        split4(w[i], p);
+      for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(lds + place_of(i)) = w[i];
+    } else {
+      uint2 p[3];
+      float odd = 0.f;
 #pragma unroll
-        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(at + k * kPiece) = p[k];
+      for (int i = 0; i < N; ++i) {
+        split4(w[i], p, odd);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(lds + place_of(i) + k * kPiece) = p[k];
+      }
+      if (odd != odd) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          split_any(w[i], p);
+#pragma unroll
+          for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(lds + place_of(i) + k * kPiece) = p[k];
+        }
       }
     }
   }
@@ -263,11 +288,17 @@ struct Tile {
   }
 };
 
-template <typename T>
-__device__ __forceinline__ void product(const Frag<T>& n, const Frag<T>& m, f32x16& acc) {
-  auto add = [&](int i, int k) __attribute__((always_inline)) {
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, n.p[i]), __builtin_bit_cast(bf16x8, m.p[k]),
-                                                  acc, 0, 0, 0);
+// acc[i][k] += m fragment i times n fragment k.  (The pieces' products outermost:
+// consecutive instructions have different sums.)
+template <typename T, int TM, int TN>
+__device__ __forceinline__ void products(const Frag<T> (&n)[TN], const Frag<T> (&m)[TM], f32x16 (&acc)[TM][TN]) {
+  auto add = [&](int a, int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int k = 0; k < TN; ++k)
+        acc[i][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, n[k].p[a]),
+                                                            __builtin_bit_cast(bf16x8, m[i].p[b]), acc[i][k], 0, 0, 0);
   };
   if constexpr (sizeof(T) == 4) {  // the small ones first
     add(2, 0);
@@ -382,7 +413,10 @@ struct Geo {
   using TA = Tile<T, BM, KIND != kWgrad>;
   using TB = Tile<T, BN, KIND == kFwd>;
   // waves per SIMD that the accumulators leave room for
-  static constexpr int kWaves = S.tm * S.tn <= 1 ? 6 : (S.tm * S.tn <= 2 || (S.tm * S.tn <= 4 && BM + BN <= 256 && KIND != kFwd)) && sizeof(T) == 2 ? 3 : 2;
+  // Steps whose loads are on their way (each takes a quarter to a half of the
+  // accumulators' registers; where that costs a resident wave, one step).
+  static constexpr int kDepth = SHAPE == k64x64 ? 3 : (SHAPE == k128x128 ? 2 : 1);
+  static constexpr int kWaves = S.tm * S.tn == 1 ? 4 : (S.tm * S.tn <= 2 || (S.tm * S.tn == 3 && sizeof(T) == 2) ? 3 : 2);
   static constexpr int kLds = TA::kBytes + TB::kBytes;
 };
 
@@ -484,13 +518,17 @@ __global__ __launch_bounds__(kMmThreads, (Geo<T, KIND, SHAPE>::kWaves)) void mm(
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave / G::S.wn * 32 * TM, wn = wave % G::S.wn * 32 * TN;
   const T *A = static_cast<const T*>(P.a), *B = static_cast<const T*>(P.b);
-  typename G::TA ta;
-  typename G::TB tb;
-  auto load = [&](int s) __attribute__((always_inline)) {
-    ta.load(A, P.lda, m0, P.M, s * BK, P.K);
-    tb.load(B, P.ldb, n0, P.N, s * BK, P.K);
+  // the loads of the next kDepth steps are on their way
+  constexpr int D = G::kDepth;
+  typename G::TA ta[D];
+  typename G::TB tb[D];
+  auto load = [&](int d, int s) __attribute__((always_inline)) {
+    ta[d].load(A, P.lda, m0, P.M, s * BK, P.K);
+    tb[d].load(B, P.ldb, n0, P.N, s * BK, P.K);
   };
-  load(s0);
+#pragma unroll
+  for (int d = 0; d < D; ++d)
+    if (d == 0 || s0 + d < s1) load(d, s0 + d);
   f32x16 acc[TM][TN];
   float dbs[TM];
 #pragma unroll
@@ -502,29 +540,31 @@ __global__ __launch_bounds__(kMmThreads, (Geo<T, KIND, SHAPE>::kWaves)) void mm(
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][k][e] = 0.f;
   const bool sum_a = KIND == kWgrad && P.want_db && nt == 0 && wn == 0;
-  for (int s = s0; s < s1; ++s) {
-    __syncthreads();  // the previous step's fragments are read
-    ta.place(m0, P.M, s * BK, P.K);
-    tb.place(n0, P.N, s * BK, P.K);
-    ta.store(lds);
-    tb.store(lds + G::TA::kBytes);
-    load(min(s + 1, s1 - 1));
-    __syncthreads();
+  for (int first = s0; first < s1; first += D) {
 #pragma unroll
-    for (int j = 0; j < Fmt<T>::kFrags; ++j) {
-      Frag<T> fm[TM], fn[TN];
+    for (int d = 0; d < D; ++d) {
+      const int s = first + d;
+      if (s >= s1) break;
+      __syncthreads();  // the previous step's fragments are read
+      ta[d].place(m0, P.M, s * BK, P.K);
+      tb[d].place(n0, P.N, s * BK, P.K);
+      ta[d].store(lds);
+      tb[d].store(lds + G::TA::kBytes);
+      if (s + D < s1) load(d, s + D);
+      __syncthreads();
 #pragma unroll
-      for (int i = 0; i < TM; ++i) fm[i] = G::TA::frag(lds, wm + 32 * i, j);
+      for (int j = 0; j < Fmt<T>::kFrags; ++j) {
+        Frag<T> fm[TM], fn[TN];
 #pragma unroll
-      for (int i = 0; i < TN; ++i) fn[i] = G::TB::frag(lds + G::TA::kBytes, wn + 32 * i, j);
-      if (sum_a) {
+        for (int i = 0; i < TM; ++i) fm[i] = G::TA::frag(lds, wm + 32 * i, j);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) dbs[i] = add_frag<T>(fm[i], dbs[i]);
+        for (int i = 0; i < TN; ++i) fn[i] = G::TB::frag(lds + G::TA::kBytes, wn + 32 * i, j);
+        if (sum_a) {
+#pragma unroll
+          for (int i = 0; i < TM; ++i) dbs[i] = add_frag<T>(fm[i], dbs[i]);
+        }
+        products<T>(fn, fm, acc);
       }
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int k = 0; k < TN; ++k) product<T>(fn[k], fm[i], acc[i][k]);
     }
   }
   if constexpr (KIND == kWgrad) {
@@ -561,14 +601,14 @@ hipError_t launch_shape(const MmPlan& pl, hipStream_t stream) {
 template <typename T, int KIND>
 hipError_t launch_kind(const MmPlan& pl, hipStream_t stream) {
   switch (pl.shape) {
-    case 0: return launch_shape<T, KIND, 0>(pl, stream);
-    case 1: return launch_shape<T, KIND, 1>(pl, stream);
-    case 2: return launch_shape<T, KIND, 2>(pl, stream);
-    case 3: return launch_shape<T, KIND, 3>(pl, stream);
-    case 4: return launch_shape<T, KIND, 4>(pl, stream);
-    case 5: return launch_shape<T, KIND, 5>(pl, stream);
-    case 6: return launch_shape<T, KIND, 6>(pl, stream);
-    default: return launch_shape<T, KIND, 7>(pl, stream);
+    case k128x128: return launch_shape<T, KIND, k128x128>(pl, stream);
+    case k64x256:
+      if constexpr (shape_used(KIND, (int)sizeof(T), k64x256)) return launch_shape<T, KIND, k64x256>(pl, stream);
+      return hipErrorInvalidValue;
+    case k64x64: return launch_shape<T, KIND, k64x64>(pl, stream);
+    case k128x96: return launch_shape<T, KIND, k128x96>(pl, stream);
+    case k64x128: return launch_shape<T, KIND, k64x128>(pl, stream);
+    default: return launch_shape<T, KIND, k128x64>(pl, stream);
   }
 }
 

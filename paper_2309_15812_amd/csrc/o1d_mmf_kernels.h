@@ -247,10 +247,7 @@ __global__ __launch_bounds__(kMmThreads, (FastGeo<T, KIND, SHAPE>::kWaves)) void
 #pragma unroll
           for (int i = 0; i < TM; ++i) dbs[i] = add_frag<T>(fm[j][i], dbs[i]);
         }
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-          for (int k = 0; k < TN; ++k) product<T>(fn[j][k], fm[j][i], acc[i][k]);
+        products<T>(fn[j], fm[j], acc);
       }
     };
     // steps whose load ahead is a whole one of this tile, then the others
@@ -304,6 +301,18 @@ hipError_t launch_fast_shape(const MmPlan& pl, hipStream_t stream) {
   hipLaunchKernelGGL((mmf<T, KIND, SHAPE>), dim3((unsigned)(blocks < most ? blocks : most)), dim3(kMmThreads), G::kLds,
                      stream, pl.p);
   return hipGetLastError();
+}
+
+template <typename T, int KIND>
+hipError_t launch_fast_kind(const MmPlan& pl, hipStream_t stream) {
+  switch (pl.shape) {
+    case k128x128: return launch_fast_shape<T, KIND, k128x128>(pl, stream);
+    case k64x64: return launch_fast_shape<T, KIND, k64x64>(pl, stream);
+    case k128x96: return launch_fast_shape<T, KIND, k128x96>(pl, stream);
+    case k64x128: return launch_fast_shape<T, KIND, k64x128>(pl, stream);
+    case k128x64: return launch_fast_shape<T, KIND, k128x64>(pl, stream);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 }  // namespace

@@ -114,8 +114,10 @@ struct MmPlan {
   MmParams p;
 };
 
-constexpr Shape kShapes[] = {{2, 2, 2, 2}, {4, 1, 2, 2}, {1, 4, 2, 2}, {2, 2, 1, 1}, {4, 1, 1, 3}, {4, 1, 2, 3}, {2, 2, 1, 2}, {4, 1, 1, 2}};
-constexpr int kShapeCount = 8;
+enum ShapeId { k128x128, k64x256, k64x64, k128x96, k64x128, k128x64, kShapeCount };
+constexpr Shape kShapes[kShapeCount] = {{2, 2, 2, 2}, {1, 4, 2, 2}, {2, 2, 1, 1}, {4, 1, 1, 3}, {2, 2, 1, 2}, {4, 1, 1, 2}};
+// (64 x 256 is planned for float32 weight gradients alone)
+constexpr bool shape_used(int kind, int esize, int shape) { return shape != k64x256 || (kind == kWgrad && esize == 4); }
 constexpr int kStepBytes = 128;  // k per step: 32 float32 or 64 bfloat16
 
 // `groups`: an 8-bit checkpoint is written (waves with 64 columns).
