@@ -21,7 +21,7 @@ constexpr Cost kCost[2][kShapeCount] = {
     // float32: 128 x 128, 64 x 256, 64 x 64, 128 x 96, 64 x 128, 128 x 64
     {{5.f, 3.0f, 2}, {}, {5.f, 1.9f, 4}, {7.f, 1.9f, 2}, {7.f, 1.9f, 3}, {6.f, 1.9f, 3}},
     // bfloat16
-    {{3.7f, 0.90f, 2}, {}, {2.3f, 0.45f, 3}, {3.0f, 0.72f, 2}, {3.0f, 0.68f, 3}, {3.0f, 0.68f, 3}}};
+    {{3.7f, 0.90f, 2}, {}, {3.3f, 0.45f, 3}, {3.0f, 0.72f, 2}, {3.0f, 0.68f, 3}, {3.0f, 0.68f, 3}}};
 
 // Weight gradients run as many pieces as fill the GPU whatever the tile, so
 // the tile that computes least past the output's edge is taken, weighted by
@@ -29,6 +29,15 @@ constexpr Cost kCost[2][kShapeCount] = {
 constexpr float kArea[2][kShapeCount] = {{1.f, 1.02f, 1.5f, 1.15f, 1.3f, 1.3f}, {1.05f, 1.f, 1.3f, 1.35f, 1.f, 1.f}};
 constexpr int kWgradBlocks = 512;
 
+// Time of the kernels of few rows (microseconds, measured as above for 1 .. 2000
+// rows): the waits of a workgroup's waves for their pieces of 32 k, of which
+// a launch that fills the GPU once hides none, and the workgroups' own work.
+double few_cost(int M, int N, int K, int esize, bool groups) {
+  const double pieces = (double)cdiv(K, 32), wgs = (double)cdiv(N, groups ? 64 : 16) * (double)cdiv(M, 64);
+  const double share = M <= 16 ? 0.35 : (M <= 32 ? 0.6 : 1.), waves = groups ? 3. : 1.;
+  return esize == 2 ? 3.3 + 0.14 * share * waves * pieces + wgs * share * (0.003 + 0.0005 * pieces)
+                    : 3.5 + 0.33 * share * waves * pieces + wgs * share * (0.006 + 0.001 * pieces);
+}
 }  // namespace
 
 MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups) {
@@ -47,10 +56,14 @@ MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups) {
     const long long tm = cdiv(M, bm), tn = cdiv(N, bn), tiles = tm * tn;
     double cost;
     if (kind == kWgrad) {
-      cost = (double)tiles * bm * bn * kArea[type][s];
+      const long long pieces = p.steps / 4 > 1 ? p.steps / 4 : 1, blocks = tiles * pieces;
+      cost = (double)tiles * bm * bn * kArea[type][s] * (blocks < 256 ? 256. / (double)blocks : 1.);
     } else {
       const Cost& c = kCost[type][s];
-      cost = (double)cdiv(tiles, 256 * c.resident) * (c.first + c.step * p.steps);
+      // (a last round of fewer workgroups per CU has shorter steps)
+      const long long slots = 256 * c.resident, rest = tiles % slots;
+      cost = (double)(tiles / slots) * (c.first + c.step * p.steps);
+      if (rest) cost += c.first + c.step * p.steps * (0.4 + 0.6 * (double)cdiv(rest, 256) / c.resident);
     }
     if (best < 0 || cost < best) {
       best = cost;
@@ -59,6 +72,7 @@ MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups) {
       p.tn = (int)tn;
     }
   }
+  pl.few = kind != kWgrad && few_cost(M, N, K, esize, groups) < best;
   p.nsplit = 1;
   p.per = p.steps;
   if (kind == kWgrad) {
@@ -108,6 +122,7 @@ __global__ __launch_bounds__(kThreads) void mm_sum(const float* __restrict__ par
 }  // namespace
 
 hipError_t launch_mm(Dtype dt, int kind, const MmPlan& pl, hipStream_t stream) {
+  if (pl.few) return dt == Dtype::F32 ? launch_few_f32(kind, pl.p, stream) : launch_few_bf16(kind, pl.p, stream);
   if (dt == Dtype::BF16 && whole_runs(kind, pl.p, 2)) {
     return kind == kFwd ? launch_mmf_fwd_bf16(pl, stream)
                         : (kind == kDgrad ? launch_mmf_dgrad_bf16(pl, stream) : launch_mmf_wgrad_bf16(pl, stream));

@@ -420,6 +420,15 @@ struct Geo {
   static constexpr int kLds = TA::kBytes + TB::kBytes;
 };
 
+// db[m] of a piece.
+template <typename T>
+__device__ __forceinline__ void put_db(const MmParams& P, int split, int m, float s) {
+  if (P.nsplit == 1)
+    static_cast<T*>(P.db)[m] = from_f32<T>(s);
+  else
+    P.part[(long long)split * ((long long)P.M * P.N + P.M) + (long long)P.M * P.N + m] = s;
+}
+
 // The wave's tile, 32 rows x 32 or (of a 64-column group) 64 columns at a time.
 // first(): called before the first store.
 template <typename T, int KIND, bool WHOLE, int TM, int TN, class F>
@@ -492,9 +501,13 @@ __device__ __forceinline__ void epilogue(const MmParams& P, int m0, int n0, int 
       for (int q = 0; q < NR; ++q) {
         if constexpr (KIND == kWgrad) {
           const int at = n + 16 * q;
-          if (WHOLE || (m < P.M && at < P.N))
-            put<float, WHOLE>(P.part + (long long)split * ((long long)P.M * P.N + P.M) + (long long)m * P.N + at,
-                              P.N - at, v[q]);
+          if (WHOLE || (m < P.M && at < P.N)) {
+            if (P.nsplit == 1)
+              put<T, WHOLE>(static_cast<T*>(P.out) + (long long)m * P.N + at, P.N - at, v[q]);
+            else
+              put<float, WHOLE>(P.part + (long long)split * ((long long)P.M * P.N + P.M) + (long long)m * P.N + at,
+                                P.N - at, v[q]);
+          }
         } else {
           finish<T, KIND, WHOLE>(P, m, n + 16 * q, ahead[q], v[q]);
         }
@@ -573,7 +586,7 @@ __global__ __launch_bounds__(kMmThreads, (Geo<T, KIND, SHAPE>::kWaves)) void mm(
       for (int i = 0; i < TM; ++i) {
         const float s = dbs[i] + __shfl_xor(dbs[i], 32, 64);
         const int m = m0 + wm + 32 * i + (lane & 31);
-        if (lane < 32 && m < P.M) P.part[(long long)split * ((long long)P.M * P.N + P.M) + (long long)P.M * P.N + m] = s;
+        if (lane < 32 && m < P.M) put_db<T>(P, split, m, s);
       }
     }
   }

@@ -269,8 +269,7 @@ __global__ __launch_bounds__(kMmThreads, (FastGeo<T, KIND, SHAPE>::kWaves)) void
         for (int i = 0; i < TM; ++i) {
           const float s = dbs[i] + __shfl_xor(dbs[i], 32, 64);
           const int m = at.m0 + wm + 32 * i + (lane & 31);
-          if (lane < 32 && m < P.M)
-            P.part[(long long)at.split * ((long long)P.M * P.N + P.M) + (long long)P.M * P.N + m] = s;
+          if (lane < 32 && m < P.M) put_db<T>(P, at.split, m, s);
         }
       }
     }

@@ -100,7 +100,8 @@ struct MmParams {
   void* pre; long long ldpre;           // forward: written; input gradient: read
   int8_t* q; float* scale;              // the same in 8 bits
   long long ldq; int groups;
-  float* part;                          // weight gradient: nsplit x (M N + M)
+  float* part;                          // weight gradient: nsplit x (M N + M), or (one piece) out and
+  void* db;
   int want_db;
 };
 
@@ -110,6 +111,7 @@ struct Shape {
 };
 
 struct MmPlan {
+  bool few;   // the kernels of few rows; else
   int shape;  // index into kShapes
   MmParams p;
 };
@@ -133,6 +135,9 @@ O1D_MM_DECL(bf16)
 hipError_t launch_mmf_fwd_bf16(const MmPlan& pl, hipStream_t stream);
 hipError_t launch_mmf_dgrad_bf16(const MmPlan& pl, hipStream_t stream);
 hipError_t launch_mmf_wgrad_bf16(const MmPlan& pl, hipStream_t stream);
+
+hipError_t launch_few_f32(int kind, const MmParams& p, hipStream_t stream);
+hipError_t launch_few_bf16(int kind, const MmParams& p, hipStream_t stream);
 
 // The product's kernel: of whole aligned runs where the operands have those.
 hipError_t launch_mm(Dtype dt, int kind, const MmPlan& pl, hipStream_t stream);

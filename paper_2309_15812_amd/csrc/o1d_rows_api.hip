@@ -132,7 +132,9 @@ WgradSpace wgrad_space(int M, int I, int O, bool rewritten, o1d_dtype_t dt) {
   WgradSpace s;
   const int es = (int)elem_size(dt), run = 16 / es;
   s.plan = rows::plan_mm(rows::kWgrad, O, I, M, es);
-  s.part = round256((size_t)s.plan.p.nsplit * ((size_t)O * I + O) * sizeof(float));
+  // (one piece is stored as it is; a workspace is asked for all the same, so
+  // that callers need not know)
+  s.part = s.plan.p.nsplit > 1 ? round256((size_t)s.plan.p.nsplit * ((size_t)O * I + O) * sizeof(float)) : 256;
   s.ldx = rows::cdiv(I, run) * run;
   s.operand = rewritten ? round256((size_t)M * s.ldx * es) : 0;
   return s;
@@ -358,6 +360,8 @@ o1d_status_t o1d_linear_bwd_weight(const void* x, long long ldx, const signed ch
   p.b = x;
   p.ldb = ldx;
   p.part = static_cast<float*>(workspace);
+  p.out = dw;
+  p.db = db;
   p.want_db = db != nullptr;
   if (rewritten) {
     void* operand = static_cast<char*>(workspace) + space.part;
@@ -367,7 +371,7 @@ o1d_status_t o1d_linear_bwd_weight(const void* x, long long ldx, const signed ch
     p.ldb = space.ldx;
   }
   O1D_TRY(hip_status(fn, rows::launch_mm((Dtype)dtype, rows::kWgrad, space.plan, s)));
-  return hip_status(fn, rows::launch_mm_sum((Dtype)dtype, space.plan, dw, db, s));
+  return p.nsplit > 1 ? hip_status(fn, rows::launch_mm_sum((Dtype)dtype, space.plan, dw, db, s)) : ok();
 }
 
 o1d_status_t o1d_act_bwd(const void* pre, long long ldpre, const signed char* preq, const float* prescale, o1d_act_t act,
