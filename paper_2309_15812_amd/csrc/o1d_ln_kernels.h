@@ -29,6 +29,10 @@ template <typename T>
 constexpr int kRun = 16 / (int)sizeof(T);  // elements of a run
 
 constexpr int kLnWaves = 4;
+// Waves of a backward workgroup: eight, so that few workgroups (partial rows of
+// dw and db) fill the GPU; with three runs per lane on, registers allow four.
+template <int CH>
+constexpr int kBwdWaves = ln_bwd_waves(CH);
 
 // Sum over LPR consecutive lanes, in all of them.
 template <int LPR>
@@ -121,15 +125,16 @@ struct RowMap {
   }
 
   // The same places of an 8-bit row (padded to 16 bytes: whole runs lie inside it).
-  __device__ __forceinline__ void load_held(const int8_t* q, const float* scale, float (&v)[CH][V]) const {
-    uint32_t w[CH][V / 4];
-    float s[CH];
+  __device__ __forceinline__ void load_held(const int8_t* q, const float* scale, uint32_t (&w)[CH][V / 4],
+                                            float (&s)[CH]) const {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int a = i < CH - 1 || n > 0 ? at[i] : 0;
       __builtin_memcpy(w[i], __builtin_assume_aligned(q + a, V), V);
       s[i] = scale[a / kGroup];
     }
+  }
+  __device__ __forceinline__ void unpack_held(const uint32_t (&w)[CH][V / 4], const float (&s)[CH], float (&v)[CH][V]) const {
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
@@ -177,50 +182,72 @@ __global__ __launch_bounds__(64 * kLnWaves) void ln_fwd_rows(LnParams P) {
   }
 }
 
+// A row's operands as they are in memory.
 template <typename T, int LPR, int CH, bool HELD>
-__global__ __launch_bounds__(64 * kLnWaves) void ln_bwd_rows(LnParams P) {
-  constexpr int V = kRun<T>, kRows = 64 / LPR * kLnWaves;
+struct BwdRow {
+  using Map = RowMap<T, LPR, CH>;
+  uint32_t g[CH][4], x[CH][HELD ? kRun<T> / 4 : 4];
+  float scale[CH], mean, rstd;
+
+  __device__ __forceinline__ void load(const LnParams& P, const Map& map, long long row, long long ldq, long long groups) {
+    map.load_raw(static_cast<const T*>(P.dy) + row * P.ldy, P.C, g);
+    if constexpr (HELD)
+      map.load_held(P.xq + row * ldq, P.xscale + row * groups, x, scale);
+    else
+      map.load_raw(static_cast<const T*>(P.x) + row * P.ldx, P.C, x);
+    mean = P.mean[row];
+    rstd = P.rstd[row];
+  }
+};
+
+template <typename T, int LPR, int CH, bool HELD>
+__global__ __launch_bounds__(64 * kBwdWaves<CH>) void ln_bwd_rows(LnParams P) {
+  constexpr int V = kRun<T>, kWaves = kBwdWaves<CH>, kRows = 64 / LPR * kWaves;
   const RowMap<T, LPR, CH> map(P.C);
   float w[CH][V], dw[CH][V], db[CH][V];
+  const long long ldq = (P.C + 15) / 16 * 16, groups = (P.C + kGroup - 1) / kGroup;
+  const long long stride = (long long)gridDim.x * kRows;
+  long long row = (long long)blockIdx.x * kRows + threadIdx.x / LPR;
+  BwdRow<T, LPR, CH, HELD> next;
+  next.load(P, map, row < P.M ? row : P.M - 1, ldq, groups);
   map.load(static_cast<const T*>(P.w), P.C, w);
 #pragma unroll
   for (int i = 0; i < CH; ++i)
 #pragma unroll
     for (int e = 0; e < V; ++e) dw[i][e] = db[i][e] = 0.f;
   const float inv = 1.f / (float)P.C;
-  const long long ldq = (P.C + 15) / 16 * 16, groups = (P.C + kGroup - 1) / kGroup;
-  for (long long row = (long long)blockIdx.x * kRows + threadIdx.x / LPR; row < P.M; row += (long long)gridDim.x * kRows) {
+  for (; row < P.M; row += stride) {
+    BwdRow<T, LPR, CH, HELD> now = next;
+    next.load(P, map, row + stride < P.M ? row + stride : P.M - 1, ldq, groups);  // during this row's sums
     float x[CH][V], g[CH][V];
-    uint32_t gw[CH][4];
-    map.load_raw(static_cast<const T*>(P.dy) + row * P.ldy, P.C, gw);
-    const float mean = P.mean[row], rstd = P.rstd[row];
     if constexpr (HELD)
-      map.load_held(P.xq + row * ldq, P.xscale + row * groups, x);
+      map.unpack_held(now.x, now.scale, x);
     else
-      map.load(static_cast<const T*>(P.x) + row * P.ldx, P.C, x);
-    map.unpack(P.C, gw, g);
+      map.unpack(P.C, now.x, x);
+    map.unpack(P.C, now.g, g);
+    const float shift = -now.mean * now.rstd;
     float s = 0.f, sx = 0.f;
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        x[i][e] = (x[i][e] - mean) * rstd;
+        x[i][e] = fmaf(x[i][e], now.rstd, shift);
         dw[i][e] = fmaf(g[i][e], x[i][e], dw[i][e]);
         db[i][e] += g[i][e];
         g[i][e] *= w[i][e];
         s += g[i][e];
         sx = fmaf(g[i][e], x[i][e], sx);
       }
-    s = lanes_sum<LPR>(s) * inv;
-    sx = lanes_sum<LPR>(sx) * inv;
+    s = -lanes_sum<LPR>(s) * inv * now.rstd;
+    sx = -lanes_sum<LPR>(sx) * inv * now.rstd;
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
-      for (int e = 0; e < V; ++e) x[i][e] = rstd * (g[i][e] - s - x[i][e] * sx);
+      for (int e = 0; e < V; ++e) x[i][e] = fmaf(x[i][e], sx, fmaf(g[i][e], now.rstd, s));
     map.store(static_cast<T*>(P.dx) + row * P.lddx, x);
   }
-  // this workgroup's sums: over a wave's rows, then wave after wave
-  __shared__ float sums[2][LPR * CH * V];
+  // this workgroup's sums: over a wave's rows, then pairs of waves
+  __shared__ float sums[kWaves / 2][2][LPR * CH * V];
 #pragma unroll
   for (int i = 0; i < CH; ++i)
 #pragma unroll
@@ -231,23 +258,39 @@ __global__ __launch_bounds__(64 * kLnWaves) void ln_bwd_rows(LnParams P) {
         db[i][e] += __shfl_xor(db[i][e], m, 64);
       }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int k = 0; k < kLnWaves; ++k) {
-    if (wave == k && lane < LPR) {
+#pragma unroll
+  for (int half = kWaves / 2; half >= 1; half /= 2) {
+    if (wave >= half && wave < 2 * half && lane < LPR) {
 #pragma unroll
       for (int i = 0; i < CH; ++i)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          const int c = map.at[i] + e;
-          sums[0][c] = (k ? sums[0][c] : 0.f) + dw[i][e];
-          sums[1][c] = (k ? sums[1][c] : 0.f) + db[i][e];
+          sums[wave - half][0][map.at[i] + e] = dw[i][e];
+          sums[wave - half][1][map.at[i] + e] = db[i][e];
+        }
+    }
+    __syncthreads();
+    if (wave < half && lane < LPR) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          dw[i][e] += sums[wave][0][map.at[i] + e];
+          db[i][e] += sums[wave][1][map.at[i] + e];
         }
     }
     __syncthreads();
   }
-  float* part = P.part + (long long)blockIdx.x * 2 * P.C;
-  for (int c = threadIdx.x; c < P.C; c += 64 * kLnWaves) {
-    part[c] = sums[0][c];
-    part[P.C + c] = sums[1][c];
+  if (wave == 0 && lane < LPR) {
+    float* part = P.part + (long long)blockIdx.x * 2 * P.C;
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (i < CH - 1 || e < map.n) {
+          part[map.at[i] + e] = dw[i][e];
+          part[P.C + map.at[i] + e] = db[i][e];
+        }
   }
 }
 
@@ -426,11 +469,39 @@ hipError_t ln_fwd_t(const LnParams& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Calls f with the backward's lanes and runs per lane (ln_bwd_map).
+template <typename T, class F>
+bool with_bwd_row(int C, F&& f) {
+  const LnMap m = ln_bwd_map(C, (int)sizeof(T));
+  auto pick = [&](auto lpr) {
+    constexpr int L = decltype(lpr)::value;
+    switch (m.runs) {
+      case 1: f(lpr, std::integral_constant<int, 1>{}); break;
+      case 2: f(lpr, std::integral_constant<int, 2>{}); break;
+      case 3: f(lpr, std::integral_constant<int, 3>{}); break;
+      case 4: if constexpr (L == 64) f(lpr, std::integral_constant<int, 4>{}); break;
+      case 5: if constexpr (L == 64) f(lpr, std::integral_constant<int, 5>{}); break;
+      case 6: if constexpr (L == 64) f(lpr, std::integral_constant<int, 6>{}); break;
+      case 7: if constexpr (L == 64) f(lpr, std::integral_constant<int, 7>{}); break;
+      case 8: if constexpr (L == 64) f(lpr, std::integral_constant<int, 8>{}); break;
+    }
+  };
+  switch (m.lanes) {
+    case 4: pick(std::integral_constant<int, 4>{}); break;
+    case 8: pick(std::integral_constant<int, 8>{}); break;
+    case 16: pick(std::integral_constant<int, 16>{}); break;
+    case 32: pick(std::integral_constant<int, 32>{}); break;
+    case 64: pick(std::integral_constant<int, 64>{}); break;
+    default: return false;
+  }
+  return true;
+}
+
 template <typename T, bool HELD>
 hipError_t ln_bwd_held(const LnParams& p, hipStream_t stream) {
-  const bool done = with_row<T>(p.C, [&](auto lpr, auto ch) {
+  const bool done = with_bwd_row<T>(p.C, [&](auto lpr, auto ch) {
     constexpr int L = decltype(lpr)::value, CH = decltype(ch)::value;
-    hipLaunchKernelGGL((ln_bwd_rows<T, L, CH, HELD>), dim3(p.blocks), dim3(64 * kLnWaves), 0, stream, p);
+    hipLaunchKernelGGL((ln_bwd_rows<T, L, CH, HELD>), dim3(p.blocks), dim3(64 * kBwdWaves<CH>), 0, stream, p);
   });
   if (!done) {
     hipLaunchKernelGGL((ln_bwd_wide<T, HELD>), dim3(p.M < 4096 ? p.M : 4096), dim3(kWide), 0, stream, p);

@@ -17,11 +17,13 @@ struct Cost {
   float first, step;
   int resident;  // workgroups of a CU
 };
-constexpr Cost kCost[2][kShapeCount] = {
+constexpr Cost kCost[3][kShapeCount] = {
     // float32: 128 x 128, 64 x 256, 64 x 64, 128 x 96, 64 x 128, 128 x 64
     {{5.f, 3.0f, 2}, {}, {5.f, 1.9f, 4}, {7.f, 1.9f, 2}, {7.f, 1.9f, 3}, {6.f, 1.9f, 3}},
-    // bfloat16
-    {{3.7f, 0.90f, 2}, {}, {3.3f, 0.45f, 3}, {3.0f, 0.72f, 2}, {3.0f, 0.68f, 3}, {3.0f, 0.68f, 3}}};
+    // bfloat16, whole runs
+    {{3.7f, 0.90f, 2}, {}, {3.3f, 0.45f, 3}, {3.0f, 0.72f, 2}, {3.0f, 0.68f, 3}, {3.0f, 0.68f, 3}},
+    // bfloat16, other runs
+    {{10.f, 1.2f, 2}, {}, {6.f, 0.8f, 4}, {7.f, 0.9f, 2}, {10.f, 1.f, 3}, {10.f, 1.f, 3}}};
 
 // Weight gradients run as many pieces as fill the GPU whatever the tile, so
 // the tile that computes least past the output's edge is taken, weighted by
@@ -40,7 +42,7 @@ double few_cost(int M, int N, int K, int esize, bool groups) {
 }
 }  // namespace
 
-MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups) {
+MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups, bool whole) {
   MmPlan pl{};
   MmParams& p = pl.p;
   p.M = M;
@@ -59,7 +61,7 @@ MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups) {
       const long long pieces = p.steps / 4 > 1 ? p.steps / 4 : 1, blocks = tiles * pieces;
       cost = (double)tiles * bm * bn * kArea[type][s] * (blocks < 256 ? 256. / (double)blocks : 1.);
     } else {
-      const Cost& c = kCost[type][s];
+      const Cost& c = kCost[type && !whole ? 2 : type][s];
       // (a last round of fewer workgroups per CU has shorter steps)
       const long long slots = 256 * c.resident, rest = tiles % slots;
       cost = (double)(tiles / slots) * (c.first + c.step * p.steps);
@@ -88,31 +90,36 @@ MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups) {
 
 namespace {
 
-// Whole 16-byte runs: along k where an operand is contiguous along it, else along its rows.
-bool whole_runs(int kind, const MmParams& p, int esize) {
-  const int v = 16 / esize;
-  auto aligned = [&](const void* t, long long ld) { return (uintptr_t)t % 16 == 0 && ld % v == 0; };
-  const bool a = kind == kWgrad ? p.M % v == 0 : p.K % v == 0, b = kind == kFwd ? p.K % v == 0 : p.N % v == 0;
-  return a && b && aligned(p.a, p.lda) && aligned(p.b, p.ldb);
-}
+// A workgroup's threads are kSumColumns outputs x kSumSlices slices of the
+// pieces, each slice added in order, then the slices: with all pieces in one thread
+// the sum waited for memory once per sixteen of them (28 pieces of 192 x 768 6.5 us).
+constexpr int kSumColumns = 64, kSumSlices = kThreads / kSumColumns;
 
-// Four outputs per thread where the partial rows allow it would not matter:
-// the loads of sixteen pieces are in flight together.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void mm_sum(const float* __restrict__ part, int pieces, long long MN, int M,
                                                    T* __restrict__ dw, T* __restrict__ db) {
+  __shared__ float red[kSumSlices][kSumColumns];
   const long long width = MN + M;
-  const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= (db ? width : MN)) return;
-  constexpr int kBatch = 16;
+  const int col = threadIdx.x % kSumColumns, slice = threadIdx.x / kSumColumns;
+  const long long i = (long long)blockIdx.x * kSumColumns + col;
+  const bool in = i < (db ? width : MN);
+  constexpr int kBatch = 8;
   float s = 0.f;
-  for (int j0 = 0; j0 < pieces; j0 += kBatch) {
-    float v[kBatch];
+  if (in) {
+    for (int j0 = slice; j0 < pieces; j0 += kSumSlices * kBatch) {
+      float v[kBatch];
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) v[u] = j0 + u < pieces ? part[(long long)(j0 + u) * width + i] : 0.f;
+      for (int u = 0; u < kBatch; ++u)
+        v[u] = j0 + u * kSumSlices < pieces ? part[(long long)(j0 + u * kSumSlices) * width + i] : 0.f;
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) s += v[u];
+      for (int u = 0; u < kBatch; ++u) s += v[u];
+    }
   }
+  red[slice][col] = s;
+  __syncthreads();
+  if (slice || !in) return;
+#pragma unroll
+  for (int k = 1; k < kSumSlices; ++k) s += red[k][col];
   if (i < MN)
     dw[i] = from_f32<T>(s);
   else
@@ -123,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void mm_sum(const float* __restrict__ par
 
 hipError_t launch_mm(Dtype dt, int kind, const MmPlan& pl, hipStream_t stream) {
   if (pl.few) return dt == Dtype::F32 ? launch_few_f32(kind, pl.p, stream) : launch_few_bf16(kind, pl.p, stream);
-  if (dt == Dtype::BF16 && whole_runs(kind, pl.p, 2)) {
+  if (dt == Dtype::BF16 && whole_runs(kind, pl.p.M, pl.p.N, pl.p.K, pl.p.a, pl.p.lda, pl.p.b, pl.p.ldb, 2)) {
     return kind == kFwd ? launch_mmf_fwd_bf16(pl, stream)
                         : (kind == kDgrad ? launch_mmf_dgrad_bf16(pl, stream) : launch_mmf_wgrad_bf16(pl, stream));
   }
@@ -136,7 +143,7 @@ hipError_t launch_mm(Dtype dt, int kind, const MmPlan& pl, hipStream_t stream) {
 
 hipError_t launch_mm_sum(Dtype dt, const MmPlan& pl, void* dw, void* db, hipStream_t stream) {
   const long long MN = (long long)pl.p.M * pl.p.N, width = MN + (db ? pl.p.M : 0);
-  const dim3 grid((unsigned)cdiv(width, kThreads)), block(kThreads);
+  const dim3 grid((unsigned)cdiv(width, kSumColumns)), block(kThreads);
   if (dt == Dtype::F32)
     hipLaunchKernelGGL(mm_sum<float>, grid, block, 0, stream, pl.p.part, pl.p.nsplit, MN, pl.p.M, static_cast<float*>(dw),
                        static_cast<float*>(db));

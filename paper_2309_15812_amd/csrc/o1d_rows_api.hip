@@ -131,7 +131,7 @@ struct WgradSpace {
 WgradSpace wgrad_space(int M, int I, int O, bool rewritten, o1d_dtype_t dt) {
   WgradSpace s;
   const int es = (int)elem_size(dt), run = 16 / es;
-  s.plan = rows::plan_mm(rows::kWgrad, O, I, M, es);
+  s.plan = rows::plan_mm(rows::kWgrad, O, I, M, es, false, true);
   // (one piece is stored as it is; a workspace is asked for all the same, so
   // that callers need not know)
   s.part = s.plan.p.nsplit > 1 ? round256((size_t)s.plan.p.nsplit * ((size_t)O * I + O) * sizeof(float)) : 256;
@@ -250,7 +250,8 @@ o1d_status_t o1d_linear_fwd(const void* x, long long ldx, const void* w, const v
                         {"pre", pre, reach(M, ldpre, O, es), true}, {"the checkpoint", q, held_q_bytes(M, O), true},
                         {"its scales", scale, held_scale_bytes(M, O), true}};
   O1D_TRY(apart(fn, spans));
-  rows::MmPlan pl = rows::plan_mm(rows::kFwd, M, O, I, (int)es, q != nullptr);
+  rows::MmPlan pl = rows::plan_mm(rows::kFwd, M, O, I, (int)es, q != nullptr,
+                                  rows::whole_runs(rows::kFwd, M, O, I, x, ldx, w, I, (int)es));
   O1D_TRY(check_blocks(fn, pl));
   (void)hipGetLastError();
   rows::MmParams& p = pl.p;
@@ -295,7 +296,8 @@ o1d_status_t o1d_linear_bwd_input(const void* dy, long long lddy, const void* w,
                         {"its scales", held ? prescale : nullptr, held_scale_bytes(M, I), false},
                         {"dx", dx, reach(M, lddx, I, es), true}};
   O1D_TRY(apart(fn, spans));
-  rows::MmPlan pl = rows::plan_mm(rows::kDgrad, M, I, O, (int)es);
+  rows::MmPlan pl = rows::plan_mm(rows::kDgrad, M, I, O, (int)es, false,
+                                  rows::whole_runs(rows::kDgrad, M, I, O, dy, lddy, w, I, (int)es));
   O1D_TRY(check_blocks(fn, pl));
   (void)hipGetLastError();
   rows::MmParams& p = pl.p;
