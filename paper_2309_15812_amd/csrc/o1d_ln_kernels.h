@@ -281,7 +281,16 @@ __global__ __launch_bounds__(64 * kBwdWaves<CH>) void ln_bwd_rows(LnParams P) {
     }
     __syncthreads();
   }
-  if (wave == 0 && lane < LPR) {
+  if (wave == 0 && lane < LPR && gridDim.x == 1) {  // the sums themselves
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (i < CH - 1 || e < map.n) {
+          static_cast<T*>(P.dw)[map.at[i] + e] = from_f32<T>(dw[i][e]);
+          static_cast<T*>(P.db)[map.at[i] + e] = from_f32<T>(db[i][e]);
+        }
+  } else if (wave == 0 && lane < LPR) {
     float* part = P.part + (long long)blockIdx.x * 2 * P.C;
 #pragma unroll
     for (int i = 0; i < CH; ++i)

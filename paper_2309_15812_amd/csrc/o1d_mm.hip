@@ -40,6 +40,15 @@ double few_cost(int M, int N, int K, int esize, bool groups) {
   return esize == 2 ? 3.3 + 0.14 * share * waves * pieces + wgs * share * (0.003 + 0.0005 * pieces)
                     : 3.5 + 0.33 * share * waves * pieces + wgs * share * (0.006 + 0.001 * pieces);
 }
+// A weight gradient's k in pieces of at least four steps.
+void split_steps(MmParams& p) {
+  const long long want = cdiv(kWgradBlocks, (long long)p.tm * p.tn), most = p.steps / 4;
+  const long long pieces = want < most ? want : most;
+  p.per = (int)cdiv(p.steps, pieces > 1 ? pieces : 1);
+  p.nsplit = (int)cdiv(p.steps, p.per);
+  p.nblocks = p.tm * p.tn * p.nsplit;
+}
+
 }  // namespace
 
 MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups, bool whole) {
@@ -78,11 +87,7 @@ MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups, bool whole
   p.nsplit = 1;
   p.per = p.steps;
   if (kind == kWgrad) {
-    // pieces of at least four steps
-    const long long want = cdiv(kWgradBlocks, (long long)p.tm * p.tn), most = p.steps / 4;
-    const long long pieces = want < most ? want : most;
-    p.per = (int)cdiv(p.steps, pieces > 1 ? pieces : 1);
-    p.nsplit = (int)cdiv(p.steps, p.per);
+    split_steps(p);
   }
   p.nblocks = p.tm * p.tn * p.nsplit;
   return pl;
@@ -128,9 +133,21 @@ __global__ __launch_bounds__(kThreads) void mm_sum(const float* __restrict__ par
 
 }  // namespace
 
+bool make_operand(MmPlan& pl) {
+  MmParams& p = pl.p;
+  if ((double)p.K * p.N * (double)cdiv(p.M, 64) > 8e6) return false;
+  if (pl.shape != k64x64 && pl.shape != k128x64) {  // those are the tiles that have the kernel
+    pl.shape = k128x64;
+    p.tm = (int)cdiv(p.M, 128);
+    p.tn = (int)cdiv(p.N, 64);
+    split_steps(p);
+  }
+  return true;
+}
+
 hipError_t launch_mm(Dtype dt, int kind, const MmPlan& pl, hipStream_t stream) {
   if (pl.few) return dt == Dtype::F32 ? launch_few_f32(kind, pl.p, stream) : launch_few_bf16(kind, pl.p, stream);
-  if (dt == Dtype::BF16 && whole_runs(kind, pl.p.M, pl.p.N, pl.p.K, pl.p.a, pl.p.lda, pl.p.b, pl.p.ldb, 2)) {
+  if (dt == Dtype::BF16 && !pl.p.made && whole_runs(kind, pl.p.M, pl.p.N, pl.p.K, pl.p.a, pl.p.lda, pl.p.b, pl.p.ldb, 2)) {
     return kind == kFwd ? launch_mmf_fwd_bf16(pl, stream)
                         : (kind == kDgrad ? launch_mmf_dgrad_bf16(pl, stream) : launch_mmf_wgrad_bf16(pl, stream));
   }

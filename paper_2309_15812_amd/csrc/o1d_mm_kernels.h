@@ -216,15 +216,51 @@ struct Tile {
     }
   }
 
+  // The same places of an 8-bit checkpoint: the integers of a run and its scale.
+  __device__ __forceinline__ void load_held(const int8_t* q, const float* scale, long long ldq, int groups, int r0, int k0,
+                                            int K) {
+    static_assert(!KC, "checkpoints lie along their rows");
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const long long k = k0 + min(k_of(i), K - 1 - k0);
+      const int r = r0 + r_of(i) < ldq ? r0 + r_of(i) : 0;  // (columns past the end are not stored)
+      uint32_t t[2] = {0u, 0u};
+      __builtin_memcpy(t, __builtin_assume_aligned(q + k * ldq + r, V), V);
+      w[i] = u32x4{t[0], t[1], __float_as_uint(scale[k * groups + r / kGroup]), 0u};
+    }
+  }
+  // Makes the operand act(x) from what was loaded (k past the end: from zeros, which every activation keeps).
+  __device__ __forceinline__ void make(bool held, int act) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float v[V];
+      if (held) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = (float)(int8_t)(w[i][e / 4] >> (8 * (e & 3))) * __uint_as_float(w[i][2]);
+      } else {
+        T t[V];
+        __builtin_memcpy(t, &w[i], 16);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = to_f32(t[e]);
+      }
+      act_values<sizeof(T) == 2>(v, act);
+      T t[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) t[e] = from_f32<T>(v[e]);
+      __builtin_memcpy(&w[i], t, 16);
+    }
+  }
+
   // Puts runs past the end in their places and clears k past the end.
-  __device__ __forceinline__ void place(int r0, int rows, int k0, int K) {
+  // (held: the runs are in their places)
+  __device__ __forceinline__ void place(int r0, int rows, int k0, int K, bool held = false) {
     if constexpr (KC) {
       if (k0 + BK <= K || K < V) return;
       const int k = k0 + (int)(threadIdx.x % 8) * V, shift = min(V, max(0, k + V - K));
 #pragma unroll
       for (int i = 0; i < N; ++i) move_down<T>(w[i], shift);
     } else {
-      if (r0 + R > rows && rows >= V) {
+      if (!held && r0 + R > rows && rows >= V) {
 #pragma unroll
         for (int i = 0; i < N; ++i) move_down<T>(w[i], min(V, max(0, r0 + r_of(i) + V - rows)));
       }
@@ -516,7 +552,8 @@ __device__ __forceinline__ void epilogue(const MmParams& P, int m0, int n0, int 
   }
 }
 
-template <typename T, int KIND, int SHAPE>
+// MADE (weight gradient): B is act(x), made from x or its checkpoint as it is staged.
+template <typename T, int KIND, int SHAPE, bool MADE = false>
 __global__ __launch_bounds__(kMmThreads, (Geo<T, KIND, SHAPE>::kWaves)) void mm(MmParams P) {
   using G = Geo<T, KIND, SHAPE>;
   constexpr int TM = G::S.tm, TN = G::S.tn, BK = Fmt<T>::BK;
@@ -537,6 +574,12 @@ __global__ __launch_bounds__(kMmThreads, (Geo<T, KIND, SHAPE>::kWaves)) void mm(
   typename G::TB tb[D];
   auto load = [&](int d, int s) __attribute__((always_inline)) {
     ta[d].load(A, P.lda, m0, P.M, s * BK, P.K);
+    if constexpr (MADE) {
+      if (P.bq) {
+        tb[d].load_held(P.bq, P.scale, P.ldq, P.groups, n0, s * BK, P.K);
+        return;
+      }
+    }
     tb[d].load(B, P.ldb, n0, P.N, s * BK, P.K);
   };
 #pragma unroll
@@ -560,7 +603,8 @@ __global__ __launch_bounds__(kMmThreads, (Geo<T, KIND, SHAPE>::kWaves)) void mm(
       if (s >= s1) break;
       __syncthreads();  // the previous step's fragments are read
       ta[d].place(m0, P.M, s * BK, P.K);
-      tb[d].place(n0, P.N, s * BK, P.K);
+      tb[d].place(n0, P.N, s * BK, P.K, MADE && P.bq);
+      if constexpr (MADE) tb[d].make(P.bq, P.act);
       ta[d].store(lds);
       tb[d].store(lds + G::TA::kBytes);
       if (s + D < s1) load(d, s + D);
@@ -596,23 +640,27 @@ __global__ __launch_bounds__(kMmThreads, (Geo<T, KIND, SHAPE>::kWaves)) void mm(
     epilogue<T, KIND, false>(P, m0 + wm, n0 + wn, split, acc, [] {});
 }
 
-template <typename T, int KIND, int SHAPE>
+template <typename T, int KIND, int SHAPE, bool MADE = false>
 hipError_t launch_shape(const MmPlan& pl, hipStream_t stream) {
   using G = Geo<T, KIND, SHAPE>;
   static std::atomic<int> allowed{0};
   if (!allowed.load(std::memory_order_acquire)) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(mm<T, KIND, SHAPE>),
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(mm<T, KIND, SHAPE, MADE>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, G::kLds);
     if (e != hipSuccess) return e;
     allowed.store(1, std::memory_order_release);
   }
-  hipLaunchKernelGGL((mm<T, KIND, SHAPE>), dim3((unsigned)(pl.p.nblocks + 7) / 8 * 8), dim3(kMmThreads), G::kLds, stream,
+  hipLaunchKernelGGL((mm<T, KIND, SHAPE, MADE>), dim3((unsigned)(pl.p.nblocks + 7) / 8 * 8), dim3(kMmThreads), G::kLds, stream,
                      pl.p);
   return hipGetLastError();
 }
 
 template <typename T, int KIND>
 hipError_t launch_kind(const MmPlan& pl, hipStream_t stream) {
+  if constexpr (KIND == kWgrad) {
+    if (pl.p.made) return pl.shape == k64x64 ? launch_shape<T, KIND, k64x64, true>(pl, stream)
+                                             : launch_shape<T, KIND, k128x64, true>(pl, stream);
+  }
   switch (pl.shape) {
     case k128x128: return launch_shape<T, KIND, k128x128>(pl, stream);
     case k64x256:

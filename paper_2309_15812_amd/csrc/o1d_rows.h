@@ -45,7 +45,7 @@ struct LnParams {
   const void *x, *w, *b, *dy;
   const int8_t* xq;
   const float* xscale;
-  void *y, *dx;
+  void *y, *dx, *dw, *db;
   float *mean, *rstd;         // written by the forward, read by the backward
   float* part;                // backward: partial sums, blocks x 2 x C
   int blocks;
@@ -80,8 +80,9 @@ constexpr int ln_bwd_waves(int runs) { return runs <= 2 ? 8 : 4; }
 constexpr int kLnMostBlocks = 512;  // (1024: 33333 x 211 bfloat16 18.3 -> 21 us, 50176 x 192 19.5 -> 25)
 inline int ln_bwd_blocks(int M, int C, int esize) {
   const LnMap m = ln_bwd_map(C, esize);
-  if (!m.lanes) return M < 256 ? M : 256;
+  if (!m.lanes) return M < 2 ? 2 : (M < 256 ? M : 256);
   const long long blocks = cdiv(M, 64 / m.lanes * ln_bwd_waves(m.runs));
+  if (blocks <= 4) return 1;  // one workgroup, whose sums are dw and db: no second launch
   if (blocks <= kLnMostBlocks) return (int)blocks;
   return (int)cdiv(blocks, cdiv(blocks, kLnMostBlocks));
 }
@@ -119,7 +120,9 @@ struct MmParams {
   int nsplit;           // weight gradient: pieces of k
   int nblocks;
   // epilogues
-  int act;
+  int act;                              // (weight gradient: of b, with made)
+  const int8_t* bq;                     // weight gradient: b's checkpoint
+  int made;                             // weight gradient: b is act(x) of a tensor or a checkpoint, made as it is staged
   const void* bias;                     // forward
   const void* res; long long ldres;     // forward
   void* out; long long ldo;             // forward, input gradient
@@ -158,6 +161,11 @@ inline bool whole_runs(int kind, int M, int N, int K, const void* a, long long l
 // `groups`: an 8-bit checkpoint is written (waves with 64 columns).  `whole`:
 // whole_runs (a weight gradient's plan, which sizes its workspace, does not go by it).
 MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups, bool whole);
+
+// Whether a weight gradient makes act(x) itself as it stages it, once per tile
+// along m, instead of reading it from a pass of its own (a launch, and act(x)
+// through memory): where all tiles together make few elements.
+bool make_operand(MmPlan& pl);
 
 #define O1D_MM_DECL(T)                                                                    \
   hipError_t launch_mm_fwd_##T(const MmPlan& pl, hipStream_t stream);                     \

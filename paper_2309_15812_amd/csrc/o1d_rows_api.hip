@@ -25,6 +25,9 @@ constexpr int kMaxRows = 0x7fffffff - 1024;
 constexpr int kMaxFeatures = 1 << 20;
 constexpr long long kMaxStride = 1 << 21;
 
+// What a call that needs no workspace asks for all the same, so that callers need not know which do.
+constexpr size_t kNoSpace = 256;
+
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 // One tensor of a call: where it lies and how far it reaches.
@@ -124,6 +127,7 @@ o1d_status_t check_blocks(const char* fn, const rows::MmPlan& pl) {
 struct WgradSpace {
   rows::MmPlan plan;
   size_t part, operand;
+  bool made;      // act(x) is made by the product
   long long ldx;  // of the operand
   size_t bytes() const { return part + operand; }
 };
@@ -132,11 +136,10 @@ WgradSpace wgrad_space(int M, int I, int O, bool rewritten, o1d_dtype_t dt) {
   WgradSpace s;
   const int es = (int)elem_size(dt), run = 16 / es;
   s.plan = rows::plan_mm(rows::kWgrad, O, I, M, es, false, true);
-  // (one piece is stored as it is; a workspace is asked for all the same, so
-  // that callers need not know)
-  s.part = s.plan.p.nsplit > 1 ? round256((size_t)s.plan.p.nsplit * ((size_t)O * I + O) * sizeof(float)) : 256;
+  s.part = s.plan.p.nsplit > 1 ? round256((size_t)s.plan.p.nsplit * ((size_t)O * I + O) * sizeof(float)) : kNoSpace;
   s.ldx = rows::cdiv(I, run) * run;
-  s.operand = rewritten ? round256((size_t)M * s.ldx * es) : 0;
+  s.made = rewritten && rows::make_operand(s.plan);
+  s.operand = rewritten && !s.made ? round256((size_t)M * s.ldx * es) : 0;
   return s;
 }
 
@@ -179,7 +182,8 @@ o1d_status_t o1d_ln_fwd(const void* x, long long ldx, const void* w, const void*
 
 size_t o1d_ln_bwd_workspace_bytes(int M, int C, o1d_dtype_t dtype) {
   if (check_dims("o1d_ln_bwd", M, C, "C", dtype) != O1D_OK || M == 0) return 0;
-  return (size_t)rows::ln_bwd_blocks(M, C, (int)elem_size(dtype)) * 2 * C * sizeof(float);
+  const int blocks = rows::ln_bwd_blocks(M, C, (int)elem_size(dtype));
+  return blocks > 1 ? (size_t)blocks * 2 * C * sizeof(float) : kNoSpace;
 }
 
 o1d_status_t o1d_ln_bwd(const void* x, long long ldx, const signed char* xq, const float* xscale, const void* dy,
@@ -223,10 +227,12 @@ o1d_status_t o1d_ln_bwd(const void* x, long long ldx, const signed char* xq, con
   p.dx = dx;
   p.mean = const_cast<float*>(mean);
   p.rstd = const_cast<float*>(rstd);
+  p.dw = dw;
+  p.db = db;
   p.part = static_cast<float*>(workspace);
   p.blocks = rows::ln_bwd_blocks(M, C, (int)es);
   O1D_TRY(hip_status(fn, dtype == O1D_F32 ? rows::launch_ln_bwd_f32(p, s) : rows::launch_ln_bwd_bf16(p, s)));
-  return hip_status(fn, rows::launch_col_sum((Dtype)dtype, p.part, p.blocks, 2ll * C, C, dw, db, s));
+  return p.blocks > 1 ? hip_status(fn, rows::launch_col_sum((Dtype)dtype, p.part, p.blocks, 2ll * C, C, dw, db, s)) : ok();
 }
 
 o1d_status_t o1d_linear_fwd(const void* x, long long ldx, const void* w, const void* b, o1d_act_t act, const void* res,
@@ -365,7 +371,14 @@ o1d_status_t o1d_linear_bwd_weight(const void* x, long long ldx, const signed ch
   p.out = dw;
   p.db = db;
   p.want_db = db != nullptr;
-  if (rewritten) {
+  if (space.made) {
+    p.made = 1;
+    p.act = (int)act;
+    p.bq = reinterpret_cast<const int8_t*>(xq);
+    p.scale = const_cast<float*>(xscale);
+    p.ldq = rows::held_ld(I);
+    p.groups = rows::held_groups(I);
+  } else if (rewritten) {
     void* operand = static_cast<char*>(workspace) + space.part;
     const rows::Operand in{x, ldx, reinterpret_cast<const int8_t*>(xq), xscale};
     O1D_TRY(hip_status(fn, rows::launch_act((Dtype)dtype, in, nullptr, 0, M, I, (int)act, operand, space.ldx, s)));

@@ -394,9 +394,19 @@ def _into(out: torch.Tensor | None, like: torch.Tensor, C: int) -> torch.Tensor:
     return like.new_empty((*like.shape[:-1], C)) if out is None else _out(out, like, (*like.shape[:-1], C))
 
 
+_NO_SPACE = 256  # what a call that uses no workspace asks for (it writes nothing there)
+_no_space: dict[int, torch.Tensor] = {}
+
+
 def _scratch(workspace: torch.Tensor | None, like: torch.Tensor, need: int) -> tuple[torch.Tensor, int]:
-    return (like.new_empty((max(need, 1),), dtype=torch.uint8), need) if workspace is None else \
-        _workspace(workspace, like, need)
+    if workspace is not None:
+        return _workspace(workspace, like, need)
+    if need > _NO_SPACE:
+        return like.new_empty((need,), dtype=torch.uint8), need
+    held = _no_space.get(like.get_device())
+    if held is None:
+        held = _no_space[like.get_device()] = torch.empty((_NO_SPACE,), dtype=torch.uint8, device=like.device)
+    return held, _NO_SPACE
 
 
 def pack8(x: torch.Tensor) -> Packed8:
@@ -540,3 +550,59 @@ def act_bwd(pre: torch.Tensor | Packed8, dy: torch.Tensor, act: str, out: torch.
     _lib.check("o1d_act_bwd", _lib.call("o1d_act_bwd", p, ldp, q, scale, a, g.data_ptr(), lddy, dh.data_ptr(), C, M, C,
                                         dt, _stream(dy)))
     return dh
+
+
+class LayerNormFunction(torch.autograd.Function):
+    """Autograd glue: ln_fwd, ln_bwd.  checkpoint=True keeps x in 8 bits for the backward."""
+
+    @staticmethod
+    def forward(ctx, x, w, b, eps=1e-6, checkpoint=False):
+        x, w, b = x.contiguous(), w.contiguous(), b.contiguous()
+        y, mean, rstd = ln_fwd(x, w, b, eps)
+        held = pack8(x) if checkpoint else None
+        ctx.cols = x.shape[-1]
+        ctx.save_for_backward(*((held.q, held.scale) if checkpoint else (x, None)), mean, rstd, w)
+        return y
+
+    @staticmethod
+    def backward(ctx, gy):
+        x, scale, mean, rstd, w = ctx.saved_tensors
+        gx, gw, gb = ln_bwd(x if scale is None else Packed8(x, scale, ctx.cols), gy.contiguous(), mean, rstd, w)
+        return gx, gw, gb, None, None
+
+
+class LinearFunction(torch.autograd.Function):
+    """Autograd glue: y = act(x w^T + b) + residual.  checkpoint=True keeps x and the pre-activation in 8 bits for the
+    backward."""
+
+    @staticmethod
+    def forward(ctx, x, w, b=None, act="none", residual=None, checkpoint=False):
+        x, w = x.contiguous(), w.contiguous()
+        save = None if act == "none" else "pack8" if checkpoint else "pre"
+        out = linear_fwd(x, w, None if b is None else b.contiguous(), act,
+                         None if residual is None else residual.contiguous(), save)
+        y, pre = (out, None) if save is None else out
+        ctx.act, ctx.bias = act, b is not None
+        ctx.save_for_backward(w, *_parts(pack8(x) if checkpoint else x), *_parts(pre))
+        ctx.cols = (w.shape[1], w.shape[0])
+        return y
+
+    @staticmethod
+    def backward(ctx, gy):
+        w, x, xs, pre, ps = ctx.saved_tensors
+        dy = gy.contiguous()
+        dh = dy if ctx.act == "none" else act_bwd(_whole(pre, ps, ctx.cols[1]), dy, ctx.act)
+        gx = linear_bwd_input(dh, w) if ctx.needs_input_grad[0] else None
+        gw = gb = None
+        if ctx.needs_input_grad[1] or (ctx.bias and ctx.needs_input_grad[2]):
+            gw, gb = linear_bwd_weight(_whole(x, xs, ctx.cols[0]), dh, bias=ctx.bias)
+        return gx, gw, gb, None, (gy if ctx.needs_input_grad[4] else None), None
+
+
+def _parts(t) -> tuple:
+    """A tensor, a checkpoint or None as two tensors (or None) that autograd can save."""
+    return (t.q, t.scale) if isinstance(t, Packed8) else (t, None)
+
+
+def _whole(t, scale, cols: int):
+    return t if scale is None else Packed8(t, scale, cols)

@@ -445,7 +445,11 @@ def test_offsets_beyond_32_bits():
     tz, th = ops.linear_fwd(tail, w, act="gelu", save="pack8")
     assert torch.equal(z[-300:], tz) and torch.equal(held.q[-300:], th.q) and torch.equal(held.scale[-300:], th.scale)
     dx = ops.linear_bwd_input(x, w, pre=held, act="gelu", out=y)
-    assert torch.equal(dx[-300:], ops.linear_bwd_input(tail, w, pre=th, act="gelu"))
+    # (300 rows alone are summed in another order)
+    g, slope = tail.double() @ w.double(), gate(value64(th), "gelu")[1]
+    e = (C + 8) * 2.0 ** -24 * (tail.double().abs() @ w.double().abs())
+    near(dx[-300:], g * slope, 1.2 * e + 4e-6 * (1 + value64(th).abs()) * (g.abs() + e) + u(BF16) * ((g * slope).abs() + 1.2 * e),
+         "dx")
     h = ops.pack8(x)
     t = ops.pack8(tail)
     assert torch.equal(h.q[-300:], t.q) and torch.equal(h.scale[-300:], t.scale)
