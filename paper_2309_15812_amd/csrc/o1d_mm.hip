@@ -18,8 +18,8 @@ struct Cost {
   int resident;  // workgroups of a CU
 };
 constexpr Cost kCost[3][kShapeCount] = {
-    // float32: 128 x 128, 64 x 256, 64 x 64, 128 x 96, 64 x 128, 128 x 64
-    {{5.f, 3.0f, 2}, {}, {5.f, 1.9f, 4}, {7.f, 1.9f, 2}, {7.f, 1.9f, 3}, {6.f, 1.9f, 3}},
+    // float32: 128 x 128, 64 x 256, 64 x 64, 128 x 96, 64 x 128, 128 x 64, 128 x 192
+    {{5.f, 3.0f, 2}, {}, {5.f, 1.9f, 4}, {7.f, 1.9f, 2}, {7.5f, 2.2f, 3}, {6.5f, 2.2f, 3}, {8.f, 4.f, 2}},
     // bfloat16, whole runs
     {{3.7f, 0.90f, 2}, {}, {3.3f, 0.45f, 3}, {3.0f, 0.72f, 2}, {3.0f, 0.68f, 3}, {3.0f, 0.68f, 3}},
     // bfloat16, other runs
@@ -28,7 +28,7 @@ constexpr Cost kCost[3][kShapeCount] = {
 // Weight gradients run as many pieces as fill the GPU whatever the tile, so
 // the tile that computes least past the output's edge is taken, weighted by
 // the time of its products (float32: smaller tiles make more pieces per product).
-constexpr float kArea[2][kShapeCount] = {{1.f, 1.02f, 1.5f, 1.15f, 1.3f, 1.3f}, {1.05f, 1.f, 1.3f, 1.35f, 1.f, 1.f}};
+constexpr float kArea[2][kShapeCount] = {{1.f, 1.02f, 1.5f, 1.15f, 1.3f, 1.3f, 1.1f}, {1.05f, 1.f, 1.3f, 1.35f, 1.f, 1.f}};
 constexpr int kWgradBlocks = 512;
 
 // Time of the kernels of few rows (microseconds, measured as above for 1 .. 2000

@@ -669,6 +669,9 @@ hipError_t launch_kind(const MmPlan& pl, hipStream_t stream) {
     case k64x64: return launch_shape<T, KIND, k64x64>(pl, stream);
     case k128x96: return launch_shape<T, KIND, k128x96>(pl, stream);
     case k64x128: return launch_shape<T, KIND, k64x128>(pl, stream);
+    case k128x192:
+      if constexpr (shape_used(KIND, (int)sizeof(T), k128x192)) return launch_shape<T, KIND, k128x192>(pl, stream);
+      return hipErrorInvalidValue;
     default: return launch_shape<T, KIND, k128x64>(pl, stream);
   }
 }

@@ -145,10 +145,13 @@ struct MmPlan {
   MmParams p;
 };
 
-enum ShapeId { k128x128, k64x256, k64x64, k128x96, k64x128, k128x64, kShapeCount };
-constexpr Shape kShapes[kShapeCount] = {{2, 2, 2, 2}, {1, 4, 2, 2}, {2, 2, 1, 1}, {4, 1, 1, 3}, {2, 2, 1, 2}, {4, 1, 1, 2}};
-// (64 x 256 is planned for float32 weight gradients alone)
-constexpr bool shape_used(int kind, int esize, int shape) { return shape != k64x256 || (kind == kWgrad && esize == 4); }
+enum ShapeId { k128x128, k64x256, k64x64, k128x96, k64x128, k128x64, k128x192, kShapeCount };
+constexpr Shape kShapes[kShapeCount] = {{2, 2, 2, 2}, {1, 4, 2, 2}, {2, 2, 1, 1}, {4, 1, 1, 3}, {2, 2, 1, 2}, {4, 1, 1, 2},
+                                         {2, 2, 2, 3}};
+// (128 x 192 is planned for float32 alone, 64 x 256 for its weight gradients)
+constexpr bool shape_used(int kind, int esize, int shape) {
+  return shape == k128x192 ? esize == 4 : (shape == k64x256 ? kind == kWgrad && esize == 4 : true);
+}
 constexpr int kStepBytes = 128;  // k per step: 32 float32 or 64 bfloat16
 
 // Whole 16-byte runs: along k where an operand is contiguous along it, else along its rows.
