@@ -19,7 +19,7 @@ struct Cost {
 };
 constexpr Cost kCost[3][kShapeCount] = {
     // float32: 128 x 128, 64 x 256, 64 x 64, 128 x 96, 64 x 128, 128 x 64, 128 x 192
-    {{5.f, 3.0f, 2}, {}, {5.f, 1.9f, 4}, {7.f, 1.9f, 2}, {7.5f, 2.2f, 3}, {6.5f, 2.2f, 3}, {8.f, 4.f, 2}},
+    {{5.f, 3.0f, 2}, {}, {5.f, 1.9f, 4}, {7.f, 1.9f, 2}, {7.5f, 2.2f, 3}, {6.5f, 2.2f, 3}, {8.f, 4.f, 2}, {}},
     // bfloat16, whole runs
     {{3.7f, 0.90f, 2}, {}, {3.3f, 0.45f, 3}, {3.0f, 0.72f, 2}, {3.0f, 0.68f, 3}, {3.0f, 0.68f, 3}},
     // bfloat16, other runs
@@ -41,8 +41,8 @@ double few_cost(int M, int N, int K, int esize, bool groups) {
                     : 3.5 + 0.33 * share * waves * pieces + wgs * share * (0.006 + 0.001 * pieces);
 }
 // A weight gradient's k in pieces of at least four steps.
-void split_steps(MmParams& p) {
-  const long long want = cdiv(kWgradBlocks, (long long)p.tm * p.tn), most = p.steps / 4;
+void split_steps(MmParams& p, int blocks = kWgradBlocks) {
+  const long long want = cdiv(blocks, (long long)p.tm * p.tn), most = p.steps / 4;
   const long long pieces = want < most ? want : most;
   p.per = (int)cdiv(p.steps, pieces > 1 ? pieces : 1);
   p.nsplit = (int)cdiv(p.steps, p.per);
@@ -133,15 +133,25 @@ __global__ __launch_bounds__(kThreads) void mm_sum(const float* __restrict__ par
 
 }  // namespace
 
-bool make_operand(MmPlan& pl) {
+bool make_operand(MmPlan& pl, int act, bool held, int esize) {
+  // Picoseconds per element: of the product that makes it (none, relu, gelu,
+  // gelu_tanh, silu), above the plain product's; and of writing it and reading it
+  // back.  50176 x 768 -> 192 bfloat16 from a checkpoint with GELU: 58 us against
+  // 68 with a pass of its own, 200704 x 384 -> 96 96 against 93.
+  constexpr double kMade[2][kActs] = {{1.2, 1.2, 3.5, 3.0, 3.0}, {0.9, 0.95, 1.05, 1.05, 1.0}};
+  constexpr double kLaunch = 3e6;
   MmParams& p = pl.p;
-  if ((double)p.K * p.N * (double)cdiv(p.M, 64) > 8e6) return false;
-  if (pl.shape != k64x64 && pl.shape != k128x64) {  // those are the tiles that have the kernel
-    pl.shape = k128x64;
-    p.tm = (int)cdiv(p.M, 128);
-    p.tn = (int)cdiv(p.N, 64);
-    split_steps(p);
-  }
+  const double elements = (double)p.K * p.N, wide = (double)cdiv(p.M, 192), narrow = (double)cdiv(p.M, 64);
+  const double per = kMade[esize == 2 ? 1 : 0][act], apart = elements * ((held ? 1. : esize) + 2. * esize) / 5. + kLaunch;
+  const bool small = elements * narrow * per < kLaunch;
+  if (!small && elements * wide * per > apart) return false;
+  // 64 x 64 tiles where there are few, else those that make an element least often
+  const int shape = small && cdiv(p.M, 192) * cdiv(p.N, 64) * (p.steps / 4) < 256 ? k64x64 : k192x64;
+  const Shape& sh = kShapes[shape];
+  pl.shape = shape;
+  p.tm = (int)cdiv(p.M, 32 * sh.tm * sh.wm);
+  p.tn = (int)cdiv(p.N, 32 * sh.tn * sh.wn);
+  split_steps(p, 768);  // (three resident workgroups per CU)
   return true;
 }
 

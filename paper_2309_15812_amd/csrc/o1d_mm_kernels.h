@@ -235,8 +235,9 @@ struct Tile {
     for (int i = 0; i < N; ++i) {
       float v[V];
       if (held) {
+        const float scale = __uint_as_float(w[i][2]);
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = (float)(int8_t)(w[i][e / 4] >> (8 * (e & 3))) * __uint_as_float(w[i][2]);
+        for (int e = 0; e < V; ++e) v[e] = unround(w[i][e / 4] ^ 0x80808080u, e & 3, scale);
       } else {
         T t[V];
         __builtin_memcpy(t, &w[i], 16);
@@ -659,7 +660,7 @@ template <typename T, int KIND>
 hipError_t launch_kind(const MmPlan& pl, hipStream_t stream) {
   if constexpr (KIND == kWgrad) {
     if (pl.p.made) return pl.shape == k64x64 ? launch_shape<T, KIND, k64x64, true>(pl, stream)
-                                             : launch_shape<T, KIND, k128x64, true>(pl, stream);
+                                             : launch_shape<T, KIND, k192x64, true>(pl, stream);
   }
   switch (pl.shape) {
     case k128x128: return launch_shape<T, KIND, k128x128>(pl, stream);

@@ -145,12 +145,13 @@ struct MmPlan {
   MmParams p;
 };
 
-enum ShapeId { k128x128, k64x256, k64x64, k128x96, k64x128, k128x64, k128x192, kShapeCount };
+enum ShapeId { k128x128, k64x256, k64x64, k128x96, k64x128, k128x64, k128x192, k192x64, kShapeCount };
 constexpr Shape kShapes[kShapeCount] = {{2, 2, 2, 2}, {1, 4, 2, 2}, {2, 2, 1, 1}, {4, 1, 1, 3}, {2, 2, 1, 2}, {4, 1, 1, 2},
-                                         {2, 2, 2, 3}};
-// (128 x 192 is planned for float32 alone, 64 x 256 for its weight gradients)
+                                         {2, 2, 2, 3}, {2, 2, 3, 1}};
+// (128 x 192 is planned for float32 alone, 64 x 256 for its weight gradients, 192 x 64
+// for weight gradients that make their operand)
 constexpr bool shape_used(int kind, int esize, int shape) {
-  return shape == k128x192 ? esize == 4 : (shape == k64x256 ? kind == kWgrad && esize == 4 : true);
+  return shape == k192x64 ? false : shape == k128x192 ? esize == 4 : (shape == k64x256 ? kind == kWgrad && esize == 4 : true);
 }
 constexpr int kStepBytes = 128;  // k per step: 32 float32 or 64 bfloat16
 
@@ -167,8 +168,8 @@ MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups, bool whole
 
 // Whether a weight gradient makes act(x) itself as it stages it, once per tile
 // along m, instead of reading it from a pass of its own (a launch, and act(x)
-// through memory): where all tiles together make few elements.
-bool make_operand(MmPlan& pl);
+// through memory); plans the product for it if so.
+bool make_operand(MmPlan& pl, int act, bool held, int esize);
 
 #define O1D_MM_DECL(T)                                                                    \
   hipError_t launch_mm_fwd_##T(const MmPlan& pl, hipStream_t stream);                     \

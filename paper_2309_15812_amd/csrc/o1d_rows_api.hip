@@ -132,13 +132,14 @@ struct WgradSpace {
   size_t bytes() const { return part + operand; }
 };
 
-WgradSpace wgrad_space(int M, int I, int O, bool rewritten, o1d_dtype_t dt) {
+WgradSpace wgrad_space(int M, int I, int O, o1d_act_t act, bool held, o1d_dtype_t dt) {
   WgradSpace s;
+  const bool rewritten = held || act != O1D_ACT_NONE;
   const int es = (int)elem_size(dt), run = 16 / es;
   s.plan = rows::plan_mm(rows::kWgrad, O, I, M, es, false, true);
+  s.made = rewritten && rows::make_operand(s.plan, (int)act, held, es);
   s.part = s.plan.p.nsplit > 1 ? round256((size_t)s.plan.p.nsplit * ((size_t)O * I + O) * sizeof(float)) : kNoSpace;
   s.ldx = rows::cdiv(I, run) * run;
-  s.made = rewritten && rows::make_operand(s.plan);
   s.operand = rewritten && !s.made ? round256((size_t)M * s.ldx * es) : 0;
   return s;
 }
@@ -327,7 +328,7 @@ o1d_status_t o1d_linear_bwd_input(const void* dy, long long lddy, const void* w,
 size_t o1d_linear_bwd_weight_workspace_bytes(int M, int I, int O, o1d_act_t act, int held, o1d_dtype_t dtype) {
   const char* fn = "o1d_linear_bwd_weight";
   if (check_dims(fn, M, I, "I", dtype) != O1D_OK || check_dims(fn, M, O, "O", dtype) != O1D_OK || M == 0) return 0;
-  return wgrad_space(M, I, O, held || act != O1D_ACT_NONE, dtype).bytes();
+  return check_act(fn, act) == O1D_OK ? wgrad_space(M, I, O, act, held != 0, dtype).bytes() : 0;
 }
 
 o1d_status_t o1d_linear_bwd_weight(const void* x, long long ldx, const signed char* xq, const float* xscale, o1d_act_t act,
@@ -347,7 +348,7 @@ o1d_status_t o1d_linear_bwd_weight(const void* x, long long ldx, const signed ch
   hipStream_t s = static_cast<hipStream_t>(stream);
   WgradSpace space{};
   if (M > 0) {
-    space = wgrad_space(M, I, O, rewritten, dtype);
+    space = wgrad_space(M, I, O, act, xq != nullptr, dtype);
     O1D_TRY(check_blocks(fn, space.plan));
   }
   const size_t need = M > 0 ? space.bytes() : 0;

@@ -248,12 +248,15 @@ __device__ __forceinline__ uint2 round8(const float (&v)[8], const Scale& s) {
   return make_uint2(four(0), four(4));
 }
 
-// q scale: the bytes plus 128 are converted (one instruction each), and
-// (q + 128) scale - 128 scale is rounded once, as q scale is.
+// q scale for byte e of a word of integers plus 128 (the word ^ 0x80808080): a
+// byte is converted in one instruction, and (q + 128) scale - 128 scale is rounded once, as q scale is.
+__device__ __forceinline__ float unround(uint32_t word, int e, float scale) {
+  return fmaf((float)((word >> (8 * e)) & 0xffu), scale, -128.f * scale);
+}
 __device__ __forceinline__ void unround8(uint2 w, float scale, float (&v)[8]) {
   const uint32_t u[2] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u};
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = fmaf((float)((u[e >> 2] >> (8 * (e & 3))) & 0xffu), scale, -128.f * scale);
+  for (int e = 0; e < 8; ++e) v[e] = unround(u[e >> 2], e & 3, scale);
 }
 
 }  // namespace rows

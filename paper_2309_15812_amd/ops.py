@@ -6,6 +6,8 @@ libo1d.so.  theta is a float32 tensor of per-channel angles in degrees.
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import _lib
@@ -314,15 +316,22 @@ def _rows(t: torch.Tensor, what: str) -> tuple[torch.Tensor, int, int, int]:
     return v, M, C, ld
 
 
+def _run(fn: str, *args) -> None:
+    status = getattr(_lib.lib(), fn)(*args)
+    if status:
+        _lib.check(fn, status)
+
+
 def _vector(t: torch.Tensor, what: str, C: int, like: torch.Tensor) -> torch.Tensor:
-    if t.shape != (C,) or t.dtype != like.dtype or t.device != like.device or not t.is_contiguous():
+    if t.dim() != 1 or t.numel() != C or t.dtype is not like.dtype or t.get_device() != like.get_device() \
+            or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous ({C},) tensor of {like.dtype} on {like.device}, got "
                          f"{tuple(t.shape)} {t.dtype} {t.device}")
     return t
 
 
 def _weight(w: torch.Tensor, like: torch.Tensor) -> tuple[int, int]:
-    if w.dim() != 2 or w.dtype != like.dtype or w.device != like.device or not w.is_contiguous():
+    if w.dim() != 2 or w.dtype is not like.dtype or w.get_device() != like.get_device() or not w.is_contiguous():
         raise ValueError(f"w must be a contiguous (O, I) tensor of {like.dtype} on {like.device}, got {tuple(w.shape)} "
                          f"{w.dtype} {w.device}")
     return int(w.shape[0]), int(w.shape[1])
@@ -336,7 +345,7 @@ def _act(act: str) -> int:
 
 def _same(t: torch.Tensor, what: str, M: int, C: int, like: torch.Tensor) -> tuple[torch.Tensor, int]:
     """t as rows, checked to be M x C like `like`; (t, row stride)."""
-    if t.dtype != like.dtype or t.device != like.device:
+    if t.dtype is not like.dtype or t.get_device() != like.get_device():
         raise ValueError(f"{what} must be {like.dtype} on {like.device}, got {t.dtype} on {t.device}")
     v, m, c, ld = _rows(t, what)
     if (m, c) != (M, C):
@@ -381,7 +390,7 @@ class Packed8:
 def _either(t, what: str, M: int, C: int, like: torch.Tensor) -> tuple:
     """(pointer, row stride, q, scale) of a tensor or a checkpoint of M rows of C features."""
     if isinstance(t, Packed8):
-        if (t.rows, t.cols) != (M, C) or t.q.device != like.device:
+        if t.cols != C or t.q.shape[0] != M or t.q.get_device() != like.get_device():
             raise ValueError(f"{what} is a checkpoint of {t.rows} rows of {t.cols} features on {t.q.device}, expected "
                              f"{M} of {C} on {like.device}")
         return None, C, t.q.data_ptr(), t.scale.data_ptr()
@@ -414,8 +423,7 @@ def pack8(x: torch.Tensor) -> Packed8:
     dt = _dt(x)
     v, M, C, ld = _rows(x, "x")
     held = Packed8.empty(M, C, x.device)
-    _lib.check("o1d_pack", _lib.call("o1d_pack", v.data_ptr(), ld, held.q.data_ptr(), held.scale.data_ptr(), M, C, dt,
-                                     _stream(x)))
+    _run("o1d_pack", v.data_ptr(), ld, held.q.data_ptr(), held.scale.data_ptr(), M, C, dt, _stream(x))
     return held
 
 
@@ -431,8 +439,8 @@ def unpack8(held: Packed8, dtype: torch.dtype, act: str = "none", out: torch.Ten
             raise ValueError(f"out must be {dtype} on {held.q.device}")
         y = out
         v, ld = _same(out, "out", held.rows, held.cols, out)
-    _lib.check("o1d_unpack", _lib.call("o1d_unpack", held.q.data_ptr(), held.scale.data_ptr(), _act(act), v.data_ptr(),
-                                       ld, held.rows, held.cols, _DT[dtype], _stream(held.q)))
+    _run("o1d_unpack", held.q.data_ptr(), held.scale.data_ptr(), _act(act), v.data_ptr(), ld, held.rows, held.cols,
+         _DT[dtype], _stream(held.q))
     return y
 
 
@@ -445,11 +453,12 @@ def ln_fwd(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor, eps: float = 1e-6,
     _vector(b, "b", C, x)
     y = _into(out, x, C)
     mean, rstd = x.new_empty((M,), dtype=torch.float32), x.new_empty((M,), dtype=torch.float32)
-    _lib.check("o1d_ln_fwd", _lib.call("o1d_ln_fwd", v.data_ptr(), ld, w.data_ptr(), b.data_ptr(), y.data_ptr(), C,
-                                       mean.data_ptr(), rstd.data_ptr(), M, C, eps, dt, _stream(x)))
+    _run("o1d_ln_fwd", v.data_ptr(), ld, w.data_ptr(), b.data_ptr(), y.data_ptr(), C, mean.data_ptr(), rstd.data_ptr(),
+         M, C, eps, dt, _stream(x))
     return y, mean, rstd
 
 
+@functools.lru_cache(maxsize=4096)
 def ln_workspace_bytes(M: int, C: int, dtype: torch.dtype) -> int:
     return int(_lib.lib().o1d_ln_bwd_workspace_bytes(M, C, _DT[dtype]))
 
@@ -463,15 +472,15 @@ def ln_bwd(x: torch.Tensor | Packed8, dy: torch.Tensor, mean: torch.Tensor, rstd
     px, ldx, q, scale = _either(x, "x", M, C, dy)
     _vector(w, "w", C, dy)
     for t, n in ((mean, "mean"), (rstd, "rstd")):
-        if t.shape != (M,) or t.dtype != torch.float32 or t.device != dy.device or not t.is_contiguous():
+        if t.dim() != 1 or t.numel() != M or t.dtype is not torch.float32 or t.get_device() != dy.get_device() \
+                or not t.is_contiguous():
             raise ValueError(f"{n} must be a contiguous float32 ({M},) tensor on {dy.device}")
     dx, dw, db = (None, None, None) if out is None else out
     dx = _into(dx, dy, C)
     dw, db = (torch.empty_like(w) if t is None else _out(t, w) for t in (dw, db))
     workspace, nbytes = _scratch(workspace, dy, ln_workspace_bytes(M, C, dy.dtype))
-    _lib.check("o1d_ln_bwd", _lib.call("o1d_ln_bwd", px, ldx, q, scale, g.data_ptr(), lddy, mean.data_ptr(),
-                                       rstd.data_ptr(), w.data_ptr(), dx.data_ptr(), C, dw.data_ptr(), db.data_ptr(), M,
-                                       C, dt, workspace.data_ptr(), nbytes, _stream(dy)))
+    _run("o1d_ln_bwd", px, ldx, q, scale, g.data_ptr(), lddy, mean.data_ptr(), rstd.data_ptr(), w.data_ptr(),
+         dx.data_ptr(), C, dw.data_ptr(), db.data_ptr(), M, C, dt, workspace.data_ptr(), nbytes, _stream(dy))
     return dx, dw, db
 
 
@@ -492,11 +501,10 @@ def linear_fwd(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor | None = None, 
     y = _into(out, x, O)
     pre = _into(None, x, O) if save == "pre" else None
     held = Packed8.empty(M, O, x.device) if save == "pack8" else None
-    _lib.check("o1d_linear_fwd", _lib.call(
-        "o1d_linear_fwd", v.data_ptr(), ldx, w.data_ptr(), None if b is None else b.data_ptr(), a,
-        None if res is None else res.data_ptr(), ldres, y.data_ptr(), O, None if pre is None else pre.data_ptr(), O,
-        None if held is None else held.q.data_ptr(), None if held is None else held.scale.data_ptr(), M, I, O, dt,
-        _stream(x)))
+    _run("o1d_linear_fwd", v.data_ptr(), ldx, w.data_ptr(), None if b is None else b.data_ptr(), a,
+         None if res is None else res.data_ptr(), ldres, y.data_ptr(), O, None if pre is None else pre.data_ptr(), O,
+         None if held is None else held.q.data_ptr(), None if held is None else held.scale.data_ptr(), M, I, O, dt,
+         _stream(x))
     return y if save is None else (y, pre if held is None else held)
 
 
@@ -513,11 +521,12 @@ def linear_bwd_input(dy: torch.Tensor, w: torch.Tensor, pre: torch.Tensor | Pack
         raise ValueError("pre and act are given together")
     p, ldp, q, scale = (None, I, None, None) if pre is None else _either(pre, "pre", M, I, dy)
     dx = _into(out, dy, I)
-    _lib.check("o1d_linear_bwd_input", _lib.call("o1d_linear_bwd_input", g.data_ptr(), lddy, w.data_ptr(), a, p, ldp, q,
-                                                 scale, dx.data_ptr(), I, M, I, O, dt, _stream(dy)))
+    _run("o1d_linear_bwd_input", g.data_ptr(), lddy, w.data_ptr(), a, p, ldp, q, scale, dx.data_ptr(), I, M, I, O, dt,
+         _stream(dy))
     return dx
 
 
+@functools.lru_cache(maxsize=4096)
 def linear_workspace_bytes(M: int, I: int, O: int, dtype: torch.dtype, act: str = "none", packed: bool = False) -> int:
     return int(_lib.lib().o1d_linear_bwd_weight_workspace_bytes(M, I, O, _act(act), int(packed), _DT[dtype]))
 
@@ -535,9 +544,8 @@ def linear_bwd_weight(x: torch.Tensor | Packed8, dy: torch.Tensor, act: str = "n
     dw = dy.new_empty((O, I)) if dw is None else _out(dw, dy, (O, I))
     db = None if not bias else dy.new_empty((O,)) if db is None else _out(db, dy, (O,))
     workspace, nbytes = _scratch(workspace, dy, linear_workspace_bytes(M, I, O, dy.dtype, act, q is not None))
-    _lib.check("o1d_linear_bwd_weight", _lib.call(
-        "o1d_linear_bwd_weight", p, ldx, q, scale, a, g.data_ptr(), lddy, dw.data_ptr(),
-        None if db is None else db.data_ptr(), M, I, O, dt, workspace.data_ptr(), nbytes, _stream(dy)))
+    _run("o1d_linear_bwd_weight", p, ldx, q, scale, a, g.data_ptr(), lddy, dw.data_ptr(),
+         None if db is None else db.data_ptr(), M, I, O, dt, workspace.data_ptr(), nbytes, _stream(dy))
     return dw, db
 
 
@@ -547,8 +555,7 @@ def act_bwd(pre: torch.Tensor | Packed8, dy: torch.Tensor, act: str, out: torch.
     g, M, C, lddy = _rows(dy, "dy")
     p, ldp, q, scale = _either(pre, "pre", M, C, dy)
     dh = _into(out, dy, C)
-    _lib.check("o1d_act_bwd", _lib.call("o1d_act_bwd", p, ldp, q, scale, a, g.data_ptr(), lddy, dh.data_ptr(), C, M, C,
-                                        dt, _stream(dy)))
+    _run("o1d_act_bwd", p, ldp, q, scale, a, g.data_ptr(), lddy, dh.data_ptr(), C, M, C, dt, _stream(dy))
     return dh
 
 
