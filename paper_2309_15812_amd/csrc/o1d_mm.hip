@@ -19,7 +19,7 @@ struct Cost {
 };
 constexpr Cost kCost[3][kShapeCount] = {
     // float32: 128 x 128, 64 x 256, 64 x 64, 128 x 96, 64 x 128, 128 x 64, 128 x 192
-    {{5.f, 3.0f, 2}, {}, {5.f, 1.9f, 4}, {7.f, 1.9f, 2}, {7.5f, 2.2f, 3}, {6.5f, 2.2f, 3}, {8.f, 4.f, 2}, {}},
+    {{5.f, 3.0f, 2}, {}, {5.f, 1.9f, 4}, {7.f, 1.9f, 2}, {}, {6.5f, 2.2f, 3}, {8.f, 4.f, 2}, {}},
     // bfloat16, whole runs
     {{3.7f, 0.90f, 2}, {}, {3.3f, 0.45f, 3}, {3.0f, 0.72f, 2}, {3.0f, 0.68f, 3}, {3.0f, 0.68f, 3}},
     // bfloat16, other runs
@@ -28,12 +28,13 @@ constexpr Cost kCost[3][kShapeCount] = {
 // Weight gradients run as many pieces as fill the GPU whatever the tile, so
 // the tile that computes least past the output's edge is taken, weighted by
 // the time of its products (float32: smaller tiles make more pieces per product).
-constexpr float kArea[2][kShapeCount] = {{1.f, 1.02f, 1.5f, 1.15f, 1.3f, 1.3f, 1.1f}, {1.05f, 1.f, 1.3f, 1.35f, 1.f, 1.f}};
+constexpr float kArea[2][kShapeCount] = {{1.f, 1.02f, 1.5f, 1.15f, 1.3f, 1.3f, 1.1f}, {0.f, 0.f, 1.3f, 0.f, 1.f, 1.f}};
 constexpr int kWgradBlocks = 512;
 
 // Time of the kernels of few rows (microseconds, measured as above for 1 .. 2000
 // rows): the waits of a workgroup's waves for their pieces of 32 k, of which
 // a launch that fills the GPU once hides none, and the workgroups' own work.
+constexpr int kFewMost = 1 << 16;
 double few_cost(int M, int N, int K, int esize, bool groups) {
   const double pieces = (double)cdiv(K, 32), wgs = (double)cdiv(N, groups ? 64 : 16) * (double)cdiv(M, 64);
   const double share = M <= 16 ? 0.35 : (M <= 32 ? 0.6 : 1.), waves = groups ? 3. : 1.;
@@ -83,7 +84,7 @@ MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups, bool whole
       p.tn = (int)tn;
     }
   }
-  pl.few = kind != kWgrad && few_cost(M, N, K, esize, groups) < best;
+  pl.few = kind != kWgrad && M <= kFewMost && few_cost(M, N, K, esize, groups) < best;
   p.nsplit = 1;
   p.per = p.steps;
   if (kind == kWgrad) {

@@ -656,6 +656,12 @@ hipError_t launch_shape(const MmPlan& pl, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <typename T, int KIND, int SHAPE>
+hipError_t launch_planned(const MmPlan& pl, hipStream_t stream) {
+  if constexpr (shape_used(KIND, (int)sizeof(T), SHAPE)) return launch_shape<T, KIND, SHAPE>(pl, stream);
+  return hipErrorInvalidValue;  // (no plan has it)
+}
+
 template <typename T, int KIND>
 hipError_t launch_kind(const MmPlan& pl, hipStream_t stream) {
   if constexpr (KIND == kWgrad) {
@@ -663,17 +669,14 @@ hipError_t launch_kind(const MmPlan& pl, hipStream_t stream) {
                                              : launch_shape<T, KIND, k192x64, true>(pl, stream);
   }
   switch (pl.shape) {
-    case k128x128: return launch_shape<T, KIND, k128x128>(pl, stream);
-    case k64x256:
-      if constexpr (shape_used(KIND, (int)sizeof(T), k64x256)) return launch_shape<T, KIND, k64x256>(pl, stream);
-      return hipErrorInvalidValue;
-    case k64x64: return launch_shape<T, KIND, k64x64>(pl, stream);
-    case k128x96: return launch_shape<T, KIND, k128x96>(pl, stream);
-    case k64x128: return launch_shape<T, KIND, k64x128>(pl, stream);
-    case k128x192:
-      if constexpr (shape_used(KIND, (int)sizeof(T), k128x192)) return launch_shape<T, KIND, k128x192>(pl, stream);
-      return hipErrorInvalidValue;
-    default: return launch_shape<T, KIND, k128x64>(pl, stream);
+    case k128x128: return launch_planned<T, KIND, k128x128>(pl, stream);
+    case k64x256: return launch_planned<T, KIND, k64x256>(pl, stream);
+    case k64x64: return launch_planned<T, KIND, k64x64>(pl, stream);
+    case k128x96: return launch_planned<T, KIND, k128x96>(pl, stream);
+    case k64x128: return launch_planned<T, KIND, k64x128>(pl, stream);
+    case k128x64: return launch_planned<T, KIND, k128x64>(pl, stream);
+    case k128x192: return launch_planned<T, KIND, k128x192>(pl, stream);
+    default: return hipErrorInvalidValue;
   }
 }
 

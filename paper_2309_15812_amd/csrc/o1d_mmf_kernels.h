@@ -181,8 +181,7 @@ __global__ __launch_bounds__(kMmThreads, (FastGeo<T, KIND, SHAPE>::kWaves)) void
     base_a += step_a;
     base_b += step_b;
   };
-  // The next step's loads, whatever it is (nothing to load: the last step's
-  // run again, which is never read).
+  // The next step's loads, whatever it is (nothing to load: zeros that are never read).
   auto issue = [&]() __attribute__((always_inline)) {
     if (ahead_left == 0 && ahead_id + stride < last) {
       ahead_id += stride;
@@ -302,14 +301,20 @@ hipError_t launch_fast_shape(const MmPlan& pl, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <typename T, int KIND, int SHAPE>
+hipError_t launch_fast_planned(const MmPlan& pl, hipStream_t stream) {
+  if constexpr (shape_used(KIND, (int)sizeof(T), SHAPE)) return launch_fast_shape<T, KIND, SHAPE>(pl, stream);
+  return hipErrorInvalidValue;  // (no plan has it)
+}
+
 template <typename T, int KIND>
 hipError_t launch_fast_kind(const MmPlan& pl, hipStream_t stream) {
   switch (pl.shape) {
-    case k128x128: return launch_fast_shape<T, KIND, k128x128>(pl, stream);
-    case k64x64: return launch_fast_shape<T, KIND, k64x64>(pl, stream);
-    case k128x96: return launch_fast_shape<T, KIND, k128x96>(pl, stream);
-    case k64x128: return launch_fast_shape<T, KIND, k64x128>(pl, stream);
-    case k128x64: return launch_fast_shape<T, KIND, k128x64>(pl, stream);
+    case k128x128: return launch_fast_planned<T, KIND, k128x128>(pl, stream);
+    case k64x64: return launch_fast_planned<T, KIND, k64x64>(pl, stream);
+    case k128x96: return launch_fast_planned<T, KIND, k128x96>(pl, stream);
+    case k64x128: return launch_fast_planned<T, KIND, k64x128>(pl, stream);
+    case k128x64: return launch_fast_planned<T, KIND, k128x64>(pl, stream);
     default: return hipErrorInvalidValue;
   }
 }

@@ -148,10 +148,20 @@ struct MmPlan {
 enum ShapeId { k128x128, k64x256, k64x64, k128x96, k64x128, k128x64, k128x192, k192x64, kShapeCount };
 constexpr Shape kShapes[kShapeCount] = {{2, 2, 2, 2}, {1, 4, 2, 2}, {2, 2, 1, 1}, {4, 1, 1, 3}, {2, 2, 1, 2}, {4, 1, 1, 2},
                                          {2, 2, 2, 3}, {2, 2, 3, 1}};
-// (128 x 192 is planned for float32 alone, 64 x 256 for its weight gradients, 192 x 64
-// for weight gradients that make their operand)
+// Tiles that are planned, by what they measured: 128 x 192 for float32 alone, 64 x
+// 256 for its weight gradients, and no large ones for bfloat16 weight gradients;
+// 192 x 64 for weight gradients that make their operand (make_operand).
 constexpr bool shape_used(int kind, int esize, int shape) {
-  return shape == k192x64 ? false : shape == k128x192 ? esize == 4 : (shape == k64x256 ? kind == kWgrad && esize == 4 : true);
+  switch (shape) {
+    case k128x128:
+    case k128x96: return kind != kWgrad || esize == 4;
+    case k64x256: return kind == kWgrad && esize == 4;
+    case k64x64:
+    case k128x64: return true;
+    case k64x128: return kind == kWgrad || esize == 2;
+    case k128x192: return esize == 4;
+    default: return false;
+  }
 }
 constexpr int kStepBytes = 128;  // k per step: 32 float32 or 64 bfloat16
 

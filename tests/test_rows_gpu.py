@@ -442,10 +442,14 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(y[-300:], ty) and torch.equal(mean[-300:], tm) and torch.equal(rstd[-300:], tr)
     w = randn(C, C, seed=5, dt=BF16, std=0.1)
     z, held = ops.linear_fwd(x, w, act="gelu", save="pack8", out=y)
-    tz, th = ops.linear_fwd(tail, w, act="gelu", save="pack8")
-    assert torch.equal(z[-300:], tz) and torch.equal(held.q[-300:], th.q) and torch.equal(held.scale[-300:], th.scale)
+    # (300 rows alone are summed in another order: bounds as in the tests of the products)
+    h = tail.double() @ w.double().t()
+    eh = (C + 8) * 2.0 ** -24 * (tail.double().abs() @ w.double().abs().t())
+    ey = 1.2 * eh + 2e-6 * (1 + h.abs())
+    near(z[-300:], gate(h, "gelu")[0], ey + u(BF16) * (gate(h, "gelu")[0].abs() + ey), "gelu")
+    th = ops.Packed8(held.q[-300:].contiguous(), held.scale[-300:].contiguous(), C)
+    near(value64(th), h, eh + (0.5 + 1e-4) * th.scale.double().repeat_interleave(64, 1)[:, :C], "checkpoint")
     dx = ops.linear_bwd_input(x, w, pre=held, act="gelu", out=y)
-    # (300 rows alone are summed in another order)
     g, slope = tail.double() @ w.double(), gate(value64(th), "gelu")[1]
     e = (C + 8) * 2.0 ** -24 * (tail.double().abs() @ w.double().abs())
     near(dx[-300:], g * slope, 1.2 * e + 4e-6 * (1 + value64(th).abs()) * (g.abs() + e) + u(BF16) * ((g * slope).abs() + 1.2 * e),
@@ -526,3 +530,56 @@ def test_products_of_extreme_values(dt):
     dw, db = ops.linear_bwd_weight(x, torch.ones(M, O, device=DEV, dtype=dt))
     assert torch.isnan(dw[:, 0]).all() and (dw[:, 7] == math.inf).all() and (dw[:, 71] == -math.inf).all()
     assert not dw[:, 9].any() and (db == M).all()
+
+
+# One size at least for every tile that the products are planned with (aligned and not), beside the small sizes above.
+TILES_BF16 = [(20000, 16, 300), (20000, 16, 32), (12544, 16, 130), (1500, 16, 32), (1500, 200, 32), (50176, 16, 96),
+              (20000, 48, 384), (6000, 696, 200)]
+TILES_BF16_ODD = [(20000, 17, 300), (70000, 17, 32), (33000, 17, 96), (33000, 17, 128), (3000, 17, 300), (6000, 699, 200)]
+TILES_F32 = [(33000, 16, 96), (33000, 16, 130), (70000, 16, 32), (33000, 48, 96), (1500, 16, 256), (33000, 17, 131)]
+
+
+@pytest.mark.parametrize("dt,M,K,N", [(BF16, *c) for c in TILES_BF16 + TILES_BF16_ODD] + [(F32, *c) for c in TILES_F32])
+def test_every_tile(dt, M, K, N):
+    odd = K % 8 != 0
+    x = sliced(M, K, 1 if odd else 0, 100, dt)
+    w, b = randn(N, K, seed=101, dt=dt, std=K ** -0.5), randn(N, seed=102, dt=dt)
+    res = sliced(M, N, 8, 103, dt)
+    X, W = x.double(), w.double()
+    h, mag = X @ W.t() + b.double(), X.abs() @ W.abs().t() + b.double().abs()
+    eh = (K + 8) * 2.0 ** -24 * mag
+    y = ops.linear_fwd(x, w, b, residual=res)
+    want = h + res.double()
+    near(y, want, eh + u(dt) * (want.abs() + eh) + 2.0 ** -23 * h.abs(), "y")
+    y, held = ops.linear_fwd(x, w, b, act="gelu", save="pack8")
+    want = gate(h, "gelu")[0]
+    ey = 1.2 * eh + 2e-6 * (1 + h.abs())
+    near(y, want, ey + u(dt) * (want.abs() + ey), "gelu")
+    step = held.scale.double().repeat_interleave(64, 1)[:, :N]
+    near(value64(held), h, eh + (0.5 + 1e-4) * step, "checkpoint")
+    # the input gradient with N features in and K out
+    dy, v = sliced(M, K, 1 if odd else 0, 104, dt), randn(K, N, seed=105, dt=dt, std=K ** -0.5)
+    g, mag = dy.double() @ v.double(), dy.double().abs() @ v.double().abs()
+    e = (K + 8) * 2.0 ** -24 * mag
+    near(ops.linear_bwd_input(dy, v), g, e + u(dt) * (g.abs() + e), "dx")
+    slope = gate(value64(held), "gelu")[1]
+    near(ops.linear_bwd_input(dy, v, pre=held, act="gelu"), g * slope,
+         1.2 * e + 4e-6 * (1 + h.abs() + step) * (g.abs() + e) + u(dt) * ((g * slope).abs() + 1.2 * e), "dx of gelu")
+
+
+@pytest.mark.parametrize("dt,O,I,M", [(BF16, 96, 130, 20000), (BF16, 130, 96, 20000), (BF16, 96, 136, 20000), (BF16, 136, 96, 20000),
+                                      (BF16, 40, 40, 600), (BF16, 192, 768, 30000), (F32, 96, 256, 20000), (F32, 512, 130, 9000),
+                                      (F32, 512, 40, 9000), (F32, 96, 130, 20000), (F32, 96, 96, 20000), (F32, 40, 768, 9000),
+                                      (F32, 40, 40, 600), (F32, 170, 300, 4000)])
+def test_every_weight_gradient_tile(dt, O, I, M):
+    dy, x = randn(M, O, seed=110, dt=dt), randn(M, I, seed=111, dt=dt)
+    D = dy.double()
+    edb = (M + 16) * 2.0 ** -24 * D.abs().sum(0)
+    for src, act in ((x, "none"), (ops.pack8(x), "gelu"), (x, "silu")):
+        X = value64(src) if act == "gelu" else x.double()
+        a = gate(X, act)[0]
+        want, mag = D.t() @ a, D.abs().t() @ a.abs()
+        e = (M + 16) * 2.0 ** -24 * mag + (act != "none") * (u(dt) * mag + 2e-6 * (D.abs().t() @ (1 + X.abs())))
+        dw, db = ops.linear_bwd_weight(src, dy, act=act)
+        near(dw, want, e + u(dt) * (want.abs() + e), act)
+        near(db, D.sum(0), edb + u(dt) * (D.sum(0).abs() + edb), "db")
