@@ -11,43 +11,89 @@ namespace rows {
 namespace {
 
 // Time of a product as rounds of resident workgroups, each with a time of its
-// own and a time per step of 128 bytes of k (microseconds, measured over
-// 784 .. 200704 rows and 96 .. 2048 features; they fit within about 15%).
+// own and a time per step of 128 bytes of k (microseconds).  Forward products and input
+// gradients: measured at 2200 sizes of 16 .. 200704 rows and 16 .. 2048 features with
+// each tile; the model fits within 16 to 19%, the plan it takes is 2 to 3% from
+// the best measured one.
 struct Cost {
   float first, step;
   int resident;  // workgroups of a CU
 };
+constexpr double kLaunch = 2.3, kAlone = 0.25;  // (the step's time of a CU's only workgroup, as a share)
 constexpr Cost kCost[3][kShapeCount] = {
-    // float32: 128 x 128, 64 x 256, 64 x 64, 128 x 96, 64 x 128, 128 x 64, 128 x 192
-    {{5.f, 3.0f, 2}, {}, {5.f, 1.9f, 4}, {7.f, 1.9f, 2}, {}, {6.5f, 2.2f, 3}, {8.f, 4.f, 2}, {}},
+    // float32: 128 x 128, 64 x 64, 128 x 96, 64 x 128, 128 x 64, 128 x 192
+    {{10.7f, 2.95f, 2}, {4.5f, 2.05f, 4}, {7.8f, 2.45f, 2}, {}, {6.9f, 2.55f, 3}, {20.f, 3.85f, 2}, {}},
     // bfloat16, whole runs
-    {{3.7f, 0.90f, 2}, {}, {3.3f, 0.45f, 3}, {3.0f, 0.72f, 2}, {3.0f, 0.68f, 3}, {3.0f, 0.68f, 3}},
+    {{6.6f, 1.03f, 2}, {2.5f, 0.61f, 3}, {5.0f, 0.89f, 2}, {4.5f, 0.88f, 3}, {4.45f, 0.99f, 3}},
     // bfloat16, other runs
-    {{10.f, 1.2f, 2}, {}, {6.f, 0.8f, 4}, {7.f, 0.9f, 2}, {10.f, 1.f, 3}, {10.f, 1.f, 3}}};
+    {{8.2f, 1.5f, 2}, {3.65f, 1.0f, 4}, {5.9f, 1.33f, 2}, {5.6f, 1.32f, 3}, {5.8f, 1.34f, 3}}};
 
-// Weight gradients run as many pieces as fill the GPU whatever the tile, so
-// the tile that computes least past the output's edge is taken, weighted by
-// the time of its products (float32: smaller tiles make more pieces per product).
-constexpr float kArea[2][kShapeCount] = {{1.f, 1.02f, 1.5f, 1.15f, 1.3f, 1.3f, 1.1f}, {0.f, 0.f, 1.3f, 0.f, 1.f, 1.f}};
-constexpr int kWgradBlocks = 512;
+// Weight gradients in the same terms, measured at 600 sizes of 300 .. 200704
+// rows with 2 to 12 numbers of pieces for each tile (the model fits within 7 to
+// 12%; the plan it takes is 3 to 5% from the best measured one.  As many pieces
+// as make about 512 workgroups, and the tile by its area alone, was 11 to 14%).
+constexpr Cost kWgradCost[3][kShapeCount] = {
+    {{1.f, 3.1f, 2}, {0.f, 2.1f, 4}, {0.f, 2.6f, 2}, {0.f, 2.8f, 3}, {0.f, 2.65f, 3}, {2.7f, 4.5f, 2}, {}},
+    {{}, {0.f, 0.61f, 3}, {}, {0.f, 0.91f, 3}, {0.f, 0.90f, 3}},
+    {{}, {0.f, 1.19f, 4}, {}, {0.f, 1.42f, 3}, {0.f, 1.41f, 3}}};
+// Those that make their operand, 64 x 64 and 192 x 64: a step's time by activation
+// (none, relu, gelu, gelu_tanh, silu).  50176 x 768 -> 192 bfloat16 from a checkpoint
+// with GELU: 54 us against 68 with a pass of its own.
+constexpr int kMadeShapes[2] = {k64x64, k192x64}, kMadeResident[2][2] = {{4, 2}, {4, 3}};
+constexpr float kMadeStep[2][2][kActs] = {{{2.5f, 2.5f, 3.6f, 3.4f, 3.35f}, {3.5f, 3.5f, 4.4f, 4.3f, 4.0f}},
+                                          {{1.6f, 1.75f, 2.3f, 2.1f, 1.95f}, {2.75f, 3.0f, 3.25f, 3.15f, 3.05f}}};
+constexpr double kWgradLaunch = 3.5, kWgradAlone = 0.4;
+constexpr double kSumEach = 0.02, kSumElement = 1.6e-6;  // the sum of the pieces: per piece, per element
+constexpr double kPassBytes = 4e6;                       // a pass of its own: bytes per microsecond
 
-// Time of the kernels of few rows (microseconds, measured as above for 1 .. 2000
-// rows): the waits of a workgroup's waves for their pieces of 32 k, of which
-// a launch that fills the GPU once hides none, and the workgroups' own work.
-constexpr int kFewMost = 1 << 16;
-double few_cost(int M, int N, int K, int esize, bool groups) {
-  const double pieces = (double)cdiv(K, 32), wgs = (double)cdiv(N, groups ? 64 : 16) * (double)cdiv(M, 64);
-  const double share = M <= 16 ? 0.35 : (M <= 32 ? 0.6 : 1.), waves = groups ? 3. : 1.;
-  return esize == 2 ? 3.3 + 0.14 * share * waves * pieces + wgs * share * (0.003 + 0.0005 * pieces)
-                    : 3.5 + 0.33 * share * waves * pieces + wgs * share * (0.006 + 0.001 * pieces);
+double rounds(const Cost& c, long long blocks, double steps, double alone) {
+  // (a last round of fewer workgroups per CU has shorter steps)
+  const long long slots = 256 * c.resident, rest = blocks % slots;
+  double t = (double)(blocks / slots) * (c.first + c.step * steps);
+  if (rest) t += c.first + c.step * steps * (alone + (1. - alone) * (double)cdiv(rest, 256) / c.resident);
+  return t;
 }
-// A weight gradient's k in pieces of at least four steps.
-void split_steps(MmParams& p, int blocks = kWgradBlocks) {
-  const long long want = cdiv(blocks, (long long)p.tm * p.tn), most = p.steps / 4;
-  const long long pieces = want < most ? want : most;
-  p.per = (int)cdiv(p.steps, pieces > 1 ? pieces : 1);
-  p.nsplit = (int)cdiv(p.steps, p.per);
-  p.nblocks = p.tm * p.tn * p.nsplit;
+
+// Time of the kernels of few rows (measured at the same sizes): a launch, the
+// waits of a workgroup's waves for their pieces of 32 k, of which a launch that
+// fills the GPU once hides none, and the workgroups' own work.
+struct FewCost {
+  double launch, piece, each, work;
+};
+constexpr FewCost kFewCost[3][2] = {{{3.8, 0.19, 0.0093, 0.00115}, {1.5, 0.95, 0.02, 0.0035}},   // float32; with a checkpoint
+                                    {{3.0, 0.068, 0.0062, 0.00045}, {3.0, 0.30, 0.014, 0.0009}},  // bfloat16, whole runs
+                                    {{2.2, 0.245, 0.0071, 0.00105}, {1.1, 1.18, 0.0138, 0.0036}}};
+constexpr int kFewMost = 1 << 16;
+double few_cost(int M, int N, int K, int type, bool groups) {
+  const FewCost& c = kFewCost[type][groups];
+  const double pieces = (double)cdiv(K, 32), wgs = (double)cdiv(N, groups ? 64 : 16) * (double)cdiv(M, 64);
+  const double share = M <= 16 ? 0.35 : (M <= 32 ? 0.6 : 1.);
+  return c.launch + c.piece * share * pieces + wgs * share * (c.each + c.work * pieces);
+}
+
+// Takes the tile for a weight gradient, with its k in the pieces that cost least
+// (numbers that just fill the GPU, of at least three steps), if it costs less than `best`.
+void try_wgrad(MmPlan& pl, int shape, const Cost& c, double& best) {
+  MmParams& p = pl.p;
+  const Shape& sh = kShapes[shape];
+  const long long tm = cdiv(p.M, 32 * sh.tm * sh.wm), tn = cdiv(p.N, 32 * sh.tn * sh.wn), tiles = tm * tn;
+  const long long most = p.steps >= 8 ? p.steps / 3 : 1;
+  for (int fill = 1; fill <= 2 * c.resident; ++fill) {
+    long long pieces = 256 * fill / tiles;
+    pieces = pieces > most ? most : (pieces < 1 ? 1 : pieces);
+    const long long per = cdiv(p.steps, pieces);
+    pieces = cdiv(p.steps, per);
+    const double sum = pieces > 1 ? kWgradLaunch + (double)pieces * (kSumEach + kSumElement * p.M * p.N) : 0.;
+    const double cost = kWgradLaunch + rounds(c, tiles * pieces, (double)per, kWgradAlone) + sum;
+    if (best >= 0 && cost >= best) continue;
+    best = cost;
+    pl.shape = shape;
+    p.tm = (int)tm;
+    p.tn = (int)tn;
+    p.per = (int)per;
+    p.nsplit = (int)pieces;
+    p.nblocks = (int)(tiles * pieces);
+  }
 }
 
 }  // namespace
@@ -59,38 +105,46 @@ MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups, bool whole
   p.N = N;
   p.K = K;
   p.steps = (int)cdiv(K, kStepBytes / esize);
-  const int type = esize == 2 ? 1 : 0;
+  p.nsplit = 1;
+  p.per = p.steps;
+  const int type = esize == 4 ? 0 : (whole ? 1 : 2);
   double best = -1.;
   for (int s = 0; s < kShapeCount; ++s) {
     const Shape& sh = kShapes[s];
     if ((groups && sh.tn % 2) || !shape_used(kind, esize, s)) continue;
-    const int bm = 32 * sh.tm * sh.wm, bn = 32 * sh.tn * sh.wn;
-    const long long tm = cdiv(M, bm), tn = cdiv(N, bn), tiles = tm * tn;
-    double cost;
-    if (kind == kWgrad) {
-      const long long pieces = p.steps / 4 > 1 ? p.steps / 4 : 1, blocks = tiles * pieces;
-      cost = (double)tiles * bm * bn * kArea[type][s] * (blocks < 256 ? 256. / (double)blocks : 1.);
-    } else {
-      const Cost& c = kCost[type && !whole ? 2 : type][s];
-      // (a last round of fewer workgroups per CU has shorter steps)
-      const long long slots = 256 * c.resident, rest = tiles % slots;
-      cost = (double)(tiles / slots) * (c.first + c.step * p.steps);
-      if (rest) cost += c.first + c.step * p.steps * (0.4 + 0.6 * (double)cdiv(rest, 256) / c.resident);
-    }
-    if (best < 0 || cost < best) {
-      best = cost;
-      pl.shape = s;
-      p.tm = (int)tm;
-      p.tn = (int)tn;
-    }
+    const long long tm = cdiv(M, 32 * sh.tm * sh.wm), tn = cdiv(N, 32 * sh.tn * sh.wn);
+    const double cost = kLaunch + rounds(kCost[type][s], tm * tn, (double)p.steps, kAlone);
+    if (best >= 0 && cost >= best) continue;
+    best = cost;
+    pl.shape = s;
+    p.tm = (int)tm;
+    p.tn = (int)tn;
   }
-  pl.few = kind != kWgrad && M <= kFewMost && few_cost(M, N, K, esize, groups) < best;
-  p.nsplit = 1;
-  p.per = p.steps;
-  if (kind == kWgrad) {
-    split_steps(p);
+  pl.few = M <= kFewMost && few_cost(M, N, K, type, groups) < best;
+  p.nblocks = p.tm * p.tn;
+  return pl;
+}
+
+MmPlan plan_wgrad(int M, int N, int K, int esize, bool held, int act, bool& made) {
+  MmPlan pl{};
+  MmParams& p = pl.p;
+  p.M = M;
+  p.N = N;
+  p.K = K;
+  p.steps = (int)cdiv(K, kStepBytes / esize);
+  const bool whole = M % (16 / esize) == 0 && N % (16 / esize) == 0;
+  double best = -1.;
+  for (int s = 0; s < kShapeCount; ++s)
+    if (shape_used(kWgrad, esize, s)) try_wgrad(pl, s, kWgradCost[esize == 4 ? 0 : (whole ? 1 : 2)][s], best);
+  made = false;
+  if (!held && act == kNone) return pl;
+  // act(x) from a pass of its own (its launch, x read, act(x) written), or made
+  const double before = best += kWgradLaunch + (double)K * N * ((held ? 1 : esize) + esize) / kPassBytes;
+  for (int i = 0; i < 2; ++i) {
+    const int type = esize == 2;
+    try_wgrad(pl, kMadeShapes[i], {0.f, kMadeStep[type][i][act], kMadeResident[type][i]}, best);
   }
-  p.nblocks = p.tm * p.tn * p.nsplit;
+  made = best < before;
   return pl;
 }
 
@@ -133,28 +187,6 @@ __global__ __launch_bounds__(kThreads) void mm_sum(const float* __restrict__ par
 }
 
 }  // namespace
-
-bool make_operand(MmPlan& pl, int act, bool held, int esize) {
-  // Picoseconds per element: of the product that makes it (none, relu, gelu,
-  // gelu_tanh, silu), above the plain product's; and of writing it and reading it
-  // back.  50176 x 768 -> 192 bfloat16 from a checkpoint with GELU: 58 us against
-  // 68 with a pass of its own, 200704 x 384 -> 96 96 against 93.
-  constexpr double kMade[2][kActs] = {{1.2, 1.2, 3.5, 3.0, 3.0}, {0.9, 0.95, 1.05, 1.05, 1.0}};
-  constexpr double kLaunch = 3e6;
-  MmParams& p = pl.p;
-  const double elements = (double)p.K * p.N, wide = (double)cdiv(p.M, 192), narrow = (double)cdiv(p.M, 64);
-  const double per = kMade[esize == 2 ? 1 : 0][act], apart = elements * ((held ? 1. : esize) + 2. * esize) / 5. + kLaunch;
-  const bool small = elements * narrow * per < kLaunch;
-  if (!small && elements * wide * per > apart) return false;
-  // 64 x 64 tiles where there are few, else those that make an element least often
-  const int shape = small && cdiv(p.M, 192) * cdiv(p.N, 64) * (p.steps / 4) < 256 ? k64x64 : k192x64;
-  const Shape& sh = kShapes[shape];
-  pl.shape = shape;
-  p.tm = (int)cdiv(p.M, 32 * sh.tm * sh.wm);
-  p.tn = (int)cdiv(p.N, 32 * sh.tn * sh.wn);
-  split_steps(p, 768);  // (three resident workgroups per CU)
-  return true;
-}
 
 hipError_t launch_mm(Dtype dt, int kind, const MmPlan& pl, hipStream_t stream) {
   if (pl.few) return dt == Dtype::F32 ? launch_few_f32(kind, pl.p, stream) : launch_few_bf16(kind, pl.p, stream);

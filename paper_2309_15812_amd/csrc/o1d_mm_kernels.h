@@ -670,7 +670,6 @@ hipError_t launch_kind(const MmPlan& pl, hipStream_t stream) {
   }
   switch (pl.shape) {
     case k128x128: return launch_planned<T, KIND, k128x128>(pl, stream);
-    case k64x256: return launch_planned<T, KIND, k64x256>(pl, stream);
     case k64x64: return launch_planned<T, KIND, k64x64>(pl, stream);
     case k128x96: return launch_planned<T, KIND, k128x96>(pl, stream);
     case k64x128: return launch_planned<T, KIND, k64x128>(pl, stream);

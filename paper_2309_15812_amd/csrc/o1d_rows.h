@@ -145,17 +145,16 @@ struct MmPlan {
   MmParams p;
 };
 
-enum ShapeId { k128x128, k64x256, k64x64, k128x96, k64x128, k128x64, k128x192, k192x64, kShapeCount };
-constexpr Shape kShapes[kShapeCount] = {{2, 2, 2, 2}, {1, 4, 2, 2}, {2, 2, 1, 1}, {4, 1, 1, 3}, {2, 2, 1, 2}, {4, 1, 1, 2},
-                                         {2, 2, 2, 3}, {2, 2, 3, 1}};
-// Tiles that are planned, by what they measured: 128 x 192 for float32 alone, 64 x
-// 256 for its weight gradients, and no large ones for bfloat16 weight gradients;
-// 192 x 64 for weight gradients that make their operand (make_operand).
+enum ShapeId { k128x128, k64x64, k128x96, k64x128, k128x64, k128x192, k192x64, kShapeCount };
+constexpr Shape kShapes[kShapeCount] = {{2, 2, 2, 2}, {2, 2, 1, 1}, {4, 1, 1, 3}, {2, 2, 1, 2},
+                                         {4, 1, 1, 2}, {2, 2, 2, 3}, {2, 2, 3, 1}};
+// Tiles that are planned, by what they measured: 128 x 192 for float32 alone and
+// no large ones for bfloat16 weight gradients; 192 x 64 for weight gradients that
+// make their operand.
 constexpr bool shape_used(int kind, int esize, int shape) {
   switch (shape) {
     case k128x128:
     case k128x96: return kind != kWgrad || esize == 4;
-    case k64x256: return kind == kWgrad && esize == 4;
     case k64x64:
     case k128x64: return true;
     case k64x128: return kind == kWgrad || esize == 2;
@@ -172,14 +171,15 @@ inline bool whole_runs(int kind, int M, int N, int K, const void* a, long long l
   return (kind == kWgrad ? M : K) % v == 0 && (kind == kFwd ? K : N) % v == 0 && aligned(a, lda) && aligned(b, ldb);
 }
 
-// `groups`: an 8-bit checkpoint is written (waves with 64 columns).  `whole`:
-// whole_runs (a weight gradient's plan, which sizes its workspace, does not go by it).
+// A forward product's or input gradient's plan.  `groups`: an 8-bit checkpoint is
+// written (waves with 64 columns).  `whole`: whole_runs.
 MmPlan plan_mm(int kind, int M, int N, int K, int esize, bool groups, bool whole);
 
-// Whether a weight gradient makes act(x) itself as it stages it, once per tile
-// along m, instead of reading it from a pass of its own (a launch, and act(x)
-// through memory); plans the product for it if so.
-bool make_operand(MmPlan& pl, int act, bool held, int esize);
+// A weight gradient's plan, which sizes its workspace (and does not go by the
+// addresses).  `made`: the product makes act(x), of a tensor or a checkpoint
+// (`held`), itself as it stages it, once per tile along m, instead of reading it
+// from a pass of its own (a launch, and act(x) through memory).
+MmPlan plan_wgrad(int M, int N, int K, int esize, bool held, int act, bool& made);
 
 #define O1D_MM_DECL(T)                                                                    \
   hipError_t launch_mm_fwd_##T(const MmPlan& pl, hipStream_t stream);                     \

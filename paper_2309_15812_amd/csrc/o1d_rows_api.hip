@@ -136,8 +136,7 @@ WgradSpace wgrad_space(int M, int I, int O, o1d_act_t act, bool held, o1d_dtype_
   WgradSpace s;
   const bool rewritten = held || act != O1D_ACT_NONE;
   const int es = (int)elem_size(dt), run = 16 / es;
-  s.plan = rows::plan_mm(rows::kWgrad, O, I, M, es, false, true);
-  s.made = rewritten && rows::make_operand(s.plan, (int)act, held, es);
+  s.plan = rows::plan_wgrad(O, I, M, es, held, (int)act, s.made);
   s.part = s.plan.p.nsplit > 1 ? round256((size_t)s.plan.p.nsplit * ((size_t)O * I + O) * sizeof(float)) : kNoSpace;
   s.ldx = rows::cdiv(I, run) * run;
   s.operand = rewritten && !s.made ? round256((size_t)M * s.ldx * es) : 0;
