@@ -19,14 +19,14 @@ struct Cost {
   float first, step;
   int resident;  // workgroups of a CU
 };
-constexpr double kLaunch = 2.3, kAlone = 0.25;  // (the step's time of a CU's only workgroup, as a share)
+constexpr double kLaunch = 2.3, kAlone = 0.25;  // (the time of a CU's only workgroup, as a share)
 constexpr Cost kCost[3][kShapeCount] = {
     // float32: 128 x 128, 64 x 64, 128 x 96, 64 x 128, 128 x 64, 128 x 192
-    {{10.7f, 2.95f, 2}, {4.5f, 2.05f, 4}, {7.8f, 2.45f, 2}, {}, {6.9f, 2.55f, 3}, {20.f, 3.85f, 2}, {}},
+    {{12.8f, 3.05f, 2}, {5.2f, 2.15f, 4}, {9.0f, 2.55f, 2}, {}, {8.4f, 2.7f, 3}, {23.f, 3.9f, 2}, {}},
     // bfloat16, whole runs
-    {{6.6f, 1.03f, 2}, {2.5f, 0.61f, 3}, {5.0f, 0.89f, 2}, {4.5f, 0.88f, 3}, {4.45f, 0.99f, 3}},
+    {{7.7f, 1.08f, 2}, {2.85f, 0.66f, 3}, {5.8f, 0.93f, 2}, {5.6f, 0.94f, 3}, {5.6f, 1.03f, 3}},
     // bfloat16, other runs
-    {{8.2f, 1.5f, 2}, {3.65f, 1.0f, 4}, {5.9f, 1.33f, 2}, {5.6f, 1.32f, 3}, {5.8f, 1.34f, 3}}};
+    {{9.5f, 1.6f, 2}, {4.5f, 1.1f, 4}, {6.5f, 1.44f, 2}, {6.7f, 1.43f, 3}, {7.2f, 1.44f, 3}}};
 
 // Weight gradients in the same terms, measured at 600 sizes of 300 .. 200704
 // rows with 2 to 12 numbers of pieces for each tile (the model fits within 7 to
@@ -47,10 +47,10 @@ constexpr double kSumEach = 0.02, kSumElement = 1.6e-6;  // the sum of the piece
 constexpr double kPassBytes = 4e6;                       // a pass of its own: bytes per microsecond
 
 double rounds(const Cost& c, long long blocks, double steps, double alone) {
-  // (a last round of fewer workgroups per CU has shorter steps)
+  // (a last round of fewer workgroups per CU is shorter)
   const long long slots = 256 * c.resident, rest = blocks % slots;
   double t = (double)(blocks / slots) * (c.first + c.step * steps);
-  if (rest) t += c.first + c.step * steps * (alone + (1. - alone) * (double)cdiv(rest, 256) / c.resident);
+  if (rest) t += (c.first + c.step * steps) * (alone + (1. - alone) * (double)cdiv(rest, 256) / c.resident);
   return t;
 }
 
