@@ -534,9 +534,11 @@ def test_products_of_extreme_values(dt):
 
 # One size at least for every tile that the products are planned with (aligned and not), beside the small sizes above.
 TILES_BF16 = [(20000, 16, 300), (20000, 16, 32), (12544, 16, 130), (1500, 16, 32), (1500, 200, 32), (50176, 16, 96),
-              (20000, 48, 384), (6000, 696, 200)]
-TILES_BF16_ODD = [(20000, 17, 300), (70000, 17, 32), (33000, 17, 96), (33000, 17, 128), (3000, 17, 300), (6000, 699, 200)]
-TILES_F32 = [(33000, 16, 96), (33000, 16, 130), (70000, 16, 32), (33000, 48, 96), (1500, 16, 256), (33000, 17, 131)]
+              (20000, 48, 384), (6000, 696, 200), (12544, 16, 200), (50176, 16, 16), (20000, 16, 384), (500, 16, 384)]
+TILES_BF16_ODD = [(20000, 17, 300), (70000, 17, 32), (33000, 17, 96), (33000, 17, 128), (3000, 17, 300), (6000, 699, 200),
+                  (20000, 17, 384), (20000, 17, 512), (70000, 383, 16), (1500, 17, 192)]
+TILES_F32 = [(33000, 16, 96), (33000, 16, 130), (70000, 16, 32), (33000, 48, 96), (1500, 16, 256), (33000, 17, 131),
+             (500, 16, 300), (50176, 16, 96), (70000, 96, 16), (20000, 48, 384), (50176, 384, 130)]
 
 
 @pytest.mark.parametrize("dt,M,K,N", [(BF16, *c) for c in TILES_BF16 + TILES_BF16_ODD] + [(F32, *c) for c in TILES_F32])
@@ -570,7 +572,11 @@ def test_every_tile(dt, M, K, N):
 @pytest.mark.parametrize("dt,O,I,M", [(BF16, 96, 130, 20000), (BF16, 130, 96, 20000), (BF16, 96, 136, 20000), (BF16, 136, 96, 20000),
                                       (BF16, 40, 40, 600), (BF16, 192, 768, 30000), (F32, 96, 256, 20000), (F32, 512, 130, 9000),
                                       (F32, 512, 40, 9000), (F32, 96, 130, 20000), (F32, 96, 96, 20000), (F32, 40, 768, 9000),
-                                      (F32, 40, 40, 600), (F32, 170, 300, 4000)])
+                                      (F32, 40, 40, 600), (F32, 170, 300, 4000), (F32, 1536, 96, 2000), (F32, 1000, 17, 9000),
+                                      (F32, 1000, 200, 9000), (F32, 1536, 130, 20000), (F32, 17, 768, 20000),
+                                      (F32, 130, 768, 9000), (F32, 17, 17, 50176), (F32, 130, 200, 50176), (BF16, 200, 768, 20000),
+                                      (BF16, 192, 768, 50176), (BF16, 1536, 17, 9000), (BF16, 17, 384, 50176),
+                                      (BF16, 192, 384, 9000), (BF16, 130, 130, 20000), (BF16, 32, 32, 300), (BF16, 1536, 130, 2000)])
 def test_every_weight_gradient_tile(dt, O, I, M):
     dy, x = randn(M, O, seed=110, dt=dt), randn(M, I, seed=111, dt=dt)
     D = dy.double()
