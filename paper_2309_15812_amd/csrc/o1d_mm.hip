@@ -4,6 +4,7 @@
 
 #include "o1d_device.h"
 #include "o1d_rows.h"
+#include "o1d_rows_device.h"
 
 namespace o1d {
 namespace rows {
@@ -34,8 +35,8 @@ constexpr Cost kCost[3][kShapeCount] = {
 // as make about 512 workgroups, and the tile by its area alone, was 11 to 14%).
 constexpr Cost kWgradCost[3][kShapeCount] = {
     {{1.f, 3.1f, 2}, {0.f, 2.1f, 4}, {0.f, 2.6f, 2}, {0.f, 2.8f, 3}, {0.f, 2.65f, 3}, {2.7f, 4.5f, 2}, {}},
-    {{}, {0.f, 0.61f, 3}, {}, {0.f, 0.91f, 3}, {0.f, 0.90f, 3}},
-    {{}, {0.f, 1.19f, 4}, {}, {0.f, 1.42f, 3}, {0.f, 1.41f, 3}}};
+    {{0.f, 1.04f, 2}, {0.f, 0.62f, 3}, {}, {0.f, 0.92f, 3}, {0.f, 0.91f, 3}},
+    {{0.f, 1.64f, 2}, {0.f, 1.19f, 4}, {}, {0.f, 1.42f, 3}, {0.f, 1.41f, 3}}};
 // Those that make their operand, 64 x 64 and 192 x 64: a step's time by activation
 // (none, relu, gelu, gelu_tanh, silu).  50176 x 768 -> 192 bfloat16 from a checkpoint
 // with GELU: 54 us against 68 with a pass of its own.
@@ -43,7 +44,7 @@ constexpr int kMadeShapes[2] = {k64x64, k192x64}, kMadeResident[2][2] = {{4, 2},
 constexpr float kMadeStep[2][2][kActs] = {{{2.5f, 2.5f, 3.6f, 3.4f, 3.35f}, {3.5f, 3.5f, 4.4f, 4.3f, 4.0f}},
                                           {{1.6f, 1.75f, 2.3f, 2.1f, 1.95f}, {2.75f, 3.0f, 3.25f, 3.15f, 3.05f}}};
 constexpr double kWgradLaunch = 3.5, kWgradAlone = 0.4;
-constexpr double kSumEach = 0.02, kSumElement = 1.6e-6;  // the sum of the pieces: per piece, per element
+constexpr double kSumEach = 0.02, kSumElement = 1.3e-6;  // the sum of the pieces: per piece, per element
 constexpr double kPassBytes = 4e6;                       // a pass of its own: bytes per microsecond
 
 double rounds(const Cost& c, long long blocks, double steps, double alone) {
@@ -186,6 +187,56 @@ __global__ __launch_bounds__(kThreads) void mm_sum(const float* __restrict__ par
     db[i - MN] = from_f32<T>(s);
 }
 
+// The same where every thread has pieces enough to wait for at once, or there are
+// outputs enough to fill the GPU: four columns per thread, all pieces.
+// 2048 x 2048 in two pieces: 28 us above, 7.4 (float32 8.7) here.
+constexpr int kWideColumns = 4;
+bool wide_sum(int pieces, long long outputs) { return pieces <= 4 || outputs >= (1 << 18); }
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void mm_sum_wide(const float* __restrict__ part, int pieces, long long MN, int M,
+                                                        T* __restrict__ dw, T* __restrict__ db) {
+  const long long width = MN + M, i = ((long long)blockIdx.x * kThreads + threadIdx.x) * kWideColumns;
+  const long long left = (db ? width : MN) - i;
+  if (left <= 0) return;
+  const int n = left < kWideColumns ? (int)left : kWideColumns;
+  constexpr int kBatch = 4;
+  float s[kWideColumns] = {};
+  for (int j0 = 0; j0 < pieces; j0 += kBatch) {
+    float v[kBatch][kWideColumns] = {};
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (j0 + u < pieces) load_some(part + (long long)(j0 + u) * width + i, n, v[u]);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+      for (int e = 0; e < kWideColumns; ++e) s[e] += v[u][e];
+  }
+  if (i + n <= MN) {
+    store_some(dw + i, n, s);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kWideColumns; ++e) {
+      if (e >= n) break;
+      if (i + e < MN)
+        dw[i + e] = from_f32<T>(s[e]);
+      else
+        db[i + e - MN] = from_f32<T>(s[e]);
+    }
+  }
+}
+
+template <typename T>
+void launch_sum(const MmPlan& pl, T* dw, T* db, hipStream_t stream) {
+  const long long MN = (long long)pl.p.M * pl.p.N, outputs = MN + (db ? pl.p.M : 0);
+  if (wide_sum(pl.p.nsplit, outputs))
+    hipLaunchKernelGGL(mm_sum_wide<T>, dim3((unsigned)cdiv(outputs, kThreads * kWideColumns)), dim3(kThreads), 0, stream,
+                       pl.p.part, pl.p.nsplit, MN, pl.p.M, dw, db);
+  else
+    hipLaunchKernelGGL(mm_sum<T>, dim3((unsigned)cdiv(outputs, kSumColumns)), dim3(kThreads), 0, stream, pl.p.part,
+                       pl.p.nsplit, MN, pl.p.M, dw, db);
+}
+
 }  // namespace
 
 hipError_t launch_mm(Dtype dt, int kind, const MmPlan& pl, hipStream_t stream) {
@@ -202,14 +253,10 @@ hipError_t launch_mm(Dtype dt, int kind, const MmPlan& pl, hipStream_t stream) {
 }
 
 hipError_t launch_mm_sum(Dtype dt, const MmPlan& pl, void* dw, void* db, hipStream_t stream) {
-  const long long MN = (long long)pl.p.M * pl.p.N, width = MN + (db ? pl.p.M : 0);
-  const dim3 grid((unsigned)cdiv(width, kSumColumns)), block(kThreads);
   if (dt == Dtype::F32)
-    hipLaunchKernelGGL(mm_sum<float>, grid, block, 0, stream, pl.p.part, pl.p.nsplit, MN, pl.p.M, static_cast<float*>(dw),
-                       static_cast<float*>(db));
+    launch_sum(pl, static_cast<float*>(dw), static_cast<float*>(db), stream);
   else
-    hipLaunchKernelGGL(mm_sum<uint16_t>, grid, block, 0, stream, pl.p.part, pl.p.nsplit, MN, pl.p.M,
-                       static_cast<uint16_t*>(dw), static_cast<uint16_t*>(db));
+    launch_sum(pl, static_cast<uint16_t*>(dw), static_cast<uint16_t*>(db), stream);
   return hipGetLastError();
 }
 
