@@ -22,19 +22,19 @@ struct Cost {
 };
 constexpr double kLaunch = 2.3, kAlone = 0.25;  // (the time of a CU's only workgroup, as a share)
 constexpr Cost kCost[3][kShapeCount] = {
-    // float32: 128 x 128, 64 x 64, 128 x 96, 64 x 128, 128 x 64, 128 x 192
-    {{12.8f, 3.05f, 2}, {5.2f, 2.15f, 4}, {9.0f, 2.55f, 2}, {}, {8.4f, 2.7f, 3}, {23.f, 3.9f, 2}, {}},
+    // float32: 128 x 128, 64 x 64, 128 x 96, 64 x 128, 128 x 64, 128 x 192, 128 x 32, 32 x 128
+    {{12.8f, 3.05f, 2}, {5.2f, 2.15f, 4}, {9.0f, 2.55f, 2}, {}, {8.4f, 2.7f, 3}, {23.f, 3.9f, 2}, {4.4f, 2.15f, 3}},
     // bfloat16, whole runs
-    {{7.7f, 1.08f, 2}, {2.85f, 0.66f, 3}, {5.8f, 0.93f, 2}, {5.6f, 0.94f, 3}, {5.6f, 1.03f, 3}},
+    {{7.7f, 1.08f, 2}, {2.85f, 0.66f, 3}, {5.8f, 0.93f, 2}, {5.6f, 0.94f, 3}, {5.6f, 1.03f, 3}, {}, {3.2f, 0.86f, 3}},
     // bfloat16, other runs
-    {{9.5f, 1.6f, 2}, {4.5f, 1.1f, 4}, {6.5f, 1.44f, 2}, {6.7f, 1.43f, 3}, {7.2f, 1.44f, 3}}};
+    {{9.5f, 1.6f, 2}, {4.5f, 1.1f, 4}, {6.5f, 1.44f, 2}, {6.7f, 1.43f, 3}, {7.2f, 1.44f, 3}, {}, {4.7f, 1.46f, 4}}};
 
 // Weight gradients in the same terms, measured at 600 sizes of 300 .. 200704
 // rows with 2 to 12 numbers of pieces for each tile (the model fits within 7 to
 // 12%; the plan it takes is 3 to 5% from the best measured one.  As many pieces
 // as make about 512 workgroups, and the tile by its area alone, was 11 to 14%).
 constexpr Cost kWgradCost[3][kShapeCount] = {
-    {{1.f, 3.1f, 2}, {0.f, 2.1f, 4}, {0.f, 2.6f, 2}, {0.f, 2.8f, 3}, {0.f, 2.65f, 3}, {2.7f, 4.5f, 2}, {}},
+    {{1.f, 3.1f, 2}, {0.f, 2.1f, 4}, {0.f, 2.6f, 2}, {0.f, 2.8f, 3}, {0.f, 2.65f, 3}, {2.7f, 4.5f, 2}, {0.f, 2.13f, 3}, {0.f, 2.08f, 3}},
     {{0.f, 1.04f, 2}, {0.f, 0.62f, 3}, {}, {0.f, 0.92f, 3}, {0.f, 0.91f, 3}},
     {{0.f, 1.64f, 2}, {0.f, 1.19f, 4}, {}, {0.f, 1.42f, 3}, {0.f, 1.41f, 3}}};
 // Those that make their operand, 64 x 64 and 192 x 64: a step's time by activation
@@ -61,9 +61,9 @@ double rounds(const Cost& c, long long blocks, double steps, double alone) {
 struct FewCost {
   double launch, piece, each, work;
 };
-constexpr FewCost kFewCost[3][2] = {{{3.8, 0.19, 0.0093, 0.00115}, {1.5, 0.95, 0.02, 0.0035}},   // float32; with a checkpoint
-                                    {{3.0, 0.068, 0.0062, 0.00045}, {3.0, 0.30, 0.014, 0.0009}},  // bfloat16, whole runs
-                                    {{2.2, 0.245, 0.0071, 0.00105}, {1.1, 1.18, 0.0138, 0.0036}}};
+constexpr FewCost kFewCost[3][2] = {{{4.0, 0.2, 0.0098, 0.0011}, {1.5, 0.95, 0.02, 0.0035}},   // float32; with a checkpoint
+                                    {{3.2, 0.072, 0.0064, 0.00043}, {3.0, 0.30, 0.014, 0.0009}},  // bfloat16, whole runs
+                                    {{2.6, 0.25, 0.0074, 0.001}, {1.1, 1.18, 0.0138, 0.0036}}};
 constexpr int kFewMost = 1 << 16;
 double few_cost(int M, int N, int K, int type, bool groups) {
   const FewCost& c = kFewCost[type][groups];

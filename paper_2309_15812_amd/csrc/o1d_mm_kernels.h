@@ -452,8 +452,9 @@ struct Geo {
   // waves per SIMD that the accumulators leave room for
   // Steps whose loads are on their way (each takes a quarter to a half of the
   // accumulators' registers; where that costs a resident wave, one step).
-  static constexpr int kDepth = SHAPE == k64x64 ? 3 : (SHAPE == k128x128 ? 2 : 1);
-  static constexpr int kWaves = S.tm * S.tn == 1 ? 4 : (S.tm * S.tn <= 2 || (S.tm * S.tn == 3 && sizeof(T) == 2) ? 3 : 2);
+  static constexpr bool kNarrow = SHAPE == k128x32 || SHAPE == k32x128;
+  static constexpr int kDepth = kNarrow && sizeof(T) == 4 ? 2 : (S.tm * S.tn == 1 ? 3 : (SHAPE == k128x128 ? 2 : 1));
+  static constexpr int kWaves = S.tm * S.tn == 1 && !(kNarrow && sizeof(T) == 4) ? 4 : (S.tm * S.tn <= 2 || (S.tm * S.tn == 3 && sizeof(T) == 2) ? 3 : 2);
   static constexpr int kLds = TA::kBytes + TB::kBytes;
 };
 
@@ -674,6 +675,8 @@ hipError_t launch_kind(const MmPlan& pl, hipStream_t stream) {
     case k128x96: return launch_planned<T, KIND, k128x96>(pl, stream);
     case k64x128: return launch_planned<T, KIND, k64x128>(pl, stream);
     case k128x64: return launch_planned<T, KIND, k128x64>(pl, stream);
+    case k128x32: return launch_planned<T, KIND, k128x32>(pl, stream);
+    case k32x128: return launch_planned<T, KIND, k32x128>(pl, stream);
     case k128x192: return launch_planned<T, KIND, k128x192>(pl, stream);
     default: return hipErrorInvalidValue;
   }

@@ -315,6 +315,7 @@ hipError_t launch_fast_kind(const MmPlan& pl, hipStream_t stream) {
     case k128x96: return launch_fast_planned<T, KIND, k128x96>(pl, stream);
     case k64x128: return launch_fast_planned<T, KIND, k64x128>(pl, stream);
     case k128x64: return launch_fast_planned<T, KIND, k128x64>(pl, stream);
+    case k128x32: return launch_fast_planned<T, KIND, k128x32>(pl, stream);
     default: return hipErrorInvalidValue;
   }
 }

@@ -145,11 +145,12 @@ struct MmPlan {
   MmParams p;
 };
 
-enum ShapeId { k128x128, k64x64, k128x96, k64x128, k128x64, k128x192, k192x64, kShapeCount };
+enum ShapeId { k128x128, k64x64, k128x96, k64x128, k128x64, k128x192, k128x32, k32x128, k192x64, kShapeCount };
 constexpr Shape kShapes[kShapeCount] = {{2, 2, 2, 2}, {2, 2, 1, 1}, {4, 1, 1, 3}, {2, 2, 1, 2},
-                                         {4, 1, 1, 2}, {2, 2, 2, 3}, {2, 2, 3, 1}};
+                                         {4, 1, 1, 2}, {2, 2, 2, 3}, {4, 1, 1, 1}, {1, 4, 1, 1}, {2, 2, 3, 1}};
 // Tiles that are planned, by what they measured: 128 x 192 for float32 alone, 128 x
-// 96 not for bfloat16 weight gradients; 192 x 64 for weight gradients that make
+// 96 not for bfloat16 weight gradients, of which narrow ones gain nothing from 128 x
+// 32 and 32 x 128 either; 192 x 64 for weight gradients that make
 // their operand.
 constexpr bool shape_used(int kind, int esize, int shape) {
   switch (shape) {
@@ -157,6 +158,8 @@ constexpr bool shape_used(int kind, int esize, int shape) {
     case k128x128:
     case k64x64:
     case k128x64: return true;
+    case k128x32: return kind != kWgrad || esize == 4;
+    case k32x128: return kind == kWgrad && esize == 4;
     case k64x128: return kind == kWgrad || esize == 2;
     case k128x192: return esize == 4;
     default: return false;

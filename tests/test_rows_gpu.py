@@ -534,11 +534,12 @@ def test_products_of_extreme_values(dt):
 
 # One size at least for every tile that the products are planned with (aligned and not), beside the small sizes above.
 TILES_BF16 = [(20000, 16, 300), (20000, 16, 32), (12544, 16, 130), (1500, 16, 32), (1500, 200, 32), (50176, 16, 96),
-              (20000, 48, 384), (6000, 696, 200), (12544, 16, 200), (50176, 16, 16), (20000, 16, 384), (500, 16, 384)]
+              (20000, 48, 384), (6000, 696, 200), (12544, 16, 200), (50176, 16, 16), (20000, 16, 384), (500, 16, 384), (20001, 16, 16)]
 TILES_BF16_ODD = [(20000, 17, 300), (70000, 17, 32), (33000, 17, 96), (33000, 17, 128), (3000, 17, 300), (6000, 699, 200),
-                  (20000, 17, 384), (20000, 17, 512), (70000, 383, 16), (1500, 17, 192)]
+                  (20000, 17, 384), (20000, 17, 512), (70000, 383, 16), (1500, 17, 192), (20000, 17, 17)]
 TILES_F32 = [(33000, 16, 96), (33000, 16, 130), (70000, 16, 32), (33000, 48, 96), (1500, 16, 256), (33000, 17, 131),
-             (500, 16, 300), (50176, 16, 96), (70000, 96, 16), (20000, 48, 384), (50176, 384, 130)]
+             (500, 16, 300), (50176, 16, 96), (70000, 96, 16), (20000, 48, 384), (50176, 384, 130),
+             (20000, 16, 16), (12001, 1001, 21)]
 
 
 @pytest.mark.parametrize("dt,M,K,N", [(BF16, *c) for c in TILES_BF16 + TILES_BF16_ODD] + [(F32, *c) for c in TILES_F32])
@@ -576,7 +577,8 @@ def test_every_tile(dt, M, K, N):
                                       (F32, 1000, 200, 9000), (F32, 1536, 130, 20000), (F32, 17, 768, 20000),
                                       (F32, 130, 768, 9000), (F32, 17, 17, 50176), (F32, 130, 200, 50176), (BF16, 200, 768, 20000),
                                       (BF16, 192, 768, 50176), (BF16, 1536, 17, 9000), (BF16, 17, 384, 50176),
-                                      (BF16, 192, 384, 9000), (BF16, 130, 130, 20000), (BF16, 32, 32, 300), (BF16, 1536, 130, 2000)])
+                                      (BF16, 192, 384, 9000), (BF16, 130, 130, 20000), (BF16, 32, 32, 300), (BF16, 1536, 130, 2000),
+                                      (F32, 17, 130, 9000), (F32, 130, 17, 9000), (BF16, 512, 200, 20000)])
 def test_every_weight_gradient_tile(dt, O, I, M):
     dy, x = randn(M, O, seed=110, dt=dt), randn(M, I, seed=111, dt=dt)
     D = dy.double()
@@ -589,3 +591,15 @@ def test_every_weight_gradient_tile(dt, O, I, M):
         dw, db = ops.linear_bwd_weight(src, dy, act=act)
         near(dw, want, e + u(dt) * (want.abs() + e), act)
         near(db, D.sum(0), edb + u(dt) * (D.sum(0).abs() + edb), "db")
+
+
+def test_weight_gradient_of_unaligned_rows():
+    """Widths of whole runs (which the plan goes by) in rows that are not aligned."""
+    M, I, O = 20000, 200, 512
+    dy, x = sliced(M, O, 1, 120, BF16), sliced(M, I, 3, 121, BF16)
+    D, X = dy.double(), x.double()
+    want, mag = D.t() @ X, D.abs().t() @ X.abs()
+    e, edb = (M + 16) * 2.0 ** -24 * mag, (M + 16) * 2.0 ** -24 * D.abs().sum(0)
+    dw, db = ops.linear_bwd_weight(x, dy)
+    near(dw, want, e + u(BF16) * (want.abs() + e), "dw")
+    near(db, D.sum(0), edb + u(BF16) * (D.sum(0).abs() + edb), "db")
