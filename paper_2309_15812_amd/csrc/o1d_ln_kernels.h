@@ -11,6 +11,11 @@
 // wave has 64 / LPR rows.  Sums, statistics and the gradients' partial sums are
 // float32.  The backward adds dw and db over a workgroup's rows in registers,
 // leaves one partial row per workgroup, and col_sum adds those in a fixed order.
+//
+// Measured: forward 200704 x 96 bfloat16 14.3 us (77 MB in and out, 5.4 TB/s; a large
+// copy reaches 5.0 to 6.9 TB/s here); backward 50176 x 192 float32 23.3 us (116 MB,
+// 5.0 TB/s) and 3.9 for the sum, 33333 x 211 bfloat16 from a checkpoint 15.0 and 3.9
+// (unaligned rows of 422 bytes).  Few rows (49 x 768: 3.5 us) are one wait for memory.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -13,7 +13,7 @@ namespace {
 
 // Time of a product as rounds of resident workgroups, each with a time of its
 // own and a time per step of 128 bytes of k (microseconds).  Forward products and input
-// gradients: measured at 2200 sizes of 16 .. 200704 rows and 16 .. 2048 features with
+// gradients: measured at 3400 sizes of 16 .. 200704 rows and 16 .. 2048 features with
 // each tile; the model fits within 16 to 19%, the plan it takes is 2 to 3% from
 // the best measured one.
 struct Cost {
@@ -29,17 +29,18 @@ constexpr Cost kCost[3][kShapeCount] = {
     // bfloat16, other runs
     {{9.5f, 1.6f, 2}, {4.5f, 1.1f, 4}, {6.5f, 1.44f, 2}, {6.7f, 1.43f, 3}, {7.2f, 1.44f, 3}, {}, {4.7f, 1.46f, 4}}};
 
-// Weight gradients in the same terms, measured at 600 sizes of 300 .. 200704
+// Weight gradients in the same terms, measured at 1100 sizes of 300 .. 200704
 // rows with 2 to 12 numbers of pieces for each tile (the model fits within 7 to
 // 12%; the plan it takes is 3 to 5% from the best measured one.  As many pieces
 // as make about 512 workgroups, and the tile by its area alone, was 11 to 14%).
 constexpr Cost kWgradCost[3][kShapeCount] = {
-    {{1.f, 3.1f, 2}, {0.f, 2.1f, 4}, {0.f, 2.6f, 2}, {0.f, 2.8f, 3}, {0.f, 2.65f, 3}, {2.7f, 4.5f, 2}, {0.f, 2.13f, 3}, {0.f, 2.08f, 3}},
+    {{1.f, 3.1f, 2}, {0.f, 2.1f, 4}, {0.f, 2.6f, 2}, {0.f, 2.8f, 3}, {0.f, 2.65f, 3}, {2.7f, 4.5f, 2}, {0.f, 2.13f, 3},
+     {0.f, 2.08f, 3}},
     {{0.f, 1.04f, 2}, {0.f, 0.62f, 3}, {}, {0.f, 0.92f, 3}, {0.f, 0.91f, 3}},
     {{0.f, 1.64f, 2}, {0.f, 1.19f, 4}, {}, {0.f, 1.42f, 3}, {0.f, 1.41f, 3}}};
 // Those that make their operand, 64 x 64 and 192 x 64: a step's time by activation
 // (none, relu, gelu, gelu_tanh, silu).  50176 x 768 -> 192 bfloat16 from a checkpoint
-// with GELU: 54 us against 68 with a pass of its own.
+// with GELU: 53 us against 68 with a pass of its own.
 constexpr int kMadeShapes[2] = {k64x64, k192x64}, kMadeResident[2][2] = {{4, 2}, {4, 3}};
 constexpr float kMadeStep[2][2][kActs] = {{{2.5f, 2.5f, 3.6f, 3.4f, 3.35f}, {3.5f, 3.5f, 4.4f, 4.3f, 4.0f}},
                                           {{1.6f, 1.75f, 2.3f, 2.1f, 1.95f}, {2.75f, 3.0f, 3.25f, 3.15f, 3.05f}}};

@@ -29,8 +29,14 @@
 // one swap between the halves gives every lane runs of eight columns, on which
 // the epilogue works with 16-byte accesses; two lanes have the 64 columns that
 // share a scale in an 8-bit checkpoint.  (Through LDS, with whole lines per
-// store, the epilogue was bound by LDS and the group's maxima: 12544 x 384 -> 1536
-// with GELU and checkpoint 36 us.)
+// store, the epilogue was bound by LDS and the group's maxima.)
+//
+// Measured: float32 4096 x 2048 -> 2048 200 us: 172 TFLOP/s of float32, of bfloat16
+// products 1.03 PFLOP/s (the library's own float32 product 140 TFLOP/s, its largest
+// bfloat16 ones 1.28 PFLOP/s).  Next to the products' matrix instructions stand
+// the pieces (6.5 vector instructions per element staged, hence the large tiles) and LDS;
+// where a wave has few steps, the first loads and the epilogue.  bfloat16 rows that
+// are not aligned pay for element shifts and masks: 9409 x 203 -> 509 18.8 us.
 //
 // Widths need not be multiples of anything: a 16-byte run past a row's end is
 // loaded from the row's last 16 bytes and moved to its place, k past the end is
@@ -449,12 +455,16 @@ struct Geo {
   static constexpr int BM = 32 * S.tm * S.wm, BN = 32 * S.tn * S.wn;
   using TA = Tile<T, BM, KIND != kWgrad>;
   using TB = Tile<T, BN, KIND == kFwd>;
-  // waves per SIMD that the accumulators leave room for
+  static constexpr int kTiles = S.tm * S.tn;  // of 32 x 32, 16 registers each, of a wave
+  // float32 in narrow tiles: a step's loads and pieces are most of the registers
+  // (three steps in 128 of them: 176 bytes of scratch, up to 1.8 times the time).
+  static constexpr bool kNarrow32 = (SHAPE == k128x32 || SHAPE == k32x128) && sizeof(T) == 4;
   // Steps whose loads are on their way (each takes a quarter to a half of the
   // accumulators' registers; where that costs a resident wave, one step).
-  static constexpr bool kNarrow = SHAPE == k128x32 || SHAPE == k32x128;
-  static constexpr int kDepth = kNarrow && sizeof(T) == 4 ? 2 : (S.tm * S.tn == 1 ? 3 : (SHAPE == k128x128 ? 2 : 1));
-  static constexpr int kWaves = S.tm * S.tn == 1 && !(kNarrow && sizeof(T) == 4) ? 4 : (S.tm * S.tn <= 2 || (S.tm * S.tn == 3 && sizeof(T) == 2) ? 3 : 2);
+  static constexpr int kDepth = kNarrow32 ? 2 : (kTiles == 1 ? 3 : (SHAPE == k128x128 ? 2 : 1));
+  // waves per SIMD that the accumulators leave room for
+  static constexpr int kWaves =
+      kTiles == 1 && !kNarrow32 ? 4 : (kTiles <= 2 || (kTiles == 3 && sizeof(T) == 2) ? 3 : 2);
   static constexpr int kLds = TA::kBytes + TB::kBytes;
 };
 

@@ -54,7 +54,7 @@ struct LnParams {
 // The backward's layout of a row: `lanes` lanes with `runs` 16-byte runs each
 // (lanes 0: too long for a wave).  Few runs per lane leave registers for more
 // waves and make the sums over a workgroup's rows short; lanes past the row's
-// end do nothing.  33333 x 211 bfloat16: 8 lanes x 4 runs 24 us, 32 x 1 12 us.
+// end do nothing.  33333 x 211 bfloat16: 8 lanes x 4 runs 24 us, 32 x 1 15 us.
 struct LnMap {
   int lanes, runs;
 };
@@ -77,7 +77,7 @@ constexpr int ln_bwd_waves(int runs) { return runs <= 2 ? 8 : 4; }
 
 // Workgroups of the backward, each of which leaves one partial row of dw and db:
 // two per CU at most, with about the same number of rows each.
-constexpr int kLnMostBlocks = 512;  // (1024: 33333 x 211 bfloat16 18.3 -> 21 us, 50176 x 192 19.5 -> 25)
+constexpr int kLnMostBlocks = 512;  // (1024: 33333 x 211 bfloat16 1.15 times, 50176 x 192 1.28 times the time)
 inline int ln_bwd_blocks(int M, int C, int esize) {
   const LnMap m = ln_bwd_map(C, esize);
   if (!m.lanes) return M < 2 ? 2 : (M < 256 ? M : 256);

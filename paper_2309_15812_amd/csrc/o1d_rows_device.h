@@ -59,7 +59,7 @@ __device__ __forceinline__ void store_some(T* p, int n, const float (&v)[N]) {
 // exp(-x^2 / 2) of the derivative on its way, for the slope.  With Q(a) =
 // 1 - Phi(a) for a = |x|, gelu(x) = max(x, 0) - a Q(a): 16 issue slots per value
 // against 40 with the library's function.  The epilogues of the products are bound by these
-// slots: 12544 x 384 -> 1536 with GELU and its checkpoint, 40 -> 31 us.
+// slots: 12544 x 384 -> 1536 with GELU and its checkpoint, 40 -> 37 us.
 template <bool FAST>
 __device__ __forceinline__ float exp_(float x) { return FAST ? __expf(x) : expf(x); }
 template <bool FAST>
