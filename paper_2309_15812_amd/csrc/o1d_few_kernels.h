@@ -49,21 +49,26 @@ __device__ __forceinline__ Frag<T> frag_of(const Run8<T>& r) {
   return f;
 }
 
-// k .. k + 7 of a row of K (zeros past it), or (STRIDED) of a column whose elements lie ld apart.
+// k .. k + 7 (zeros past K) of the row that starts `row` elements from base, or
+// (STRIDED) of the column there, whose elements lie ld apart.  (Offsets from the
+// workgroup's own rows, in 32 bits: half the registers of addresses.)
 template <typename T, bool STRIDED>
-__device__ __forceinline__ Run8<T> load8(const T* p, long long ld, int k, int K) {
+__device__ __forceinline__ Run8<T> load8(const T* base, uint32_t row, long long ld, int k, int K) {
   Run8<T> r;
   if constexpr (STRIDED) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const T v = p[(long long)min(k + e, K - 1) * ld];
+      const T v = base[(long long)min(k + e, K - 1) * ld + row];
       r.e[e] = k + e < K ? v : T(0);
     }
-  } else if (k + 8 <= K) {
-    __builtin_memcpy(r.e, p + k, sizeof(r.e));
   } else {
+    const uint32_t at = row + (uint32_t)k;
+    if (k + 8 <= K) {
+      __builtin_memcpy(r.e, reinterpret_cast<const char*>(base) + at * (uint32_t)sizeof(T), sizeof(r.e));
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r.e[e] = k + e < K ? p[k + e] : T(0);
+      for (int e = 0; e < 8; ++e) r.e[e] = k + e < K ? base[at + e] : T(0);
+    }
   }
   return r;
 }
@@ -86,21 +91,20 @@ __device__ __forceinline__ f32x4 few_product(const Frag<T>& n, const Frag<T>& m,
 }
 
 template <typename T, int KIND, int MB, int NB>
-__global__ __launch_bounds__(kFewThreads) void few(MmParams P) {
-  constexpr int kSplit = 8 / NB, kBatch = MB == 4 && sizeof(T) == 4 ? 2 : 4, kPitch = 16 * NB + 4;
+__global__ __launch_bounds__(kFewThreads, (MB == 4 ? 4 : 2)) void few(MmParams P) {
+  constexpr int kSplit = 8 / NB, kBatch = MB == 4 && sizeof(T) == 4 ? 1 : 4, kPitch = 16 * NB + 4;
   __shared__ float red[kSplit][16 * MB][kPitch];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nb = wave % NB, ks = wave / NB;
   const int n0 = blockIdx.x * 16 * NB;
   const long long m0 = (long long)blockIdx.y * 16 * MB;
-  const T *A = static_cast<const T*>(P.a), *B = static_cast<const T*>(P.b);
-  const int n = min(n0 + 16 * nb + (lane & 15), P.N - 1);
-  const T* bp = KIND == kFwd ? B + (long long)n * P.ldb : B + n;
-  const T* ap[MB];
+  const T *A = static_cast<const T*>(P.a) + m0 * P.lda,
+          *B = static_cast<const T*>(P.b) + (KIND == kFwd ? (long long)n0 * P.ldb : (long long)n0);
+  const uint32_t n = (uint32_t)min(16 * nb + (lane & 15), P.N - 1 - n0);
+  const uint32_t br = KIND == kFwd ? n * (uint32_t)P.ldb : n;
+  uint32_t ar[MB];
 #pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    const long long m = m0 + 16 * i + (lane & 15);
-    ap[i] = A + (m < P.M ? m : P.M - 1) * P.lda;
-  }
+  for (int i = 0; i < MB; ++i)
+    ar[i] = (uint32_t)min((long long)(16 * i + (lane & 15)), P.M - 1 - m0) * (uint32_t)P.lda;
   f32x4 acc[MB];
 #pragma unroll
   for (int i = 0; i < MB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -112,9 +116,9 @@ __global__ __launch_bounds__(kFewThreads) void few(MmParams P) {
       const int c = c0 + u * kSplit;
       if (c < pieces) {
         const int k = 32 * c + 8 * (lane >> 4);
-        b[u] = load8<T, KIND == kDgrad>(bp, P.ldb, k, P.K);
+        b[u] = load8<T, KIND == kDgrad>(B, br, P.ldb, k, P.K);
 #pragma unroll
-        for (int i = 0; i < MB; ++i) a[u][i] = load8<T, false>(ap[i], 0, k, P.K);
+        for (int i = 0; i < MB; ++i) a[u][i] = load8<T, false>(A, ar[i], 0, k, P.K);
       }
     }
 #pragma unroll

@@ -400,7 +400,10 @@ def _either(t, what: str, M: int, C: int, like: torch.Tensor) -> tuple:
 
 def _into(out: torch.Tensor | None, like: torch.Tensor, C: int) -> torch.Tensor:
     """Output with like's leading axes and C features."""
-    return like.new_empty((*like.shape[:-1], C)) if out is None else _out(out, like, (*like.shape[:-1], C))
+    shape = like.shape
+    if out is not None:
+        return _out(out, like, (*shape[:-1], C))
+    return torch.empty_like(like) if shape[-1] == C and like.is_contiguous() else like.new_empty((*shape[:-1], C))
 
 
 _NO_SPACE = 256  # what a call that uses no workspace asks for (it writes nothing there)
