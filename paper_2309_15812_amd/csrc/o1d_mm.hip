@@ -62,9 +62,9 @@ double rounds(const Cost& c, long long blocks, double steps, double alone) {
 struct FewCost {
   double launch, piece, each, work;
 };
-constexpr FewCost kFewCost[3][2] = {{{4.0, 0.2, 0.0098, 0.0011}, {1.5, 0.95, 0.02, 0.0035}},   // float32; with a checkpoint
-                                    {{3.2, 0.072, 0.0064, 0.00043}, {3.0, 0.30, 0.014, 0.0009}},  // bfloat16, whole runs
-                                    {{2.6, 0.25, 0.0074, 0.001}, {1.1, 1.18, 0.0138, 0.0036}}};
+constexpr FewCost kFewCost[3][2] = {{{3.4, 0.27, 0.0072, 0.00093}, {4.0, 0.75, 0.012, 0.00325}},   // float32; with a checkpoint
+                                    {{3.3, 0.09, 0.0047, 0.00035}, {3.5, 0.29, 0.009, 0.00078}},  // bfloat16, whole runs
+                                    {{3.4, 0.31, 0.006, 0.0004}, {3.5, 1.0, 0.011, 0.001}}};
 constexpr int kFewMost = 1 << 16;
 double few_cost(int M, int N, int K, int type, bool groups) {
   const FewCost& c = kFewCost[type][groups];
