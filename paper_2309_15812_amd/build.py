@@ -4,7 +4,8 @@ Usage: ``python -m paper_2309_15812_amd.build`` (or ``build()`` from Python).
 Cross-compiles without a GPU.  Every ``csrc/*.hip`` translation unit is
 compiled to an object in parallel (the strip kernels are split per family,
 storage type and cell bound for this), then the objects are linked into the
-library.
+library.  ``_rows.so``, host code that calls the library from torch tensors, is
+compiled with g++ beside it.
 """
 from __future__ import annotations
 
@@ -22,6 +23,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libo1d.so")
+BINDING = os.path.join(PKG, "_rows.so")  # Python's calls of the row operators (csrc/o1d_torch.cpp, host code only)
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -66,7 +68,7 @@ def _run(cmd: list[str], verbose: bool) -> None:
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError(f"hipcc failed with exit code {res.returncode}: {' '.join(cmd[-3:])}")
+        raise RuntimeError(f"{cmd[0]} failed with exit code {res.returncode}: {' '.join(cmd[-3:])}")
     if REMARK in cmd:
         _check_no_scratch(cmd[-1], res.stderr)
 
@@ -80,8 +82,26 @@ def _key(src: str, flags: list[str]) -> str:
     return h.hexdigest()[:20]
 
 
+def build_binding(verbose: bool = False) -> str:
+    """Compiles the Python module against this torch's headers."""
+    import sysconfig
+
+    import torch
+
+    t = os.path.dirname(torch.__file__)
+    tmp = BINDING + ".tmp"
+    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-DUSE_ROCM", "-D__HIP_PLATFORM_AMD__",
+          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
+          "-isystem", os.path.join(t, "include"), "-isystem", os.path.join(t, "include", "torch", "csrc", "api", "include"),
+          "-isystem", "/opt/rocm/include", "-isystem", sysconfig.get_paths()["include"],
+          os.path.join(CSRC, "o1d_torch.cpp"), "-o", tmp, "-L", os.path.join(t, "lib"), "-ltorch", "-ltorch_cpu", "-lc10",
+          "-lc10_hip", "-ltorch_python"], verbose)
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 def build(verbose: bool = False, jobs: int | None = None, incremental: bool = False) -> str:
-    """Compiles every translation unit and links libo1d.so.  With incremental=True, objects whose source,
+    """Compiles every translation unit, links libo1d.so and builds _rows.so.  With incremental=True, objects whose source,
     headers and flags are unchanged are reused from _build/ (a development aid; the default always
     recompiles everything)."""
     srcs = sources()
@@ -110,6 +130,7 @@ def build(verbose: bool = False, jobs: int | None = None, incremental: bool = Fa
         tmp = LIB + ".tmp"
         _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs], verbose)
         os.replace(tmp, LIB)
+        build_binding(verbose)
     finally:
         shutil.rmtree(tmpdir, ignore_errors=True)
     return LIB

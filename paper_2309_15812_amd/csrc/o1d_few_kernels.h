@@ -90,6 +90,9 @@ __device__ __forceinline__ f32x4 few_product(const Frag<T>& n, const Frag<T>& m,
   return acc;
 }
 
+// 64 rows: registers for two workgroups per CU, which takes float32 to one piece at
+// a time; one workgroup with twice the loads is as fast up to 256 workgroups and
+// takes 1.05 to 1.2 times as long above.
 template <typename T, int KIND, int MB, int NB>
 __global__ __launch_bounds__(kFewThreads, (MB == 4 ? 4 : 2)) void few(MmParams P) {
   constexpr int kSplit = 8 / NB, kBatch = MB == 4 && sizeof(T) == 4 ? 1 : 4, kPitch = 16 * NB + 4;

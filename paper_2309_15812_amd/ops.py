@@ -6,6 +6,7 @@ libo1d.so.  theta is a float32 tensor of per-channel angles in degrees.
 """
 from __future__ import annotations
 
+import ctypes
 import functools
 
 import torch
@@ -294,6 +295,26 @@ def dsc_bwd(x: torch.Tensor, z: torch.Tensor, dy: torch.Tensor, w_dw: torch.Tens
 # An activation is any tensor whose last axis holds the features and whose other axes collapse to rows a fixed stride
 # apart: a dense (N, H, W, C) tensor, an (M, C) matrix, or a slice of a wider one.
 
+_bound = None
+_BOUND = ("o1d_ln_fwd", "o1d_ln_bwd", "o1d_ln_bwd_workspace_bytes", "o1d_linear_fwd", "o1d_linear_bwd_input",
+          "o1d_linear_bwd_weight", "o1d_linear_bwd_weight_workspace_bytes", "o1d_pack", "o1d_unpack")
+
+
+def _direct():
+    """The native calls of the common case (contiguous tensors that match, outputs made by the call); each returns None
+    where it is another, which the checked code below takes."""
+    global _bound
+    if _bound is None:
+        try:
+            from . import _rows as native
+        except ImportError as e:
+            raise ImportError(f"{e}; build it with `python -m paper_2309_15812_amd.build`") from None
+        lib = _lib.lib()
+        native.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in _BOUND))
+        _bound = native
+    return _bound
+
+
 def _rows(t: torch.Tensor, what: str) -> tuple[torch.Tensor, int, int, int]:
     """(t or a view of it that starts where it does, rows, features, row stride); refuses what the kernels cannot
     address."""
@@ -371,12 +392,15 @@ class Packed8:
         self.q, self.scale, self.cols = q, scale, cols
 
     @staticmethod
-    def empty(M: int, cols: int, device) -> "Packed8":
+    def of(q: torch.Tensor, scale: torch.Tensor, cols: int) -> "Packed8":  # (tensors made for it)
         held = object.__new__(Packed8)
-        held.q = torch.empty((M, -(-cols // 16) * 16), dtype=torch.int8, device=device)
-        held.scale = torch.empty((M, -(-cols // _lib.GROUP)), dtype=torch.float32, device=device)
-        held.cols = cols
+        held.q, held.scale, held.cols = q, scale, cols
         return held
+
+    @staticmethod
+    def empty(M: int, cols: int, device) -> "Packed8":
+        return Packed8.of(torch.empty((M, -(-cols // 16) * 16), dtype=torch.int8, device=device),
+                          torch.empty((M, -(-cols // _lib.GROUP)), dtype=torch.float32, device=device), cols)
 
     @property
     def rows(self) -> int:
@@ -423,6 +447,9 @@ def _scratch(workspace: torch.Tensor | None, like: torch.Tensor, need: int) -> t
 
 def pack8(x: torch.Tensor) -> Packed8:
     """The 8-bit checkpoint of x's rows."""
+    made = _direct().pack8(x)
+    if made is not None:
+        return Packed8.of(*made, x.shape[-1])
     dt = _dt(x)
     v, M, C, ld = _rows(x, "x")
     held = Packed8.empty(M, C, x.device)
@@ -434,6 +461,10 @@ def unpack8(held: Packed8, dtype: torch.dtype, act: str = "none", out: torch.Ten
     """act(what a checkpoint stands for), as (M, cols) of dtype."""
     if dtype not in _DT:
         raise TypeError(f"unsupported dtype {dtype}; use float32 or bfloat16")
+    if out is None:
+        y = _direct().unpack8(held.q, held.scale, held.cols, _DT[dtype], _act(act))
+        if y is not None:
+            return y
     if out is None:
         y = v = torch.empty((held.rows, held.cols), dtype=dtype, device=held.q.device)
         ld = held.cols
@@ -450,6 +481,10 @@ def unpack8(held: Packed8, dtype: torch.dtype, act: str = "none", out: torch.Ten
 def ln_fwd(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor, eps: float = 1e-6, out: torch.Tensor | None = None
            ) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(y, mean, rstd): layer norm over the last axis; mean and rstd (M,) float32 are for ln_bwd."""
+    if out is None:
+        made = _direct().ln_fwd(x, w, b, eps)
+        if made is not None:
+            return made
     dt = _dt(x)
     v, M, C, ld = _rows(x, "x")
     _vector(w, "w", C, x)
@@ -470,6 +505,11 @@ def ln_bwd(x: torch.Tensor | Packed8, dy: torch.Tensor, mean: torch.Tensor, rstd
            out: tuple[torch.Tensor, torch.Tensor, torch.Tensor] | None = None,
            workspace: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(dx, dw, db) of ln_fwd given its input (or the input's checkpoint), dy and its mean and rstd."""
+    if out is None and workspace is None:
+        held = isinstance(x, Packed8)
+        made = _direct().ln_bwd(x.q if held else x, x.scale if held else None, x.cols if held else 0, dy, mean, rstd, w)
+        if made is not None:
+            return made
     dt = _dt(dy)
     g, M, C, lddy = _rows(dy, "dy")
     px, ldx, q, scale = _either(x, "x", M, C, dy)
@@ -493,7 +533,12 @@ def linear_fwd(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor | None = None, 
     tensor, save="pack8" returns (y, its checkpoint)."""
     if save not in (None, "pre", "pack8"):
         raise ValueError(f"save must be None, 'pre' or 'pack8', got {save!r}")
-    dt, a = _dt(x), _act(act)
+    a = _act(act)
+    if out is None:
+        made = _direct().linear_fwd(x, w, b, a, residual, 0 if save is None else 1 if save == "pre" else 2)
+        if made is not None:
+            return made if save != "pack8" else (made[0], Packed8.of(made[1], made[2], w.shape[0]))
+    dt = _dt(x)
     v, M, I, ldx = _rows(x, "x")
     O, wi = _weight(w, x)
     if wi != I:
@@ -515,7 +560,14 @@ def linear_bwd_input(dy: torch.Tensor, w: torch.Tensor, pre: torch.Tensor | Pack
                      out: torch.Tensor | None = None) -> torch.Tensor:
     """dx = (dy w) act'(pre): the gradient in a product's input, carried through the activation that made it
     (pre: that activation's argument, a tensor or a checkpoint)."""
-    dt, a = _dt(dy), _act(act)
+    a = _act(act)
+    if out is None:
+        held = isinstance(pre, Packed8)
+        made = _direct().linear_bwd_input(dy, w, pre.q if held else pre, pre.scale if held else None,
+                                          pre.cols if held else 0, a)
+        if made is not None:
+            return made
+    dt = _dt(dy)
     g, M, O, lddy = _rows(dy, "dy")
     wo, I = _weight(w, dy)
     if wo != O:
@@ -539,9 +591,14 @@ def linear_bwd_weight(x: torch.Tensor | Packed8, dy: torch.Tensor, act: str = "n
                       workspace: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor | None]:
     """(dw, db): dw (O, I) = dy^T act(x), db = dy's sum over rows (None with bias=False).  x is the product's input, or
     (with act) the pre-activation that it was made from, as a tensor or a checkpoint."""
-    dt, a = _dt(dy), _act(act)
+    a, held = _act(act), isinstance(x, Packed8)
+    I = x.cols if held else int(x.shape[-1]) if x.dim() else 0
+    if out is None and workspace is None:
+        made = _direct().linear_bwd_weight(x.q if held else x, x.scale if held else None, I, dy, a, bias)
+        if made is not None:
+            return made
+    dt = _dt(dy)
     g, M, O, lddy = _rows(dy, "dy")
-    I = x.cols if isinstance(x, Packed8) else int(x.shape[-1]) if x.dim() else 0
     p, ldx, q, scale = _either(x, "x", M, I, dy)
     dw, db = (None, None) if out is None else out
     dw = dy.new_empty((O, I)) if dw is None else _out(dw, dy, (O, I))

@@ -603,3 +603,50 @@ def test_weight_gradient_of_unaligned_rows():
     dw, db = ops.linear_bwd_weight(x, dy)
     near(dw, want, e + u(BF16) * (want.abs() + e), "dw")
     near(db, D.sum(0), edb + u(BF16) * (D.sum(0).abs() + edb), "db")
+
+
+def test_the_call_without_python_and_the_checked_one():
+    """The common case's native calls give what the checked path gives, on the current stream; others are left to it."""
+    M, I, O = 37, 70, 33
+    x, dy, w, b, lw = (randn(*s, seed=130 + i) for i, s in enumerate(((M, I), (M, O), (O, I), (O,), (I,))))
+    held = ops.pack8(x)
+    direct = ops._direct()
+    for s in (x, sliced(M, I, 3, 140, F32, lead=2), x.view(1, M, I)):
+        y, mean, rstd = direct.ln_fwd(s, lw, lw, 1e-6)
+        out = torch.empty_like(y)
+        _, m2, r2 = ops.ln_fwd(s, lw, lw, out=out)
+        assert y.shape == s.shape and torch.equal(y, out) and torch.equal(mean, m2) and torch.equal(rstd, r2)
+        assert torch.equal(direct.linear_fwd(s, w, b, 0, None, 0), ops.linear_fwd(s, w, b, out=torch.empty(*s.shape[:-1], O,
+                                                                                                       device=DEV)))
+    _, mean, rstd = ops.ln_fwd(x, lw, lw)
+    g = randn(M, I, seed=141)
+    for src, scale, cols in ((x, None, 0), (held.q, held.scale, I)):
+        made = direct.ln_bwd(src, scale, cols, g, mean, rstd, lw)
+        want = ops.ln_bwd(x if scale is None else held, g, mean, rstd, lw,
+                          out=(torch.empty_like(x), torch.empty_like(lw), torch.empty_like(lw)))
+        assert all(torch.equal(a, c) for a, c in zip(made, want))
+        made = direct.linear_bwd_weight(src, scale, I, dy, 2, True)
+        want = ops.linear_bwd_weight(x if scale is None else held, dy, act="gelu",
+                                     out=(torch.empty(O, I, device=DEV), torch.empty(O, device=DEV)))
+        assert all(torch.equal(a, c) for a, c in zip(made, want))
+        assert torch.equal(direct.linear_bwd_input(dy, w, src, scale, cols, 2),
+                           ops.linear_bwd_input(dy, w, x if scale is None else held, "gelu", out=torch.empty_like(x)))
+    # left to the checked path: other types, devices, sizes, strides, empty tensors, checkpoints of other widths
+    assert direct.ln_fwd(x.half(), lw, lw, 1e-6) is None and direct.ln_fwd(x.cpu(), lw, lw, 1e-6) is None
+    assert direct.ln_fwd(x, lw[:-1], lw, 1e-6) is None and direct.ln_fwd(x, lw.bfloat16(), lw, 1e-6) is None
+    assert direct.ln_fwd(x.t(), lw, lw, 1e-6) is None and direct.ln_fwd(x[:0], lw, lw, 1e-6) is None
+    assert direct.ln_fwd(x, lw, lw, -1.0) is None and direct.ln_fwd(3, lw, lw, 1e-6) is None
+    assert direct.linear_fwd(x, w.t(), b, 0, None, 0) is None and direct.linear_fwd(x, w, b, 9, None, 0) is None
+    assert direct.ln_bwd(held.q, held.scale, I + 1, g, mean, rstd, lw) is None
+    with pytest.raises(ValueError, match="checkpoint of"):
+        ops.ln_bwd(ops.pack8(randn(M, I + 1, seed=142)), g, mean, rstd, lw)
+    # the current stream: work queued there before the call is seen by it
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        z = torch.zeros(4096, 4096, device=DEV)
+        for _ in range(20):
+            z = z + 1
+        y = ops.linear_fwd(z, torch.eye(8, 4096, device=DEV))
+    side.synchronize()
+    assert (y == 20).all()
