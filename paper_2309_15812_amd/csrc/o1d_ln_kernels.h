@@ -230,25 +230,25 @@ __global__ __launch_bounds__(64 * kBwdWaves<CH>) void ln_bwd_rows(LnParams P) {
     else
       map.unpack(P.C, now.x, x);
     map.unpack(P.C, now.g, g);
-    const float shift = -now.mean * now.rstd;
     float s = 0.f, sx = 0.f;
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        x[i][e] = fmaf(x[i][e], now.rstd, shift);
+        // (the difference first: x rstd - mean rstd loses what the mean and the spread differ by)
+        x[i][e] = (x[i][e] - now.mean) * now.rstd;
         dw[i][e] = fmaf(g[i][e], x[i][e], dw[i][e]);
         db[i][e] += g[i][e];
         g[i][e] *= w[i][e];
         s += g[i][e];
         sx = fmaf(g[i][e], x[i][e], sx);
       }
-    s = -lanes_sum<LPR>(s) * inv * now.rstd;
-    sx = -lanes_sum<LPR>(sx) * inv * now.rstd;
+    s = -lanes_sum<LPR>(s) * inv;
+    sx = -lanes_sum<LPR>(sx) * inv;
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
-      for (int e = 0; e < V; ++e) x[i][e] = fmaf(x[i][e], sx, fmaf(g[i][e], now.rstd, s));
+      for (int e = 0; e < V; ++e) x[i][e] = now.rstd * fmaf(x[i][e], sx, g[i][e] + s);
     map.store(static_cast<T*>(P.dx) + row * P.lddx, x);
   }
   // this workgroup's sums: over a wave's rows, then pairs of waves

@@ -650,3 +650,26 @@ def test_the_call_without_python_and_the_checked_one():
         y = ops.linear_fwd(z, torch.eye(8, 4096, device=DEV))
     side.synchronize()
     assert (y == 20).all()
+
+
+@pytest.mark.parametrize("M,C", [(1408, 2), (300, 96), (77, 211), (40, 5000)])
+def test_layer_norm_backward_of_rows_far_from_zero(M, C):
+    """A row's mean far above its spread: xh is the rounded difference from the mean times rstd, not a difference of products."""
+    x = randn(M, C, seed=150) * 2.0 ** -6 + 8.0
+    dy, w = randn(M, C, seed=151), randn(C, seed=152)
+    X = x.double()
+    mean = X.mean(1).float()
+    rstd = (1 / (X.var(1, correction=0) + 1e-6).sqrt()).float()
+    m, r = mean.double()[:, None], rstd.double()[:, None]
+    xh, g = (X - m) * r, dy.double() * w.double()
+    mg, mgx = g.mean(1, keepdim=True), (g * xh).mean(1, keepdim=True)
+    want = r * (g - mg - xh * mgx)
+    eps = 2.0 ** -24
+    exh = 2 * eps * xh.abs()
+    emg, emgx = (C + 4) * eps * g.abs().mean(1, keepdim=True), (C + 8) * eps * (g * xh).abs().mean(1, keepdim=True)
+    edx = 1.1 * r * (6 * eps * (g.abs() + mg.abs() + (xh * mgx).abs()) + emg + xh.abs() * emgx + exh * mgx.abs())
+    D = dy.double().abs()
+    dx, dw, db = ops.ln_bwd(x, dy, mean, rstd, w)
+    near(dx, want, edx, "dx")
+    near(dw, (dy.double() * xh).sum(0), (D * (exh + (M + 16) * eps * xh.abs())).sum(0) * 1.01, "dw")
+    near(db, dy.double().sum(0), (M + 16) * eps * D.sum(0), "db")
