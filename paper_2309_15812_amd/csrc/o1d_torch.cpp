@@ -84,7 +84,8 @@ const at::Tensor* matrix(PyObject* o, const Rows& r) {
              : nullptr;
 }
 
-// A tensor of r's rows of C features, or (scale not None) a checkpoint (q, scale) of `cols` features, which have to be C.
+// A tensor of r's rows of C features, or (scale not None) a checkpoint (q, scale) of
+// `cols` features, which have to be C.
 struct Source {
   const void* x = nullptr;
   const signed char* q = nullptr;
@@ -188,13 +189,15 @@ PyObject* ln_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
         !t->is_cuda() || t->get_device() != dy.t->get_device())
       return none();
   if (!w) return none();
-  at::Tensor dx = empty_rows(dy, dy.C), dw = empty({dy.C}, *w, w->scalar_type()), db = empty({dy.C}, *w, w->scalar_type());
+  at::Tensor dx = empty_rows(dy, dy.C), dw = empty({dy.C}, *w, w->scalar_type()),
+             db = empty({dy.C}, *w, w->scalar_type());
   const size_t need = p_ln_bytes((int)dy.M, dy.C, dy.dt);
   at::Tensor ws = space(need, *dy.t);
   void* s = stream_of(*dy.t);
   const auto st = call([&] {
     return p_ln_bwd(x.x, x.ld, x.q, x.scale, dy.data(), dy.ld, (const float*)mean->data_ptr(),
-                    (const float*)rstd->data_ptr(), w->data_ptr(), dx.data_ptr(), dy.C, dw.data_ptr(), db.data_ptr(), (int)dy.M, dy.C, dy.dt, ws.data_ptr(),
+                    (const float*)rstd->data_ptr(), w->data_ptr(), dx.data_ptr(), dy.C, dw.data_ptr(), db.data_ptr(),
+                    (int)dy.M, dy.C, dy.dt, ws.data_ptr(),
                     (size_t)ws.numel(), s);
   });
   return st ? none() : result({wrap(dx), wrap(dw), wrap(db)});
