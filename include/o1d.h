@@ -218,8 +218,9 @@ size_t o1d_dsc_bwd_workspace_bytes(int N, int C, int Cout, int H, int W, int K, 
  * other entry points; no output may overlap an input, another output or the
  * workspace, measured over the rows' whole reach.  A workspace is 16-byte aligned
  * and has at least the bytes that the call's ..._workspace_bytes gives for the same arguments (256
- * where the work needs none; 0 for M = 0); what it holds before a call does not
- * matter.  M = 0 is valid: nothing is launched, except that weight gradients are
+ * where the work needs none, and nothing is written to them; at least 512 where it needs some;
+ * 0 for M = 0); what it holds before a call does not matter.  Calls that may run
+ * at the same time need workspaces of their own, unless nothing is written to them.  M = 0 is valid: nothing is launched, except that weight gradients are
  * set to zeros. */
 typedef enum {
   O1D_ACT_NONE = 0,

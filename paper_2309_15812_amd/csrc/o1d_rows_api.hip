@@ -25,8 +25,11 @@ constexpr int kMaxRows = 0x7fffffff - 1024;
 constexpr int kMaxFeatures = 1 << 20;
 constexpr long long kMaxStride = 1 << 21;
 
-// What a call that needs no workspace asks for all the same, so that callers need not know which do.
-constexpr size_t kNoSpace = 256;
+// What a call that needs no workspace asks for all the same, so that callers need not know which do.  One that
+// writes to its workspace asks for more, however little that is: callers may share
+// a workspace of kNoSpace bytes between calls that run at the same time.
+constexpr size_t kNoSpace = 256, kLeastSpace = 2 * kNoSpace;
+size_t space_for(size_t bytes) { return bytes < kLeastSpace ? kLeastSpace : bytes; }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -137,7 +140,8 @@ WgradSpace wgrad_space(int M, int I, int O, o1d_act_t act, bool held, o1d_dtype_
   const bool rewritten = held || act != O1D_ACT_NONE;
   const int es = (int)elem_size(dt), run = 16 / es;
   s.plan = rows::plan_wgrad(O, I, M, es, held, (int)act, s.made);
-  s.part = s.plan.p.nsplit > 1 ? round256((size_t)s.plan.p.nsplit * ((size_t)O * I + O) * sizeof(float)) : kNoSpace;
+  s.part = s.plan.p.nsplit > 1 ? space_for(round256((size_t)s.plan.p.nsplit * ((size_t)O * I + O) * sizeof(float)))
+                               : kNoSpace;
   s.ldx = rows::cdiv(I, run) * run;
   s.operand = rewritten && !s.made ? round256((size_t)M * s.ldx * es) : 0;
   return s;
@@ -183,7 +187,7 @@ o1d_status_t o1d_ln_fwd(const void* x, long long ldx, const void* w, const void*
 size_t o1d_ln_bwd_workspace_bytes(int M, int C, o1d_dtype_t dtype) {
   if (check_dims("o1d_ln_bwd", M, C, "C", dtype) != O1D_OK || M == 0) return 0;
   const int blocks = rows::ln_bwd_blocks(M, C, (int)elem_size(dtype));
-  return blocks > 1 ? (size_t)blocks * 2 * C * sizeof(float) : kNoSpace;
+  return blocks > 1 ? space_for((size_t)blocks * 2 * C * sizeof(float)) : kNoSpace;
 }
 
 o1d_status_t o1d_ln_bwd(const void* x, long long ldx, const signed char* xq, const float* xscale, const void* dy,

@@ -125,7 +125,8 @@ at::Tensor empty_rows(const Rows& r, int C) {
   return empty(shape, *r.t, r.t->scalar_type());
 }
 // Workspace.  Calls that need none ask for 256 bytes, to which nothing is
-// written: one such tensor per device, never freed, serves them all.
+// written (those that write ask for 512 at least): one such tensor per device,
+// never freed, serves them all, on whichever streams they run.
 at::Tensor space(size_t need, const at::Tensor& like) {
   if (need > 256) return empty({(int64_t)need}, like, at::kByte);
   static std::array<at::Tensor*, 64> held{};

@@ -430,7 +430,9 @@ def _into(out: torch.Tensor | None, like: torch.Tensor, C: int) -> torch.Tensor:
     return torch.empty_like(like) if shape[-1] == C and like.is_contiguous() else like.new_empty((*shape[:-1], C))
 
 
-_NO_SPACE = 256  # what a call that uses no workspace asks for (it writes nothing there)
+# What a call that uses no workspace asks for: it writes nothing there, so one tensor serves all such calls on all streams.
+# Calls that write to theirs ask for 512 bytes at least.
+_NO_SPACE = 256
 _no_space: dict[int, torch.Tensor] = {}
 
 

@@ -1,0 +1,82 @@
+"""Edges of the row operators: the largest values, infinities, the tails of the activations, small calls side by side.
+
+Bounds as in the tests of the operators: u = 2^-24 for float32 and 2^-8 for bfloat16 results (one rounding is half of that), n
+float32 sums (n + 8) 2^-24 of the terms' sizes, and what a test adds is derived beside it.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2309_15812_amd import ops
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+DTYPES = [F32, BF16]
+ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
+
+
+def u(dt):
+    return 2.0 ** -24 if dt == F32 else 2.0 ** -8
+
+
+def randn(*shape, seed, dt=F32, std=1.0):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    return (torch.randn(*shape, generator=gen, device=DEV) * std).to(dt)
+
+
+def near(got, want, tol, what):
+    got = got.double()
+    assert got.shape == want.shape, what
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), f"{what}: NaN elsewhere"
+    ok = ((got - want).abs() <= tol) | (got == want) | torch.isnan(want)
+    assert bool(ok.all()), f"{what}: off by {float(((got - want).abs() - tol).nan_to_num(0).max()):.3g} over its bound"
+
+
+def gate(h, act):
+    """An activation and its derivative in 64 bits."""
+    if act == "none":
+        return h, torch.ones_like(h)
+    if act == "relu":
+        return h.clamp(min=0), (h > 0).double()
+    if act == "gelu":
+        area = 0.5 * torch.special.erfc(-h / math.sqrt(2))
+        return h * area, area + h * torch.exp(-h * h / 2) / math.sqrt(2 * math.pi)
+    k = 2 * math.sqrt(2 / math.pi)
+    g = torch.sigmoid(h if act == "silu" else k * (h + 0.044715 * h ** 3))
+    inner = 1.0 if act == "silu" else k * (1 + 0.134145 * h * h)
+    return h * g, g + h * g * (1 - g) * inner
+
+
+def value64(held):
+    """What a checkpoint stands for, in 64 bits."""
+    return held.q[:, :held.cols].double() * held.scale.double().repeat_interleave(64, 1)[:, :held.cols]
+
+
+@pytest.mark.parametrize("checked", [False, True])
+def test_small_gradients_on_two_streams(checked):
+    """Calls with few partial results, side by side: each has its own workspace."""
+    def ln(M, C, seed):
+        x, dy, w = randn(M, C, seed=seed), randn(M, C, seed=seed + 1), randn(C, seed=seed + 2)
+        mean, rstd = x.mean(1), (x.var(1, unbiased=False) + 1e-6).rsqrt()
+        return lambda: ops.ln_bwd(x, dy, mean, rstd, w, out=(None, None, None) if checked else None)
+
+    def linear(M, I, O, dt, seed):
+        x, dy = randn(M, I, seed=seed, dt=dt), randn(M, O, seed=seed + 1, dt=dt)
+        return lambda: ops.linear_bwd_weight(x, dy, out=(None, None) if checked else None)
+
+    pairs = [[ln(M, C, 100 * k) for k in (1, 2)] for M, C in ((513, 1), (513, 6), (4096, 1))]
+    pairs += [[linear(*c, 100 * k) for k in (3, 4)] for c in ((256, 7, 4, F32), (600, 1, 8, BF16))]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for pair in pairs:
+        want = [f() for f in pair]
+        torch.cuda.synchronize()
+        got = [[], []]
+        for _ in range(40):
+            for s, f, g in zip(streams, pair, got):
+                with torch.cuda.stream(s):
+                    g.append(f())
+        torch.cuda.synchronize()
+        for w, g in zip(want, got):
+            assert all(torch.equal(a, b) for r in g for a, b in zip(w, r))
