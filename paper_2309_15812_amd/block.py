@@ -75,9 +75,16 @@ class OrientedBlock(torch.nn.Module):
         self.w1, self.b1 = torch.nn.Parameter(torch.randn(hidden, C) * C ** -0.5), torch.nn.Parameter(torch.zeros(hidden))
         self.w2, self.b2 = torch.nn.Parameter(torch.randn(C, hidden) * hidden ** -0.5), torch.nn.Parameter(torch.zeros(C))
 
+    def _apply(self, fn, *args, **kwargs):
+        # a cast of the module is one of its weights: the angles move with it and stay float32 (bfloat16 makes 158 of 157.5)
+        theta = self.theta
+        super()._apply(fn, *args, **kwargs)
+        if self.theta.dtype != torch.float32:
+            self.theta = theta.to(self.theta.device)
+        return self
+
     def forward(self, x: torch.Tensor) -> torch.Tensor:
-        # (the angles stay float32 when the module is cast)
-        return OrientedBlockFunction.apply(x, self.theta.float(), self.w_dw, self.ln_w, self.ln_b, self.w1, self.b1, self.w2,
+        return OrientedBlockFunction.apply(x, self.theta, self.w_dw, self.ln_w, self.ln_b, self.w1, self.b1, self.w2,
                                            self.b2, self.act, self.eps, self.checkpoint)
 
 
