@@ -234,7 +234,7 @@ typedef enum {
  * C rounded up to 16 (q 16-byte aligned; the padding is zero) and float
  * scale[M][ceil(C / 64)].  A group of 64 columns of a row shares a scale:
  *   amax = max |x|, scale = amax / 127, q = rint(x (127 / amax)), which stands for q scale,
- * an error of at most amax / 254 (and float32 rounding).  A group that holds a
+ * an error of at most amax / 254 (and float32 rounding; it is finite also for the largest amax).  A group that holds a
  * NaN or an infinity gets the scale NaN: all of it reads NaN.  One whose amax is
  * below 2^-100 gets scale 0. */
 o1d_status_t o1d_pack(const void* x, long long ldx, signed char* q, float* scale, int M, int C, o1d_dtype_t dtype,

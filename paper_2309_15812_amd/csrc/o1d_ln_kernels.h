@@ -141,10 +141,11 @@ struct RowMap {
   }
   __device__ __forceinline__ void unpack_held(const uint32_t (&w)[CH][V / 4], const float (&s)[CH], float (&v)[CH][V]) const {
 #pragma unroll
-    for (int i = 0; i < CH; ++i)
+    for (int i = 0; i < CH; ++i) {
+      const float scale = scale_read(s[i]);
 #pragma unroll
-      for (int e = 0; e < V; ++e)
-        v[i][e] = i < CH - 1 || e < n ? (float)(int8_t)(w[i][e / 4] >> (8 * (e & 3))) * s[i] : 0.f;
+      for (int e = 0; e < V; ++e) v[i][e] = i < CH - 1 || e < n ? unround(w[i][e / 4], e & 3, scale) : 0.f;
+    }
   }
 };
 
@@ -374,9 +375,9 @@ __device__ __forceinline__ void load_x(const LnParams& P, long long row, int c, 
     const long long ldq = (P.C + 15) / 16 * 16, groups = (P.C + kGroup - 1) / kGroup;
     uint32_t w[V / 4];
     __builtin_memcpy(w, __builtin_assume_aligned(P.xq + row * ldq + c, V), V);
-    const float s = P.xscale[row * groups + c / kGroup];
+    const float s = scale_read(P.xscale[row * groups + c / kGroup]);
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = (float)(int8_t)(w[e / 4] >> (8 * (e & 3))) * s;
+    for (int e = 0; e < V; ++e) v[e] = unround(w[e / 4], e & 3, s);
   } else {
     load_some(static_cast<const T*>(P.x) + row * P.ldx + c, P.C - c, v);
   }

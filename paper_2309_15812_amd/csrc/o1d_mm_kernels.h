@@ -241,9 +241,9 @@ struct Tile {
     for (int i = 0; i < N; ++i) {
       float v[V];
       if (held) {
-        const float scale = __uint_as_float(w[i][2]);
+        const float scale = scale_read(__uint_as_float(w[i][2]));
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = unround(w[i][e / 4] ^ 0x80808080u, e & 3, scale);
+        for (int e = 0; e < V; ++e) v[e] = unround(w[i][e / 4], e & 3, scale);
       } else {
         T t[V];
         __builtin_memcpy(t, &w[i], 16);

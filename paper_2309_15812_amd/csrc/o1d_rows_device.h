@@ -248,15 +248,23 @@ __device__ __forceinline__ uint2 round8(const float (&v)[8], const Scale& s) {
   return make_uint2(four(0), four(4));
 }
 
-// q scale for byte e of a word of integers plus 128 (the word ^ 0x80808080): a
-// byte is converted in one instruction, and (q + 128) scale - 128 scale is rounded once, as q scale is.
+// A scale as it is read.  Of float32's largest value amax / 127 is rounded up, and
+// 127 of it would be infinite: the scale below stands in, 2^-24 smaller.
+__device__ __forceinline__ float scale_read(float scale) {
+  constexpr float kLast = 0x1.020406p+121f;            // the largest whose 127 is finite
+  return __builtin_elementwise_minimum(scale, kLast);  // (NaN stays)
+}
+
+// q scale for byte e of a word of integers, rounded once.  (As (q + 128) scale - 128 scale, for the
+// conversion of unsigned bytes, it overflows in the top 127th of float32's range.)
 __device__ __forceinline__ float unround(uint32_t word, int e, float scale) {
-  return fmaf((float)((word >> (8 * e)) & 0xffu), scale, -128.f * scale);
+  return (float)(int8_t)(word >> (8 * e)) * scale;
 }
 __device__ __forceinline__ void unround8(uint2 w, float scale, float (&v)[8]) {
-  const uint32_t u[2] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u};
+  const uint32_t u[2] = {w.x, w.y};
+  const float s = scale_read(scale);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = unround(u[e >> 2], e & 3, scale);
+  for (int e = 0; e < 8; ++e) v[e] = unround(u[e >> 2], e & 3, s);
 }
 
 }  // namespace rows

@@ -80,3 +80,38 @@ def test_small_gradients_on_two_streams(checked):
         torch.cuda.synchronize()
         for w, g in zip(want, got):
             assert all(torch.equal(a, b) for r in g for a, b in zip(w, r))
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+def test_checkpoints_of_the_largest_values(dt):
+    """Groups that reach the type's largest value, as masks do: their finite values, and only theirs, stay finite."""
+    big = torch.finfo(dt).max
+    x = torch.zeros(7, 130, device=DEV, dtype=dt)
+    x[0, 3], x[1, 70], x[2, :], x[3, ::2], x[4, 129] = big, -big, big, -big, big
+    x[5] = randn(130, seed=1, dt=dt) * 1e30
+    x[5, 100] = -big
+    held = ops.pack8(x)
+    v = value64(held)
+    for act in ("none", "relu", "gelu", "silu"):
+        y = ops.unpack8(held, dt, act)
+        want = gate(v, act)[0]
+        assert torch.isfinite(y).all()
+        near(y, want, (u(dt) + 2.0 ** -22) * want.abs() + (0 if act in ("none", "relu") else 2e-6), act)
+        if act != "none":
+            dy = randn(7, 130, seed=2, dt=dt)
+            slope = gate(v, act)[1]
+            near(ops.act_bwd(held, dy, act), dy.double() * slope, u(dt) * 2 * dy.double().abs() + 4e-6, act)
+            # (the product's own error: 24 terms)
+            w, g = randn(24, 130, seed=3, dt=dt, std=0.2), randn(7, 24, seed=4, dt=dt)
+            p, mag = g.double() @ w.double(), g.double().abs() @ w.double().abs()
+            near(ops.linear_bwd_input(g, w, pre=held, act=act), p * slope,
+                 2 * (32 * 2.0 ** -24 + 4e-6) * mag + u(dt) * p.abs() * 1.2, act)
+    # sums over rows that stay in range; an operand rounded to bfloat16 adds 2^-9 of the terms
+    g = torch.full((7, 40), 2.0 ** -6, device=DEV, dtype=dt)
+    dw, _ = ops.linear_bwd_weight(held, g)
+    want, mag = g.double().t() @ v, g.double().t() @ v.abs()
+    near(dw, want, (16 * 2.0 ** -24 + (u(dt) if dt == BF16 else 0)) * mag + u(dt) * want.abs(), "dw")
+    mean, rstd = torch.zeros(7, device=DEV), torch.full((7,), 2.0 ** -122, device=DEV)
+    dx, dw, db = ops.ln_bwd(held, torch.ones(7, 130, device=DEV, dtype=dt), mean, rstd,
+                            torch.ones(130, device=DEV, dtype=dt))
+    near(dw, (v * 2.0 ** -122).sum(0), (24 * 2.0 ** -24 + u(dt)) * (v * 2.0 ** -122).abs().sum(0), "layer norm's dw")
