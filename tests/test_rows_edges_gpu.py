@@ -115,3 +115,45 @@ def test_checkpoints_of_the_largest_values(dt):
     dx, dw, db = ops.ln_bwd(held, torch.ones(7, 130, device=DEV, dtype=dt), mean, rstd,
                             torch.ones(130, device=DEV, dtype=dt))
     near(dw, (v * 2.0 ** -122).sum(0), (24 * 2.0 ** -24 + u(dt)) * (v * 2.0 ** -122).abs().sum(0), "layer norm's dw")
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("M", [3, 5000])
+def test_activations_of_infinity(M, dt):
+    """x sigma(x) of +infinity is +infinity, in the products' epilogues and where a weight gradient makes it."""
+    I, O = 16, 40
+    x, w = randn(M, I, seed=5, dt=dt), randn(O, I, seed=6, dt=dt)
+    w[:, 0] = 1
+    x[1, 0] = math.inf
+    x[2, 5] = math.nan
+    for act in ACTS:
+        y = ops.linear_fwd(x, w, act=act)
+        assert (y[1] == math.inf).all() and torch.isnan(y[2]).all(), act
+        assert torch.isfinite(y[0]).all() and torch.isfinite(y[3:]).all(), act
+        z = x.clone()
+        z[2, 5] = 0
+        dy = randn(M, O, seed=7, dt=dt)
+        dw, _ = ops.linear_bwd_weight(z, dy, act=act)
+        assert torch.equal(dw[:, 0], torch.copysign(torch.full((O,), math.inf, device=DEV), dy[1].float()).to(dt)), act
+        assert torch.isfinite(dw[:, 1:]).all(), act
+
+
+def test_gelu_of_bfloat16_keeps_its_bits_in_the_tail():
+    """Every bfloat16 value from -12.875 (below, exp(-x^2 / 2) leaves float32's normal range) to 12, through a product with 1.
+    One rounding is half a unit of the last of 8 bits; the evaluation's error is far below, 2^-14: a fit's 4e-6 and the exponent's, of
+    which x^2 / 2 < 83 in float32 is off by 2^-24 twice, 1e-5.  The slope is a difference of Q(a) and a exp(-a^2 / 2) / sqrt(2 pi):
+    2^-14 of both."""
+    def rounding(v):
+        return torch.ldexp(torch.ones_like(v), torch.frexp(v).exponent - 9)
+
+    bits = torch.arange(0x8000, device=DEV, dtype=torch.int32)
+    a = (bits << 16).view(torch.float32)
+    a = a[(a >= 2.0 ** -20) & (a <= 12.875)]
+    x = torch.cat((-a, a))[:, None].to(BF16)
+    X = x.double()
+    want, slope = gate(X, "gelu")
+    near(ops.linear_fwd(x, torch.ones(1, 1, device=DEV, dtype=BF16), act="gelu"), want,
+         rounding(want) + 2.0 ** -14 * want.abs(), "gelu")
+    q = 0.5 * torch.special.erfc(X.abs() / math.sqrt(2))
+    parts = q + X.abs() * torch.exp(-X * X / 2) / math.sqrt(2 * math.pi)
+    near(ops.act_bwd(x, torch.ones_like(x), "gelu"), slope, rounding(slope) + 2.0 ** -14 * parts, "slope")
