@@ -121,7 +121,9 @@ __device__ __forceinline__ float act_slope(float x, int act) {
     case kGelu: return gelu_slope<FAST>(x);
     case kGeluTanh: {
       const float g = recip<FAST>(1.f + exp_<FAST>(-kTanhScale * (x + kTanhCube * x * x * x)));
-      return g + x * g * (1.f - g) * kTanhScale * fmaf(3.f * kTanhCube * x, x, 1.f);
+      // g (1 - g) is 0 long before |x| = 32, and x^2 leaves float32 at 2e19: the other factors end there
+      const float c = fminf(fmaxf(x, -32.f), 32.f);
+      return g + c * g * (1.f - g) * kTanhScale * fmaf(3.f * kTanhCube * c, c, 1.f);
     }
     case kSilu: {
       const float g = recip<FAST>(1.f + exp_<FAST>(-x));

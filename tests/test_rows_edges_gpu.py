@@ -157,3 +157,16 @@ def test_gelu_of_bfloat16_keeps_its_bits_in_the_tail():
     q = 0.5 * torch.special.erfc(X.abs() / math.sqrt(2))
     parts = q + X.abs() * torch.exp(-X * X / 2) / math.sqrt(2 * math.pi)
     near(ops.act_bwd(x, torch.ones_like(x), "gelu"), slope, rounding(slope) + 2.0 ** -14 * parts, "slope")
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("act", ACTS[1:])
+def test_slopes_of_large_finite_values(dt, act):
+    """The slopes' limits, 0 and 1, wherever the argument is finite."""
+    big = torch.finfo(dt).max
+    x = torch.tensor([[s * v for v in (30.0, 1e10, 2e19, 1e26, 1e35, float(big)) for s in (1, -1)]], device=DEV).to(dt)
+    dy = torch.full_like(x, 1.5)
+    want = torch.where(x > 0, 1.5, 0.0).double()
+    near(ops.act_bwd(x, dy, act), want, 1e-6, act)
+    w = torch.ones(1, x.shape[1], device=DEV, dtype=dt)
+    near(ops.linear_bwd_input(dy[:, :1], w, pre=x, act=act), want, 1e-6, act)
