@@ -661,11 +661,12 @@ class LinearFunction(torch.autograd.Function):
         w, x, xs, pre, ps = ctx.saved_tensors
         dy = gy.contiguous()
         dh = dy if ctx.act == "none" else act_bwd(_whole(pre, ps, ctx.cols[1]), dy, ctx.act)
-        gx = linear_bwd_input(dh, w) if ctx.needs_input_grad[0] else None
+        wants = (*ctx.needs_input_grad, False, False, False)  # (arguments left out have no entry)
+        gx = linear_bwd_input(dh, w) if wants[0] else None
         gw = gb = None
-        if ctx.needs_input_grad[1] or (ctx.bias and ctx.needs_input_grad[2]):
+        if wants[1] or (ctx.bias and wants[2]):
             gw, gb = linear_bwd_weight(_whole(x, xs, ctx.cols[0]), dh, bias=ctx.bias)
-        return gx, gw, gb, None, (gy if ctx.needs_input_grad[4] else None), None
+        return gx, gw, gb, None, (gy if wants[4] else None), None
 
 
 def _parts(t) -> tuple:

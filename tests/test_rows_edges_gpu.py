@@ -170,3 +170,18 @@ def test_slopes_of_large_finite_values(dt, act):
     near(ops.act_bwd(x, dy, act), want, 1e-6, act)
     w = torch.ones(1, x.shape[1], device=DEV, dtype=dt)
     near(ops.linear_bwd_input(dy[:, :1], w, pre=x, act=act), want, 1e-6, act)
+
+
+def test_arguments_of_the_autograd_functions_can_be_left_out():
+    x, w, b = randn(6, 24, seed=8), randn(40, 24, seed=9), randn(40, seed=10)
+    dy, lw = randn(6, 40, seed=11), randn(24, seed=12)
+    full = [x.clone().requires_grad_(True), w.clone().requires_grad_(True), b.clone().requires_grad_(True)]
+    ops.LinearFunction.apply(*full, "none", None, False).backward(dy)
+    for n in (2, 3):
+        part = [t.detach().clone().requires_grad_(True) for t in full[:n]]
+        ops.LinearFunction.apply(*part).backward(dy)
+        assert torch.equal(part[0].grad, full[0].grad) and torch.equal(part[1].grad, full[1].grad)
+    y, t = (x.clone().requires_grad_(True) for _ in range(2))
+    ops.LayerNormFunction.apply(y, lw, lw).sum().backward()
+    ops.LayerNormFunction.apply(t, lw, lw, 1e-6, False).sum().backward()
+    assert torch.equal(y.grad, t.grad)
