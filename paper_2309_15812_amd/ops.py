@@ -652,6 +652,7 @@ class LinearFunction(torch.autograd.Function):
                          None if residual is None else residual.contiguous(), save)
         y, pre = (out, None) if save is None else out
         ctx.act, ctx.bias = act, b is not None
+        ctx.residual = None if residual is None else residual.shape  # (its leading axes may be others)
         ctx.save_for_backward(w, *_parts(pack8(x) if checkpoint else x), *_parts(pre))
         ctx.cols = (w.shape[1], w.shape[0])
         return y
@@ -666,7 +667,7 @@ class LinearFunction(torch.autograd.Function):
         gw = gb = None
         if wants[1] or (ctx.bias and wants[2]):
             gw, gb = linear_bwd_weight(_whole(x, xs, ctx.cols[0]), dh, bias=ctx.bias)
-        return gx, gw, gb, None, (gy if wants[4] else None), None
+        return gx, gw, gb, None, (gy.reshape(ctx.residual) if wants[4] else None), None
 
 
 def _parts(t) -> tuple:

@@ -185,3 +185,11 @@ def test_arguments_of_the_autograd_functions_can_be_left_out():
     ops.LayerNormFunction.apply(y, lw, lw).sum().backward()
     ops.LayerNormFunction.apply(t, lw, lw, 1e-6, False).sum().backward()
     assert torch.equal(y.grad, t.grad)
+
+
+def test_a_residual_of_other_leading_axes_gets_its_gradient():
+    x, w, r = randn(2, 3, 5, 24, seed=8).requires_grad_(True), randn(40, 24, seed=9), randn(30, 40, seed=10).requires_grad_(True)
+    y = ops.LinearFunction.apply(x, w, None, "gelu", r, False)
+    dy = randn(2, 3, 5, 40, seed=11)
+    y.backward(dy)
+    assert x.grad.shape == x.shape and torch.equal(r.grad, dy.view(30, 40))
