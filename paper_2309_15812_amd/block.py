@@ -19,6 +19,7 @@ bfloat16 and 40 in float32.
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import ops
 
@@ -41,6 +42,7 @@ class OrientedBlockFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy):
         x, theta, w_dw, ln_w, w1, w2, mean, rstd, a, u, us, v, vs, pre, ps = ctx.saved_tensors
         C, hidden = ctx.cols

@@ -10,6 +10,7 @@ import ctypes
 import functools
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import _lib
 
@@ -229,6 +230,7 @@ class OrientedConv1dFunction(torch.autograd.Function):
         return fwd(x, w, theta)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy):
         x, w, theta = ctx.saved_tensors
         gy = gy.contiguous()
@@ -634,6 +636,7 @@ class LayerNormFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy):
         x, scale, mean, rstd, w = ctx.saved_tensors
         gx, gw, gb = ln_bwd(x if scale is None else Packed8(x, scale, ctx.cols), gy.contiguous(), mean, rstd, w)
@@ -658,6 +661,7 @@ class LinearFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy):
         w, x, xs, pre, ps = ctx.saved_tensors
         dy = gy.contiguous()

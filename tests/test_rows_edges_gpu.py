@@ -193,3 +193,19 @@ def test_a_residual_of_other_leading_axes_gets_its_gradient():
     dy = randn(2, 3, 5, 40, seed=11)
     y.backward(dy)
     assert x.grad.shape == x.shape and torch.equal(r.grad, dy.view(30, 40))
+
+
+def test_second_derivatives_are_refused():
+    """The gradients' own graph is not there: asking for it says so."""
+    from paper_2309_15812_amd.block import OrientedBlock
+
+    x, w, b = randn(6, 24, seed=12), randn(40, 24, seed=13), randn(24, seed=14)
+    img, theta, k = randn(1, 24, 8, 8, seed=15), torch.zeros(24, device=DEV), randn(24, 5, seed=16)
+    block = OrientedBlock(24, 5).to(DEV)
+    calls = [(lambda t: ops.LayerNormFunction.apply(t, b, b), x), (lambda t: ops.LinearFunction.apply(t, w, None, "gelu"), x),
+             (block, img.permute(0, 2, 3, 1).contiguous()), (lambda t: ops.OrientedConv1dFunction.apply(t, k, theta), img)]
+    for f, t in calls:
+        t = t.clone().requires_grad_(True)
+        g, = torch.autograd.grad(f(t).sum(), t, create_graph=True)
+        with pytest.raises(RuntimeError):
+            torch.autograd.grad((g * g).sum(), t)
