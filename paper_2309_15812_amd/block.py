@@ -25,13 +25,16 @@ from . import ops
 
 
 class OrientedBlockFunction(torch.autograd.Function):
-    """apply(x, theta, w_dw, ln_w, ln_b, w1, b1, w2, b2, act, eps, checkpoint); theta gets no gradient."""
+    """apply(x, theta, w_dw, ln_w, ln_b, w1, b1, w2, b2, act, eps, checkpoint, keep=True); theta gets no gradient.  keep=False:
+    there will be no backward, and nothing is kept for it."""
 
     @staticmethod
-    def forward(ctx, x, theta, w_dw, ln_w, ln_b, w1, b1, w2, b2, act, eps, checkpoint):
+    def forward(ctx, x, theta, w_dw, ln_w, ln_b, w1, b1, w2, b2, act, eps, checkpoint, keep=True):
         x = x.contiguous()
         u = ops.fwd_ex(x, w_dw, theta, layout="nhwc")
         v, mean, rstd = ops.ln_fwd(u, ln_w, ln_b, eps)
+        if not (keep and any(ctx.needs_input_grad)):
+            return ops.linear_fwd(ops.linear_fwd(v, w1, b1, act=act), w2, b2, residual=x)
         a, pre = ops.linear_fwd(v, w1, b1, act=act, save="pack8" if checkpoint else "pre")
         y = ops.linear_fwd(a, w2, b2, residual=x)
         if checkpoint:
@@ -60,7 +63,7 @@ class OrientedBlockFunction(torch.autograd.Function):
             dx = ops.bwd_input_ex(du, w_dw, theta, tuple(x.shape[1:3]), layout="nhwc").add_(dy)
         if ctx.needs_input_grad[2]:
             dw_dw = ops.bwd_weight_ex(x, du, theta, w_dw.shape[1], layout="nhwc")
-        return dx, None, dw_dw, dln_w, dln_b, dw1, db1, dw2, db2, None, None, None
+        return dx, None, dw_dw, dln_w, dln_b, dw1, db1, dw2, db2, None, None, None, None
 
 
 class OrientedBlock(torch.nn.Module):
@@ -87,7 +90,7 @@ class OrientedBlock(torch.nn.Module):
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         return OrientedBlockFunction.apply(x, self.theta, self.w_dw, self.ln_w, self.ln_b, self.w1, self.b1, self.w2,
-                                           self.b2, self.act, self.eps, self.checkpoint)
+                                           self.b2, self.act, self.eps, self.checkpoint, torch.is_grad_enabled())
 
 
 def main(steps: int = 20) -> None:

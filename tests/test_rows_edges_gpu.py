@@ -209,3 +209,32 @@ def test_second_derivatives_are_refused():
         g, = torch.autograd.grad(f(t).sum(), t, create_graph=True)
         with pytest.raises(RuntimeError):
             torch.autograd.grad((g * g).sum(), t)
+
+
+def counted(monkeypatch, *names):
+    """How often each of these operators is called."""
+    calls = dict.fromkeys(names, 0)
+    for n in names:
+        def call(*args, _n=n, _f=getattr(ops, n), **kw):
+            calls[_n] += 1
+            return _f(*args, **kw)
+
+        monkeypatch.setattr(ops, n, call)
+    return calls
+
+
+@pytest.mark.parametrize("checkpoint", [False, True])
+def test_a_call_without_gradients_keeps_nothing(monkeypatch, checkpoint):
+    from paper_2309_15812_amd.block import OrientedBlock
+
+    block = OrientedBlock(24, 5, checkpoint=checkpoint).to(DEV)
+    x = randn(2, 9, 9, 24, seed=17)
+    want = block(x).detach()
+    lin, calls = ops.linear_fwd, counted(monkeypatch, "pack8")
+    saved = []
+    monkeypatch.setattr(ops, "linear_fwd", lambda *a, save=None, **kw: saved.append(save) or lin(*a, save=save, **kw))
+    with torch.no_grad():
+        assert torch.equal(block(x), want)
+    block.requires_grad_(False)
+    assert torch.equal(block(x), want)
+    assert saved == [None] * 4 and calls["pack8"] == 0
