@@ -50,18 +50,23 @@ class OrientedBlockFunction(torch.autograd.Function):
         x, theta, w_dw, ln_w, w1, w2, mean, rstd, a, u, us, v, vs, pre, ps = ctx.saved_tensors
         C, hidden = ctx.cols
         u, v, pre = ops._whole(u, us, C), ops._whole(v, vs, C), ops._whole(pre, ps, hidden)
-        dy = gy.contiguous()
-        has_act = ctx.act != "none"
-        dh = ops.linear_bwd_input(dy, w2, pre=pre if has_act else None, act=ctx.act)
-        # the second product's input is kept, or made again from the pre-activation
-        dw2, db2 = ops.linear_bwd_weight(pre, dy, act=ctx.act) if a is None else ops.linear_bwd_weight(a, dy)
-        dv = ops.linear_bwd_input(dh, w1)
-        dw1, db1 = ops.linear_bwd_weight(v, dh)
-        du, dln_w, dln_b = ops.ln_bwd(u, dv, mean, rstd, ln_w)
-        dx = dw_dw = None
-        if ctx.needs_input_grad[0]:
+        dy, act = gy.contiguous(), ctx.act
+        want_x, _, want_dw, want_ln_w, want_ln_b, want_w1, want_b1, want_w2, want_b2 = ctx.needs_input_grad[:9]
+        deep = want_x or want_dw or want_ln_w or want_ln_b
+        dx = dw_dw = dln_w = dln_b = dw1 = db1 = dw2 = db2 = None
+        if want_w2 or want_b2:
+            # the second product's input is kept, or made again from the pre-activation
+            src, src_act = (pre, act) if a is None else (a, "none")
+            dw2, db2 = ops.linear_bwd_weight(src, dy, act=src_act, bias=want_b2)
+        if deep or want_w1 or want_b1:
+            dh = ops.linear_bwd_input(dy, w2, pre=None if act == "none" else pre, act=act)
+            if want_w1 or want_b1:
+                dw1, db1 = ops.linear_bwd_weight(v, dh, bias=want_b1)
+        if deep:
+            du, dln_w, dln_b = ops.ln_bwd(u, ops.linear_bwd_input(dh, w1), mean, rstd, ln_w)
+        if want_x:
             dx = ops.bwd_input_ex(du, w_dw, theta, tuple(x.shape[1:3]), layout="nhwc").add_(dy)
-        if ctx.needs_input_grad[2]:
+        if want_dw:
             dw_dw = ops.bwd_weight_ex(x, du, theta, w_dw.shape[1], layout="nhwc")
         return dx, None, dw_dw, dln_w, dln_b, dw1, db1, dw2, db2, None, None, None, None
 

@@ -238,3 +238,31 @@ def test_a_call_without_gradients_keeps_nothing(monkeypatch, checkpoint):
     block.requires_grad_(False)
     assert torch.equal(block(x), want)
     assert saved == [None] * 4 and calls["pack8"] == 0
+
+
+def test_gradients_that_nobody_wants_are_not_computed(monkeypatch):
+    from paper_2309_15812_amd.block import OrientedBlock
+
+    block = OrientedBlock(24, 5).to(DEV)
+    x, dy = randn(2, 9, 9, 24, seed=18), randn(2, 9, 9, 24, seed=19)
+    block(x).backward(dy)
+    want = {n: p.grad for n, p in block.named_parameters()}
+    for wanted in ({"w2", "b2"}, {"b1"}, {"ln_b"}, {"w_dw"}, {"ln_w", "b2"}):
+        for n, p in block.named_parameters():
+            p.grad = None
+            p.requires_grad_(n in wanted)
+        with monkeypatch.context() as m:
+            calls = counted(m, "linear_bwd_input", "linear_bwd_weight", "ln_bwd", "bwd_input_ex", "bwd_weight_ex")
+            block(x).backward(dy)
+        for n, p in block.named_parameters():
+            assert (p.grad is None) if n not in wanted else torch.equal(p.grad, want[n]), n
+        deep = bool(wanted & {"ln_w", "ln_b", "w_dw"})
+        assert calls == {"linear_bwd_input": deep + bool(deep or wanted & {"w1", "b1"}),
+                         "linear_bwd_weight": bool(wanted & {"w2", "b2"}) + bool(wanted & {"w1", "b1"}), "ln_bwd": int(deep),
+                         "bwd_input_ex": 0, "bwd_weight_ex": int("w_dw" in wanted)}
+    y = randn(6, 24, seed=20)
+    w, b = randn(24, seed=21).requires_grad_(True), randn(24, seed=22)
+    calls = counted(monkeypatch, "ln_bwd")
+    n = ops.LayerNormFunction.apply(y, w, b)
+    n.sum().backward()
+    assert w.grad is not None and calls["ln_bwd"] == 1
