@@ -33,11 +33,11 @@ __device__ const u32x4 g_zero_run = {0u, 0u, 0u, 0u};
 // lane order.  The instruction is invisible to the compiler's wait counts: the
 // caller waits (wait_loads) before a barrier that precedes the reads.
 __device__ __forceinline__ void fetch(const char* from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory", "m0");
 }
 __device__ __forceinline__ void fetch(const char* base, uint32_t off, uint32_t stage, uint32_t block) {
   asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(stage), "s"(block)
-               : "memory", "scc");
+               : "memory", "scc", "m0");
 }
 
 template <int N>
