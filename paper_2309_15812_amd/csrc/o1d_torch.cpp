@@ -6,11 +6,13 @@
 // Each function returns None where its case is not the common one (a tensor of
 // other strides or one that does not match, no rows, an error status): the caller
 // then takes its checked path, which also names what is wrong.  Outputs are new
-// tensors; kernels run on the current stream of the first tensor's device.
+// tensors; kernels run on the current stream of the first tensor's device, which is
+// made the current one for the call (the default stream's handle means the current device's).
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -169,6 +171,7 @@ PyObject* ln_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const double eps = PyFloat_Check(a[3]) ? PyFloat_AS_DOUBLE(a[3]) : -1.;
   if (!w || !b || eps < 0.) return none();
   at::Tensor y = empty_rows(x, x.C), mean = empty({x.M}, *x.t, at::kFloat), rstd = empty({x.M}, *x.t, at::kFloat);
+  const c10::DeviceGuard guard(x.t->device());
   void* s = stream_of(*x.t);
   const auto st = call([&] {
     return p_ln_fwd(x.data(), x.ld, w->data_ptr(), b->data_ptr(), y.data_ptr(), x.C, (float*)mean.data_ptr(),
@@ -194,6 +197,7 @@ PyObject* ln_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
              db = empty({dy.C}, *w, w->scalar_type());
   const size_t need = p_ln_bytes((int)dy.M, dy.C, dy.dt);
   at::Tensor ws = space(need, *dy.t);
+  const c10::DeviceGuard guard(dy.t->device());
   void* s = stream_of(*dy.t);
   const auto st = call([&] {
     return p_ln_bwd(x.x, x.ld, x.q, x.scale, dy.data(), dy.ld, (const float*)mean->data_ptr(),
@@ -223,6 +227,7 @@ PyObject* linear_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     q = empty({x.M, (O + 15) / 16 * 16}, *x.t, at::kChar);
     scale = empty({x.M, (O + kGroup - 1) / kGroup}, *x.t, at::kFloat);
   }
+  const c10::DeviceGuard guard(x.t->device());
   void* s = stream_of(*x.t);
   const auto st = call([&] {
     return p_linear_fwd(x.data(), x.ld, w->data_ptr(), b ? b->data_ptr() : nullptr, (o1d_act_t)act,
@@ -251,6 +256,7 @@ PyObject* linear_bwd_input(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (I < 1 || (a[2] == Py_None) != (act == O1D_ACT_NONE)) return none();
   if (a[2] != Py_None && !source_of(a[2], a[3], a[4], dy, I, pre)) return none();
   at::Tensor dx = empty_rows(dy, I);
+  const c10::DeviceGuard guard(dy.t->device());
   void* s = stream_of(*dy.t);
   const auto st = call([&] {
     return p_linear_bwd_input(dy.data(), dy.ld, w->data_ptr(), (o1d_act_t)act, pre.x, pre.x ? pre.ld : I, pre.q,
@@ -275,6 +281,7 @@ PyObject* linear_bwd_weight(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (bias) db = empty({O}, *dy.t, dy.t->scalar_type());
   const size_t need = p_linear_bytes((int)dy.M, (int)I, O, (o1d_act_t)act, x.q != nullptr, dy.dt);
   at::Tensor ws = space(need, *dy.t);
+  const c10::DeviceGuard guard(dy.t->device());
   void* s = stream_of(*dy.t);
   const auto st = call([&] {
     return p_linear_bwd_weight(x.x, x.ld, x.q, x.scale, (o1d_act_t)act, dy.data(), dy.ld, dw.data_ptr(),
@@ -294,6 +301,7 @@ PyObject* pack8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 1 || !rows_of(a[0], x)) return none();
   at::Tensor q = empty({x.M, (x.C + 15) / 16 * 16}, *x.t, at::kChar),
              scale = empty({x.M, (x.C + kGroup - 1) / kGroup}, *x.t, at::kFloat);
+  const c10::DeviceGuard guard(x.t->device());
   void* s = stream_of(*x.t);
   const auto st = call([&] {
     return p_pack(x.data(), x.ld, (signed char*)q.data_ptr(), (float*)scale.data_ptr(), (int)x.M, x.C, x.dt, s);
@@ -310,6 +318,7 @@ PyObject* unpack8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const long C = PyLong_AsLong(a[2]), dt = PyLong_AsLong(a[3]), act = PyLong_AsLong(a[4]);
   if (C < 1 || q->size(1) != (C + 15) / 16 * 16) return none();
   at::Tensor y = empty({q->size(0), C}, *q, dt == O1D_F32 ? at::kFloat : at::kBFloat16);
+  const c10::DeviceGuard guard(q->device());
   void* s = stream_of(*q);
   const auto st = call([&] {
     return p_unpack((const signed char*)q->data_ptr(), (const float*)scale->data_ptr(), (o1d_act_t)act, y.data_ptr(), C,

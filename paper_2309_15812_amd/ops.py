@@ -339,8 +339,14 @@ def _rows(t: torch.Tensor, what: str) -> tuple[torch.Tensor, int, int, int]:
     return v, M, C, ld
 
 
-def _run(fn: str, *args) -> None:
-    status = getattr(_lib.lib(), fn)(*args)
+def _run(fn: str, like: torch.Tensor, *args) -> None:
+    """The C entry point on the current stream of like's device."""
+    f, device = getattr(_lib.lib(), fn), like.get_device()
+    if device == torch.cuda.current_device():
+        status = f(*args, _stream(like))
+    else:  # (the default stream's handle means the current device's)
+        with torch.cuda.device(device):
+            status = f(*args, _stream(like))
     if status:
         _lib.check(fn, status)
 
@@ -457,7 +463,7 @@ def pack8(x: torch.Tensor) -> Packed8:
     dt = _dt(x)
     v, M, C, ld = _rows(x, "x")
     held = Packed8.empty(M, C, x.device)
-    _run("o1d_pack", v.data_ptr(), ld, held.q.data_ptr(), held.scale.data_ptr(), M, C, dt, _stream(x))
+    _run("o1d_pack", x, v.data_ptr(), ld, held.q.data_ptr(), held.scale.data_ptr(), M, C, dt)
     return held
 
 
@@ -477,8 +483,8 @@ def unpack8(held: Packed8, dtype: torch.dtype, act: str = "none", out: torch.Ten
             raise ValueError(f"out must be {dtype} on {held.q.device}")
         y = out
         v, ld = _same(out, "out", held.rows, held.cols, out)
-    _run("o1d_unpack", held.q.data_ptr(), held.scale.data_ptr(), _act(act), v.data_ptr(), ld, held.rows, held.cols,
-         _DT[dtype], _stream(held.q))
+    _run("o1d_unpack", held.q, held.q.data_ptr(), held.scale.data_ptr(), _act(act), v.data_ptr(), ld, held.rows, held.cols,
+         _DT[dtype])
     return y
 
 
@@ -495,8 +501,8 @@ def ln_fwd(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor, eps: float = 1e-6,
     _vector(b, "b", C, x)
     y = _into(out, x, C)
     mean, rstd = x.new_empty((M,), dtype=torch.float32), x.new_empty((M,), dtype=torch.float32)
-    _run("o1d_ln_fwd", v.data_ptr(), ld, w.data_ptr(), b.data_ptr(), y.data_ptr(), C, mean.data_ptr(), rstd.data_ptr(),
-         M, C, eps, dt, _stream(x))
+    _run("o1d_ln_fwd", x, v.data_ptr(), ld, w.data_ptr(), b.data_ptr(), y.data_ptr(), C, mean.data_ptr(), rstd.data_ptr(),
+         M, C, eps, dt)
     return y, mean, rstd
 
 
@@ -526,8 +532,8 @@ def ln_bwd(x: torch.Tensor | Packed8, dy: torch.Tensor, mean: torch.Tensor, rstd
     dx = _into(dx, dy, C)
     dw, db = (torch.empty_like(w) if t is None else _out(t, w) for t in (dw, db))
     workspace, nbytes = _scratch(workspace, dy, ln_workspace_bytes(M, C, dy.dtype))
-    _run("o1d_ln_bwd", px, ldx, q, scale, g.data_ptr(), lddy, mean.data_ptr(), rstd.data_ptr(), w.data_ptr(),
-         dx.data_ptr(), C, dw.data_ptr(), db.data_ptr(), M, C, dt, workspace.data_ptr(), nbytes, _stream(dy))
+    _run("o1d_ln_bwd", dy, px, ldx, q, scale, g.data_ptr(), lddy, mean.data_ptr(), rstd.data_ptr(), w.data_ptr(),
+         dx.data_ptr(), C, dw.data_ptr(), db.data_ptr(), M, C, dt, workspace.data_ptr(), nbytes)
     return dx, dw, db
 
 
@@ -553,10 +559,9 @@ def linear_fwd(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor | None = None, 
     y = _into(out, x, O)
     pre = _into(None, x, O) if save == "pre" else None
     held = Packed8.empty(M, O, x.device) if save == "pack8" else None
-    _run("o1d_linear_fwd", v.data_ptr(), ldx, w.data_ptr(), None if b is None else b.data_ptr(), a,
+    _run("o1d_linear_fwd", x, v.data_ptr(), ldx, w.data_ptr(), None if b is None else b.data_ptr(), a,
          None if res is None else res.data_ptr(), ldres, y.data_ptr(), O, None if pre is None else pre.data_ptr(), O,
-         None if held is None else held.q.data_ptr(), None if held is None else held.scale.data_ptr(), M, I, O, dt,
-         _stream(x))
+         None if held is None else held.q.data_ptr(), None if held is None else held.scale.data_ptr(), M, I, O, dt)
     return y if save is None else (y, pre if held is None else held)
 
 
@@ -580,8 +585,7 @@ def linear_bwd_input(dy: torch.Tensor, w: torch.Tensor, pre: torch.Tensor | Pack
         raise ValueError("pre and act are given together")
     p, ldp, q, scale = (None, I, None, None) if pre is None else _either(pre, "pre", M, I, dy)
     dx = _into(out, dy, I)
-    _run("o1d_linear_bwd_input", g.data_ptr(), lddy, w.data_ptr(), a, p, ldp, q, scale, dx.data_ptr(), I, M, I, O, dt,
-         _stream(dy))
+    _run("o1d_linear_bwd_input", dy, g.data_ptr(), lddy, w.data_ptr(), a, p, ldp, q, scale, dx.data_ptr(), I, M, I, O, dt)
     return dx
 
 
@@ -608,8 +612,8 @@ def linear_bwd_weight(x: torch.Tensor | Packed8, dy: torch.Tensor, act: str = "n
     dw = dy.new_empty((O, I)) if dw is None else _out(dw, dy, (O, I))
     db = None if not bias else dy.new_empty((O,)) if db is None else _out(db, dy, (O,))
     workspace, nbytes = _scratch(workspace, dy, linear_workspace_bytes(M, I, O, dy.dtype, act, q is not None))
-    _run("o1d_linear_bwd_weight", p, ldx, q, scale, a, g.data_ptr(), lddy, dw.data_ptr(),
-         None if db is None else db.data_ptr(), M, I, O, dt, workspace.data_ptr(), nbytes, _stream(dy))
+    _run("o1d_linear_bwd_weight", dy, p, ldx, q, scale, a, g.data_ptr(), lddy, dw.data_ptr(),
+         None if db is None else db.data_ptr(), M, I, O, dt, workspace.data_ptr(), nbytes)
     return dw, db
 
 
@@ -619,7 +623,7 @@ def act_bwd(pre: torch.Tensor | Packed8, dy: torch.Tensor, act: str, out: torch.
     g, M, C, lddy = _rows(dy, "dy")
     p, ldp, q, scale = _either(pre, "pre", M, C, dy)
     dh = _into(out, dy, C)
-    _run("o1d_act_bwd", p, ldp, q, scale, a, g.data_ptr(), lddy, dh.data_ptr(), C, M, C, dt, _stream(dy))
+    _run("o1d_act_bwd", dy, p, ldp, q, scale, a, g.data_ptr(), lddy, dh.data_ptr(), C, M, C, dt)
     return dh
 
 
