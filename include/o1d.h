@@ -210,18 +210,25 @@ size_t o1d_dsc_bwd_workspace_bytes(int N, int C, int Cout, int H, int W, int K, 
  * elements apart (at least the number of features, below 2^21), so that a slice
  * of a wider tensor can be given.  Weights are dense and, like the biases,
  * of the activations' dtype.  Any number of features from 1 to 2^20 and any
- * element-aligned address is accepted.  Sums, statistics and products
- * accumulate in float32 and are rounded once when stored, except that the weight
- * gradient of a checkpointed or activated input rounds that input to dtype
- * first (the matrix cores' operand).  All sums have a fixed order: results are
- * bitwise reproducible.  Ownership, asynchrony and error rules are those of the
- * other entry points; no output may overlap an input, another output or the
- * workspace, measured over the rows' whole reach.  A workspace is 16-byte aligned
- * and has at least the bytes that the call's ..._workspace_bytes gives for the same arguments (256
- * where the work needs none, and nothing is written to them; at least 512 where it needs some;
- * 0 for M = 0); what it holds before a call does not matter.  Calls that may run
- * at the same time need workspaces of their own, unless nothing is written to them.  M = 0 is valid: nothing is launched, except that weight gradients are
- * set to zeros. */
+ * element-aligned address is accepted.
+ *
+ * Sums, statistics and products accumulate in float32 and are rounded once when
+ * stored.  Products of float32 take each operand to 24 bits or to a multiple of
+ * 2^-133, whichever is coarser, and each product to 2^-24 of itself (an infinity
+ * times an operand that rounds to 0 is NaN).  The weight gradient of a checkpointed
+ * or activated input rounds that input, act(x), to dtype first, as the
+ * forward's product was given it (the matrix cores' operand).  All sums have a
+ * fixed order: results are bitwise reproducible.
+ *
+ * Ownership, asynchrony and error rules are those of the other entry points; no
+ * output may overlap an input, another output or the workspace, measured over
+ * the rows' whole reach.  A workspace is 16-byte aligned and has at least the
+ * bytes that the call's ..._workspace_bytes gives for the same arguments (256
+ * where the work needs none, and nothing is written to them; at least 512 where
+ * it needs some; 0 for M = 0); what it holds before a call does not matter.
+ * Calls that may run at the same time need workspaces of their own, unless nothing
+ * is written to them.  M = 0 is valid: nothing is launched, except that weight
+ * gradients are set to zeros. */
 typedef enum {
   O1D_ACT_NONE = 0,
   O1D_ACT_RELU = 1,

@@ -18,11 +18,12 @@
 // float32 operands are staged as three bfloat16 pieces, x = x1 + x2 + x3 with
 // x1 the nearest bfloat16 to x, x2 that to x - x1 and x3 the rest: 24 bits, all
 // of a float32's.  x y is summed as x1 y1 + x1 y2 + x2 y1 + x2 y2 + x1 y3 + x3 y1,
-// six exact products; the ones left out are below 2^-25 |x y|, under float32's own
-// rounding (2^-24).  The six take 3/8 of the time of the float32 instruction, and
+// six exact products; the ones left out, x2 y3 + x3 y2 and x3 y3, are below 2^-24 |x y| (at
+// most 2^-8 and 2^-17 of x and y, as for 1 + 2^-8 - 2^-17), which is float32's own rounding of a
+// product.  The six take 3/8 of the time of the float32 instruction, and
 // sixteen products enter each rounding of the sum instead of two: measured against
-// 64 bits the results are no further off.  (Values below 2^-110, whose
-// pieces leave bfloat16's range, keep fewer bits.)
+// 64 bits the results are no further off.  Pieces are multiples of 2^-133, bfloat16's
+// smallest value, which the instruction keeps: operands below 2^-110 are rounded to that.
 //
 // B's fragment is the instruction's first operand, so that a lane holds four
 // consecutive columns n of one row m, and the other half-wave the next four:
@@ -74,7 +75,7 @@ struct Fmt {
 
 // The three pieces of four float32, two words each.  A value that is not
 // finite is (+-1, 0, itself): only the third piece meets every other operand
-// once (times its first piece, which is 0 only if that operand is), so that the
+// once (times its first piece, which is 0 only if that operand is below 2^-134), so that the
 // sum is what float32 products give: infinite with its sign, or NaN.
 __device__ __forceinline__ uint32_t pair_bf16(float a, float b) {
   return (uint32_t)from_f32<uint16_t>(a) | (uint32_t)from_f32<uint16_t>(b) << 16;

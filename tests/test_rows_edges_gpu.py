@@ -266,3 +266,30 @@ def test_gradients_that_nobody_wants_are_not_computed(monkeypatch):
     n = ops.LayerNormFunction.apply(y, w, b)
     n.sum().backward()
     assert w.grad is not None and calls["ln_bwd"] == 1
+
+
+@pytest.mark.parametrize("M", [4, 3000])
+def test_float32_products_where_the_dropped_pieces_are_largest(M):
+    """1 + 2^-8 - 2^-17 is (1, 2^-8, -2^-17) in bfloat16 pieces: its square without the products of the second and third is 0.99 x 2^-24
+    off.  Beside that stand the sums' roundings, at most 2^-23 for the largest and 5 x 2^-31 for the small ones."""
+    v = 1 + 2.0 ** -8 - 2.0 ** -17
+    x, w = torch.zeros(M, 64, device=DEV), torch.zeros(50, 64, device=DEV)
+    x[:, 9], w[:, 9] = v, v
+    want = torch.full((M, 50), v * v, device=DEV, dtype=torch.float64)
+    near(ops.linear_fwd(x, w), want, 4 * 2.0 ** -24 * v * v, "y")
+    near(ops.linear_bwd_input(x, w.t().contiguous()), want, 4 * 2.0 ** -24 * v * v, "dx")
+    dw, _ = ops.linear_bwd_weight(x[:1].contiguous(), x[:1].contiguous())
+    near(dw[9, 9], torch.tensor(v * v, device=DEV, dtype=torch.float64), 4 * 2.0 ** -24 * v * v, "dw")
+
+
+@pytest.mark.parametrize("M", [8, 3000])
+@pytest.mark.parametrize("e", [-105, -112, -120, -126, -130, -133])
+def test_float32_products_of_small_operands(M, e):
+    """A piece is a multiple of 2^-133: an operand is off by 2^-134 at most, which other operands of 2^100 make visible."""
+    I, O = 64, 40
+    x, w = (1 + randn(M, I, seed=23).abs()) * 2.0 ** e, randn(O, I, seed=24) * 2.0 ** 100
+    X, W = x.double(), w.double()
+    tol = (I + 8) * 2.0 ** -24 * (X @ W.t().abs()) + 2.0 ** -134 * W.abs().sum(1)
+    near(ops.linear_fwd(x, w), X @ W.t(), tol, "y")
+    v = w.t().contiguous()
+    near(ops.linear_bwd_input(x, v), X @ v.double(), tol, "dx")
