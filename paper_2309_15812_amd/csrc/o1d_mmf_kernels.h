@@ -32,6 +32,9 @@ __device__ const u32x4 g_zero_run = {0u, 0u, 0u, 0u};
 // 64 lanes' 16-byte runs to 1 KB of LDS at `lds` (the same in all lanes), in
 // lane order.  The instruction is invisible to the compiler's wait counts: the
 // caller waits (wait_loads) before a barrier that precedes the reads.
+// (m0 is no register that values are given to, which the compiler warns of where it is named.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void fetch(const char* from, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds) : "memory", "m0");
 }
@@ -39,6 +42,7 @@ __device__ __forceinline__ void fetch(const char* base, uint32_t off, uint32_t s
   asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(stage), "s"(block)
                : "memory", "scc", "m0");
 }
+#pragma clang diagnostic pop
 
 template <int N>
 __device__ __forceinline__ void wait_loads() {
