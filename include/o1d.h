@@ -305,6 +305,14 @@ const char* o1d_kernel_name(int op, int N, int C, int H, int W, int K, int strid
                             o1d_sampling_t sampling, o1d_dtype_t dtype, int aligned);
 const char* o1d_kernel_variant(int i);
 
+/* The same for the row operators: e.g. "mmf/fwd/bf16/128x64" (its tile) or
+ * "act+mm/wgrad/f32/64x64+mm_sum", launches joined by '+'.  op: 0 = o1d_linear_fwd (held: it
+ * writes a checkpoint), 1 = o1d_linear_bwd_input, 2 = o1d_linear_bwd_weight (held: of a
+ * checkpoint; act as there), 3 = o1d_ln_fwd, 4 = o1d_ln_bwd (held: of a checkpoint), both with I
+ * features; act and O are read where the call has them.  `aligned` != 0 states that tensors
+ * and row strides are multiples of 16 bytes. */
+const char* o1d_rows_kernel_name(int op, int M, int I, int O, o1d_act_t act, int held, o1d_dtype_t dtype, int aligned);
+
 /* Static description of a status code. */
 const char* o1d_status_str(o1d_status_t status);
 

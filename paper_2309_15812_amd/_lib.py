@@ -48,6 +48,7 @@ SIGNATURES = {
     "o1d_act_bwd": (_i, [_vp, _ll, _vp, _vp, _i, _vp, _ll, _vp, _ll, _i, _i, _i, _vp]),
     "o1d_kernel_name": (ctypes.c_char_p, [_i, _i, _i, _i, _i, _i, _i, _i, _i, _i, _i]),
     "o1d_kernel_variant": (ctypes.c_char_p, [_i]),
+    "o1d_rows_kernel_name": (ctypes.c_char_p, [_i, _i, _i, _i, _i, _i, _i, _i]),
     "o1d_status_str": (ctypes.c_char_p, [_i]),
     "o1d_last_error": (ctypes.c_char_p, []),
     "o1d_version": (ctypes.c_char_p, []),
@@ -87,6 +88,15 @@ def kernel_name(op: int, N: int, C: int, H: int, W: int, K: int, stride: int = 1
     """The kernel(s) a call would launch (host-side planning only, no GPU needed).
     op: 0 forward, 1 input gradient, 2 weight gradient, 3 both gradients (o1d_bwd)."""
     return lib().o1d_kernel_name(op, N, C, H, W, K, stride, layout, sampling, dtype, int(aligned)).decode()
+
+
+ROWS_OP = {"linear_fwd": 0, "linear_bwd_input": 1, "linear_bwd_weight": 2, "ln_fwd": 3, "ln_bwd": 4}
+
+
+def rows_kernel_name(op: str, M: int, I: int, O: int = 1, act: str = "none", held: bool = False, dtype: int = O1D_F32,
+                     aligned: bool = True) -> str:
+    """The kernel(s) a row operator's call would launch (host-side planning only, no GPU needed)."""
+    return lib().o1d_rows_kernel_name(ROWS_OP[op], M, I, O, ACT[act], int(held), dtype, int(aligned)).decode()
 
 
 def kernel_variants() -> list[str]:

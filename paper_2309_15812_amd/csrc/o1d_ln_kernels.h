@@ -444,14 +444,13 @@ __global__ __launch_bounds__(kWide) void ln_dw_wide(LnParams P) {
     }
 }
 
-// Calls f with the row's lanes and runs per lane: the fewest lanes that hold
-// the row in four runs each, up to a wave with eight.
+// Calls f with the forward's lanes and runs per lane (ln_fwd_map).
 template <typename T, class F>
 bool with_row(int C, F&& f) {
-  const long long runs = cdiv(C, kRun<T>);
+  const LnMap m = ln_fwd_map(C, (int)sizeof(T));
   auto pick = [&](auto lpr) {
     constexpr int L = decltype(lpr)::value;
-    switch ((int)cdiv(runs, L)) {
+    switch (m.runs) {
       case 1: if constexpr (L == 4) f(lpr, std::integral_constant<int, 1>{}); break;
       case 2: if constexpr (L == 4) f(lpr, std::integral_constant<int, 2>{}); break;
       case 3: f(lpr, std::integral_constant<int, 3>{}); break;
@@ -462,12 +461,14 @@ bool with_row(int C, F&& f) {
       case 8: if constexpr (L == 64) f(lpr, std::integral_constant<int, 8>{}); break;
     }
   };
-  if (runs <= 16) pick(std::integral_constant<int, 4>{});
-  else if (runs <= 32) pick(std::integral_constant<int, 8>{});
-  else if (runs <= 64) pick(std::integral_constant<int, 16>{});
-  else if (runs <= 128) pick(std::integral_constant<int, 32>{});
-  else if (runs <= 512) pick(std::integral_constant<int, 64>{});
-  else return false;
+  switch (m.lanes) {
+    case 4: pick(std::integral_constant<int, 4>{}); break;
+    case 8: pick(std::integral_constant<int, 8>{}); break;
+    case 16: pick(std::integral_constant<int, 16>{}); break;
+    case 32: pick(std::integral_constant<int, 32>{}); break;
+    case 64: pick(std::integral_constant<int, 64>{}); break;
+    default: return false;
+  }
   return true;
 }
 

@@ -192,7 +192,6 @@ __global__ __launch_bounds__(kThreads) void mm_sum(const float* __restrict__ par
 // outputs enough to fill the GPU: four columns per thread, all pieces.
 // 2048 x 2048 in two pieces: 28 us above, 7.4 (float32 8.7) here.
 constexpr int kWideColumns = 4;
-bool wide_sum(int pieces, long long outputs) { return pieces <= 4 || outputs >= (1 << 18); }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void mm_sum_wide(const float* __restrict__ part, int pieces, long long MN, int M,

@@ -51,13 +51,24 @@ struct LnParams {
   int blocks;
 };
 
-// The backward's layout of a row: `lanes` lanes with `runs` 16-byte runs each
-// (lanes 0: too long for a wave).  Few runs per lane leave registers for more
-// waves and make the sums over a workgroup's rows short; lanes past the row's
-// end do nothing.  33333 x 211 bfloat16: 8 lanes x 4 runs 24 us, 32 x 1 15 us.
+// Layouts of a row: `lanes` lanes with `runs` 16-byte runs each (lanes 0: too
+// long for a wave).  The forward's: the fewest lanes that hold it in four
+// runs each, up to a wave with eight.
 struct LnMap {
   int lanes, runs;
 };
+inline LnMap ln_fwd_map(int C, int esize) {
+  const long long total = cdiv(C, 16 / esize);
+  int lanes = 4;
+  while (lanes < 64 && total > 4 * lanes) lanes *= 2;
+  const int runs = (int)cdiv(total, lanes);
+  return runs <= 8 ? LnMap{lanes, runs} : LnMap{0, 0};
+}
+
+// The backward's: `lanes` lanes with `runs` 16-byte runs each
+// (lanes 0: too long for a wave).  Few runs per lane leave registers for more
+// waves and make the sums over a workgroup's rows short; lanes past the row's
+// end do nothing.  33333 x 211 bfloat16: 8 lanes x 4 runs 24 us, 32 x 1 15 us.
 inline LnMap ln_bwd_map(int C, int esize) {
   const long long total = cdiv(C, 16 / esize);
   LnMap best{0, 0};
@@ -202,6 +213,8 @@ hipError_t launch_few_bf16(int kind, const MmParams& p, hipStream_t stream);
 hipError_t launch_mm(Dtype dt, int kind, const MmPlan& pl, hipStream_t stream);
 
 // dw[i] = sum of the pieces' partials (i < M N), db[o] likewise behind them.
+// (wide_sum: of four columns per thread)
+inline bool wide_sum(int pieces, long long outputs) { return pieces <= 4 || outputs >= (1 << 18); }
 hipError_t launch_mm_sum(Dtype dt, const MmPlan& pl, void* dw, void* db, hipStream_t stream);
 
 }  // namespace rows

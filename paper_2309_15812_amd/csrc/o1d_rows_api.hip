@@ -3,6 +3,7 @@
 // Argument checks and dispatch; no device memory is allocated here.
 #include <hip/hip_runtime.h>
 #include <math.h>
+#include <stdio.h>
 
 #include <initializer_list>
 
@@ -147,9 +148,65 @@ WgradSpace wgrad_space(int M, int I, int O, o1d_act_t act, bool held, o1d_dtype_
   return s;
 }
 
+// ---- names
+
+thread_local char g_name[128] = "";
+
+const char* dt_name(o1d_dtype_t dt) { return dt == O1D_BF16 ? "bf16" : "f32"; }
+
+// The product's launch, as launch_mm and the kernels' own launchers choose it.
+void name_mm(char* out, size_t n, int kind, const rows::MmPlan& pl, o1d_dtype_t dt, bool whole, bool held) {
+  const char *op = kind == rows::kFwd ? "fwd" : (kind == rows::kDgrad ? "dgrad" : "wgrad"), *d = dt_name(dt);
+  const rows::Shape& s = rows::kShapes[pl.shape];
+  const int bm = 32 * s.tm * s.wm, bn = 32 * s.tn * s.wn;
+  if (pl.few)
+    snprintf(out, n, "few/%s/%s/%d%s", op, d, pl.p.M <= 16 ? 16 : (pl.p.M <= 32 ? 32 : 64), held ? "/held" : "");
+  else if (dt == O1D_BF16 && !pl.p.made && whole)
+    snprintf(out, n, "mmf/%s/%s/%dx%d", op, d, bm, bn);
+  else
+    snprintf(out, n, "mm/%s/%s/%dx%d%s", op, d, bm, bn, pl.p.made ? "/made" : "");
+}
+
 }  // namespace
 
 extern "C" {
+
+const char* o1d_rows_kernel_name(int op, int M, int I, int O, o1d_act_t act, int held, o1d_dtype_t dtype, int aligned) {
+  const char* fn = "o1d_rows_kernel_name";
+  g_name[0] = '\0';
+  if (op < 0 || op > 4 || check_dims(fn, M, I, "I", dtype) != O1D_OK || M == 0) return g_name;
+  const int es = (int)elem_size(dtype);
+  if (op >= 3) {
+    const rows::LnMap m = op == 3 ? rows::ln_fwd_map(I, es) : rows::ln_bwd_map(I, es);
+    char size[32] = "wide";
+    if (m.lanes) snprintf(size, sizeof(size), "%dx%d", m.lanes, m.runs);
+    if (op == 3)
+      snprintf(g_name, sizeof(g_name), "ln_fwd/%s/%s", dt_name(dtype), size);
+    else
+      snprintf(g_name, sizeof(g_name), "ln_bwd/%s/%s%s%s", dt_name(dtype), size, held ? "/held" : "",
+               rows::ln_bwd_blocks(M, I, es) > 1 ? "+col_sum" : "");
+    return g_name;
+  }
+  if (check_dims(fn, M, O, "O", dtype) != O1D_OK || check_act(fn, act) != O1D_OK) return g_name;
+  const auto whole = [&](int kind, int m, int n, int k) {
+    return aligned && rows::whole_runs(kind, m, n, k, nullptr, 0, nullptr, 0, es);
+  };
+  if (op < 2) {
+    const int kind = op == 0 ? rows::kFwd : rows::kDgrad, n = op == 0 ? O : I, k = op == 0 ? I : O;
+    const bool w = whole(kind, M, n, k), writes = op == 0 && held;
+    name_mm(g_name, sizeof(g_name), kind, rows::plan_mm(kind, M, n, k, es, writes, w), dtype, w, writes);
+    return g_name;
+  }
+  WgradSpace s = wgrad_space(M, I, O, act, held != 0, dtype);
+  s.plan.p.made = s.made;
+  // (an operand from a pass of its own has whole rows)
+  char mm[64];
+  name_mm(mm, sizeof(mm), rows::kWgrad, s.plan, dtype, whole(rows::kWgrad, O, I, M), false);
+  const int parts = s.plan.p.nsplit;
+  snprintf(g_name, sizeof(g_name), "%s%s%s", s.operand ? "act+" : "", mm,
+           parts == 1 ? "" : (rows::wide_sum(parts, (long long)O * I + O) ? "+mm_sum_wide" : "+mm_sum"));
+  return g_name;
+}
 
 o1d_status_t o1d_ln_fwd(const void* x, long long ldx, const void* w, const void* b, void* y, long long ldy, float* mean,
                         float* rstd, int M, int C, float eps, o1d_dtype_t dtype, void* stream) {

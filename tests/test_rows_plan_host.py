@@ -43,3 +43,25 @@ def test_workspaces_are_nothing_or_larger_than_what_calls_share():
         for act, held in ((NONE, 0), (NONE, 1), (GELU, 0), (GELU, 1)):
             b = wgrad_bytes(M, I, O, dt, act, held)
             assert b == ops._NO_SPACE or b >= 2 * ops._NO_SPACE, (M, I, O, dt, act, held)
+
+
+def test_the_tests_reach_every_kernel_that_is_planned():
+    """A kernel that drawn calls take and no size of the GPU tests does: add a size for it (rows_cases.py)."""
+    import rows_cases
+
+    missing = {n: c for n, c in rows_cases.planned(40000).items() if n not in rows_cases.reached()}
+    assert not missing, missing
+
+
+def test_names_of_planned_kernels():
+    def name(*args, **kw):
+        return _lib.rows_kernel_name(*args, **kw)
+
+    assert name("ln_fwd", 49, 768) == "ln_fwd/f32/64x3" and name("ln_bwd", 33333, 211, held=True, dtype=BF16).endswith("/held+col_sum")
+    assert name("ln_fwd", 3, 9001) == "ln_fwd/f32/wide" and name("linear_fwd", 16, 768, 1000, dtype=BF16) == "few/fwd/bf16/16"
+    assert name("linear_fwd", 20000, 768, 768, dtype=BF16).startswith("mmf/fwd/bf16/")
+    assert name("linear_fwd", 20000, 768, 768, dtype=BF16, aligned=False).startswith("mm/fwd/bf16/")
+    assert name("linear_bwd_weight", 50176, 768, 192, act="gelu", held=True, dtype=BF16).startswith("mm/wgrad/bf16/192x64/made+mm_sum")
+    assert name("linear_bwd_weight", 8192, 2048, 2048, act="gelu", held=True, dtype=BF16).startswith("act+mmf/wgrad/")
+    assert name("linear_fwd", 0, 8, 8) == name("linear_fwd", 8, 0, 8) == name("ln_fwd", 8, -1) == ""
+    assert _lib.lib().o1d_rows_kernel_name(5, 8, 8, 8, 0, 0, F32, 1) == _lib.lib().o1d_rows_kernel_name(0, 8, 8, 8, 9, 0, F32, 1) == b""
