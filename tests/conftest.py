@@ -18,3 +18,18 @@ def _oracle_built():
 
     oracle.build(force=False)
     yield
+
+
+# Their calls name invented device addresses and rely on being refused: where a GPU is present, a lost check would launch a
+# kernel on those.
+HOST_ONLY = {"test_abi_host.py", "test_rows_host.py"}
+
+
+def pytest_collection_modifyitems(config, items):
+    mine = [i for i in items if os.path.basename(str(i.path)) in HOST_ONLY]
+    if mine:
+        import torch
+
+        if torch.cuda.device_count():
+            for item in mine:
+                item.add_marker(pytest.mark.skip(reason="calls with invented addresses run only where there is no GPU"))
