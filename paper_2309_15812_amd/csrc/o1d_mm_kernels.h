@@ -381,10 +381,16 @@ __device__ __forceinline__ float add_frag(const Frag<T>& f, float s) {
 // (`Ahead`), so that one wait covers them.  WHOLE: the tile lies inside the output.
 template <typename T, int KIND, bool WHOLE>
 struct Ahead {
-  T e[8];      // residual (forward) or pre (input gradient)
-  uint2 q;     // or the latter's checkpoint
-  float scale;
+  // residual (forward) or pre (input gradient), or the latter's checkpoint in the same registers: its
+  // integers and their scale
+  uint32_t w[2 * sizeof(T)];
 
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    T e[8];
+    __builtin_memcpy(e, w, sizeof(e));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = to_f32(e[k]);
+  }
   __device__ __forceinline__ void load(const MmParams& P, int m, int n) {
     if constexpr (KIND == kFwd) {
       if (P.res) run(static_cast<const T*>(P.res) + (long long)m * P.ldres + n, P.N - n, m < P.M);
@@ -392,8 +398,10 @@ struct Ahead {
       if (P.act == kNone) return;
       if (P.q) {
         if (WHOLE || (m < P.M && n < P.N)) {
-          q = *reinterpret_cast<const uint2*>(P.q + (long long)m * P.ldq + n);
-          scale = P.scale[(long long)m * P.groups + n / kGroup];
+          const uint2 q = *reinterpret_cast<const uint2*>(P.q + (long long)m * P.ldq + n);
+          w[0] = q.x;
+          w[1] = q.y;
+          w[2] = __float_as_uint(P.scale[(long long)m * P.groups + n / kGroup]);
         }
       } else {
         run(static_cast<const T*>(P.pre) + (long long)m * P.ldpre + n, P.N - n, m < P.M);
@@ -402,11 +410,12 @@ struct Ahead {
   }
   __device__ __forceinline__ void run(const T* p, int left, bool in) {
     if (WHOLE || (in && left >= 8)) {
-      __builtin_memcpy(e, p, sizeof(e));
+      __builtin_memcpy(w, p, sizeof(w));
     } else if (in) {
+      T e[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k < left) e[k] = p[k];
+      for (int k = 0; k < 8; ++k) e[k] = k < left ? p[k] : T(0);
+      __builtin_memcpy(w, e, sizeof(w));
     }
   }
 };
@@ -428,18 +437,19 @@ __device__ __forceinline__ void finish(const MmParams& P, int m, int n, const Ah
     if (P.pre) put<T, WHOLE>(static_cast<T*>(P.pre) + (long long)m * P.ldpre + n, left, v);
     act_values<kFast>(v, P.act);
     if (P.res) {
+      float r[8];
+      a.values(r);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += WHOLE || e < left ? to_f32(a.e[e]) : 0.f;
+      for (int e = 0; e < 8; ++e) v[e] += r[e];
     }
     put<T, WHOLE>(static_cast<T*>(P.out) + (long long)m * P.ldo + n, left, v);
   } else if constexpr (KIND == kDgrad) {
     if (P.act != kNone) {
       float x[8];
       if (P.q) {
-        unround8(a.q, a.scale, x);
+        unround8(make_uint2(a.w[0], a.w[1]), __uint_as_float(a.w[2]), x);
       } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = WHOLE || e < left ? to_f32(a.e[e]) : 0.f;
+        a.values(x);
       }
       act_slopes<kFast>(v, x, P.act);
     }
