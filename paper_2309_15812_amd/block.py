@@ -3,9 +3,10 @@
     y = x + W2 act(W1 LN(conv(x)) + b1) + b2
 
 The block the paper puts its convolution into: oriented depthwise 1D convolution, layer norm over the channels, a hidden
-layer and the residual.  Everything runs in the library's kernels: the convolution's channels-last entry points, layer
+layer and the residual.  It runs in the library's kernels: the convolution's channels-last entry points, layer
 norm, and the two products, whose epilogues add the biases, the activation and the residual; in the backward the activation's
-derivative is applied in the epilogue of the second product's input gradient.
+derivative is applied in the epilogue of the second product's input gradient.  One pass is torch's: the sum of the
+convolution's input gradient and the residual's, which in bfloat16 is rounded a second time there.
 
 checkpoint=True keeps what the backward needs of the block's inside (the convolution's output, layer norm's output and the
 hidden pre-activation) in 8 bits, 6.4 bytes per pixel and channel with a hidden layer four times as wide, instead of 20 in

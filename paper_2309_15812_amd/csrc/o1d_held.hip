@@ -5,7 +5,7 @@
 // columns each (one 16-byte access in bfloat16, two in float32), so that a
 // group's largest value takes three lane moves and its integers leave as eight
 // bytes per lane.  50176 x 768 bfloat16: written 20.9 us (118 MB, 5.6 TB/s), read
-// back through GELU 25.9 (4.6 TB/s; its slots per element), dy gelu'(x) 35.1 (195 MB, 5.6 TB/s).
+// back through GELU 27.3 (4.3 TB/s; its slots per element), dy gelu'(x) 35.0 (195 MB, 5.6 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

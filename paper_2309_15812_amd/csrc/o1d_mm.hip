@@ -40,7 +40,7 @@ constexpr Cost kWgradCost[3][kShapeCount] = {
     {{0.f, 1.64f, 2}, {0.f, 1.19f, 4}, {}, {0.f, 1.42f, 3}, {0.f, 1.41f, 3}}};
 // Those that make their operand, 64 x 64 and 192 x 64: a step's time by activation
 // (none, relu, gelu, gelu_tanh, silu).  50176 x 768 -> 192 bfloat16 from a checkpoint
-// with GELU: 53 us against 68 with a pass of its own.
+// with GELU: 55 to 58 us against 68 with a pass of its own.
 constexpr int kMadeShapes[2] = {k64x64, k192x64}, kMadeResident[2][2] = {{4, 2}, {4, 3}};
 constexpr float kMadeStep[2][2][kActs] = {{{2.5f, 2.5f, 3.6f, 3.4f, 3.35f}, {3.5f, 3.5f, 4.4f, 4.3f, 4.0f}},
                                           {{1.6f, 1.75f, 2.3f, 2.1f, 1.95f}, {2.75f, 3.0f, 3.25f, 3.15f, 3.05f}}};

@@ -32,12 +32,15 @@
 // share a scale in an 8-bit checkpoint.  (Through LDS, with whole lines per
 // store, the epilogue was bound by LDS and the group's maxima.)
 //
-// Measured: float32 4096 x 2048 -> 2048 200 us: 172 TFLOP/s of float32, of bfloat16
-// products 1.03 PFLOP/s (the library's own float32 product 140 TFLOP/s, its largest
-// bfloat16 ones 1.28 PFLOP/s).  Next to the products' matrix instructions stand
+// Measured: float32 4096 x 2048 -> 2048 189 to 213 us: 161 to 182 TFLOP/s of float32, of
+// bfloat16 products 0.97 to 1.09 PFLOP/s (the library's own float32 product 147 TFLOP/s, its
+// largest bfloat16 ones 1.28 PFLOP/s).  Next to the products' matrix instructions stand
 // the pieces (6.5 vector instructions per element staged, hence the large tiles) and LDS;
-// where a wave has few steps, the first loads and the epilogue.  bfloat16 rows that
-// are not aligned pay for element shifts and masks: 9409 x 203 -> 509 18.8 us.
+// where a wave has few steps, the first loads and the epilogue.  bfloat16 products of rows
+// that are not whole aligned runs come here, both operands through registers, one
+// step ahead.  9409 x 203 -> 509 with residual and pre-activation 18.4 to 19.1 us, the most of what
+// it loses by the three matrices of 509 columns, whose rows share cache lines: into 512 15.9, of
+// 208 and into 512 (o1d_mmf_kernels.h) 14.5.
 //
 // Widths need not be multiples of anything: a 16-byte run past a row's end is
 // loaded from the row's last 16 bytes and moved to its place, k past the end is

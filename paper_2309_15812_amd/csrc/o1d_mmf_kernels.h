@@ -12,9 +12,8 @@
 //
 // Bound by the CU's loads from L2: a step of 128 x 128 brings 32 KB, about 26 bytes a
 // clock and CU, while its products take two fifths of that time; 8192 x 2048 -> 2048
-// 67 to 76 us (0.9 to 1.0 PFLOP/s).  With few steps per tile the epilogue's vector
-// instructions come next to that: 12544 x 384 -> 1536 with GELU and checkpoint (22
-// per element, 11 us by themselves) 37 us.
+// 66 to 77 us (0.9 to 1.04 PFLOP/s).  With few steps per tile the epilogue's vector
+// instructions come next to that: 12544 x 384 -> 1536 with GELU and checkpoint 37 to 40 us.
 //
 // Runs past K are fetched from a zeroed run, rows past the end from the last row.
 #pragma once

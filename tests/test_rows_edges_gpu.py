@@ -1,6 +1,6 @@
 """Edges of the row operators: the largest values, infinities, the tails of the activations, small calls side by side.
 
-Bounds as in the tests of the operators: u = 2^-24 for float32 and 2^-8 for bfloat16 results (one rounding is half of that), n
+Bounds as in the tests of the operators: u = 2^-24 for float32 and 2^-8 for bfloat16 results (the most that one rounding is), n
 float32 sums (n + 8) 2^-24 of the terms' sizes, and what a test adds is derived beside it.
 """
 import math
