@@ -289,6 +289,89 @@ o1d_status_t o1d_act_bwd(const void* pre, long long ldpre, const signed char* pr
                          const void* dy, long long lddy, void* dh, long long lddh, int M, int C, o1d_dtype_t dtype,
                          void* stream);
 
+/* Group norm with an activation on channels-last samples: x is N samples of P pixels, rows of C = groups x D channels (x, y
+ * and their gradients are N P rows, ld elements apart).  Over the P D values of a sample's group, mean = sum x / (P D),
+ * var = sum (x - mean)^2 / (P D), rstd = (var + eps)^-1/2, xh = (x - mean) rstd, h = xh w + b, y = act(h).  mean and
+ * rstd (float32, [N][groups]) are always written.  groups divides C and a group has at most 1024 channels; P >= 1.
+ * A call that passes its samples twice keeps statistics of their parts in the workspace. */
+o1d_status_t o1d_gn_fwd(const void* x, long long ldx, const void* w, const void* b, o1d_act_t act, void* y, long long ldy,
+                        float* mean, float* rstd, int N, int P, int C, int groups, float eps, o1d_dtype_t dtype,
+                        void* workspace, size_t workspace_bytes, void* stream);
+size_t o1d_gn_fwd_workspace_bytes(int N, int P, int C, int groups, o1d_dtype_t dtype);
+/* Its gradients: with dh = dy act'(h) and g = dh w,
+ *   dx = rstd (g - mean(g) - xh mean(g xh)),  dw = sum dh xh,  db = sum dh (over samples and pixels). */
+o1d_status_t o1d_gn_bwd(const void* x, long long ldx, const void* dy, long long lddy, const float* mean, const float* rstd,
+                        const void* w, const void* b, o1d_act_t act, void* dx, long long lddx, void* dw, void* db, int N,
+                        int P, int C, int groups, o1d_dtype_t dtype, void* workspace, size_t workspace_bytes, void* stream);
+size_t o1d_gn_bwd_workspace_bytes(int N, int P, int C, int groups, o1d_dtype_t dtype);
+
+/* ---- Products of 8-bit floating point operands with a power-of-two scale for each 128 values.
+ *
+ * An operand of R rows of K values is unsigned char q[R][ldq], ldq = K rounded up to 128 (zeros behind a row's end), of
+ * OCP e4m3 or e5m2 values, and unsigned char e[ceil(K / 128)][lde], lde = R rounded up to 16 (127 behind the last row): value k of row r
+ * stands for q[r][k] 2^(e[k / 128][r] - 127).  q and e are 16-byte aligned.
+ *
+ * o1d_pack_scaled makes the operand of x (M rows of C values): by rows (q, e: R = M, K = C), transposed (qt, et: R = C, K = M,
+ * groups of 128 rows of x), or both.  The power of two is the least one that leaves the group's largest finite value in the type's
+ * range (448, 57344), at least 2^-127, and 2^0 for a group of zeros; the quotient is rounded once, to nearest with ties to
+ * even, and a value that is not finite becomes NaN.  sums (or NULL; with qt only): the sums of x's columns,
+ * [C] of dtype, by way of the workspace. */
+typedef enum { O1D_E4M3 = 0, O1D_E5M2 = 1 } o1d_scaled_t;
+o1d_status_t o1d_pack_scaled(const void* x, long long ldx, o1d_scaled_t type, unsigned char* q, unsigned char* e,
+                             unsigned char* qt, unsigned char* et, void* sums, int M, int C, o1d_dtype_t dtype,
+                             void* workspace, size_t workspace_bytes, void* stream);
+size_t o1d_pack_scaled_workspace_bytes(int M, int C, int sums);
+/* The products of o1d_linear_*, of packed operands, accumulated in float32, with results of dtype.  The first operand has the
+ * given type, the second is e4m3.
+ *   fwd:        h = x W^T + b, y = act(h) + residual; pre (or NULL) = h.   x: M rows of I, W: O rows of I
+ *   bwd_input:  dx = (dy W) act'(pre).                                     dy: M rows of O, W^T: I rows of O
+ *   bwd_weight: dw = dy^T x ([O][I]).                                      dy^T: O rows of M, x^T: I rows of M */
+o1d_status_t o1d_scaled_linear_fwd(const unsigned char* xq, const unsigned char* xe, o1d_scaled_t type,
+                                   const unsigned char* wq, const unsigned char* we, const void* b, o1d_act_t act,
+                                   const void* res, long long ldres, void* y, long long ldy, void* pre, long long ldpre, int M,
+                                   int I, int O, o1d_dtype_t dtype, void* stream);
+o1d_status_t o1d_scaled_linear_bwd_input(const unsigned char* dyq, const unsigned char* dye, o1d_scaled_t type,
+                                         const unsigned char* wtq, const unsigned char* wte, o1d_act_t act, const void* pre,
+                                         long long ldpre, void* dx, long long lddx, int M, int I, int O, o1d_dtype_t dtype,
+                                         void* stream);
+o1d_status_t o1d_scaled_linear_bwd_weight(const unsigned char* dytq, const unsigned char* dyte, o1d_scaled_t type,
+                                          const unsigned char* xtq, const unsigned char* xte, void* dw, int M, int I, int O,
+                                          o1d_dtype_t dtype, void* workspace, size_t workspace_bytes, void* stream);
+size_t o1d_scaled_linear_bwd_weight_workspace_bytes(int M, int I, int O);
+
+/* ---- AdamW over many tensors at once.  With t = steps taken + 1 and g the gradient (times max_norm / norm where the norm is
+ * larger):
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ *
+ * Tensor i has n values p (param_dtype) and g (grad_dtype), and its part of the states starts at value `at`, a multiple
+ * of 128; behind its end the states' values up to the next multiple of 128 are set to zeros.  state_bits 32: m and v
+ * are float32.  8: m and the root of v are e4m3 (a positive root at least the type's smallest value), with a scale
+ * m_scale, v_scale for each 128 values: the largest / 448.  master (or NULL): the parameters in float32, from which p is rounded;
+ * without it p itself is read.  The states are 16-byte aligned.
+ * step: two device integers, the steps taken (read and counted up) and 0.  lr_at: the learning rate in device memory, or NULL for
+ * lr.  max_norm > 0 limits the norm of all gradients to it; the norm is then written to `norm`, and where it is not finite
+ * nothing else changes.  max_norm 0: no limit, norm is not written and may be NULL. */
+typedef struct {
+  void* p;
+  const void* g;
+  long long n, at;
+} o1d_adamw_tensor_t;
+typedef struct {
+  void *m, *v;
+  float *m_scale, *v_scale, *master;
+  int* step;
+  int bits;
+} o1d_adamw_state_t;
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay, max_norm;
+  const float* lr_at;
+} o1d_adamw_options_t;
+o1d_status_t o1d_adamw(const o1d_adamw_tensor_t* tensors, int count, o1d_dtype_t param_dtype, o1d_dtype_t grad_dtype,
+                       const o1d_adamw_state_t* state, const o1d_adamw_options_t* options, float* norm, void* workspace,
+                       size_t workspace_bytes, void* stream);
+size_t o1d_adamw_workspace_bytes(double max_norm);
+
 /* ---- Planning introspection (host only, no device work; for tests and tools).
  *
  * o1d_kernel_name: the kernel(s) a call with these arguments would launch,

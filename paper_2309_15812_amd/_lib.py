@@ -16,12 +16,28 @@ O1D_NCHW, O1D_NHWC = 0, 1
 O1D_FLOOR, O1D_BILINEAR = 0, 1
 ACT = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 GROUP = 64  # columns that share a scale in an 8-bit checkpoint
+SCALED = {"e4m3": 0, "e5m2": 1}
+SCALED_GROUP = 128  # values that share a scale in an 8-bit floating point operand, or in an 8-bit state of AdamW
 STATUS = {0: "O1D_OK", 1: "O1D_ERR_INVALID", 2: "O1D_ERR_UNSUPPORTED", 3: "O1D_ERR_WORKSPACE", 4: "O1D_ERR_HIP"}
 MAX_K = 127
 
 # name -> (restype, argtypes), mirroring include/o1d.h
 _vp, _i, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
-_ll, _f = ctypes.c_longlong, ctypes.c_float
+_ll, _f, _d = ctypes.c_longlong, ctypes.c_float, ctypes.c_double
+
+
+class AdamTensor(ctypes.Structure):
+    _fields_ = [("p", _vp), ("g", _vp), ("n", _ll), ("at", _ll)]
+
+
+class AdamState(ctypes.Structure):
+    _fields_ = [("m", _vp), ("v", _vp), ("m_scale", _vp), ("v_scale", _vp), ("master", _vp), ("step", _vp), ("bits", _i)]
+
+
+class AdamOptions(ctypes.Structure):
+    _fields_ = [("lr", _d), ("beta1", _d), ("beta2", _d), ("eps", _d), ("weight_decay", _d), ("max_norm", _d), ("lr_at", _vp)]
+
+
 SIGNATURES = {
     "o1d_fwd": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp]),
     "o1d_bwd_input": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp]),
@@ -46,6 +62,18 @@ SIGNATURES = {
     "o1d_linear_bwd_weight": (_i, [_vp, _ll, _vp, _vp, _i, _vp, _ll, _vp, _vp, _i, _i, _i, _i, _vp, _sz, _vp]),
     "o1d_linear_bwd_weight_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
     "o1d_act_bwd": (_i, [_vp, _ll, _vp, _vp, _i, _vp, _ll, _vp, _ll, _i, _i, _i, _vp]),
+    "o1d_gn_fwd": (_i, [_vp, _ll, _vp, _vp, _i, _vp, _ll, _vp, _vp, _i, _i, _i, _i, _f, _i, _vp, _sz, _vp]),
+    "o1d_gn_fwd_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
+    "o1d_gn_bwd": (_i, [_vp, _ll, _vp, _ll, _vp, _vp, _vp, _vp, _i, _vp, _ll, _vp, _vp, _i, _i, _i, _i, _i, _vp, _sz, _vp]),
+    "o1d_gn_bwd_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
+    "o1d_pack_scaled": (_i, [_vp, _ll, _i, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp, _sz, _vp]),
+    "o1d_pack_scaled_workspace_bytes": (_sz, [_i, _i, _i]),
+    "o1d_scaled_linear_fwd": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _i, _vp, _ll, _vp, _ll, _vp, _ll, _i, _i, _i, _i, _vp]),
+    "o1d_scaled_linear_bwd_input": (_i, [_vp, _vp, _i, _vp, _vp, _i, _vp, _ll, _vp, _ll, _i, _i, _i, _i, _vp]),
+    "o1d_scaled_linear_bwd_weight": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _sz, _vp]),
+    "o1d_scaled_linear_bwd_weight_workspace_bytes": (_sz, [_i, _i, _i]),
+    "o1d_adamw": (_i, [_vp, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "o1d_adamw_workspace_bytes": (_sz, [_d]),
     "o1d_kernel_name": (ctypes.c_char_p, [_i, _i, _i, _i, _i, _i, _i, _i, _i, _i, _i]),
     "o1d_kernel_variant": (ctypes.c_char_p, [_i]),
     "o1d_rows_kernel_name": (ctypes.c_char_p, [_i, _i, _i, _i, _i, _i, _i, _i]),

@@ -46,7 +46,8 @@ def sources() -> list[str]:
 # scratch memory would cost far more than it saves, so their translation
 # units are compiled with resource remarks and rejected if any kernel in them
 # uses scratch memory.  The general kernels and the row operators are checked the same way.
-CHECKED = ("o1d_strip_", "o1d_gen_", "o1d_plane_", "o1d_pw_", "o1d_walk_", "o1d_ln_", "o1d_held", "o1d_mm", "o1d_few_")
+CHECKED = ("o1d_strip_", "o1d_gen_", "o1d_plane_", "o1d_pw_", "o1d_walk_", "o1d_ln_", "o1d_held", "o1d_mm", "o1d_few_",
+           "o1d_gn_", "o1d_f8_", "o1d_adam")
 # Kernels that keep some values in scratch memory, with the bytes per lane they may.  In float32 tiles of 128 x 192 the
 # gradients reload up to 17 words per step of 4 us; the others touch it outside their loops.
 SCRATCH = {

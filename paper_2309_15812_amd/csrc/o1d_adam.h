@@ -1,0 +1,44 @@
+// Host-side interface of the AdamW step over many tensors.
+#pragma once
+
+#include "o1d_rows.h"
+
+namespace o1d {
+namespace rows {
+
+constexpr int kAdamGroup = 128;  // values of an 8-bit state that share a scale; parts of the states start at multiples of it
+
+struct AdamTensor {
+  void* p;
+  const void* g;
+  long long n, at;  // values, and where their part of the states starts
+};
+
+struct AdamState {
+  void *m, *v;            // float32, or e4m3 (of v the root)
+  float *ms, *vs;         // 8 bits: a scale for each 128 values
+  float* master;          // (or NULL) the parameters in float32
+  int* step;              // {steps taken, 0}
+  int bits;
+};
+
+struct AdamHyper {
+  float lr, beta1, beta2, eps, decay;
+  double beta1_64, beta2_64;
+  float rest1, rest2, keep;  // 1 - beta1, 1 - beta2, 1 - lr decay
+  const float* lr_at;     // (or NULL) device value of the learning rate
+  const float* norm;      // (or NULL) the gradients' norm, to be limited to max_norm
+  float max_norm;
+};
+
+constexpr int kAdamMost = 96;  // tensors of a launch
+// Tensors 0 .. count - 1 of a call; the call's last launch counts the step.
+hipError_t launch_adam(Dtype pdt, Dtype gdt, const AdamTensor* t, int count, const AdamState& s, const AdamHyper& h,
+                       hipStream_t stream);
+
+constexpr int kNormBlocks = 1024;  // partial sums (float64) of a call
+// norm = sqrt(sum of squares over all gradients); part: kNormBlocks doubles
+hipError_t launch_grad_norm(Dtype gdt, const AdamTensor* t, int count, double* part, float* norm, hipStream_t stream);
+
+}  // namespace rows
+}  // namespace o1d

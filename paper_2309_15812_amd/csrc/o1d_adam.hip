@@ -1,0 +1,291 @@
+// AdamW over many tensors at once, with states of 32 or 8 bits.
+//
+//   g = factor gradient,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+//   w = w (1 - lr decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+//
+// factor limits the gradients' norm over all tensors (launch_grad_norm) to max_norm; where
+// that norm is not finite, nothing changes, the count of steps included.  The count
+// lies in device memory, so that a captured step counts on every replay.
+//
+// In 8 bits, m and r = sqrt(v) are e4m3 with a float32 scale, the largest / 448, for each 128 values.  The root halves
+// v's range; a positive r is at least the type's smallest value, so that no m meets a v that was rounded to zero.
+// Every operation is rounded by itself (no fused multiply-add): the 8-bit values do not depend on
+// how a compiler joins them.
+//
+// Memory bounds it: 28 bytes per value in float32, 16.1 (bfloat16 parameters and gradients, their
+// float32 values, 8-bit states).  A thread has eight values, 16 threads a scale; a workgroup
+// finds the tensor of each piece of 2048 values among those in its arguments.
+#include <hip/hip_runtime.h>
+
+#include "o1d_adam.h"
+#include "o1d_rows_device.h"
+
+namespace o1d {
+namespace rows {
+namespace {
+
+constexpr int kAdamThreads = 256, kAdamRun = 8, kAdamPiece = kAdamThreads * kAdamRun;
+
+struct AdamList {
+  AdamTensor t[kAdamMost];
+  int first[kAdamMost];  // piece of all
+  int count, pieces;
+};
+
+// The tensor of a piece: the last that starts at or before it.
+__device__ __forceinline__ int tensor_of(const AdamList& L, int piece) {
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+#pragma unroll
+  for (int k = 0; k < (kAdamMost + 63) / 64; ++k) {
+    const int i = lane + 64 * k;
+    n += __popcll(__ballot(i < L.count && L.first[i < L.count ? i : 0] <= piece));
+  }
+  return __builtin_amdgcn_readfirstlane(n) - 1;
+}
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, long long left, float (&v)[kAdamRun]) {
+  if (left >= kAdamRun) {
+    load_run(p, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kAdamRun; ++e) v[e] = e < left ? to_f32(p[e]) : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, long long left, const float (&v)[kAdamRun]) {
+  if (left >= kAdamRun) {
+    store_run(p, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kAdamRun; ++e)
+      if (e < left) p[e] = from_f32<T>(v[e]);
+  }
+}
+
+// b^t for whole t, by squaring.
+__device__ __forceinline__ double power(double b, int t) {
+  double r = 1.;
+  for (; t; t >>= 1, b *= b)
+    if (t & 1) r *= b;
+  return r;
+}
+
+// Eight e4m3 values times their scale, and back: the scale is the largest of 16 lanes' values / 448.
+__device__ __forceinline__ void from8(const uint8_t* p, float scale, float (&v)[kAdamRun]) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int u = (int)(k ? w.y : w.x);
+    v[4 * k] = __builtin_amdgcn_cvt_f32_fp8(u, 0) * scale;
+    v[4 * k + 1] = __builtin_amdgcn_cvt_f32_fp8(u, 1) * scale;
+    v[4 * k + 2] = __builtin_amdgcn_cvt_f32_fp8(u, 2) * scale;
+    v[4 * k + 3] = __builtin_amdgcn_cvt_f32_fp8(u, 3) * scale;
+  }
+}
+template <bool LEAST>
+__device__ __forceinline__ void to8(const float (&v)[kAdamRun], uint8_t* p, float* scale) {
+#pragma clang fp contract(off)
+  uint32_t most = max8(amax_bits(v));
+  most = max(most, (uint32_t)__builtin_amdgcn_mov_dpp((int)most, 0x140, 0xF, 0xF, true));
+  const float amax = __uint_as_float(most), inv = amax > 0.f ? 448.f / amax : 0.f;
+  float u[kAdamRun];
+#pragma unroll
+  for (int e = 0; e < kAdamRun; ++e) {
+    u[e] = v[e] * inv;
+    if (LEAST && v[e] > 0.f) u[e] = fmaxf(u[e], 0x1p-9f);
+  }
+  int w[2] = {0, 0};
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    w[k] = __builtin_amdgcn_cvt_pk_fp8_f32(u[4 * k], u[4 * k + 1], w[k], false);
+    w[k] = __builtin_amdgcn_cvt_pk_fp8_f32(u[4 * k + 2], u[4 * k + 3], w[k], true);
+  }
+  *reinterpret_cast<uint2*>(p) = make_uint2((uint32_t)w[0], (uint32_t)w[1]);
+  if ((threadIdx.x & 15) == 0) *scale = amax * (1.f / 448.f);
+}
+
+struct Coefs {
+  float factor, lr, keep, c1, c2;
+  int go;
+};
+
+template <typename TP, typename TG, bool HELD8, bool MASTER>
+__global__ __launch_bounds__(kAdamThreads) void adam(AdamList L, AdamState S, AdamHyper H, int counts) {
+#pragma clang fp contract(off)
+  __shared__ Coefs coefs;
+  if (threadIdx.x == 0) {
+    const int t = S.step[0] + 1;
+    Coefs c;
+    c.factor = 1.f;
+    c.go = 1;
+    if (H.norm) {
+      const float norm = *H.norm;
+      c.go = norm < __builtin_huge_valf();  // (false for NaN)
+      if (norm > H.max_norm) c.factor = H.max_norm / norm;
+    }
+    c.lr = H.lr_at ? *H.lr_at : H.lr;
+    c.keep = H.lr_at ? 1.f - c.lr * H.decay : H.keep;
+    c.c1 = (float)(1. / (1. - power(H.beta1_64, t)));
+    c.c2 = (float)sqrt(1. / (1. - power(H.beta2_64, t)));
+    coefs = c;
+  }
+  __syncthreads();
+  const Coefs c = coefs;
+  if (c.go) {
+    for (int piece = blockIdx.x; piece < L.pieces; piece += gridDim.x) {
+      const int k = tensor_of(L, piece);
+      const AdamTensor& t = L.t[k];
+      const long long i = (long long)(piece - L.first[k]) * kAdamPiece + threadIdx.x * kAdamRun, left = t.n - i;
+      const long long padded = (t.n + kAdamGroup - 1) / kAdamGroup * kAdamGroup;
+      if (i >= padded) continue;
+      const long long at = t.at + i;
+      float g[kAdamRun], w[kAdamRun], m[kAdamRun], v[kAdamRun];
+      load8(static_cast<const TG*>(t.g) + i, left, g);
+      if constexpr (MASTER)
+        load_run(S.master + at, w);
+      else
+        load8(static_cast<const TP*>(t.p) + i, left, w);
+      if constexpr (HELD8) {
+        from8(static_cast<const uint8_t*>(S.m) + at, S.ms[at / kAdamGroup], m);
+        from8(static_cast<const uint8_t*>(S.v) + at, S.vs[at / kAdamGroup], v);
+      } else {
+        load_run(static_cast<const float*>(S.m) + at, m);
+        load_run(static_cast<const float*>(S.v) + at, v);
+      }
+#pragma unroll
+      for (int e = 0; e < kAdamRun; ++e) {
+        if (H.norm) g[e] *= c.factor;
+        if constexpr (HELD8) v[e] *= v[e];
+        m[e] = H.beta1 * m[e] + H.rest1 * g[e];
+        v[e] = H.beta2 * v[e] + H.rest2 * (g[e] * g[e]);
+        const float r = sqrtf(v[e]);
+        w[e] = w[e] * c.keep - c.lr * ((m[e] * c.c1) / (r * c.c2 + H.eps));
+        if constexpr (HELD8) v[e] = r;
+        if (e >= left) m[e] = v[e] = w[e] = 0.f;  // (behind the tensor's end the states are zeros)
+      }
+      store8(static_cast<TP*>(t.p) + i, left, w);
+      if constexpr (MASTER) store_run(S.master + at, w);
+      if constexpr (HELD8) {
+        to8<false>(m, static_cast<uint8_t*>(S.m) + at, S.ms + at / kAdamGroup);
+        to8<true>(v, static_cast<uint8_t*>(S.v) + at, S.vs + at / kAdamGroup);
+      } else {
+        store_run(static_cast<float*>(S.m) + at, m);
+        store_run(static_cast<float*>(S.v) + at, v);
+      }
+    }
+  }
+  // The last workgroup to end counts the step: all others have read it.
+  if (counts && threadIdx.x == 0) {
+    if (atomicAdd(&S.step[1], 1) == (int)gridDim.x - 1) {
+      S.step[1] = 0;
+      if (c.go) S.step[0] += 1;
+    }
+  }
+}
+
+// ---- the gradients' norm: squares are summed in 64 bits, so that none overflows
+
+constexpr int kNormThreads = 256;
+
+__device__ __forceinline__ double block_sum64(double s) {
+  __shared__ double red[kNormThreads / 64];
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) s += __shfl_xor(s, m, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  s = 0.;
+#pragma unroll
+  for (int k = 0; k < kNormThreads / 64; ++k) s += red[k];
+  return s;
+}
+
+template <typename TG>
+__global__ __launch_bounds__(kNormThreads) void squares(AdamList L, double* part, int add) {
+  double s = 0.;
+  for (int piece = blockIdx.x; piece < L.pieces; piece += gridDim.x) {
+    const int k = tensor_of(L, piece);
+    const AdamTensor& t = L.t[k];
+    const long long i = (long long)(piece - L.first[k]) * kAdamPiece + threadIdx.x * kAdamRun, left = t.n - i;
+    if (left <= 0) continue;
+    float g[kAdamRun];
+    load8(static_cast<const TG*>(t.g) + i, left, g);
+#pragma unroll
+    for (int e = 0; e < kAdamRun; ++e) s = fma((double)g[e], (double)g[e], s);
+  }
+  s = block_sum64(s);
+  if (threadIdx.x == 0) part[blockIdx.x] = add ? part[blockIdx.x] + s : s;
+}
+
+__global__ __launch_bounds__(kNormThreads) void norm_of(const double* part, int parts, float* norm) {
+  double s = 0.;
+  for (int i = threadIdx.x; i < parts; i += kNormThreads) s += part[i];
+  s = block_sum64(s);
+  if (threadIdx.x == 0) *norm = (float)sqrt(s);
+}
+
+// Calls f with each launch's list; `last`: the call's last.
+template <typename F>
+hipError_t with_lists(const AdamTensor* t, int count, F&& f) {
+  for (int from = 0; from < count;) {
+    AdamList L{};
+    while (from < count && L.count < kAdamMost) {
+      L.t[L.count] = t[from];
+      L.first[L.count++] = L.pieces;
+      L.pieces += (int)cdiv(t[from++].n, kAdamPiece);
+    }
+    f(L, from == count);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <typename TP, typename TG>
+hipError_t adam_t(const AdamTensor* t, int count, const AdamState& s, const AdamHyper& h, hipStream_t stream) {
+  return with_lists(t, count, [&](const AdamList& L, bool last) {
+    const dim3 grid((unsigned)(L.pieces < 4096 ? L.pieces : 4096)), threads(kAdamThreads);
+    if (s.bits == 8) {
+      if (s.master)
+        hipLaunchKernelGGL((adam<TP, TG, true, true>), grid, threads, 0, stream, L, s, h, (int)last);
+      else
+        hipLaunchKernelGGL((adam<TP, TG, true, false>), grid, threads, 0, stream, L, s, h, (int)last);
+    } else {
+      if (s.master)
+        hipLaunchKernelGGL((adam<TP, TG, false, true>), grid, threads, 0, stream, L, s, h, (int)last);
+      else
+        hipLaunchKernelGGL((adam<TP, TG, false, false>), grid, threads, 0, stream, L, s, h, (int)last);
+    }
+  });
+}
+
+}  // namespace
+
+hipError_t launch_adam(Dtype pdt, Dtype gdt, const AdamTensor* t, int count, const AdamState& s, const AdamHyper& h,
+                       hipStream_t stream) {
+  if (pdt == Dtype::F32)
+    return gdt == Dtype::F32 ? adam_t<float, float>(t, count, s, h, stream) : adam_t<float, uint16_t>(t, count, s, h, stream);
+  return gdt == Dtype::F32 ? adam_t<uint16_t, float>(t, count, s, h, stream)
+                           : adam_t<uint16_t, uint16_t>(t, count, s, h, stream);
+}
+
+hipError_t launch_grad_norm(Dtype gdt, const AdamTensor* t, int count, double* part, float* norm, hipStream_t stream) {
+  int parts = 0;
+  const hipError_t e = with_lists(t, count, [&](const AdamList& L, bool) {
+    // (a later list adds to the first parts; the first list's count is the largest that is read)
+    const int blocks = parts ? (L.pieces < parts ? L.pieces : parts) : (L.pieces < kNormBlocks ? L.pieces : kNormBlocks);
+    if (gdt == Dtype::F32)
+      hipLaunchKernelGGL((squares<float>), dim3((unsigned)blocks), dim3(kNormThreads), 0, stream, L, part, (int)(parts > 0));
+    else
+      hipLaunchKernelGGL((squares<uint16_t>), dim3((unsigned)blocks), dim3(kNormThreads), 0, stream, L, part,
+                         (int)(parts > 0));
+    if (!parts) parts = blocks;
+  });
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(norm_of, dim3(1), dim3(kNormThreads), 0, stream, part, parts, norm);
+  return hipGetLastError();
+}
+
+}  // namespace rows
+}  // namespace o1d

@@ -1,0 +1,54 @@
+// Host-side plan and launchers of group norm with an activation on channels-last activations.
+#pragma once
+
+#include "o1d_rows.h"
+
+namespace o1d {
+namespace rows {
+
+struct GnParams {
+  int N, P, C, G, D;        // samples, pixels of one, channels = G groups of D
+  long long ldx, ldy, ldd;  // rows apart: of x, of y (forward) or dx, of dy
+  float eps;
+  int act;
+  const void *x, *w, *b, *dy;
+  void* out;                // y or dx
+  float *mean, *rstd;       // N x G: written by the forward, read by the backward
+  float* part;              // partial results (below)
+  int gb, bundles;          // groups of a workgroup's channels, and how many such pieces
+  int chunks, rows;         // not held: pieces of a sample's pixels, and their rows (the last may have fewer)
+};
+
+// A workgroup's channels are the `gb` groups of a bundle.  Held: it holds all
+// pixels of a sample in registers (`runs` 16-byte runs of `threads` threads) and memory is
+// passed once.  Else a first pass leaves partial statistics of each chunk of
+// pixels, and a second reads the chunk again.
+struct GnPlan {
+  bool held;
+  int threads, runs;
+  int gb, bundles, chunks, rows;
+};
+constexpr int kGnMostChannels = 1024;  // of a group
+constexpr int kGnMostChunks = 64;      // (a lane each)
+// Threads of the larger workgroups and most runs of a held sample: in bfloat16 the backward unpacks its
+// registers twice and needs 256 of them per thread.
+constexpr int gn_big(bool backward, int esize) { return backward && esize == 2 ? 512 : 1024; }
+constexpr int gn_most_runs(bool backward, int esize) { return backward ? (esize == 2 ? 6 : 8) : 10; }
+GnPlan plan_gn(bool backward, int N, int P, int C, int G, int esize);
+
+// Floats of workspace: the forward's, not held: (mean, sum of squares) of each sample, chunk and
+// group.  The backward's: dw and db of each sample and chunk (2 C each), then, not held, the two sums
+// over each group.
+inline long long gn_parts(const GnPlan& pl, int N) { return (long long)N * (pl.held ? 1 : pl.chunks); }
+inline long long gn_fwd_floats(const GnPlan& pl, int N, int G) { return pl.held ? 0 : gn_parts(pl, N) * G * 2; }
+inline long long gn_bwd_floats(const GnPlan& pl, int N, int C, int G) {
+  return gn_parts(pl, N) * (2ll * C + (pl.held ? 0 : 2ll * G));
+}
+
+hipError_t launch_gn_fwd_f32(const GnPlan& pl, const GnParams& p, hipStream_t stream);
+hipError_t launch_gn_fwd_bf16(const GnPlan& pl, const GnParams& p, hipStream_t stream);
+hipError_t launch_gn_bwd_f32(const GnPlan& pl, const GnParams& p, hipStream_t stream);
+hipError_t launch_gn_bwd_bf16(const GnPlan& pl, const GnParams& p, hipStream_t stream);
+
+}  // namespace rows
+}  // namespace o1d

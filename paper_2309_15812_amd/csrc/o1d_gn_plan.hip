@@ -1,0 +1,55 @@
+// The plan of group norm.
+#include "o1d_gn.h"
+
+namespace o1d {
+namespace rows {
+
+GnPlan plan_gn(bool backward, int N, int P, int C, int G, int esize) {
+  const int D = C / G, V = 16 / esize, big = gn_big(backward, esize);
+  GnPlan best{};
+  best.held = false;
+  // Held: the largest bundles that a workgroup holds and that still give every CU one
+  double cost = -1.;
+  for (int bundles = 1; bundles <= G; ++bundles) {
+    const int gb = (int)cdiv(G, bundles), CB = gb * D;
+    if (bundles > 1 && (int)cdiv(G, bundles - 1) == gb) continue;  // (the same with fewer)
+    if (CB > kGnMostChannels) continue;
+    if ((C >= V && CB < V) || (C < V && bundles > 1)) break;
+    const int real = (int)cdiv(G, gb);
+    for (int threads : {256, big}) {
+      const int run = (int)cdiv(CB, V);
+      if (run > threads) continue;
+      const long long rows = threads / run, need = cdiv(P, rows);
+      const int runs = need <= 2 ? 2 : (int)cdiv(need, 2) * 2;
+      if (runs > gn_most_runs(backward, esize)) continue;
+      // time: what a CU moves, at the rate it has, and the two reductions
+      const double bytes = (double)P * CB * esize, piece = CB * esize;
+      const double groups = (double)N * real, rounds = (double)cdiv((long long)groups, 256);
+      const double per_cu = groups >= 256 ? 20e3 : 50e3;  // bytes per us
+      const double t = rounds * (bytes / per_cu * (piece < 64 ? 64 / piece : 1.) + (threads == 256 ? 1.5 : 3.));
+      if (cost >= 0. && t >= cost) continue;
+      cost = t;
+      best = {true, threads, runs, gb, real, 1, P};
+    }
+  }
+  const double twice = 6. + (double)N * P * C * esize * 1.6 / 5.0e6;
+  if (best.held && cost <= twice) return best;
+  // In chunks: bundles as wide as a workgroup takes, pieces enough to fill the GPU
+  GnPlan pl{};
+  pl.gb = kGnMostChannels / D < G ? kGnMostChannels / D : G;
+  pl.bundles = (int)cdiv(G, pl.gb);
+  pl.gb = (int)cdiv(G, pl.bundles);
+  pl.bundles = (int)cdiv(G, pl.gb);
+  const int rows = 256 / (int)cdiv((long long)pl.gb * D, V);  // at a time
+  long long chunks = cdiv(2048, (long long)N * pl.bundles);
+  const long long least = cdiv(P, 4ll * (rows > 0 ? rows : 1));
+  if (chunks > least) chunks = least;
+  if (chunks > kGnMostChunks) chunks = kGnMostChunks;
+  if (chunks < 1) chunks = 1;
+  pl.rows = (int)cdiv(P, chunks);
+  pl.chunks = (int)cdiv(P, pl.rows);
+  return pl;
+}
+
+}  // namespace rows
+}  // namespace o1d

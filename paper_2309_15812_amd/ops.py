@@ -685,3 +685,402 @@ def _parts(t) -> tuple:
 
 def _whole(t, scale, cols: int):
     return t if scale is None else Packed8(t, scale, cols)
+
+
+# ---------------------------------------------------------------- group norm with an activation (channels last)
+
+def _samples(t: torch.Tensor, what: str) -> tuple[torch.Tensor, int, int, int, int]:
+    """(t or a view of it, samples, pixels of one, channels, row stride) of a tensor (N, ..., C)."""
+    if t.dim() < 2:
+        raise ValueError(f"{what} must be (N, ..., C), got {tuple(t.shape)}")
+    v, M, C, ld = _rows(t, what)
+    N = int(t.shape[0])
+    if N and not M:
+        raise ValueError(f"{what} {tuple(t.shape)} has samples without pixels")
+    return v, N, M // N if N else 0, C, ld
+
+
+def _stats(t: torch.Tensor, what: str, shape: tuple[int, int] | None, like: torch.Tensor) -> torch.Tensor:
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape) or t.dtype is not torch.float32 \
+            or t.get_device() != like.get_device() or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous float32 (N, groups) tensor on {like.device}, got {tuple(t.shape)} "
+                         f"{t.dtype} {t.device}")
+    return t
+
+
+@functools.lru_cache(maxsize=4096)
+def gn_workspace_bytes(N: int, P: int, C: int, groups: int, dtype: torch.dtype, backward: bool) -> int:
+    f = _lib.lib().o1d_gn_bwd_workspace_bytes if backward else _lib.lib().o1d_gn_fwd_workspace_bytes
+    return int(f(N, P, C, groups, _DT[dtype]))
+
+
+def gn_fwd(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor, groups: int, eps: float = 1e-5, act: str = "none",
+           out: torch.Tensor | None = None, workspace: torch.Tensor | None = None
+           ) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(y, mean, rstd): act of the group norm of x (N, ..., C) over a sample's pixels and the C / groups channels of a group;
+    mean and rstd (N, groups) float32 are for gn_bwd."""
+    dt, a = _dt(x), _act(act)
+    v, N, P, C, ld = _samples(x, "x")
+    _vector(w, "w", C, x)
+    _vector(b, "b", C, x)
+    if groups < 1 or C % groups:
+        raise ValueError(f"groups={groups} do not divide {C} channels")
+    y = _into(out, x, C)
+    mean, rstd = (x.new_empty((N, groups), dtype=torch.float32) for _ in range(2))
+    workspace, nbytes = _scratch(workspace, x, gn_workspace_bytes(N, P, C, groups, x.dtype, False))
+    _run("o1d_gn_fwd", x, v.data_ptr(), ld, w.data_ptr(), b.data_ptr(), a, y.data_ptr(), C, mean.data_ptr(),
+         rstd.data_ptr(), N, P, C, groups, eps, dt, workspace.data_ptr(), nbytes)
+    return y, mean, rstd
+
+
+def gn_bwd(x: torch.Tensor, dy: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, w: torch.Tensor, b: torch.Tensor,
+           act: str = "none", out: tuple[torch.Tensor, torch.Tensor, torch.Tensor] | None = None,
+           workspace: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(dx, dw, db) of gn_fwd given its input, dy and its mean and rstd."""
+    dt, a = _dt(dy), _act(act)
+    g, N, P, C, lddy = _samples(dy, "dy")
+    v, ldx = _same(x, "x", N * P, C, dy)
+    _stats(mean, "mean", None, dy)
+    groups = int(mean.shape[1])
+    _stats(rstd, "rstd", (N, groups), dy)
+    _stats(mean, "mean", (N, groups), dy)
+    _vector(w, "w", C, dy)
+    _vector(b, "b", C, dy)
+    if groups < 1 or C % groups:
+        raise ValueError(f"{groups} groups of the statistics do not divide {C} channels")
+    dx, dw, db = (None, None, None) if out is None else out
+    dx = _into(dx, dy, C)
+    dw, db = (torch.empty_like(w) if t is None else _out(t, w) for t in (dw, db))
+    workspace, nbytes = _scratch(workspace, dy, gn_workspace_bytes(N, P, C, groups, dy.dtype, True))
+    _run("o1d_gn_bwd", dy, v.data_ptr(), ldx, g.data_ptr(), lddy, mean.data_ptr(), rstd.data_ptr(), w.data_ptr(),
+         b.data_ptr(), a, dx.data_ptr(), C, dw.data_ptr(), db.data_ptr(), N, P, C, groups, dt, workspace.data_ptr(), nbytes)
+    return dx, dw, db
+
+
+class GroupNormFunction(torch.autograd.Function):
+    """Autograd glue: gn_fwd, gn_bwd."""
+
+    @staticmethod
+    def forward(ctx, x, w, b, groups, eps=1e-5, act="none"):
+        x, w, b = x.contiguous(), w.contiguous(), b.contiguous()
+        y, mean, rstd = gn_fwd(x, w, b, groups, eps, act)
+        ctx.act = act
+        ctx.save_for_backward(x, mean, rstd, w, b)
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gy):
+        x, mean, rstd, w, b = ctx.saved_tensors
+        gx, gw, gb = gn_bwd(x, gy.contiguous(), mean, rstd, w, b, ctx.act)
+        return gx, gw, gb, None, None, None
+
+
+# ---------------------------------------------------------------- products of 8-bit floating point operands
+
+_F8 = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+_F8_OF = {t: _lib.SCALED[n] for n, t in _F8.items()}
+
+
+class F8:
+    """A matrix of rows of `cols` values in 8-bit floating point with a power-of-two scale for each 128 values of a row: q
+    (R, cols rounded up to 128) float8_e4m3fn or float8_e5m2, zeros behind a row's end, and exponents e (ceil(cols / 128), R
+    rounded up to 16) uint8; q[r, k] 2^(e[k / 128, r] - 127) is the value."""
+
+    __slots__ = ("q", "e", "cols")
+
+    def __init__(self, q: torch.Tensor, e: torch.Tensor, cols: int):
+        groups = -(-cols // _lib.SCALED_GROUP)
+        if cols < 1 or q.dim() != 2 or q.dtype not in _F8_OF or q.shape[1] != groups * _lib.SCALED_GROUP \
+                or not q.is_contiguous():
+            raise ValueError(f"q must be a contiguous (R, {groups * _lib.SCALED_GROUP}) tensor of float8_e4m3fn or "
+                             f"float8_e5m2, got {tuple(q.shape)} {q.dtype}")
+        if tuple(e.shape) != (groups, -(-q.shape[0] // 16) * 16) or e.dtype != torch.uint8 or not e.is_contiguous():
+            raise ValueError(f"e must be a contiguous uint8 ({groups}, {-(-q.shape[0] // 16) * 16}) tensor, got "
+                             f"{tuple(e.shape)} {e.dtype}")
+        if not q.is_cuda or q.device != e.device:
+            raise ValueError("an operand's tensors must be on one GPU")
+        self.q, self.e, self.cols = q, e, cols
+
+    @staticmethod
+    def of(q: torch.Tensor, e: torch.Tensor, cols: int) -> "F8":  # (tensors made for it)
+        held = object.__new__(F8)
+        held.q, held.e, held.cols = q, e, cols
+        return held
+
+    @staticmethod
+    def empty(R: int, cols: int, fmt: str, device) -> "F8":
+        groups = -(-cols // _lib.SCALED_GROUP)
+        return F8.of(torch.empty((R, groups * _lib.SCALED_GROUP), dtype=_F8[fmt], device=device),
+                     torch.empty((groups, -(-R // 16) * 16), dtype=torch.uint8, device=device), cols)
+
+    @property
+    def rows(self) -> int:
+        return int(self.q.shape[0])
+
+    @property
+    def nbytes(self) -> int:
+        return self.q.numel() + self.e.numel()
+
+    def float(self) -> torch.Tensor:
+        """What it stands for, in float32 (by torch: for looking at, not for computing with)."""
+        scale = torch.exp2(self.e[:, :self.rows].float() - 127).t().repeat_interleave(_lib.SCALED_GROUP, 1)
+        return (self.q.float() * scale)[:, :self.cols]
+
+
+def _f8(t: F8, what: str, R: int | None, cols: int, like: torch.Tensor, second: bool = False) -> F8:
+    if not isinstance(t, F8):
+        raise TypeError(f"{what} must be packed (pack_f8), got {type(t).__name__}")
+    if t.cols != cols or (R is not None and t.rows != R) or t.q.get_device() != like.get_device():
+        raise ValueError(f"{what} has {t.rows} rows of {t.cols} values on {t.q.device}, expected "
+                         f"{'' if R is None else R} rows of {cols} on {like.device}")
+    if second and t.q.dtype is not torch.float8_e4m3fn:
+        raise TypeError(f"{what} must be e4m3, got {t.q.dtype}")
+    return t
+
+
+def pack_f8(x: torch.Tensor, fmt: str = "e4m3", along: str = "features", sums: bool = False,
+            workspace: torch.Tensor | None = None):
+    """x's rows as 8-bit operands of products that sum along: "features" -> F8 of (M, C); "rows" -> F8 of x transposed
+    (C, M), "both" -> the two.  sums=True (not with "features" alone) appends the columns' sums, a bias gradient, in
+    x's type."""
+    if fmt not in _F8 or along not in ("features", "rows", "both"):
+        raise ValueError(f"fmt must be one of {list(_F8)}, along 'features', 'rows' or 'both'; got {fmt!r}, {along!r}")
+    if sums and along == "features":
+        raise ValueError("sums come with along='rows' or 'both'")
+    dt = _dt(x)
+    v, M, C, ld = _rows(x, "x")
+    r = F8.empty(M, C, fmt, x.device) if along != "rows" else None
+    t = None
+    if along != "features":
+        if M < 1:
+            raise ValueError("no rows to sum along")
+        t = F8.empty(C, M, fmt, x.device)
+    total = x.new_empty((C,)) if sums else None
+    pw, nbytes = None, 0
+    if sums:
+        workspace, nbytes = _scratch(workspace, x, int(_lib.lib().o1d_pack_scaled_workspace_bytes(M, C, 1)))
+        pw = workspace.data_ptr()
+    _run("o1d_pack_scaled", x, v.data_ptr(), ld, _lib.SCALED[fmt], *((r.q.data_ptr(), r.e.data_ptr()) if r else (None, None)),
+         *((t.q.data_ptr(), t.e.data_ptr()) if t else (None, None)), None if total is None else total.data_ptr(), M, C, dt,
+         pw, nbytes)
+    got = tuple(k for k in (r, t, total) if k is not None)
+    return got if len(got) > 1 else got[0]
+
+
+def f8_linear_fwd(x: F8, w: F8, b: torch.Tensor | None = None, act: str = "none", residual: torch.Tensor | None = None,
+                  save: str | None = None, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None):
+    """y = act(x w^T + b) + residual of packed x (M, I) and w (O, I), in dtype.  save="pre" returns (y, pre) with the
+    pre-activation."""
+    if save not in (None, "pre"):
+        raise ValueError(f"save must be None or 'pre', got {save!r}")
+    if dtype not in _DT:
+        raise TypeError(f"unsupported dtype {dtype}; use float32 or bfloat16")
+    a = _act(act)
+    _f8(x, "x", None, x.cols, x.q)
+    _f8(w, "w", None, x.cols, x.q, second=True)
+    M, I, O = x.rows, x.cols, w.rows
+    y = torch.empty((M, O), dtype=dtype, device=x.q.device) if out is None else out
+    if y.dtype is not dtype:
+        raise TypeError(f"out must be {dtype}, got {y.dtype}")
+    v, ldy = _same(y, "out", M, O, y)
+    if y.get_device() != x.q.get_device():
+        raise ValueError(f"out must be on {x.q.device}")
+    if b is not None:
+        _vector(b, "b", O, y)
+    res, ldres = (None, O) if residual is None else _same(residual, "residual", M, O, y)
+    pre = torch.empty((M, O), dtype=dtype, device=x.q.device) if save == "pre" else None
+    _run("o1d_scaled_linear_fwd", x.q, x.q.data_ptr(), x.e.data_ptr(), _F8_OF[x.q.dtype], w.q.data_ptr(), w.e.data_ptr(),
+         None if b is None else b.data_ptr(), a, None if res is None else res.data_ptr(), ldres, v.data_ptr(), ldy,
+         None if pre is None else pre.data_ptr(), O, M, I, O, _DT[dtype])
+    return y if pre is None else (y, pre)
+
+
+def f8_linear_bwd_input(dy: F8, wt: F8, pre: torch.Tensor | None = None, act: str = "none",
+                        dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """dx = (dy w) act'(pre) of packed dy (M, O) and wt, the weights transposed (I, O), in dtype; pre has that type."""
+    if dtype not in _DT:
+        raise TypeError(f"unsupported dtype {dtype}; use float32 or bfloat16")
+    a = _act(act)
+    if (pre is None) != (act == "none"):
+        raise ValueError("pre and act are given together")
+    _f8(dy, "dy", None, dy.cols, dy.q)
+    _f8(wt, "wt", None, dy.cols, dy.q, second=True)
+    M, O, I = dy.rows, dy.cols, wt.rows
+    dx = torch.empty((M, I), dtype=dtype, device=dy.q.device) if out is None else out
+    if dx.dtype is not dtype:
+        raise TypeError(f"out must be {dtype}, got {dx.dtype}")
+    v, lddx = _same(dx, "out", M, I, dx)
+    if dx.get_device() != dy.q.get_device():
+        raise ValueError(f"out must be on {dy.q.device}")
+    p, ldp = (None, I) if pre is None else _same(pre, "pre", M, I, dx)
+    _run("o1d_scaled_linear_bwd_input", dy.q, dy.q.data_ptr(), dy.e.data_ptr(), _F8_OF[dy.q.dtype], wt.q.data_ptr(),
+         wt.e.data_ptr(), a, None if p is None else p.data_ptr(), ldp, v.data_ptr(), lddx, M, I, O, _DT[dtype])
+    return dx
+
+
+@functools.lru_cache(maxsize=4096)
+def f8_linear_workspace_bytes(M: int, I: int, O: int) -> int:
+    return int(_lib.lib().o1d_scaled_linear_bwd_weight_workspace_bytes(M, I, O))
+
+
+def f8_linear_bwd_weight(dyt: F8, xt: F8, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
+                         workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """dw (O, I) = dy^T x of the packed transposes dyt (O, M) and xt (I, M), in dtype."""
+    if dtype not in _DT:
+        raise TypeError(f"unsupported dtype {dtype}; use float32 or bfloat16")
+    _f8(dyt, "dyt", None, dyt.cols, dyt.q)
+    _f8(xt, "xt", None, dyt.cols, dyt.q, second=True)
+    M, O, I = dyt.cols, dyt.rows, xt.rows
+    if O < 1 or I < 1:
+        raise ValueError("a weight has at least one row and one column")
+    dw = torch.empty((O, I), dtype=dtype, device=dyt.q.device) if out is None else out
+    if tuple(dw.shape) != (O, I) or dw.dtype is not dtype or dw.device != dyt.q.device or not dw.is_contiguous():
+        raise ValueError(f"out must be a contiguous ({O}, {I}) tensor of {dtype} on {dyt.q.device}")
+    workspace, nbytes = _scratch(workspace, dyt.q, f8_linear_workspace_bytes(M, I, O))
+    _run("o1d_scaled_linear_bwd_weight", dyt.q, dyt.q.data_ptr(), dyt.e.data_ptr(), _F8_OF[dyt.q.dtype], xt.q.data_ptr(),
+         xt.e.data_ptr(), dw.data_ptr(), M, I, O, _DT[dtype], workspace.data_ptr(), nbytes)
+    return dw
+
+
+class F8LinearFunction(torch.autograd.Function):
+    """Autograd glue: y = act(x w^T + b) + residual with products of e4m3 operands; gradients are packed as `grad` ("e5m2"
+    or "e4m3").  What the backward needs of x is kept in 8 bits."""
+
+    @staticmethod
+    def forward(ctx, x, w, b=None, act="none", residual=None, grad="e5m2"):
+        x, w = x.contiguous(), w.contiguous()
+        wants = (*ctx.needs_input_grad, False, False, False)  # (arguments left out have no entry)
+        xr, xt = pack_f8(x, along="both") if wants[1] and x.numel() else (pack_f8(x), None)
+        wr, wt = pack_f8(w, along="both") if wants[0] else (pack_f8(w), None)
+        save = None if act == "none" else "pre"
+        out = f8_linear_fwd(xr, wr, None if b is None else b.contiguous(), act,
+                            None if residual is None else residual.reshape(-1, w.shape[0]).contiguous(), save, x.dtype)
+        y, pre = (out, None) if save is None else out
+        ctx.act, ctx.grad, ctx.bias, ctx.shape, ctx.dtype = act, grad, b is not None and wants[2], x.shape, x.dtype
+        ctx.residual = None if residual is None else residual.shape
+        ctx.cols = (x.numel() // x.shape[-1], w.shape)
+        ctx.save_for_backward(pre, *(k for t in (xt, wt) for k in ((t.q, t.e) if t is not None else (None, None))))
+        return y.view(*x.shape[:-1], w.shape[0])
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gy):
+        pre, xq, xe, wq, we = ctx.saved_tensors
+        M, (O, I) = ctx.cols
+        wants = (*ctx.needs_input_grad, False, False, False)
+        dy = gy.reshape(-1, O).contiguous()
+        dh = dy if ctx.act == "none" else act_bwd(pre, dy, ctx.act)
+        gx = gw = gb = None
+        if wants[0]:
+            gx = f8_linear_bwd_input(pack_f8(dh, ctx.grad), F8.of(wq, we, O), dtype=ctx.dtype).view(ctx.shape)
+        if wants[1] or ctx.bias:
+            if M == 0:
+                gw, gb = (dh.new_zeros((O, I)) if wants[1] else None), (dh.new_zeros((O,)) if ctx.bias else None)
+            else:
+                dyt, gb = pack_f8(dh, ctx.grad, along="rows", sums=True)
+                gb = gb if ctx.bias else None
+                gw = f8_linear_bwd_weight(dyt, F8.of(xq, xe, M), dtype=ctx.dtype) if wants[1] else None
+        return gx, gw, gb, None, (gy.reshape(ctx.residual) if wants[4] else None), None
+
+
+# ---------------------------------------------------------------- AdamW over many tensors
+
+class AdamState:
+    """The states of AdamW for tensors of `sizes` values, flat: tensor i's part starts at `starts[i]`, the sum of the sizes
+    before it, each rounded up to 128.  m and v are float32, or float8_e4m3fn (v its root) with float32 scales ms and vs for
+    each 128 values; master (or None) the parameters in float32; step int32 (2,), the steps taken and 0."""
+
+    __slots__ = ("sizes", "starts", "m", "v", "step", "ms", "vs", "master")
+
+    def __init__(self, sizes, m: torch.Tensor, v: torch.Tensor, step: torch.Tensor, ms: torch.Tensor | None = None,
+                 vs: torch.Tensor | None = None, master: torch.Tensor | None = None):
+        self.sizes, self.starts, total = [int(n) for n in sizes], [], 0
+        for n in self.sizes:
+            self.starts.append(total)
+            total += -(-n // _lib.SCALED_GROUP) * _lib.SCALED_GROUP
+        held8 = m.dtype is torch.float8_e4m3fn
+        kinds = [("m", m, (total,), torch.float8_e4m3fn if held8 else torch.float32),
+                 ("v", v, (total,), torch.float8_e4m3fn if held8 else torch.float32), ("step", step, (2,), torch.int32)]
+        if held8 != (ms is not None) or held8 != (vs is not None):
+            raise ValueError("ms and vs are the scales of states in 8 bits, and only of those")
+        if held8:
+            kinds += [(n, t, (total // _lib.SCALED_GROUP,), torch.float32) for n, t in (("ms", ms), ("vs", vs))]
+        if master is not None:
+            kinds.append(("master", master, (total,), torch.float32))
+        for name, t, shape, dtype in kinds:
+            if tuple(t.shape) != shape or t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda \
+                    or t.device != m.device:
+                raise ValueError(f"{name} must be a contiguous {shape} tensor of {dtype} on one GPU, got {tuple(t.shape)} "
+                                 f"{t.dtype} {t.device}")
+        self.m, self.v, self.step, self.ms, self.vs, self.master = m, v, step, ms, vs, master
+
+    @staticmethod
+    def zeros(params, bits: int = 32, master: bool = False) -> "AdamState":
+        """New states of these parameters (one device), with master=True their values in float32."""
+        params = list(params)
+        if bits not in (8, 32) or not params:
+            raise ValueError(f"states have 8 or 32 bits, of at least one tensor; got {bits}, {len(params)} tensors")
+        device, sizes = params[0].device, [p.numel() for p in params]
+        total = sum(-(-n // _lib.SCALED_GROUP) * _lib.SCALED_GROUP for n in sizes)
+        kind = torch.float8_e4m3fn if bits == 8 else torch.float32
+        m, v = (torch.zeros(total, dtype=torch.uint8 if bits == 8 else kind, device=device).view(kind) for _ in range(2))
+        ms, vs = (torch.zeros(total // _lib.SCALED_GROUP, device=device) if bits == 8 else None for _ in range(2))
+        flat = torch.zeros(total, device=device) if master else None
+        state = AdamState(sizes, m, v, torch.zeros(2, dtype=torch.int32, device=device), ms, vs, flat)
+        if master:
+            with torch.no_grad():
+                for p, n, at in zip(params, sizes, state.starts):
+                    flat[at:at + n].copy_(p.reshape(-1))
+        return state
+
+    @property
+    def nbytes(self) -> int:
+        return sum(t.numel() * t.element_size() for t in (self.m, self.v, self.ms, self.vs, self.master) if t is not None)
+
+
+def adamw(params, grads, state: AdamState, lr: float | torch.Tensor = 1e-3, betas: tuple[float, float] = (0.9, 0.999),
+          eps: float = 1e-8, weight_decay: float = 0.01, max_norm: float | None = None,
+          workspace: torch.Tensor | None = None) -> torch.Tensor | None:
+    """One AdamW step over all params (of one type, contiguous) in place, given their grads (of one type; None leaves a
+    parameter and its states as they are).  lr may be a float32 tensor of one value on the GPU.  max_norm limits the norm of all
+    gradients, which is returned; where it is not finite, nothing changes."""
+    params, grads = list(params), list(grads)
+    if len(params) != len(state.sizes) or len(grads) != len(params):
+        raise ValueError(f"{len(params)} parameters and {len(grads)} gradients for the states of {len(state.sizes)}")
+    device, pdt, gdt = state.m.device, None, None
+    table = (_lib.AdamTensor * max(1, len(params)))()
+    count = 0
+    for p, g, n, at in zip(params, grads, state.sizes, state.starts):
+        if p.numel() != n or p.device != device or not p.is_contiguous() or (pdt is not None and p.dtype is not pdt):
+            raise ValueError(f"parameters must be contiguous tensors of one type on {device} with the states' sizes, got "
+                             f"{tuple(p.shape)} {p.dtype} {p.device} for {n} values")
+        pdt = p.dtype
+        if g is None or n == 0:
+            continue
+        if g.shape != p.shape or g.device != device or not g.is_contiguous() or (gdt is not None and g.dtype is not gdt):
+            raise ValueError(f"gradients must be contiguous tensors of one type with their parameters' shapes, got "
+                             f"{tuple(g.shape)} {g.dtype} {g.device} for {tuple(p.shape)}")
+        gdt = g.dtype
+        table[count] = _lib.AdamTensor(p.data_ptr(), g.data_ptr(), n, at)
+        count += 1
+    for t in (pdt, gdt):
+        if t is not None and t not in _DT:
+            raise TypeError(f"unsupported dtype {t}; use float32 or bfloat16")
+    lr_at = None
+    if isinstance(lr, torch.Tensor):
+        if lr.numel() != 1 or lr.dtype is not torch.float32 or lr.device != device:
+            raise ValueError(f"lr must be a number or one float32 value on {device}")
+        lr, lr_at = 0.0, lr.data_ptr()
+    if max_norm is not None and not max_norm > 0:
+        raise ValueError(f"max_norm must be positive, got {max_norm}")
+    s = _lib.AdamState(state.m.data_ptr(), state.v.data_ptr(), None if state.ms is None else state.ms.data_ptr(),
+                       None if state.vs is None else state.vs.data_ptr(),
+                       None if state.master is None else state.master.data_ptr(), state.step.data_ptr(),
+                       32 if state.ms is None else 8)
+    o = _lib.AdamOptions(lr, betas[0], betas[1], eps, weight_decay, max_norm or 0.0, lr_at)
+    norm = state.step.new_empty((), dtype=torch.float32) if max_norm is not None else None
+    workspace, nbytes = _scratch(workspace, state.step, int(_lib.lib().o1d_adamw_workspace_bytes(max_norm or 0.0)))
+    _run("o1d_adamw", state.step, ctypes.addressof(table), count, _DT[pdt] if pdt else 0, _DT[gdt] if gdt else 0,
+         ctypes.addressof(s), ctypes.addressof(o), None if norm is None else norm.data_ptr(), workspace.data_ptr(), nbytes)
+    return norm
