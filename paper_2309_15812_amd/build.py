@@ -4,8 +4,8 @@ Usage: ``python -m paper_2309_15812_amd.build`` (or ``build()`` from Python).
 Cross-compiles without a GPU.  Every ``csrc/*.hip`` translation unit is
 compiled to an object in parallel (the strip kernels are split per family,
 storage type and cell bound for this), then the objects are linked into the
-library.  ``_rows.so``, host code that calls the library from torch tensors, is
-compiled with g++ beside it.
+library.  ``_rows.so`` and ``_train.so``, host code that calls the library from torch
+tensors, are compiled with g++ beside it.
 """
 from __future__ import annotations
 
@@ -23,7 +23,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libo1d.so")
-BINDING = os.path.join(PKG, "_rows.so")  # Python's calls of the row operators (csrc/o1d_torch.cpp, host code only)
+# Python's calls of the row operators and of group norm, 8-bit products and AdamW (host code only)
+BINDINGS = {os.path.join(PKG, "_rows.so"): "o1d_torch.cpp", os.path.join(PKG, "_train.so"): "o1d_torch_train.cpp"}
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -91,26 +92,26 @@ def _key(src: str, flags: list[str]) -> str:
     return h.hexdigest()[:20]
 
 
-def build_binding(verbose: bool = False) -> str:
-    """Compiles the Python module against this torch's headers."""
+def build_binding(lib: str, verbose: bool = False) -> str:
+    """Compiles a Python module against this torch's headers."""
     import sysconfig
 
     import torch
 
     t = os.path.dirname(torch.__file__)
-    tmp = BINDING + ".tmp"
+    tmp = lib + ".tmp"
     _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-DUSE_ROCM", "-D__HIP_PLATFORM_AMD__",
           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
           "-isystem", os.path.join(t, "include"), "-isystem", os.path.join(t, "include", "torch", "csrc", "api", "include"),
           "-isystem", "/opt/rocm/include", "-isystem", sysconfig.get_paths()["include"],
-          os.path.join(CSRC, "o1d_torch.cpp"), "-o", tmp, "-L", os.path.join(t, "lib"), "-ltorch", "-ltorch_cpu", "-lc10",
+          os.path.join(CSRC, BINDINGS[lib]), "-o", tmp, "-L", os.path.join(t, "lib"), "-ltorch", "-ltorch_cpu", "-lc10",
           "-lc10_hip", "-ltorch_python"], verbose)
-    os.replace(tmp, BINDING)
-    return BINDING
+    os.replace(tmp, lib)
+    return lib
 
 
 def build(verbose: bool = False, jobs: int | None = None, incremental: bool = False) -> str:
-    """Compiles every translation unit, links libo1d.so and builds _rows.so.  With incremental=True, objects whose source,
+    """Compiles every translation unit, links libo1d.so and builds _rows.so and _train.so.  With incremental=True, objects whose source,
     headers and flags are unchanged are reused from _build/ (a development aid; the default always
     recompiles everything)."""
     srcs = sources()
@@ -139,7 +140,8 @@ def build(verbose: bool = False, jobs: int | None = None, incremental: bool = Fa
         tmp = LIB + ".tmp"
         _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs], verbose)
         os.replace(tmp, LIB)
-        build_binding(verbose)
+        with concurrent.futures.ThreadPoolExecutor(max_workers=len(BINDINGS)) as ex:
+            list(ex.map(lambda so: build_binding(so, verbose), BINDINGS))
     finally:
         shutil.rmtree(tmpdir, ignore_errors=True)
     return LIB

@@ -714,12 +714,38 @@ def gn_workspace_bytes(N: int, P: int, C: int, groups: int, dtype: torch.dtype, 
     return int(f(N, P, C, groups, _DT[dtype]))
 
 
+_bound_train = None
+_BOUND_TRAIN = ("o1d_gn_fwd", "o1d_gn_fwd_workspace_bytes", "o1d_gn_bwd", "o1d_gn_bwd_workspace_bytes", "o1d_pack_scaled",
+                "o1d_pack_scaled_workspace_bytes", "o1d_scaled_linear_fwd", "o1d_scaled_linear_bwd_input",
+                "o1d_scaled_linear_bwd_weight", "o1d_scaled_linear_bwd_weight_workspace_bytes", "o1d_adamw",
+                "o1d_adamw_workspace_bytes")
+
+
+def _train():
+    """The native calls of the common case of what follows; each returns None where it is another."""
+    global _bound_train
+    if _bound_train is None:
+        try:
+            from . import _train as native
+        except ImportError as e:
+            raise ImportError(f"{e}; build it with `python -m paper_2309_15812_amd.build`") from None
+        lib = _lib.lib()
+        native.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in _BOUND_TRAIN))
+        _bound_train = native
+    return _bound_train
+
+
 def gn_fwd(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor, groups: int, eps: float = 1e-5, act: str = "none",
            out: torch.Tensor | None = None, workspace: torch.Tensor | None = None
            ) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(y, mean, rstd): act of the group norm of x (N, ..., C) over a sample's pixels and the C / groups channels of a group;
     mean and rstd (N, groups) float32 are for gn_bwd."""
-    dt, a = _dt(x), _act(act)
+    a = _act(act)
+    if out is None and workspace is None:
+        made = _train().gn_fwd(x, w, b, groups, eps, a)
+        if made is not None:
+            return made
+    dt = _dt(x)
     v, N, P, C, ld = _samples(x, "x")
     _vector(w, "w", C, x)
     _vector(b, "b", C, x)
@@ -737,7 +763,12 @@ def gn_bwd(x: torch.Tensor, dy: torch.Tensor, mean: torch.Tensor, rstd: torch.Te
            act: str = "none", out: tuple[torch.Tensor, torch.Tensor, torch.Tensor] | None = None,
            workspace: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(dx, dw, db) of gn_fwd given its input, dy and its mean and rstd."""
-    dt, a = _dt(dy), _act(act)
+    a = _act(act)
+    if out is None and workspace is None:
+        made = _train().gn_bwd(x, dy, mean, rstd, w, b, a)
+        if made is not None:
+            return made
+    dt = _dt(dy)
     g, N, P, C, lddy = _samples(dy, "dy")
     v, ldx = _same(x, "x", N * P, C, dy)
     _stats(mean, "mean", None, dy)
@@ -780,6 +811,7 @@ class GroupNormFunction(torch.autograd.Function):
 
 _F8 = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
 _F8_OF = {t: _lib.SCALED[n] for n, t in _F8.items()}
+_ALONG = {"features": 1, "rows": 2, "both": 3}
 
 
 class F8:
@@ -844,10 +876,20 @@ def pack_f8(x: torch.Tensor, fmt: str = "e4m3", along: str = "features", sums: b
     """x's rows as 8-bit operands of products that sum along: "features" -> F8 of (M, C); "rows" -> F8 of x transposed
     (C, M), "both" -> the two.  sums=True (not with "features" alone) appends the columns' sums, a bias gradient, in
     x's type."""
-    if fmt not in _F8 or along not in ("features", "rows", "both"):
+    if fmt not in _F8 or along not in _ALONG:
         raise ValueError(f"fmt must be one of {list(_F8)}, along 'features', 'rows' or 'both'; got {fmt!r}, {along!r}")
     if sums and along == "features":
         raise ValueError("sums come with along='rows' or 'both'")
+    if workspace is None:
+        made = _train().pack(x, _lib.SCALED[fmt], _ALONG[along], sums)
+        if made is not None:
+            C = x.shape[-1]
+            if along == "features":
+                return F8.of(*made, C)
+            M = x.numel() // C
+            if along == "rows":
+                return (F8.of(made[0], made[1], M), made[2]) if sums else F8.of(*made, M)
+            return (F8.of(made[0], made[1], C), F8.of(made[2], made[3], M), *made[4:])
     dt = _dt(x)
     v, M, C, ld = _rows(x, "x")
     r = F8.empty(M, C, fmt, x.device) if along != "rows" else None
@@ -877,7 +919,12 @@ def f8_linear_fwd(x: F8, w: F8, b: torch.Tensor | None = None, act: str = "none"
     if dtype not in _DT:
         raise TypeError(f"unsupported dtype {dtype}; use float32 or bfloat16")
     a = _act(act)
-    _f8(x, "x", None, x.cols, x.q)
+    if out is None and type(x) is F8 and type(w) is F8 and x.cols == w.cols:
+        made = _train().linear_fwd(x.q, x.e, w.q, w.e, x.cols, b, a, residual, save is not None, _DT[dtype])
+        if made is not None:
+            return made
+    if not isinstance(x, F8):
+        raise TypeError(f"x must be packed (pack_f8), got {type(x).__name__}")
     _f8(w, "w", None, x.cols, x.q, second=True)
     M, I, O = x.rows, x.cols, w.rows
     y = torch.empty((M, O), dtype=dtype, device=x.q.device) if out is None else out
@@ -904,7 +951,12 @@ def f8_linear_bwd_input(dy: F8, wt: F8, pre: torch.Tensor | None = None, act: st
     a = _act(act)
     if (pre is None) != (act == "none"):
         raise ValueError("pre and act are given together")
-    _f8(dy, "dy", None, dy.cols, dy.q)
+    if out is None and type(dy) is F8 and type(wt) is F8 and dy.cols == wt.cols:
+        made = _train().linear_bwd_input(dy.q, dy.e, wt.q, wt.e, dy.cols, pre, a, _DT[dtype])
+        if made is not None:
+            return made
+    if not isinstance(dy, F8):
+        raise TypeError(f"dy must be packed (pack_f8), got {type(dy).__name__}")
     _f8(wt, "wt", None, dy.cols, dy.q, second=True)
     M, O, I = dy.rows, dy.cols, wt.rows
     dx = torch.empty((M, I), dtype=dtype, device=dy.q.device) if out is None else out
@@ -929,7 +981,12 @@ def f8_linear_bwd_weight(dyt: F8, xt: F8, dtype: torch.dtype = torch.bfloat16, o
     """dw (O, I) = dy^T x of the packed transposes dyt (O, M) and xt (I, M), in dtype."""
     if dtype not in _DT:
         raise TypeError(f"unsupported dtype {dtype}; use float32 or bfloat16")
-    _f8(dyt, "dyt", None, dyt.cols, dyt.q)
+    if out is None and workspace is None and type(dyt) is F8 and type(xt) is F8 and dyt.cols == xt.cols:
+        dw = _train().linear_bwd_weight(dyt.q, dyt.e, xt.q, xt.e, dyt.cols, _DT[dtype])
+        if dw is not None:
+            return dw
+    if not isinstance(dyt, F8):
+        raise TypeError(f"dyt must be packed (pack_f8), got {type(dyt).__name__}")
     _f8(xt, "xt", None, dyt.cols, dyt.q, second=True)
     M, O, I = dyt.cols, dyt.rows, xt.rows
     if O < 1 or I < 1:
@@ -995,10 +1052,12 @@ class AdamState:
 
     def __init__(self, sizes, m: torch.Tensor, v: torch.Tensor, step: torch.Tensor, ms: torch.Tensor | None = None,
                  vs: torch.Tensor | None = None, master: torch.Tensor | None = None):
-        self.sizes, self.starts, total = [int(n) for n in sizes], [], 0
-        for n in self.sizes:
-            self.starts.append(total)
-            total += -(-n // _lib.SCALED_GROUP) * _lib.SCALED_GROUP
+        self.sizes = list(sizes)
+        self.m, self.v, self.step, self.ms, self.vs, self.master = m, v, step, ms, vs, master
+        self.starts = _train().adam_starts(self.sizes, m, v, step, ms, vs, master)
+        if self.starts is not None:
+            return
+        total = sum(-(-n // _lib.SCALED_GROUP) * _lib.SCALED_GROUP for n in self.sizes)
         held8 = m.dtype is torch.float8_e4m3fn
         kinds = [("m", m, (total,), torch.float8_e4m3fn if held8 else torch.float32),
                  ("v", v, (total,), torch.float8_e4m3fn if held8 else torch.float32), ("step", step, (2,), torch.int32)]
@@ -1013,7 +1072,7 @@ class AdamState:
                     or t.device != m.device:
                 raise ValueError(f"{name} must be a contiguous {shape} tensor of {dtype} on one GPU, got {tuple(t.shape)} "
                                  f"{t.dtype} {t.device}")
-        self.m, self.v, self.step, self.ms, self.vs, self.master = m, v, step, ms, vs, master
+        raise ValueError(f"no sizes of tensors: {self.sizes}")
 
     @staticmethod
     def zeros(params, bits: int = 32, master: bool = False) -> "AdamState":
@@ -1045,7 +1104,14 @@ def adamw(params, grads, state: AdamState, lr: float | torch.Tensor = 1e-3, beta
     """One AdamW step over all params (of one type, contiguous) in place, given their grads (of one type; None leaves a
     parameter and its states as they are).  lr may be a float32 tensor of one value on the GPU.  max_norm limits the norm of all
     gradients, which is returned; where it is not finite, nothing changes."""
+    if max_norm is not None and not max_norm > 0:
+        raise ValueError(f"max_norm must be positive, got {max_norm}")
     params, grads = list(params), list(grads)
+    if workspace is None:
+        made = _train().adamw(params, grads, state.sizes, (state.m, state.v, state.step, state.ms, state.vs, state.master), lr,
+                              betas[0], betas[1], eps, weight_decay, max_norm or 0.0)
+        if made is not None:
+            return None if max_norm is None else made
     if len(params) != len(state.sizes) or len(grads) != len(params):
         raise ValueError(f"{len(params)} parameters and {len(grads)} gradients for the states of {len(state.sizes)}")
     device, pdt, gdt = state.m.device, None, None
@@ -1072,8 +1138,6 @@ def adamw(params, grads, state: AdamState, lr: float | torch.Tensor = 1e-3, beta
         if lr.numel() != 1 or lr.dtype is not torch.float32 or lr.device != device:
             raise ValueError(f"lr must be a number or one float32 value on {device}")
         lr, lr_at = 0.0, lr.data_ptr()
-    if max_norm is not None and not max_norm > 0:
-        raise ValueError(f"max_norm must be positive, got {max_norm}")
     s = _lib.AdamState(state.m.data_ptr(), state.v.data_ptr(), None if state.ms is None else state.ms.data_ptr(),
                        None if state.vs is None else state.vs.data_ptr(),
                        None if state.master is None else state.master.data_ptr(), state.step.data_ptr(),
