@@ -337,7 +337,7 @@ o1d_status_t o1d_scaled_linear_bwd_input(const unsigned char* dyq, const unsigne
 o1d_status_t o1d_scaled_linear_bwd_weight(const unsigned char* dytq, const unsigned char* dyte, o1d_scaled_t type,
                                           const unsigned char* xtq, const unsigned char* xte, void* dw, int M, int I, int O,
                                           o1d_dtype_t dtype, void* workspace, size_t workspace_bytes, void* stream);
-size_t o1d_scaled_linear_bwd_weight_workspace_bytes(int M, int I, int O);
+size_t o1d_scaled_linear_bwd_weight_workspace_bytes(int M, int I, int O, o1d_dtype_t dtype);
 
 /* ---- AdamW over many tensors at once.  With t = steps taken + 1 and g the gradient (times max_norm / norm where the norm is
  * larger):

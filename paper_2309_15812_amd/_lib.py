@@ -71,7 +71,7 @@ SIGNATURES = {
     "o1d_scaled_linear_fwd": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _i, _vp, _ll, _vp, _ll, _vp, _ll, _i, _i, _i, _i, _vp]),
     "o1d_scaled_linear_bwd_input": (_i, [_vp, _vp, _i, _vp, _vp, _i, _vp, _ll, _vp, _ll, _i, _i, _i, _i, _vp]),
     "o1d_scaled_linear_bwd_weight": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _sz, _vp]),
-    "o1d_scaled_linear_bwd_weight_workspace_bytes": (_sz, [_i, _i, _i]),
+    "o1d_scaled_linear_bwd_weight_workspace_bytes": (_sz, [_i, _i, _i, _i]),
     "o1d_adamw": (_i, [_vp, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "o1d_adamw_workspace_bytes": (_sz, [_d]),
     "o1d_kernel_name": (ctypes.c_char_p, [_i, _i, _i, _i, _i, _i, _i, _i, _i, _i, _i]),

@@ -33,16 +33,17 @@ struct F8MmParams {
   MmParams mm;
   const uint8_t *ea, *eb;
   long long lea, leb;
+  int band;  // rows of tiles that are taken together
 };
-enum F8ShapeId { kF8_128x128, kF8_64x64, kF8ShapeCount };
-constexpr Shape kF8Shapes[kF8ShapeCount] = {{2, 2, 2, 2}, {2, 2, 1, 1}};
+enum F8ShapeId { kF8_256x256, kF8_128x128, kF8_64x64, kF8ShapeCount };
+constexpr Shape kF8Shapes[kF8ShapeCount] = {{2, 4, 4, 2}, {2, 2, 2, 2}, {2, 2, 1, 1}};
 
 struct F8Plan {
   int shape, atype;
   F8MmParams p;
 };
 // kFwd or kDgrad (which differ in their epilogue), or kWgrad (pieces of k).
-F8Plan plan_f8(int kind, int M, int N, int K);
+F8Plan plan_f8(int kind, int M, int N, int K, int esize);
 
 #define O1D_F8_DECL(T)                                                   \
   hipError_t launch_f8_fwd_##T(const F8Plan& pl, hipStream_t stream);    \

@@ -15,13 +15,16 @@ o1d_status_t check_packed(const char* fn, const char* what, const unsigned char*
   return O1D_OK;
 }
 
+// Rows that a weight gradient sums: the offsets of a tile's 256 rows stay below 2^31 bytes.
+constexpr int kMostSummed = 8 * (int)kMaxStride - 1024;
+
 size_t q_bytes(int R, int K) { return (size_t)R * (size_t)rows::f8_ld(K); }
 size_t e_bytes(int R, int K) { return (size_t)rows::f8_le(R) * (size_t)rows::f8_groups(K); }
 
 // A product's plan with its operands: A of M rows, B of N rows, K values each.
 rows::F8Plan planned(int kind, int M, int N, int K, const unsigned char* aq, const unsigned char* ae, o1d_scaled_t type,
-                     const unsigned char* bq, const unsigned char* be) {
-  rows::F8Plan pl = rows::plan_f8(kind, M, N, K);
+                     const unsigned char* bq, const unsigned char* be, o1d_dtype_t dt) {
+  rows::F8Plan pl = rows::plan_f8(kind, M, N, K, (int)elem_size(dt));
   pl.atype = (int)type;
   pl.p.mm.a = aq;
   pl.p.mm.b = bq;
@@ -110,7 +113,7 @@ o1d_status_t o1d_scaled_linear_fwd(const unsigned char* xq, const unsigned char*
                         {"the residual", res, reach(M, ldres, O, es), false}, {"y", y, reach(M, ldy, O, es), true},
                         {"pre", pre, reach(M, ldpre, O, es), true}};
   O1D_TRY(apart(fn, spans));
-  rows::F8Plan pl = planned(rows::kFwd, M, O, I, xq, xe, type, wq, we);
+  rows::F8Plan pl = planned(rows::kFwd, M, O, I, xq, xe, type, wq, we, dtype);
   O1D_TRY(check_tiles(fn, pl));
   (void)hipGetLastError();
   rows::MmParams& p = pl.p.mm;
@@ -149,7 +152,7 @@ o1d_status_t o1d_scaled_linear_bwd_input(const unsigned char* dyq, const unsigne
                         {"w", wtq, q_bytes(I, O), false}, {"w's exponents", wte, e_bytes(I, O), false},
                         {"pre", slope, reach(M, ldpre, I, es), false}, {"dx", dx, reach(M, lddx, I, es), true}};
   O1D_TRY(apart(fn, spans));
-  rows::F8Plan pl = planned(rows::kDgrad, M, I, O, dyq, dye, type, wtq, wte);
+  rows::F8Plan pl = planned(rows::kDgrad, M, I, O, dyq, dye, type, wtq, wte, dtype);
   O1D_TRY(check_tiles(fn, pl));
   (void)hipGetLastError();
   rows::MmParams& p = pl.p.mm;
@@ -162,11 +165,11 @@ o1d_status_t o1d_scaled_linear_bwd_input(const unsigned char* dyq, const unsigne
   return hip_status(fn, dtype == O1D_F32 ? rows::launch_f8_dgrad_f32(pl, s) : rows::launch_f8_dgrad_bf16(pl, s));
 }
 
-size_t o1d_scaled_linear_bwd_weight_workspace_bytes(int M, int I, int O) {
+size_t o1d_scaled_linear_bwd_weight_workspace_bytes(int M, int I, int O, o1d_dtype_t dtype) {
   const char* fn = "o1d_scaled_linear_bwd_weight";
-  if (check_dims(fn, M, I, "I", O1D_F32) != O1D_OK || check_dims(fn, M, O, "O", O1D_F32) != O1D_OK || M == 0) return 0;
-  if (M > kMaxFeatures * 1024) return 0;
-  const int pieces = rows::plan_f8(rows::kWgrad, O, I, M).p.mm.nsplit;
+  if (check_dims(fn, M, I, "I", dtype) != O1D_OK || check_dims(fn, M, O, "O", dtype) != O1D_OK || M == 0) return 0;
+  if (M > kMostSummed) return 0;
+  const int pieces = rows::plan_f8(rows::kWgrad, O, I, M, (int)elem_size(dtype)).p.mm.nsplit;
   return pieces > 1 ? space_for((size_t)pieces * ((size_t)O * I + O) * sizeof(float)) : kNoSpace;
 }
 
@@ -178,12 +181,11 @@ o1d_status_t o1d_scaled_linear_bwd_weight(const unsigned char* dytq, const unsig
   O1D_TRY(check_dims(fn, M, O, "O", dtype));
   O1D_TRY(check_type(fn, type));
   O1D_TRY(check_null(fn, {dw}));
-  const size_t es = elem_size(dtype), need = o1d_scaled_linear_bwd_weight_workspace_bytes(M, I, O);
+  const size_t es = elem_size(dtype), need = o1d_scaled_linear_bwd_weight_workspace_bytes(M, I, O, dtype);
   O1D_TRY(check_elem_aligned(fn, dw, "dw", es));
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (M == 0) return hip_status(fn, o1d::launch_zero((Dtype)dtype, dw, (size_t)O * I, s));
-  if (M > kMaxStride * 8)  // (a tile's offsets stay below 2^31 bytes)
-    return fail(O1D_ERR_UNSUPPORTED, "%s: M=%d rows exceed %lld", fn, M, kMaxStride * 8);
+  if (M > kMostSummed) return fail(O1D_ERR_UNSUPPORTED, "%s: M=%d rows exceed %d", fn, M, kMostSummed);
   O1D_TRY(check_packed(fn, "dy", dytq, dyte));
   O1D_TRY(check_packed(fn, "x", xtq, xte));
   O1D_TRY(check_workspace(fn, workspace, workspace_bytes, need));
@@ -191,7 +193,7 @@ o1d_status_t o1d_scaled_linear_bwd_weight(const unsigned char* dytq, const unsig
                         {"x", xtq, q_bytes(I, M), false}, {"x's exponents", xte, e_bytes(I, M), false},
                         {"dw", dw, (size_t)O * I * es, true}, {"the workspace", workspace, need, true}};
   O1D_TRY(apart(fn, spans));
-  rows::F8Plan pl = planned(rows::kWgrad, O, I, M, dytq, dyte, type, xtq, xte);
+  rows::F8Plan pl = planned(rows::kWgrad, O, I, M, dytq, dyte, type, xtq, xte, dtype);
   O1D_TRY(check_tiles(fn, pl));
   (void)hipGetLastError();
   rows::MmParams& p = pl.p.mm;

@@ -15,6 +15,7 @@
 
 #include "o1d_f8.h"
 #include "o1d_mmf_kernels.h"
+#include "o1d_wave.h"
 
 namespace o1d {
 namespace rows {
@@ -22,22 +23,38 @@ namespace {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// acc[i][k] += m fragment i times n fragment k, 64 of k: fragments of two runs,
-// the same two for both operands, and their rows' exponents.
-template <int ATYPE, int TM, int TN>
-__device__ __forceinline__ void f8_products(const u32x4 (&n)[TN][2], const u32x4 (&m)[TM][2], const uint32_t (&sn)[TN],
-                                            const uint32_t (&sm)[TM], f32x16 (&acc)[TM][TN]) {
+// As fetch, of the lanes in `mask` (all or none: no branch parts the products); and 64 lanes' words to
+// 256 bytes of LDS at `lds`.  All lanes are active before and after.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void fetch_if(uint64_t mask, const char* base, uint32_t off, uint32_t stage, uint32_t block) {
+  asm volatile("s_add_u32 m0, %2, %3\n\ts_mov_b64 exec, %4\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1" ::"v"(off),
+               "s"(base), "s"(stage), "s"(block), "s"(mask)
+               : "memory", "scc", "m0");
+}
+__device__ __forceinline__ void fetch_words_if(uint64_t mask, const char* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 exec, %2\n\tglobal_load_lds_dword %0, off\n\ts_mov_b64 exec, -1" ::"v"(from),
+               "s"(lds), "s"(mask)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// acc[k] += m fragment times n fragment k, 64 of k: fragments of two runs, the same two
+// for both operands, and their rows' exponents.  between(): called after each product.
+template <int ATYPE, int TN, class F>
+__device__ __forceinline__ void f8_products(const u32x4 (&n)[TN][2], const u32x4 (&m)[2], const uint32_t (&sn)[TN],
+                                            uint32_t sm, f32x16 (&acc)[TN], F&& between) {
   auto whole = [](const u32x4(&f)[2]) __attribute__((always_inline)) {
     i32x8 r;
     __builtin_memcpy(&r, f, 32);
     return r;
   };
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int k = 0; k < TN; ++k)
-      acc[i][k] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(n[k]), whole(m[i]), acc[i][k], kE4M3, ATYPE, 0,
-                                                                  (int)sn[k], 0, (int)sm[i]);
+  wave::static_for<TN>([&](auto kc) __attribute__((always_inline)) {
+    constexpr int k = decltype(kc)::value;
+    acc[k] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(n[k]), whole(m), acc[k], kE4M3, ATYPE, 0, (int)sn[k], 0,
+                                                             (int)sm);
+    between(kc);
+  });
 }
 
 // Eight values of a run, two words, widened.
@@ -61,43 +78,141 @@ __device__ __forceinline__ bf16x8 widened(uint32_t lo, uint32_t hi, uint32_t exp
   __builtin_memcpy(&r, p, 16);
   return r;
 }
-template <int ATYPE, int TM, int TN>
-__device__ __forceinline__ void wide_products(const u32x4 (&n)[TN][2], const u32x4 (&m)[TM][2], const uint32_t (&sn)[TN],
-                                              const uint32_t (&sm)[TM], f32x16 (&acc)[TM][TN]) {
+template <int ATYPE, int TN, class F>
+__device__ __forceinline__ void wide_products(const u32x4 (&n)[TN][2], const u32x4 (&m)[2], const uint32_t (&sn)[TN],
+                                              uint32_t sm, f32x16 (&acc)[TN], F&& between) {
+  wave::static_for<TN>(between);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    bf16x8 wn[TN], wm[TM];
+    const bf16x8 wm = widened<ATYPE>(m[j / 2][j % 2 * 2], m[j / 2][j % 2 * 2 + 1], sm);
 #pragma unroll
-    for (int k = 0; k < TN; ++k) wn[k] = widened<kE4M3>(n[k][j / 2][j % 2 * 2], n[k][j / 2][j % 2 * 2 + 1], sn[k]);
+    for (int k = 0; k < TN; ++k)
+      acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widened<kE4M3>(n[k][j / 2][j % 2 * 2], n[k][j / 2][j % 2 * 2 + 1], sn[k]),
+                                                       wm, acc[k], 0, 0, 0);
+  }
+}
+
+// The wave's tile, a block of 32 rows x 64 columns (32 of a tile that narrow) after the other, by way of LDS (`mine`,
+// 8 or 4 KB): from the products' layout, 32 rows in a store of 32 bytes each, to whole cache lines of
+// eight rows; what the block's epilogue reads comes the same way.  (Straight from the products' layout, rows 16 KB
+// apart, the epilogue of a tile of 256 x 256 took 21 us.)  ACT: the activation (kActs: P.act, whatever it is);
+// one choice for the tile, not one for every run.
+template <typename T, int KIND, bool WHOLE, int ACT, int TM, int TN>
+__device__ __forceinline__ void f8_blocks(const MmParams& Q, int m0, int n0, int split, const f32x16 (&acc)[TM][TN],
+                                          char* mine) {
+  constexpr int NB = TN % 2 ? 1 : 2, kCols = 32 * NB, kRuns = kCols / 4, kSame = kCols / 8, kRows = 64 / kSame;
+  constexpr int kSets = 32 / kRows, kBlocks = TM * TN / NB;
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));  // (what follows from it is not computed before the products, for registers)
+  const int half = lane >> 5, row = lane & 31;
+  MmParams P = Q;
+  if constexpr (ACT != kActs) P.act = ACT;
+  const int r = lane / kSame, c = lane % kSame;  // this lane's row (of every kRows) and run of eight columns
+  // runs of four columns lie in an order of their row's own, so that neither side has bank conflicts
+  float* const to = reinterpret_cast<float*>(mine) + row * kCols;
+  const float* const from = reinterpret_cast<const float*>(mine) + r * kCols;
+  static_assert(kRows % 8 == 0 && kRuns % 8 == 0, "the order repeats");
+  wave::static_for<kBlocks>([&](auto bc) __attribute__((always_inline)) {
+    constexpr int b = decltype(bc)::value, i = b % TM, k = b / TM;
+    const int m = m0 + 32 * i + r, n = n0 + kCols * k + 8 * c;
+    Ahead<T, KIND, WHOLE> ahead[kSets];
+    if constexpr (KIND != kWgrad) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) wm[i] = widened<ATYPE>(m[i][j / 2][j % 2 * 2], m[i][j / 2][j % 2 * 2 + 1], sm[i]);
+      for (int q = 0; q < kSets; ++q) ahead[q].load(P, m + kRows * q, n);
+    }
+    T bias[8];
+    const bool biased = KIND == kFwd && P.bias;
+    if (biased) {
+      const T* p = static_cast<const T*>(P.bias) + n;
+      if (WHOLE || n + 8 <= P.N) {
+        __builtin_memcpy(bias, p, sizeof(bias));
+      } else {
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+        for (int e = 0; e < 8; ++e) bias[e] = n + e < P.N ? p[e] : T(0);
+      }
+    }
 #pragma unroll
-      for (int k = 0; k < TN; ++k) acc[i][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wn[k], wm[i], acc[i][k], 0, 0, 0);
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float v[4] = {acc[i][NB * k + j][4 * g], acc[i][NB * k + j][4 * g + 1], acc[i][NB * k + j][4 * g + 2],
+                            acc[i][NB * k + j][4 * g + 3]};
+        __builtin_memcpy(__builtin_assume_aligned(to + 4 * ((8 * j + 2 * g + half) ^ (row & (kRuns - 1))), 16), v, 16);
+      }
+    asm volatile("" ::: "memory");  // (a wave's accesses of LDS keep their order)
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int q = 0; q < kSets; ++q) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        __builtin_memcpy(v + 4 * j,
+                         __builtin_assume_aligned(from + kRows * q * kCols + 4 * ((2 * c + j) ^ ((r + kRows * q) & (kRuns - 1))), 16),
+                         16);
+      if (biased) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += to_f32(bias[e]);
+      }
+      const int mq = m + kRows * q;
+      if constexpr (KIND == kWgrad) {
+        if (WHOLE || (mq < P.M && n < P.N)) {
+          if (P.nsplit == 1)
+            put<T, WHOLE>(static_cast<T*>(P.out) + (long long)mq * P.N + n, P.N - n, v);
+          else
+            put<float, WHOLE>(P.part + (long long)split * ((long long)P.M * P.N + P.M) + (long long)mq * P.N + n, P.N - n, v);
+        }
+      } else {
+        finish<T, KIND, WHOLE>(P, mq, n, ahead[q], v);
+      }
+      if constexpr (TM * TN > 4) __builtin_amdgcn_sched_barrier(0);  // (registers)
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  });
+}
+
+template <typename T, int KIND, int TM, int TN>
+__device__ __forceinline__ void f8_epilogue(const MmParams& P, bool whole, int m0, int n0, int split,
+                                            const f32x16 (&acc)[TM][TN], char* mine) {
+  if (!whole) return f8_blocks<T, KIND, false, kActs>(P, m0, n0, split, acc, mine);
+  if constexpr (KIND == kWgrad) return f8_blocks<T, KIND, true, kNone>(P, m0, n0, split, acc, mine);
+  switch (P.act) {
+    case kRelu: return f8_blocks<T, KIND, true, kRelu>(P, m0, n0, split, acc, mine);
+    case kGelu: return f8_blocks<T, KIND, true, kGelu>(P, m0, n0, split, acc, mine);
+    case kGeluTanh: return f8_blocks<T, KIND, true, kGeluTanh>(P, m0, n0, split, acc, mine);
+    case kSilu: return f8_blocks<T, KIND, true, kSilu>(P, m0, n0, split, acc, mine);
+    default: return f8_blocks<T, KIND, true, kNone>(P, m0, n0, split, acc, mine);
   }
 }
 
 template <int SHAPE>
 struct F8Geo {
   static constexpr Shape S = kF8Shapes[SHAPE];
+  static constexpr int kCount = S.wm * S.wn, kThreads = 64 * kCount;  // waves and threads of a workgroup
   static constexpr int BM = 32 * S.tm * S.wm, BN = 32 * S.tn * S.wn;
   using TA = FastTile<uint8_t, BM, true>;
   using TB = FastTile<uint8_t, BN, true>;
-  static constexpr int kBlocks = TA::kBlocks + TB::kBlocks + 1;  // the last: both operands' exponents
-  static constexpr int kFetches = (kBlocks + 3) / 4;             // of a wave, per step
-  static constexpr int kScales = TA::kBytes + TB::kBytes;
-  static constexpr int kStage = kBlocks * 1024;
-  static constexpr int kStages = 3;
-  static constexpr int kLds = kStage * kStages;
-  static constexpr int kWaves = S.tm * S.tn <= 2 ? 3 : 1;  // per SIMD
+  static constexpr int kBlocks = TA::kBlocks + TB::kBlocks, kFetches = kBlocks / kCount;  // KB, and a wave's, of a step
+  static_assert(kBlocks % kCount == 0 && TA::kBlocks % kCount == 0, "a wave's first fetches are A's");
+  static constexpr int kScales = kBlocks * 1024;  // where the exponents of a step lie, A's then B's
+  static constexpr int kStage = kScales + 256 * kCount;
+  static_assert(BM + BN <= 256 * kCount, "a word of exponents for each thread");
+  static constexpr int kLds = kStage * 2;
+  static constexpr int kMine = 32 * (S.tn % 2 ? 32 : 64) * 4;  // of a wave, for the epilogue, in a stage
+  static_assert(kMine * kCount <= kStage, "a block of sums for each wave");
+  static constexpr int kWaves = SHAPE == kF8_64x64 ? 4 : 2;  // per SIMD
 };
 
+// Two stages of LDS.  A step's products go by 32 rows of m and 64 of k at a time (a part), whose fragments
+// are read kAhead parts before.  When a step's last fragments are on their way to registers and the next step has
+// landed, its stage is free: the loads of the step after the next go there, and the next step's first fragments are
+// read during the products that are left.  One barrier per step; the loads have a whole step to arrive.
 template <typename T, int KIND, int SHAPE, int ATYPE>
-__global__ __launch_bounds__(kMmThreads, F8Geo<SHAPE>::kWaves) void f8mm(F8MmParams Q) {
+__global__ __launch_bounds__(F8Geo<SHAPE>::kThreads, F8Geo<SHAPE>::kWaves) void f8mm(F8MmParams Q) {
   using G = F8Geo<SHAPE>;
   const MmParams& P = Q.mm;
-  constexpr int TM = G::S.tm, TN = G::S.tn, BK = kF8Group, S = G::kStages, NF = G::kFetches;
+  constexpr int TM = G::S.tm, TN = G::S.tn, BK = kF8Group, NF = G::kFetches;
   extern __shared__ __align__(16) char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / G::S.wn * 32 * TM, wn = wave % G::S.wn * 32 * TN;
@@ -109,68 +224,114 @@ __global__ __launch_bounds__(kMmThreads, F8Geo<SHAPE>::kWaves) void f8mm(F8MmPar
   struct At {
     int m0, n0, split, s0, s1;
   };
+  // Tiles in bands of `band` rows of tiles, column after column: those at work at a time share both operands.
   auto tile_of = [&](int t) __attribute__((always_inline)) {
-    const int nt = t % P.tn, rest = t / P.tn;
     auto scalar = [](int v) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(v); };
+    const int per = P.tm * P.tn, split = t / per, in = t - split * per;
+    const int band = in / (Q.band * P.tn), first = band * Q.band, rows = min(Q.band, P.tm - first);
+    const int rest = in - first * P.tn;
     At a;
-    a.m0 = scalar(rest % P.tm * G::BM);
-    a.n0 = scalar(nt * G::BN);
-    a.split = scalar(rest / P.tm);
+    a.m0 = scalar((first + rest % rows) * G::BM);
+    a.n0 = scalar(rest / rows * G::BN);
+    a.split = scalar(split);
     a.s0 = a.split * P.per;
     a.s1 = min(P.steps, a.s0 + P.per);
     return a;
   };
 
+  // ---- the loads, two steps ahead of the products: a lane's offsets stay for a tile, the operands'
+  // (scalar) addresses go from step to step
+  uint32_t off[NF], block[NF];
+#pragma unroll
+  for (int f = 0; f < NF; ++f) block[f] = (uint32_t)(wave + G::kCount * f) * 1024;
+  const char *base_a = nullptr, *base_b = nullptr, *exps = nullptr;
+  long long exps_by = 0;
   int ahead_id = id, ahead_left = 0;
   uint32_t ahead_stage = 0;
-  const char* from[NF];      // where this lane's runs of the next step lie
-  long long by[NF];          // and how far the next step's are (0: zeros)
+  auto is_a = [](int f) __attribute__((always_inline)) { return G::kCount * f < G::TA::kBlocks; };
   auto aim = [&]() __attribute__((always_inline)) {
     const At a = tile_of(ahead_id);
     ahead_left = a.s1 - a.s0;
+    base_a = G::TA::origin(P.a, P.lda, a.m0, a.s0);
+    base_b = G::TB::origin(P.b, P.ldb, a.n0, a.s0);
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
-      const int b = min(wave + 4 * f, G::kBlocks - 1);
-      if (b < G::TA::kBlocks) {
-        from[f] = G::TA::origin(P.a, P.lda, a.m0, a.s0) + G::TA::source(b, lane, P.lda, a.m0, P.M);
-        by[f] = BK;
-      } else if (b < G::kBlocks - 1) {
-        from[f] = G::TB::origin(P.b, P.ldb, a.n0, a.s0) + G::TB::source(b - G::TA::kBlocks, lane, P.ldb, a.n0, P.N);
-        by[f] = BK;
-      } else {
-        const int at = 16 * lane;  // of the two operands' rows
-        const bool of_a = at < G::BM;
-        const int row = of_a ? a.m0 + at : a.n0 + at - G::BM;
-        const long long le = of_a ? Q.lea : Q.leb;
-        const uint8_t* e = of_a ? Q.ea : Q.eb;
-        const bool in = at < G::BM + G::BN && row < le;
-        from[f] = in ? reinterpret_cast<const char*>(e + a.s0 * le + row) : reinterpret_cast<const char*>(&g_zero_run);
-        by[f] = in ? le : 0;
-      }
+      const int b = (int)(block[f] / 1024);
+      off[f] = is_a(f) ? G::TA::source(b, lane, P.lda, a.m0, P.M) : G::TB::source(b - G::TA::kBlocks, lane, P.ldb, a.n0, P.N);
     }
+    // a thread's four exponents of the tile's rows, A's then B's
+    const int at = 4 * (int)threadIdx.x;
+    const bool of_a = at < G::BM;
+    const int row = of_a ? a.m0 + at : a.n0 + at - G::BM;
+    const long long le = of_a ? Q.lea : Q.leb;
+    const bool in = at < G::BM + G::BN && row < le;  // (others: rows past the end, whose results are not stored)
+    exps = in ? reinterpret_cast<const char*>((of_a ? Q.ea : Q.eb) + a.s0 * le + row)
+              : reinterpret_cast<const char*>(&g_zero_run);
+    exps_by = in ? le : 0;
   };
-  auto issue = [&]() __attribute__((always_inline)) {
-    if (ahead_left == 0 && ahead_id + stride < last) {
+  // Whether there is a step to fetch, as a mask of the lanes; the tile's steps done, it is the next tile's first.
+  auto ahead = [&]() __attribute__((always_inline)) {
+    if (ahead_left == 0) {
+      if (ahead_id + stride >= last) return (uint64_t)0;
       ahead_id += stride;
       aim();
     }
-    const bool any = ahead_left > 0;
+    return ~(uint64_t)0;
+  };
+  // that step's fetch f (NF: the exponents'), and what follows the last of them
+  auto issue_one = [&](uint64_t mask, auto fc) __attribute__((always_inline)) {
+    constexpr int f = decltype(fc)::value;
+    if constexpr (f < NF)
+      fetch_if(mask, is_a(f) ? base_a : base_b, off[f], ahead_stage, block[f]);
+    else
+      fetch_words_if(mask, exps, ahead_stage + (uint32_t)G::kScales + 256u * (uint32_t)wave);
+  };
+  // (no branch: the compiler would move the products behind it)
+  auto issued = [&](uint64_t mask) __attribute__((always_inline)) {
+    const int by = (int)mask & BK;
+    exps += exps_by & (long long)mask;
+    base_a += by;
+    base_b += by;
+    ahead_stage ^= (uint32_t)mask & (uint32_t)G::kStage;
+    ahead_left += (int)mask;
+  };
+  auto issue = [&]() __attribute__((always_inline)) {
+    const uint64_t mask = ahead();
+    if (!mask) return;
+    wave::static_for<NF + 1>([&](auto fc) __attribute__((always_inline)) { issue_one(mask, fc); });
+    issued(mask);
+  };
+
+  constexpr int kParts = 2 * TM, kHeld = kParts < 4 ? kParts : 4, kAhead = kHeld / 2;
+  uint32_t stage = 0;
+  u32x4 fm[kHeld][2], fn[2][TN][2];
+  uint32_t sm[TM], sn[TN], next_m[TM], next_n[TN];
+  // the fragments of part u of the step at `at`
+  auto read = [&](uint32_t at, auto u) __attribute__((always_inline)) {
+    constexpr int U = decltype(u)::value, h = U / TM, i = U % TM;
+    const char *la = lds + at, *lb = la + G::TA::kBytes;
+    if constexpr (U == 0) {
+      const char* le = lds + at + G::kScales;
 #pragma unroll
-    for (int f = 0; f < NF; ++f) {
-      fetch(any ? from[f] : reinterpret_cast<const char*>(&g_zero_run),
-            ahead_stage + (uint32_t)min(wave + 4 * f, G::kBlocks - 1) * 1024);
-      from[f] += by[f];
+      for (int k = 0; k < TM; ++k) next_m[k] = (uint8_t)le[wm + 32 * k + (lane & 31)];
+#pragma unroll
+      for (int k = 0; k < TN; ++k) next_n[k] = (uint8_t)le[G::BM + wn + 32 * k + (lane & 31)];
     }
-    ahead_stage = ahead_stage == (S - 1) * G::kStage ? 0 : ahead_stage + G::kStage;
-    if (any) --ahead_left;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if constexpr (i == 0) {
+#pragma unroll
+        for (int k = 0; k < TN; ++k) fn[h][k][j] = G::TB::frag(lb, wn + 32 * k, 2 * h + j).p[0];
+      }
+      fm[U % kHeld][j] = G::TA::frag(la, wm + 32 * i, 2 * h + j).p[0];
+    }
   };
 
   aim();
-#pragma unroll
-  for (int s = 0; s < S - 1; ++s) issue();
-
-  uint32_t stage = 0;
-  int landed = 0;
+  issue();
+  wait_loads<0>();
+  step_barrier();
+  issue();
   for (; id < last; id += stride) {
     const At at = tile_of(id);
     f32x16 acc[TM][TN];
@@ -180,46 +341,52 @@ __global__ __launch_bounds__(kMmThreads, F8Geo<SHAPE>::kWaves) void f8mm(F8MmPar
       for (int k = 0; k < TN; ++k)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][k][e] = 0.f;
+    wave::static_for<kAhead>([&](auto u) __attribute__((always_inline)) { read(stage, u); });
     for (int s = at.s0; s < at.s1; ++s) {
-      if (landed > 0)
-        --landed;
-      else
-        wait_loads<(S - 2) * NF>();
-      step_barrier();
-      const char *la = lds + stage, *lb = la + G::TA::kBytes, *le = la + G::kScales;
-      stage = stage == (S - 1) * G::kStage ? 0 : stage + G::kStage;
-      u32x4 fm[2][TM][2], fn[2][TN][2];
-      uint32_t sm[TM], sn[TN];
+      // (the last step's stage is the epilogue's: nothing is fetched to it before)
+      const uint64_t mask = s + 1 < at.s1 ? ahead() : 0;
 #pragma unroll
-      for (int i = 0; i < TM; ++i) sm[i] = (uint8_t)le[wm + 32 * i + (lane & 31)];
+      for (int i = 0; i < TM; ++i) sm[i] = next_m[i];
 #pragma unroll
-      for (int i = 0; i < TN; ++i) sn[i] = (uint8_t)le[G::BM + wn + 32 * i + (lane & 31)];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i) fm[j / 2][i][j % 2] = G::TA::frag(la, wm + 32 * i, j).p[0];
-#pragma unroll
-        for (int i = 0; i < TN; ++i) fn[j / 2][i][j % 2] = G::TB::frag(lb, wn + 32 * i, j).p[0];
-      }
-      issue();
-      __builtin_amdgcn_sched_barrier(0);  // the reads before the products
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int i = 0; i < TN; ++i) sn[i] = next_n[i];
+      wave::static_for<kParts>([&](auto part) __attribute__((always_inline)) {
+        constexpr int t = decltype(part)::value, u = t + kAhead;
+        if constexpr (u < kParts) {
+          read(stage, std::integral_constant<int, u>{});
+        } else {
+          if constexpr (u == kParts) {
+            wait_loads<0>();
+            step_barrier();
+            stage ^= (uint32_t)G::kStage;
+          }
+          read(stage, std::integral_constant<int, u - kParts>{});
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // (a load between two products, not all of them before)
+        auto between = [&](auto kc) __attribute__((always_inline)) {
+          constexpr int slots = kAhead * TN, slot = (t - (kParts - kAhead)) * TN + decltype(kc)::value;
+          if constexpr (slot >= 0) {
+            constexpr int from = slot * (NF + 1) / slots, to = (slot + 1) * (NF + 1) / slots;
+            wave::static_for<to - from>([&](auto i) __attribute__((always_inline)) {
+              issue_one(mask, std::integral_constant<int, from + decltype(i)::value>{});
+            });
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        };
         if constexpr (sizeof(T) == 4)
-          wide_products<ATYPE>(fn[j], fm[j], sn, sm, acc);
+          wide_products<ATYPE>(fn[t / TM], fm[t % kHeld], sn, sm[t % TM], acc[t % TM], between);
         else
-          f8_products<ATYPE>(fn[j], fm[j], sn, sm, acc);
-      }
+          f8_products<ATYPE>(fn[t / TM], fm[t % kHeld], sn, sm[t % TM], acc[t % TM], between);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      issued(mask);
     }
-    auto first = [&]() __attribute__((always_inline)) {
-      wait_loads<0>();
-      landed = S - 1;
-    };
-    if constexpr (KIND == kWgrad) first();
-    if (at.m0 + G::BM <= P.M && at.n0 + G::BN <= P.N)
-      epilogue<T, KIND, true>(P, at.m0 + wm, at.n0 + wn, at.split, acc, first);
-    else
-      epilogue<T, KIND, false>(P, at.m0 + wm, at.n0 + wn, at.split, acc, first);
+    // The next tile's first step has landed (the tile's last step waited for it); the stage of this tile's last step
+    // is free for the sums.  Its loads are the next tile's second step's, behind the epilogue.
+    f8_epilogue<T, KIND>(P, at.m0 + G::BM <= P.M && at.n0 + G::BN <= P.N, at.m0 + wm, at.n0 + wn, at.split, acc,
+                         lds + (stage ^ (uint32_t)G::kStage) + G::kMine * wave);
+    step_barrier();
+    issue();
   }
   wait_loads<0>();  // nothing is on its way to LDS when the workgroup ends
 }
@@ -234,13 +401,13 @@ hipError_t launch_f8_shape(const F8Plan& pl, hipStream_t stream) {
     hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, G::kLds);
     if (e != hipSuccess) return e;
     int per_cu = 0;
-    e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, f, kMmThreads, G::kLds);
+    e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, f, G::kThreads, G::kLds);
     if (e != hipSuccess) return e;
     resident.store(per_cu > 0 ? per_cu : 1);
     allowed.store(1, std::memory_order_release);
   }
   const int most = 256 * resident.load(), blocks = (pl.p.mm.nblocks + 7) / 8 * 8;
-  hipLaunchKernelGGL((f8mm<T, KIND, SHAPE, ATYPE>), dim3((unsigned)(blocks < most ? blocks : most)), dim3(kMmThreads),
+  hipLaunchKernelGGL((f8mm<T, KIND, SHAPE, ATYPE>), dim3((unsigned)(blocks < most ? blocks : most)), dim3(G::kThreads),
                      G::kLds, stream, pl.p);
   return hipGetLastError();
 }
@@ -255,6 +422,9 @@ template <typename T, int KIND>
 hipError_t launch_f8_kind(const F8Plan& pl, hipStream_t stream) {
   switch (pl.shape) {
     case kF8_128x128: return launch_f8_type<T, KIND, kF8_128x128>(pl, stream);
+    case kF8_256x256:
+      if constexpr (sizeof(T) == 2) return launch_f8_type<T, KIND, kF8_256x256>(pl, stream);
+      return hipErrorInvalidValue;  // (no plan has it)
     case kF8_64x64: return launch_f8_type<T, KIND, kF8_64x64>(pl, stream);
     default: return hipErrorInvalidValue;
   }

@@ -159,28 +159,60 @@ hipError_t launch_f8_pack(Dtype dt, const F8PackParams& p, hipStream_t stream) {
   return p.type == kE4M3 ? launch_pack<uint16_t, kE4M3>(p, stream) : launch_pack<uint16_t, kE5M2>(p, stream);
 }
 
-F8Plan plan_f8(int kind, int M, int N, int K) {
+namespace {
+
+// Times in us, fitted to 70 products of 16 .. 60000 rows and 16 .. 8192 features and 24 weight gradients, each in every
+// tile (the plans taken are within 10% of the best one measured): a workgroup's step of 128 k, alone on its CU
+// and per workgroup where several share it, and its first loads and epilogue, likewise per workgroup.
+struct F8Cost {
+  double alone, shared, ends;
+  int resident;
+};
+constexpr F8Cost kF8Costs[3][kF8ShapeCount] = {
+    {{0., 0., 0., 0}, {0.9, 0.88, 2.0, 2}, {0.4, 0.37, 0.6, 4}},            // float32 results
+    {{1.4, 1.98, 5.3, 1}, {0.52, 0.565, 1.7, 2}, {0.27, 0.225, 0.55, 4}},   // bfloat16
+    {{1.6, 1.98, 5.3, 1}, {0.68, 0.43, 1.7, 2}, {0.45, 0.19, 0.55, 4}}};    // bfloat16 weight gradients, whose rows are far apart
+
+double f8_time(const F8Cost& c, long long groups, long long steps) {
+  auto round = [&](long long per_cu) {
+    const double step = per_cu * c.shared > c.alone ? per_cu * c.shared : c.alone;
+    return steps * step + c.ends * per_cu;
+  };
+  const long long slots = 256ll * c.resident, rest = groups % slots;
+  return (double)(groups / slots) * round(c.resident) + (rest ? round(cdiv(rest, 256)) : 0.);
+}
+
+}  // namespace
+
+F8Plan plan_f8(int kind, int M, int N, int K, int esize) {
   F8Plan pl{};
   MmParams& p = pl.p.mm;
   p.M = M;
   p.N = N;
   p.K = (int)f8_ld(K);
   p.steps = f8_groups(K);
-  const long long big = cdiv(M, 128) * cdiv(N, 128);
-  pl.shape = big >= 256 ? kF8_128x128 : kF8_64x64;
-  const Shape& s = kF8Shapes[pl.shape];
-  p.tm = (int)cdiv(M, 32 * s.tm * s.wm);
-  p.tn = (int)cdiv(N, 32 * s.tn * s.wn);
-  long long pieces = 1;
-  if (kind == kWgrad) {
-    const long long tiles = (long long)p.tm * p.tn;
-    pieces = cdiv(512, tiles);
-    if (pieces > p.steps / 4) pieces = p.steps / 4;
-    if (pieces < 1) pieces = 1;
+  double best = -1.;
+  for (int s = esize == 4 ? 1 : 0; s < kF8ShapeCount; ++s) {
+    const Shape& sh = kF8Shapes[s];
+    const long long tm = cdiv(M, 32 * sh.tm * sh.wm), tn = cdiv(N, 32 * sh.tn * sh.wn);
+    for (long long pieces = 1; pieces <= p.steps; pieces += 1 + pieces / 4) {
+      const long long per = cdiv(p.steps, pieces), n = cdiv(p.steps, per);
+      // (the pieces' sum: a launch, and each piece's results through memory)
+      const double sum = n > 1 ? 3.5 + (double)n * M * N * 8 / 9.0e6 : 0.;
+      const double t = f8_time(kF8Costs[esize == 4 ? 0 : (kind == kWgrad ? 2 : 1)][s], tm * tn * n, per) + sum;
+      if (best < 0. || t < best) {
+        best = t;
+        pl.shape = s;
+        p.tm = (int)tm;
+        p.tn = (int)tn;
+        p.per = (int)per;
+        p.nsplit = (int)n;
+      }
+      if (kind != kWgrad) break;
+    }
   }
-  p.per = (int)cdiv(p.steps, pieces);
-  p.nsplit = (int)cdiv(p.steps, p.per);
   p.nblocks = p.tm * p.tn * p.nsplit;
+  pl.p.band = pl.shape == kF8_64x64 ? 8 : 4;  // (1, 4, 8, 16: 8192 x 8192 -> 8192 in 128 x 128 694, 605, 606, 622 us)
   return pl;
 }
 

@@ -207,7 +207,7 @@ PyObject* linear_bwd_weight(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 6 || !packed_of(a[0], a[1], a[4], dy) || !packed_of(a[2], a[3], a[4], x) || !goes_with(x, dy)) return none();
   const long dt = PyLong_AsLong(a[5]);
   at::Tensor dw = empty({dy.R, x.R}, *dy.q, stored((o1d_dtype_t)dt));
-  at::Tensor ws = space(p_bwd_weight_bytes(dy.K, x.R, dy.R), *dy.q);
+  at::Tensor ws = space(p_bwd_weight_bytes(dy.K, x.R, dy.R, (o1d_dtype_t)dt), *dy.q);
   const c10::DeviceGuard guard(dy.q->device());
   void* s = stream_of(*dy.q);
   const auto st = call([&] {

@@ -972,8 +972,8 @@ def f8_linear_bwd_input(dy: F8, wt: F8, pre: torch.Tensor | None = None, act: st
 
 
 @functools.lru_cache(maxsize=4096)
-def f8_linear_workspace_bytes(M: int, I: int, O: int) -> int:
-    return int(_lib.lib().o1d_scaled_linear_bwd_weight_workspace_bytes(M, I, O))
+def f8_linear_workspace_bytes(M: int, I: int, O: int, dtype: torch.dtype) -> int:
+    return int(_lib.lib().o1d_scaled_linear_bwd_weight_workspace_bytes(M, I, O, _DT[dtype]))
 
 
 def f8_linear_bwd_weight(dyt: F8, xt: F8, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
@@ -994,7 +994,7 @@ def f8_linear_bwd_weight(dyt: F8, xt: F8, dtype: torch.dtype = torch.bfloat16, o
     dw = torch.empty((O, I), dtype=dtype, device=dyt.q.device) if out is None else out
     if tuple(dw.shape) != (O, I) or dw.dtype is not dtype or dw.device != dyt.q.device or not dw.is_contiguous():
         raise ValueError(f"out must be a contiguous ({O}, {I}) tensor of {dtype} on {dyt.q.device}")
-    workspace, nbytes = _scratch(workspace, dyt.q, f8_linear_workspace_bytes(M, I, O))
+    workspace, nbytes = _scratch(workspace, dyt.q, f8_linear_workspace_bytes(M, I, O, dtype))
     _run("o1d_scaled_linear_bwd_weight", dyt.q, dyt.q.data_ptr(), dyt.e.data_ptr(), _F8_OF[dyt.q.dtype], xt.q.data_ptr(),
          xt.e.data_ptr(), dw.data_ptr(), M, I, O, _DT[dtype], workspace.data_ptr(), nbytes)
     return dw
