@@ -31,14 +31,15 @@ struct AdamHyper {
   float max_norm;
 };
 
-constexpr int kAdamMost = 96;  // tensors of a launch
+constexpr int kAdamMost = 112;  // tensors of a launch (what its arguments hold)
 // Tensors 0 .. count - 1 of a call; the call's last launch counts the step.
 hipError_t launch_adam(Dtype pdt, Dtype gdt, const AdamTensor* t, int count, const AdamState& s, const AdamHyper& h,
                        hipStream_t stream);
 
-constexpr int kNormBlocks = 1024;  // partial sums (float64) of a call
-// norm = sqrt(sum of squares over all gradients); part: kNormBlocks doubles
-hipError_t launch_grad_norm(Dtype gdt, const AdamTensor* t, int count, double* part, float* norm, hipStream_t stream);
+constexpr int kNormBlocks = 256;  // partial sums (float64) of a call
+// norm = sqrt(sum of squares over all gradients); part: kNormBlocks doubles; arrived: a device integer that is 0
+hipError_t launch_grad_norm(Dtype gdt, const AdamTensor* t, int count, double* part, int* arrived, float* norm,
+                            hipStream_t stream);
 
 }  // namespace rows
 }  // namespace o1d

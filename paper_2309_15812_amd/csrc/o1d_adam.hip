@@ -24,15 +24,21 @@ namespace o1d {
 namespace rows {
 namespace {
 
+constexpr int kAdamBlocks = 2048;  // eight of a CU, all there at once
 constexpr int kAdamThreads = 256, kAdamRun = 8, kAdamPiece = kAdamThreads * kAdamRun;
 
 struct AdamList {
-  AdamTensor t[kAdamMost];
-  int first[kAdamMost];  // piece of all
-  int count, pieces;
+  int first[kAdamMost];  // of all pieces
+  int at[kAdamMost];     // where its states start, in groups of 128
+  void* p[kAdamMost];
+  const void* g[kAdamMost];
+  long long n[kAdamMost];
+  int count, pieces, per;  // pieces of a workgroup, one behind the other
 };
+static_assert(sizeof(AdamList) + sizeof(AdamState) + sizeof(AdamHyper) + 4 <= 4096, "a kernel's arguments");
 
-// The tensor of a piece: the last that starts at or before it.
+// The tensor of a piece: the last that starts at or before it.  Arguments lie in host memory: a
+// workgroup searches them once (448 bytes in a row; 32 bytes apart the step took 1.6 times the time) and then goes on from there.
 __device__ __forceinline__ int tensor_of(const AdamList& L, int piece) {
   const int lane = threadIdx.x & 63;
   int n = 0;
@@ -73,8 +79,7 @@ __device__ __forceinline__ double power(double b, int t) {
 }
 
 // Eight e4m3 values times their scale, and back: the scale is the largest of 16 lanes' values / 448.
-__device__ __forceinline__ void from8(const uint8_t* p, float scale, float (&v)[kAdamRun]) {
-  const uint2 w = *reinterpret_cast<const uint2*>(p);
+__device__ __forceinline__ void from8(uint2 w, float scale, float (&v)[kAdamRun]) {
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int u = (int)(k ? w.y : w.x);
@@ -115,6 +120,49 @@ template <typename TP, typename TG, bool HELD8, bool MASTER>
 __global__ __launch_bounds__(kAdamThreads) void adam(AdamList L, AdamState S, AdamHyper H, int counts) {
 #pragma clang fp contract(off)
   __shared__ Coefs coefs;
+  int piece = blockIdx.x * L.per, k = tensor_of(L, piece);
+  const int end = min(L.pieces, piece + L.per);
+  struct Place {
+    TP* p;
+    const TG* g;
+    long long i, left, at;
+    bool in;
+  };
+  auto place = [&]() __attribute__((always_inline)) {
+    while (k + 1 < L.count && L.first[k + 1] <= piece) ++k;
+    Place q;
+    const long long n = L.n[k];
+    q.i = (long long)(piece - L.first[k]) * kAdamPiece + threadIdx.x * kAdamRun;
+    q.p = static_cast<TP*>(L.p[k]) + q.i;
+    q.g = static_cast<const TG*>(L.g[k]) + q.i;
+    q.left = n - q.i;
+    q.at = (long long)L.at[k] * kAdamGroup + q.i;
+    q.in = q.i < (n + kAdamGroup - 1) / kAdamGroup * kAdamGroup;  // (the same for 16 threads, a group)
+    return q;
+  };
+  float g[kAdamRun], w[kAdamRun], m[kAdamRun], v[kAdamRun];
+  uint2 m8, v8;
+  float ms, vs;
+  auto load = [&](const Place& q) __attribute__((always_inline)) {
+    if (!q.in) return;
+    load8(q.g, q.left, g);
+    if constexpr (MASTER)
+      load_run(S.master + q.at, w);
+    else
+      load8(static_cast<const TP*>(q.p), q.left, w);
+    if constexpr (HELD8) {
+      m8 = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(S.m) + q.at);
+      v8 = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(S.v) + q.at);
+      ms = S.ms[q.at / kAdamGroup];
+      vs = S.vs[q.at / kAdamGroup];
+    } else {
+      load_run(static_cast<const float*>(S.m) + q.at, m);
+      load_run(static_cast<const float*>(S.v) + q.at, v);
+    }
+  };
+  // (the first piece is on its way while one thread works out the step's factors)
+  Place q = place();
+  load(q);
   if (threadIdx.x == 0) {
     const int t = S.step[0] + 1;
     Coefs c;
@@ -134,46 +182,36 @@ __global__ __launch_bounds__(kAdamThreads) void adam(AdamList L, AdamState S, Ad
   __syncthreads();
   const Coefs c = coefs;
   if (c.go) {
-    for (int piece = blockIdx.x; piece < L.pieces; piece += gridDim.x) {
-      const int k = tensor_of(L, piece);
-      const AdamTensor& t = L.t[k];
-      const long long i = (long long)(piece - L.first[k]) * kAdamPiece + threadIdx.x * kAdamRun, left = t.n - i;
-      const long long padded = (t.n + kAdamGroup - 1) / kAdamGroup * kAdamGroup;
-      if (i >= padded) continue;
-      const long long at = t.at + i;
-      float g[kAdamRun], w[kAdamRun], m[kAdamRun], v[kAdamRun];
-      load8(static_cast<const TG*>(t.g) + i, left, g);
-      if constexpr (MASTER)
-        load_run(S.master + at, w);
-      else
-        load8(static_cast<const TP*>(t.p) + i, left, w);
-      if constexpr (HELD8) {
-        from8(static_cast<const uint8_t*>(S.m) + at, S.ms[at / kAdamGroup], m);
-        from8(static_cast<const uint8_t*>(S.v) + at, S.vs[at / kAdamGroup], v);
-      } else {
-        load_run(static_cast<const float*>(S.m) + at, m);
-        load_run(static_cast<const float*>(S.v) + at, v);
-      }
+    for (;;) {
+      if (q.in) {
+        if constexpr (HELD8) {
+          from8(m8, ms, m);
+          from8(v8, vs, v);
+        }
 #pragma unroll
-      for (int e = 0; e < kAdamRun; ++e) {
-        if (H.norm) g[e] *= c.factor;
-        if constexpr (HELD8) v[e] *= v[e];
-        m[e] = H.beta1 * m[e] + H.rest1 * g[e];
-        v[e] = H.beta2 * v[e] + H.rest2 * (g[e] * g[e]);
-        const float r = sqrtf(v[e]);
-        w[e] = w[e] * c.keep - c.lr * ((m[e] * c.c1) / (r * c.c2 + H.eps));
-        if constexpr (HELD8) v[e] = r;
-        if (e >= left) m[e] = v[e] = w[e] = 0.f;  // (behind the tensor's end the states are zeros)
+        for (int e = 0; e < kAdamRun; ++e) {
+          if (H.norm) g[e] *= c.factor;
+          if constexpr (HELD8) v[e] *= v[e];
+          m[e] = H.beta1 * m[e] + H.rest1 * g[e];
+          v[e] = H.beta2 * v[e] + H.rest2 * (g[e] * g[e]);
+          const float r = sqrtf(v[e]);
+          w[e] = w[e] * c.keep - c.lr * ((m[e] * c.c1) / (r * c.c2 + H.eps));
+          if constexpr (HELD8) v[e] = r;
+          if (e >= q.left) m[e] = v[e] = w[e] = 0.f;  // (behind the tensor's end the states are zeros)
+        }
+        store8(q.p, q.left, w);
+        if constexpr (MASTER) store_run(S.master + q.at, w);
+        if constexpr (HELD8) {
+          to8<false>(m, static_cast<uint8_t*>(S.m) + q.at, S.ms + q.at / kAdamGroup);
+          to8<true>(v, static_cast<uint8_t*>(S.v) + q.at, S.vs + q.at / kAdamGroup);
+        } else {
+          store_run(static_cast<float*>(S.m) + q.at, m);
+          store_run(static_cast<float*>(S.v) + q.at, v);
+        }
       }
-      store8(static_cast<TP*>(t.p) + i, left, w);
-      if constexpr (MASTER) store_run(S.master + at, w);
-      if constexpr (HELD8) {
-        to8<false>(m, static_cast<uint8_t*>(S.m) + at, S.ms + at / kAdamGroup);
-        to8<true>(v, static_cast<uint8_t*>(S.v) + at, S.vs + at / kAdamGroup);
-      } else {
-        store_run(static_cast<float*>(S.m) + at, m);
-        store_run(static_cast<float*>(S.v) + at, v);
-      }
+      if (++piece >= end) break;
+      q = place();
+      load(q);
     }
   }
   // The last workgroup to end counts the step: all others have read it.
@@ -187,10 +225,13 @@ __global__ __launch_bounds__(kAdamThreads) void adam(AdamList L, AdamState S, Ad
 
 // ---- the gradients' norm: squares are summed in 64 bits, so that none overflows
 
-constexpr int kNormThreads = 256;
+// (few and large workgroups: their arrivals at one address take turns; 47 MB in 1951 workgroups of 256 threads 38.8 us, in 255
+// of 1024 20.2)
+constexpr int kNormThreads = 1024, kNormSide = kNormThreads / kAdamThreads;  // pieces side by side
 
 __device__ __forceinline__ double block_sum64(double s) {
   __shared__ double red[kNormThreads / 64];
+  __syncthreads();  // (an earlier sum is read)
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) s += __shfl_xor(s, m, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
@@ -201,39 +242,66 @@ __device__ __forceinline__ double block_sum64(double s) {
   return s;
 }
 
+// A workgroup's sum is its own part; the last of a call's last launch to end adds all parts, in their order, and takes
+// the root.  (The parts pass between XCDs: they are written and read by accesses of the device's scope.)
 template <typename TG>
-__global__ __launch_bounds__(kNormThreads) void squares(AdamList L, double* part, int add) {
+__global__ __launch_bounds__(kNormThreads) void squares(AdamList L, double* part, int add, int ends, int parts, int* arrived,
+                                                        float* norm) {
+  __shared__ int last;
   double s = 0.;
-  for (int piece = blockIdx.x; piece < L.pieces; piece += gridDim.x) {
-    const int k = tensor_of(L, piece);
-    const AdamTensor& t = L.t[k];
-    const long long i = (long long)(piece - L.first[k]) * kAdamPiece + threadIdx.x * kAdamRun, left = t.n - i;
-    if (left <= 0) continue;
-    float g[kAdamRun];
-    load8(static_cast<const TG*>(t.g) + i, left, g);
+  const int end = min(L.pieces, ((int)blockIdx.x + 1) * L.per);
+  int piece = min((int)blockIdx.x * L.per + __builtin_amdgcn_readfirstlane(threadIdx.x / kAdamThreads), end - 1);
+  const bool any = piece == (int)blockIdx.x * L.per + (int)(threadIdx.x / kAdamThreads);
+  int t = tensor_of(L, piece);
+  constexpr int B = 2;  // pieces at a time
+  for (; any && piece < end; piece += B * kNormSide) {
+    float g[B][kAdamRun];
 #pragma unroll
-    for (int e = 0; e < kAdamRun; ++e) s = fma((double)g[e], (double)g[e], s);
+    for (int k = 0; k < B; ++k) {
+      const int at = piece + k * kNormSide;
+      while (t + 1 < L.count && L.first[t + 1] <= min(at, end - 1)) ++t;
+      const long long i = (long long)(at - L.first[t]) * kAdamPiece + threadIdx.x % kAdamThreads * kAdamRun;
+      const long long left = at < end ? L.n[t] - i : 0;
+      load8(static_cast<const TG*>(L.g[t]) + (left > 0 ? i : 0), left, g[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < B; ++k)
+#pragma unroll
+      for (int e = 0; e < kAdamRun; ++e) s = fma((double)g[k][e], (double)g[k][e], s);
   }
   s = block_sum64(s);
-  if (threadIdx.x == 0) part[blockIdx.x] = add ? part[blockIdx.x] + s : s;
-}
-
-__global__ __launch_bounds__(kNormThreads) void norm_of(const double* part, int parts, float* norm) {
-  double s = 0.;
-  for (int i = threadIdx.x; i < parts; i += kNormThreads) s += part[i];
+  if (threadIdx.x == 0) {
+    if (add) s += part[blockIdx.x];  // (of the launch before)
+    atomicExch(reinterpret_cast<unsigned long long*>(part + blockIdx.x), __builtin_bit_cast(unsigned long long, s));
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the part is there before its arrival is)
+    last = ends && atomicAdd(arrived, 1) == (int)gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  s = 0.;
+  for (int i = threadIdx.x; i < parts; i += kNormThreads)
+    s += __hip_atomic_load(part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   s = block_sum64(s);
-  if (threadIdx.x == 0) *norm = (float)sqrt(s);
+  if (threadIdx.x == 0) {
+    *norm = (float)sqrt(s);
+    *arrived = 0;
+  }
 }
 
 // Calls f with each launch's list; `last`: the call's last.
 template <typename F>
 hipError_t with_lists(const AdamTensor* t, int count, F&& f) {
   for (int from = 0; from < count;) {
-    AdamList L{};
-    while (from < count && L.count < kAdamMost) {
-      L.t[L.count] = t[from];
-      L.first[L.count++] = L.pieces;
-      L.pieces += (int)cdiv(t[from++].n, kAdamPiece);
+    AdamList L;
+    L.count = L.pieces = 0;
+    for (; from < count && L.count < kAdamMost; ++from, ++L.count) {
+      const int k = L.count;
+      L.first[k] = L.pieces;
+      L.at[k] = (int)(t[from].at / kAdamGroup);
+      L.p[k] = t[from].p;
+      L.g[k] = t[from].g;
+      L.n[k] = t[from].n;
+      L.pieces += (int)cdiv(t[from].n, kAdamPiece);
     }
     f(L, from == count);
     const hipError_t e = hipGetLastError();
@@ -244,8 +312,9 @@ hipError_t with_lists(const AdamTensor* t, int count, F&& f) {
 
 template <typename TP, typename TG>
 hipError_t adam_t(const AdamTensor* t, int count, const AdamState& s, const AdamHyper& h, hipStream_t stream) {
-  return with_lists(t, count, [&](const AdamList& L, bool last) {
-    const dim3 grid((unsigned)(L.pieces < 4096 ? L.pieces : 4096)), threads(kAdamThreads);
+  return with_lists(t, count, [&](AdamList& L, bool last) {
+    L.per = (int)cdiv(L.pieces, kAdamBlocks);
+    const dim3 grid((unsigned)cdiv(L.pieces, L.per)), threads(kAdamThreads);
     if (s.bits == 8) {
       if (s.master)
         hipLaunchKernelGGL((adam<TP, TG, true, true>), grid, threads, 0, stream, L, s, h, (int)last);
@@ -270,21 +339,22 @@ hipError_t launch_adam(Dtype pdt, Dtype gdt, const AdamTensor* t, int count, con
                            : adam_t<uint16_t, uint16_t>(t, count, s, h, stream);
 }
 
-hipError_t launch_grad_norm(Dtype gdt, const AdamTensor* t, int count, double* part, float* norm, hipStream_t stream) {
+hipError_t launch_grad_norm(Dtype gdt, const AdamTensor* t, int count, double* part, int* arrived, float* norm,
+                            hipStream_t stream) {
+  // (a later list adds to the first list's parts)
   int parts = 0;
-  const hipError_t e = with_lists(t, count, [&](const AdamList& L, bool) {
-    // (a later list adds to the first parts; the first list's count is the largest that is read)
-    const int blocks = parts ? (L.pieces < parts ? L.pieces : parts) : (L.pieces < kNormBlocks ? L.pieces : kNormBlocks);
-    if (gdt == Dtype::F32)
-      hipLaunchKernelGGL((squares<float>), dim3((unsigned)blocks), dim3(kNormThreads), 0, stream, L, part, (int)(parts > 0));
-    else
-      hipLaunchKernelGGL((squares<uint16_t>), dim3((unsigned)blocks), dim3(kNormThreads), 0, stream, L, part,
-                         (int)(parts > 0));
+  return with_lists(t, count, [&](AdamList& L, bool last) {
+    const int most = parts ? parts : kNormBlocks, add = parts > 0;
+    L.per = (int)cdiv(L.pieces, most);
+    const int blocks = (int)cdiv(L.pieces, L.per);
     if (!parts) parts = blocks;
+    if (gdt == Dtype::F32)
+      hipLaunchKernelGGL((squares<float>), dim3((unsigned)blocks), dim3(kNormThreads), 0, stream, L, part, add, (int)last,
+                         parts, arrived, norm);
+    else
+      hipLaunchKernelGGL((squares<uint16_t>), dim3((unsigned)blocks), dim3(kNormThreads), 0, stream, L, part, add, (int)last,
+                         parts, arrived, norm);
   });
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(norm_of, dim3(1), dim3(kNormThreads), 0, stream, part, parts, norm);
-  return hipGetLastError();
 }
 
 }  // namespace rows

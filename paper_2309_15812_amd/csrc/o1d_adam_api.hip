@@ -63,7 +63,7 @@ o1d_status_t o1d_adamw(const o1d_adamw_tensor_t* tensors, int count, o1d_dtype_t
       const o1d_adamw_tensor_t& t = tensors[i];
       if (t.n < 0 || t.at < 0) return fail(O1D_ERR_INVALID, "%s: tensor %d has a negative size or place", fn, i);
       if (t.n == 0) continue;
-      if (t.n > (1ll << 40) || t.at > (1ll << 40)) return fail(O1D_ERR_UNSUPPORTED, "%s: tensor %d exceeds 2^40 values", fn, i);
+      if (t.n > (1ll << 37) || t.at > (1ll << 37)) return fail(O1D_ERR_UNSUPPORTED, "%s: tensor %d exceeds 2^37 values", fn, i);
       if (t.at % rows::kAdamGroup)
         return fail(O1D_ERR_INVALID, "%s: tensor %d's states start at %lld, no multiple of %d", fn, i, t.at, rows::kAdamGroup);
       O1D_TRY(check_null(fn, {t.p, t.g}));
@@ -116,8 +116,9 @@ o1d_status_t o1d_adamw(const o1d_adamw_tensor_t* tensors, int count, o1d_dtype_t
   (void)hipGetLastError();
   hipStream_t s = static_cast<hipStream_t>(stream);
   const Dtype pdt = (Dtype)param_dtype, gdt = (Dtype)grad_dtype;
+  if (list.empty()) return clip ? hip_status(fn, o1d::launch_zero(Dtype::F32, norm, 1, s)) : ok();
   if (clip)
-    O1D_TRY(hip_status(fn, rows::launch_grad_norm(gdt, list.data(), (int)list.size(), static_cast<double*>(workspace), norm, s)));
+    O1D_TRY(hip_status(fn, rows::launch_grad_norm(gdt, list.data(), (int)list.size(), static_cast<double*>(workspace), S.step + 1, norm, s)));
   const rows::AdamState st{S.m, S.v, S.m_scale, S.v_scale, S.master, S.step, S.bits};
   rows::AdamHyper h{};
   h.lr = (float)H.lr;

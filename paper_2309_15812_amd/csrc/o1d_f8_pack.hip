@@ -16,8 +16,8 @@ namespace rows {
 namespace {
 
 constexpr int kPackThreads = 256;
-template <typename T>
-constexpr int kPackPitch = kF8Group + 4 / (int)sizeof(T);  // of the tile's rows: a word more than they hold
+template <typename T, int COLS>
+constexpr int kPackPitch = COLS + 4 / (int)sizeof(T);  // of the tile's rows: a word more than they hold
 
 template <int TYPE>
 __device__ __forceinline__ int exponent_of(uint32_t amax) {
@@ -56,99 +56,174 @@ __device__ __forceinline__ uint32_t max16(uint32_t m) {
   return max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x140, 0xF, 0xF, true));  // row_mirror
 }
 
-// A workgroup takes 128 rows x 128 columns.  16 lanes hold a row's group, eight
-// columns each, which is packed by rows from there; the tile then lies in LDS, where
-// two columns x 32 rows go to a lane, and four waves hold a column's group.
+// Eight columns of a row from column c on, as they are in memory; zeros past the row's end.
+template <typename T>
+struct PackRun {
+  uint32_t w[2 * sizeof(T)];
+  __device__ __forceinline__ void load(const T* row, int c, int C) {
+    if (c + 8 <= C) {
+      __builtin_memcpy(w, row + c, sizeof(w));
+    } else {
+      T t[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = c + e < C ? row[c + e] : T(0);
+      __builtin_memcpy(w, t, sizeof(w));
+    }
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    T t[8];
+    __builtin_memcpy(t, w, sizeof(t));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = to_f32(t[e]);
+  }
+};
+
+// Sixteen lanes' eight columns each of a row: the group's exponent, and this lane's values.
+template <int TYPE>
+__device__ __forceinline__ int pack_group(const float (&v)[8], uint2& q) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = max(m, size_of(v[e]));
+  const int e = exponent_of<TYPE>(max16(m));
+  q = make_uint2(four8<TYPE>(v[0], v[1], v[2], v[3], e), four8<TYPE>(v[4], v[5], v[6], v[7], e));
+  return e;
+}
+
+// By rows alone: 64 rows of a group of columns in a workgroup, four in a row of 16 lanes, all loads before the
+// first group is made.  8192 x 8192 bfloat16: see launch_pack.
+constexpr int kRowsAtOnce = 4, kRowsPerGroup = kPackThreads / 16 * kRowsAtOnce;
+
 template <typename T, int TYPE>
+__global__ __launch_bounds__(kPackThreads) void f8_pack_rows(F8PackParams P) {
+  const int lane16 = threadIdx.x & 15, c = blockIdx.y * kF8Group + 8 * lane16;
+  const long long ldq = (P.C + kF8Group - 1) / kF8Group * (long long)kF8Group, lem = (P.M + 15) / 16 * 16;
+  const int r0 = blockIdx.x * kRowsPerGroup + (int)(threadIdx.x >> 4);
+  PackRun<T> run[kRowsAtOnce];
+#pragma unroll
+  for (int i = 0; i < kRowsAtOnce; ++i)
+    run[i].load(static_cast<const T*>(P.x) + (long long)min(r0 + 16 * i, P.M - 1) * P.ldx, c, P.C);
+#pragma unroll
+  for (int i = 0; i < kRowsAtOnce; ++i) {
+    const int r = r0 + 16 * i;
+    float v[8];
+    run[i].values(v);
+    uint2 q;
+    const int e = pack_group<TYPE>(v, q);
+    if (r < P.M) *reinterpret_cast<uint2*>(P.q + (long long)r * ldq + c) = q;
+    if (lane16 == 0 && r < lem) P.e[(long long)blockIdx.y * lem + r] = r < P.M ? (uint8_t)(e + 127) : 127;
+  }
+}
+
+// Transposed, and by rows too where COLS is 128: a workgroup takes 128 rows x COLS columns.  COLS / 8 lanes hold a
+// row's columns, which are packed by rows from there; the tile then lies in LDS, where two columns of some rows
+// go to a lane, and the lanes' largest values are joined there.  (Of 64 columns alone, twice the workgroups:
+// 50176 x 192 bfloat16: see launch_pack.)
+template <typename T, int TYPE, int COLS>
 __global__ __launch_bounds__(kPackThreads) void f8_pack(F8PackParams P) {
-  __shared__ uint32_t most[4][kF8Group];
-  __shared__ float sums[16][kF8Group];
+  constexpr int kLanes = COLS / 8, kRows = kPackThreads / kLanes, kPasses = kF8Group / kRows;  // lanes of a row, rows at a time
+  constexpr int kPairs = COLS / 2, kStrips = kPackThreads / kPairs, kStrip = kF8Group / kStrips;  // a strip: a lane's rows
+  __shared__ uint32_t most[kStrips][COLS];
+  __shared__ float sums[kRows][COLS];
   __shared__ uint8_t rexp[kF8Group];
   extern __shared__ __align__(16) char lds[];
-  T(*tile)[kPackPitch<T>] = reinterpret_cast<T(*)[kPackPitch<T>]>(lds);
-  const int r0 = blockIdx.x * kF8Group, c0 = blockIdx.y * kF8Group;
-  const int lane16 = threadIdx.x & 15, c = c0 + 8 * lane16;
-  const long long ldq = (P.C + kF8Group - 1) / kF8Group * (long long)kF8Group;
+  typedef T Row[kPackPitch<T, COLS>];
+  Row* const tile = reinterpret_cast<Row*>(lds);
+  const int r0 = blockIdx.x * kF8Group, c0 = blockIdx.y * COLS;
+  const int in_row = threadIdx.x % kLanes, c = c0 + 8 * in_row;
+  const long long ldq = (P.C + kF8Group - 1) / kF8Group * (long long)kF8Group, lem = (P.M + 15) / 16 * 16;
+  PackRun<T> run[kPasses];
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i)
+    run[i].load(static_cast<const T*>(P.x) + (long long)min(r0 + (int)(threadIdx.x / kLanes) + kRows * i, P.M - 1) * P.ldx, c, P.C);
   float sum[8] = {};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = (int)(threadIdx.x >> 4) + 16 * i, r = r0 + row;
-    float v[8] = {};
-    if (r < P.M && c < P.C) load_some(static_cast<const T*>(P.x) + (long long)r * P.ldx + c, P.C - c, v);
-    if (P.q) {
-      uint32_t m = 0;
+  for (int i = 0; i < kPasses; ++i) {
+    const int row = (int)(threadIdx.x / kLanes) + kRows * i, r = r0 + row;
+    float v[8];
+    run[i].values(v);
+    if (r >= P.M) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) m = max(m, size_of(v[e]));
-      const int e = exponent_of<TYPE>(max16(m));
-      if (r < P.M)
-        *reinterpret_cast<uint2*>(P.q + (long long)r * ldq + c) =
-            make_uint2(four8<TYPE>(v[0], v[1], v[2], v[3], e), four8<TYPE>(v[4], v[5], v[6], v[7], e));
-      if (lane16 == 0) rexp[row] = (uint8_t)(e + 127);
+      for (int e = 0; e < 8; ++e) v[e] = 0.f;
     }
-    if (P.qt) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        tile[row][8 * lane16 + e] = from_f32<T>(v[e]);
-        sum[e] += v[e];
+    if constexpr (COLS == kF8Group) {
+      if (P.q) {
+        uint2 q;
+        const int e = pack_group<TYPE>(v, q);
+        if (r < P.M) *reinterpret_cast<uint2*>(P.q + (long long)r * ldq + c) = q;
+        if (in_row == 0) rexp[row] = (uint8_t)(e + 127);
       }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      tile[row][8 * in_row + e] = from_f32<T>(v[e]);
+      sum[e] += v[e];
     }
   }
   if (P.part) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sums[threadIdx.x >> 4][8 * lane16 + e] = sum[e];
+    for (int e = 0; e < 8; ++e) sums[threadIdx.x / kLanes][8 * in_row + e] = sum[e];
   }
   __syncthreads();
-  const long long lem = (P.M + 15) / 16 * 16;
-  if (P.q && threadIdx.x < kF8Group && r0 + (int)threadIdx.x < lem)
+  if (COLS == kF8Group && P.q && threadIdx.x < kF8Group && r0 + (int)threadIdx.x < lem)
     P.e[(long long)blockIdx.y * lem + r0 + threadIdx.x] = r0 + (int)threadIdx.x < P.M ? rexp[threadIdx.x] : 127;
-  if (!P.qt) return;
-  if (P.part && threadIdx.x < kF8Group && c0 + (int)threadIdx.x < P.C) {
+  if (P.part && threadIdx.x < COLS && c0 + (int)threadIdx.x < P.C) {
     float s = 0.f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s += sums[k][threadIdx.x];
+    for (int k = 0; k < kRows; ++k) s += sums[k][threadIdx.x];
     P.part[(long long)blockIdx.x * P.C + c0 + threadIdx.x] = s;
   }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  float v[2][32];
+  const int pair = threadIdx.x % kPairs, strip = threadIdx.x / kPairs;
+  float v[2][kStrip];
   uint32_t m[2] = {0, 0};
 #pragma unroll
-  for (int k = 0; k < 32; ++k)
+  for (int k = 0; k < kStrip; ++k)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      v[j][k] = to_f32(tile[32 * wave + k][2 * lane + j]);
+      v[j][k] = to_f32(tile[kStrip * strip + k][2 * pair + j]);
       m[j] = max(m[j], size_of(v[j][k]));
     }
 #pragma unroll
-  for (int j = 0; j < 2; ++j) most[wave][2 * lane + j] = m[j];
+  for (int j = 0; j < 2; ++j) most[strip][2 * pair + j] = m[j];
   __syncthreads();
   const long long ldqt = (P.M + kF8Group - 1) / kF8Group * (long long)kF8Group, lec = (P.C + 15) / 16 * 16;
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const int col = 2 * lane + j;
-    const uint32_t a = max(max(most[0][col], most[1][col]), max(most[2][col], most[3][col]));
+    const int col = 2 * pair + j;
+    uint32_t a = most[0][col];
+#pragma unroll
+    for (int k = 1; k < kStrips; ++k) a = max(a, most[k][col]);
     const int e = exponent_of<TYPE>(a);
     if (c0 + col < P.C) {
-      uint32_t w[8];
+      uint32_t w[kStrip / 4];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = four8<TYPE>(v[j][4 * k], v[j][4 * k + 1], v[j][4 * k + 2], v[j][4 * k + 3], e);
-      __builtin_memcpy(__builtin_assume_aligned(P.qt + (long long)(c0 + col) * ldqt + r0 + 32 * wave, 16), w, 32);
+      for (int k = 0; k < kStrip / 4; ++k)
+        w[k] = four8<TYPE>(v[j][4 * k], v[j][4 * k + 1], v[j][4 * k + 2], v[j][4 * k + 3], e);
+      __builtin_memcpy(__builtin_assume_aligned(P.qt + (long long)(c0 + col) * ldqt + r0 + kStrip * strip, 16), w, kStrip);
     }
-    if (wave == 0 && c0 + col < lec) P.et[(long long)blockIdx.x * lec + c0 + col] = c0 + col < P.C ? (uint8_t)(e + 127) : 127;
+    if (strip == 0 && c0 + col < lec) P.et[(long long)blockIdx.x * lec + c0 + col] = c0 + col < P.C ? (uint8_t)(e + 127) : 127;
   }
 }
 
-template <typename T, int TYPE>
-hipError_t launch_pack(const F8PackParams& p, hipStream_t stream) {
-  constexpr int kLds = kF8Group * kPackPitch<T> * (int)sizeof(T);
+template <typename T, int TYPE, int COLS>
+hipError_t launch_pack_tiles(const F8PackParams& p, hipStream_t stream) {
+  constexpr int kLds = kF8Group * kPackPitch<T, COLS> * (int)sizeof(T);
   static std::atomic<int> allowed{0};
   if (!allowed.load(std::memory_order_acquire)) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f8_pack<T, TYPE>),
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f8_pack<T, TYPE, COLS>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     if (e != hipSuccess) return e;
     allowed.store(1, std::memory_order_release);
   }
-  hipLaunchKernelGGL((f8_pack<T, TYPE>), dim3((unsigned)f8_groups(p.M), (unsigned)f8_groups(p.C)), dim3(kPackThreads),
-                     p.qt ? kLds : 0, stream, p);
+  hipLaunchKernelGGL((f8_pack<T, TYPE, COLS>), dim3((unsigned)f8_groups(p.M), (unsigned)cdiv(p.C, COLS)),
+                     dim3(kPackThreads), kLds, stream, p);
+  return hipGetLastError();
+}
+
+template <typename T, int TYPE>
+hipError_t launch_pack(const F8PackParams& p, hipStream_t stream) {
+  if (p.qt) return p.q ? launch_pack_tiles<T, TYPE, 128>(p, stream) : launch_pack_tiles<T, TYPE, 64>(p, stream);
+  hipLaunchKernelGGL((f8_pack_rows<T, TYPE>), dim3((unsigned)cdiv(p.M, kRowsPerGroup), (unsigned)f8_groups(p.C)),
+                     dim3(kPackThreads), 0, stream, p);
   return hipGetLastError();
 }
 
