@@ -15,6 +15,9 @@
 // Memory bounds it: 28 bytes per value in float32, 16.1 (bfloat16 parameters and gradients, their
 // float32 values, 8-bit states).  A thread has eight values, 16 threads a scale; a workgroup
 // finds the tensor of each piece of 2048 values among those in its arguments.
+//
+// Measured, the parameters of 15 blocks (11.8 million values in 105 tensors): float32 67 us, 4.95 TB/s, and 20 us for the norm; in
+// bfloat16 with 8-bit states 46 us, 4.6 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "o1d_adam.h"

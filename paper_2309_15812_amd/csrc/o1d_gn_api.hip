@@ -28,6 +28,7 @@ rows::GnParams gn_params(const rows::GnPlan& pl, int N, int P, int C, int groups
   p.C = C;
   p.G = groups;
   p.D = C / groups;
+  p.over_d = p.D > 1 ? (uint32_t)(((1ull << 32) + p.D - 1) / p.D) : 0;
   p.act = (int)act;
   p.gb = pl.gb;
   p.bundles = pl.bundles;
