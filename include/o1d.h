@@ -325,7 +325,10 @@ size_t o1d_pack_scaled_workspace_bytes(int M, int C, int sums);
  * given type, the second is e4m3.
  *   fwd:        h = x W^T + b, y = act(h) + residual; pre (or NULL) = h.   x: M rows of I, W: O rows of I
  *   bwd_input:  dx = (dy W) act'(pre).                                     dy: M rows of O, W^T: I rows of O
- *   bwd_weight: dw = dy^T x ([O][I]).                                      dy^T: O rows of M, x^T: I rows of M */
+ *   bwd_weight: dw = dy^T x ([O][I]).                                      dy^T: O rows of M, x^T: I rows of M
+ * Results of float32 are of exact products, summed in float32 (values below 2^-126 keep fewer of their bits).  For results of
+ * bfloat16, products are summed eight at a time with 13 bits behind the power of two of the largest, and those sums in
+ * float32.  An exponent of 255 makes its values NaN. */
 o1d_status_t o1d_scaled_linear_fwd(const unsigned char* xq, const unsigned char* xe, o1d_scaled_t type,
                                    const unsigned char* wq, const unsigned char* we, const void* b, o1d_act_t act,
                                    const void* res, long long ldres, void* y, long long ldy, void* pre, long long ldpre, int M,
@@ -347,11 +350,13 @@ size_t o1d_scaled_linear_bwd_weight_workspace_bytes(int M, int I, int O, o1d_dty
  * Tensor i has n values p (param_dtype) and g (grad_dtype), and its part of the states starts at value `at`, a multiple
  * of 128; behind its end the states' values up to the next multiple of 128 are set to zeros.  state_bits 32: m and v
  * are float32.  8: m and the root of v are e4m3 (a positive root at least the type's smallest value), with a scale
- * m_scale, v_scale for each 128 values: the largest / 448.  master (or NULL): the parameters in float32, from which p is rounded;
+ * m_scale, v_scale for each 128 values: the largest / 448, at least 2^-126, or 0 for zeros.  master (or NULL): the parameters in float32, from which p is rounded;
  * without it p itself is read.  The states are 16-byte aligned.
  * step: two device integers, the steps taken (read and counted up) and 0.  lr_at: the learning rate in device memory, or NULL for
  * lr.  max_norm > 0 limits the norm of all gradients to it; the norm is then written to `norm`, and where it is not finite
- * nothing else changes.  max_norm 0: no limit, norm is not written and may be NULL. */
+ * nothing else changes.  max_norm 0: no limit, norm is not written and may be NULL.
+ * Without max_norm a value that is not finite makes its parameter and states NaN, 8-bit ones with the 128 values of its scale.  A
+ * call without values counts no step.  Tensors that are written overlap no other one; gradients may be shared. */
 typedef struct {
   void* p;
   const void* g;

@@ -97,7 +97,9 @@ __device__ __forceinline__ void to8(const float (&v)[kAdamRun], uint8_t* p, floa
 #pragma clang fp contract(off)
   uint32_t most = max8(amax_bits(v));
   most = max(most, (uint32_t)__builtin_amdgcn_mov_dpp((int)most, 0x140, 0xF, 0xF, true));
-  const float amax = __uint_as_float(most), inv = amax > 0.f ? 448.f / amax : 0.f;
+  // (below that, 448 / amax leaves float32 and a zero's product with it is NaN)
+  const float amax = __uint_as_float(most), top = amax < 448 * 0x1p-126f ? 448 * 0x1p-126f : amax;
+  const float inv = most ? 448.f / top : 0.f;
   float u[kAdamRun];
 #pragma unroll
   for (int e = 0; e < kAdamRun; ++e) {
@@ -111,7 +113,7 @@ __device__ __forceinline__ void to8(const float (&v)[kAdamRun], uint8_t* p, floa
     w[k] = __builtin_amdgcn_cvt_pk_fp8_f32(u[4 * k + 2], u[4 * k + 3], w[k], true);
   }
   *reinterpret_cast<uint2*>(p) = make_uint2((uint32_t)w[0], (uint32_t)w[1]);
-  if ((threadIdx.x & 15) == 0) *scale = amax * (1.f / 448.f);
+  if ((threadIdx.x & 15) == 0) *scale = most ? top * (1.f / 448.f) : 0.f;
 }
 
 struct Coefs {

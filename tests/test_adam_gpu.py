@@ -132,6 +132,26 @@ def test_a_norm_that_is_not_finite_changes_nothing():
             check_step(ps, gs, state, max_norm=1.0)
 
 
+def test_states_of_the_smallest_gradients():
+    # e4m3's steps of a scale of 2^-126: 2^-4 of a value, or 2^-10 of the scale; a root is at least 2^-9 of it
+    sizes = (1e-30, 1e-36, 1e-37, 1e-38, 1e-40)
+    ps, gs, state = make([(256,)] * len(sizes), F32, F32, 8, False)
+    for g, size in zip(gs, sizes):
+        g.copy_(torch.linspace(-1, 1, 256, device=DEV) * size)
+        g[::3] = 0
+    before = [p.clone() for p in ps]
+    ops.adamw(ps, gs, state, lr=1e-2, weight_decay=0.0)
+    m = state.m.float().double() * state.ms.double().repeat_interleave(128)
+    r = state.v.float().double() * state.vs.double().repeat_interleave(128)
+    for i, g in enumerate(gs):
+        at_ = slice(256 * i, 256 * i + 256)
+        want = 0.1 * g.double()
+        unit = state.ms[2 * i:2 * i + 2].double().repeat_interleave(128)
+        assert bool(((m[at_] - want).abs() <= torch.maximum(want.abs() * 2.0 ** -4, unit * 2.0 ** -10) * (1 + 1e-5) + 2.0 ** -148).all())
+        assert bool((state.ms[2 * i:2 * i + 2] >= 2.0 ** -126).all()) and not r[at_].any()  # (squares below 1e-60)
+        assert bool((ps[i] - before[i]).abs().max() <= 2.0 ** -20)  # eps is far above them
+
+
 def test_an_update_counts_where_a_small_one_would_be_lost():
     # bfloat16 parameters with their float32 values: steps below bfloat16's spacing add up
     ps, gs, state = make([(256,)], BF16, BF16, 8, True)
