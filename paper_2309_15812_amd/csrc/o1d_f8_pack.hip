@@ -122,8 +122,9 @@ template <typename T, int TYPE, int COLS>
 __global__ __launch_bounds__(kPackThreads) void f8_pack(F8PackParams P) {
   constexpr int kLanes = COLS / 8, kRows = kPackThreads / kLanes, kPasses = kF8Group / kRows;  // lanes of a row, rows at a time
   constexpr int kPairs = COLS / 2, kStrips = kPackThreads / kPairs, kStrip = kF8Group / kStrips;  // a strip: a lane's rows
+  constexpr int kSummed = 16;  // rows of a partial sum: sums have one order whatever COLS is
   __shared__ uint32_t most[kStrips][COLS];
-  __shared__ float sums[kRows][COLS];
+  __shared__ float sums[kF8Group / kSummed][COLS];
   __shared__ uint8_t rexp[kF8Group];
   extern __shared__ __align__(16) char lds[];
   typedef T Row[kPackPitch<T, COLS>];
@@ -135,7 +136,6 @@ __global__ __launch_bounds__(kPackThreads) void f8_pack(F8PackParams P) {
 #pragma unroll
   for (int i = 0; i < kPasses; ++i)
     run[i].load(static_cast<const T*>(P.x) + (long long)min(r0 + (int)(threadIdx.x / kLanes) + kRows * i, P.M - 1) * P.ldx, c, P.C);
-  float sum[8] = {};
 #pragma unroll
   for (int i = 0; i < kPasses; ++i) {
     const int row = (int)(threadIdx.x / kLanes) + kRows * i, r = r0 + row;
@@ -154,24 +154,11 @@ __global__ __launch_bounds__(kPackThreads) void f8_pack(F8PackParams P) {
       }
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      tile[row][8 * in_row + e] = from_f32<T>(v[e]);
-      sum[e] += v[e];
-    }
-  }
-  if (P.part) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sums[threadIdx.x / kLanes][8 * in_row + e] = sum[e];
+    for (int e = 0; e < 8; ++e) tile[row][8 * in_row + e] = from_f32<T>(v[e]);
   }
   __syncthreads();
   if (COLS == kF8Group && P.q && threadIdx.x < kF8Group && r0 + (int)threadIdx.x < lem)
     P.e[(long long)blockIdx.y * lem + r0 + threadIdx.x] = r0 + (int)threadIdx.x < P.M ? rexp[threadIdx.x] : 127;
-  if (P.part && threadIdx.x < COLS && c0 + (int)threadIdx.x < P.C) {
-    float s = 0.f;
-#pragma unroll
-    for (int k = 0; k < kRows; ++k) s += sums[k][threadIdx.x];
-    P.part[(long long)blockIdx.x * P.C + c0 + threadIdx.x] = s;
-  }
   const int pair = threadIdx.x % kPairs, strip = threadIdx.x / kPairs;
   float v[2][kStrip];
   uint32_t m[2] = {0, 0};
@@ -184,7 +171,24 @@ __global__ __launch_bounds__(kPackThreads) void f8_pack(F8PackParams P) {
     }
 #pragma unroll
   for (int j = 0; j < 2; ++j) most[strip][2 * pair + j] = m[j];
+  if (P.part) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int h = 0; h < kStrip / kSummed; ++h) {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < kSummed; ++k) s += v[j][kSummed * h + k];
+        sums[kStrip / kSummed * strip + h][2 * pair + j] = s;
+      }
+  }
   __syncthreads();
+  if (P.part && threadIdx.x < COLS && c0 + (int)threadIdx.x < P.C) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < kF8Group / kSummed; ++k) s += sums[k][threadIdx.x];
+    P.part[(long long)blockIdx.x * P.C + c0 + threadIdx.x] = s;
+  }
   const long long ldqt = (P.M + kF8Group - 1) / kF8Group * (long long)kF8Group, lec = (P.C + 15) / 16 * 16;
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
