@@ -12,7 +12,8 @@ run in hand-written HIP kernels behind the C ABI of include/o1d.h.
     dw = ops.bwd_weight(x, dy, theta, K)
 
 `ops` also has what stands around the convolution in a channels-last block (layer norm, products with an epilogue, 8-bit
-checkpoints, each with its gradients), and `block` that block as a module.
+checkpoints, group norm, products of 8-bit operands, each with its gradients; AdamW over many tensors), `block` that block as a
+module, and `optim` the step as an optimizer.
 """
 
-__all__ = ["ops", "block", "synth", "build"]
+__all__ = ["ops", "block", "optim", "synth", "build"]
