@@ -54,7 +54,7 @@ CHECKED = ("o1d_strip_", "o1d_gen_", "o1d_plane_", "o1d_pw_", "o1d_walk_", "o1d_
 SCRATCH = {
     "2mmIfLi0ELi1ELb0EE": 8, "2mmIfLi1ELi1ELb0EE": 8, "2mmIfLi2ELi1ELb1EE": 12,  # float32, 64 x 64
     "2mmIfLi0ELi5ELb0EE": 8, "2mmIfLi1ELi5ELb0EE": 80, "2mmIfLi2ELi5ELb0EE": 80,  # float32, 128 x 192
-    "4f8mmItLi0ELi0E": 48, "4f8mmItLi1ELi0E": 28, "4f8mmItLi2ELi0E": 12,  # 8-bit operands, 256 x 256: in the epilogue
+    "4f8mmItLi0ELi0E": 48, "4f8mmItLi1ELi0E": 28,  # 8-bit operands, 256 x 256: in the epilogue
     "11ln_bwd_rowsItLi64ELi8ELb1EE": 20,  # layer norm's backward of 4096 bfloat16 features, from a checkpoint
 }
 REMARK = "-Rpass-analysis=kernel-resource-usage"

@@ -42,7 +42,8 @@ struct F8Plan {
   int shape, atype;
   F8MmParams p;
 };
-// kFwd or kDgrad (which differ in their epilogue), or kWgrad (pieces of k).
+// kFwd or kDgrad (which differ in their epilogue), or kWgrad (pieces of k; no tiles of 256 x 256, whose rows far apart it reads no
+// faster).
 F8Plan plan_f8(int kind, int M, int N, int K, int esize);
 
 #define O1D_F8_DECL(T)                                                   \

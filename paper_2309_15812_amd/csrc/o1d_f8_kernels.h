@@ -429,7 +429,7 @@ hipError_t launch_f8_kind(const F8Plan& pl, hipStream_t stream) {
   switch (pl.shape) {
     case kF8_128x128: return launch_f8_type<T, KIND, kF8_128x128>(pl, stream);
     case kF8_256x256:
-      if constexpr (sizeof(T) == 2) return launch_f8_type<T, KIND, kF8_256x256>(pl, stream);
+      if constexpr (sizeof(T) == 2 && KIND != kWgrad) return launch_f8_type<T, KIND, kF8_256x256>(pl, stream);
       return hipErrorInvalidValue;  // (no plan has it)
     case kF8_64x64: return launch_f8_type<T, KIND, kF8_64x64>(pl, stream);
     default: return hipErrorInvalidValue;

@@ -250,7 +250,7 @@ struct F8Cost {
 constexpr F8Cost kF8Costs[3][kF8ShapeCount] = {
     {{0., 0., 0., 0}, {0.9, 0.88, 2.0, 2}, {0.4, 0.37, 0.6, 4}},            // float32 results
     {{1.4, 1.98, 5.3, 1}, {0.52, 0.565, 1.7, 2}, {0.27, 0.225, 0.55, 4}},   // bfloat16
-    {{1.6, 1.98, 5.3, 1}, {0.68, 0.43, 1.7, 2}, {0.45, 0.19, 0.55, 4}}};    // bfloat16 weight gradients, whose rows are far apart
+    {{0., 0., 0., 0}, {0.68, 0.43, 1.7, 2}, {0.45, 0.19, 0.55, 4}}};    // bfloat16 weight gradients, whose rows are far apart
 
 double f8_time(const F8Cost& c, long long groups, long long steps) {
   auto round = [&](long long per_cu) {
@@ -271,7 +271,7 @@ F8Plan plan_f8(int kind, int M, int N, int K, int esize) {
   p.K = (int)f8_ld(K);
   p.steps = f8_groups(K);
   double best = -1.;
-  for (int s = esize == 4 ? 1 : 0; s < kF8ShapeCount; ++s) {
+  for (int s = esize == 4 || kind == kWgrad ? kF8_128x128 : kF8_256x256; s < kF8ShapeCount; ++s) {
     const Shape& sh = kF8Shapes[s];
     const long long tm = cdiv(M, 32 * sh.tm * sh.wm), tn = cdiv(N, 32 * sh.tn * sh.wn);
     for (long long pieces = 1; pieces <= p.steps; pieces += 1 + pieces / 4) {

@@ -652,7 +652,9 @@ bool with_gn(const GnPlan& pl, F&& f) {
   constexpr int kBig = gn_big(BACKWARD, ESIZE), kMost = gn_most_runs(BACKWARD, ESIZE);
   auto runs = [&](auto threads) {
     switch (pl.runs) {
-      case 2: f(threads, integral_constant<int, 2>{}); return true;
+      case 2:  // (two runs of 512 threads are at most five of 256, which the plan prefers)
+        if constexpr (decltype(threads)::value != 512) { f(threads, integral_constant<int, 2>{}); return true; }
+        return false;
       case 4: f(threads, integral_constant<int, 4>{}); return true;
       case 6: f(threads, integral_constant<int, 6>{}); return true;
       case 8: if constexpr (kMost >= 8) { f(threads, integral_constant<int, 8>{}); return true; } return false;

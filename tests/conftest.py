@@ -22,7 +22,7 @@ def _oracle_built():
 
 # Their calls name invented device addresses and rely on being refused: where a GPU is present, a lost check would launch a
 # kernel on those.
-HOST_ONLY = {"test_abi_host.py", "test_rows_host.py"}
+HOST_ONLY = {"test_abi_host.py", "test_rows_host.py", "test_train_host.py"}
 
 
 def pytest_collection_modifyitems(config, items):

@@ -152,6 +152,12 @@ def test_states_of_the_smallest_gradients():
         assert bool((ps[i] - before[i]).abs().max() <= 2.0 ** -20)  # eps is far above them
 
 
+def test_tensors_may_share_a_gradient():
+    for bits in (32, 8):
+        ps, gs, state = make([(300,), (300,)], F32, F32, bits, False)
+        check_step(ps, [gs[0], gs[0]], state, max_norm=1.0)
+
+
 def test_an_update_counts_where_a_small_one_would_be_lost():
     # bfloat16 parameters with their float32 values: steps below bfloat16's spacing add up
     ps, gs, state = make([(256,)], BF16, BF16, 8, True)
