@@ -35,8 +35,9 @@ struct F8MmParams {
   long long lea, leb;
   int band;  // rows of tiles that are taken together
 };
-enum F8ShapeId { kF8_256x256, kF8_128x128, kF8_64x64, kF8ShapeCount };
-constexpr Shape kF8Shapes[kF8ShapeCount] = {{2, 4, 4, 2}, {2, 2, 2, 2}, {2, 2, 1, 1}};
+enum F8ShapeId { kF8_256x256, kF8_128x128, kF8_64x64, kF8_32x32, kF8ShapeCount };
+constexpr Shape kF8Shapes[kF8ShapeCount] = {{2, 4, 4, 2}, {2, 2, 2, 2}, {2, 2, 1, 1}, {1, 1, 1, 1}};
+// (Tiles of 32 x 32 are of another kernel, whose waves each take steps of their own.)
 
 struct F8Plan {
   int shape, atype;

@@ -418,6 +418,126 @@ hipError_t launch_f8_shape(const F8Plan& pl, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Few tiles: 32 x 32 results in a workgroup, whose waves take steps of their own, one behind the other, straight from memory to
+// the fragments' registers, DEPTH steps ahead of the products; the waves' sums are joined in LDS.  No step waits for another wave's,
+// and four times the workgroups share them, at twice the reads of 64 x 64.  Measured with its launch, bfloat16 results, against
+// 64 x 64: 16 x 768 -> 1000 3.8 us against 4.8, 5 x 5671 -> 568 10.2 against 15.4, 512 x 2048 -> 512 6.6 against 7.6, but
+// 1000 x 768 -> 768 7.1 against 5.4; float32 results 3.9, 10.2 and 6.8 against 6.0, 21.9 and 10.3.  Sixteen waves of one step
+// each: 44 x 1418 -> 1884 5.5, in eight waves 6.4; four steps ahead 10.0 (more loads than the first products need).
+template <typename T, int KIND, int ATYPE, int WAVES, int DEPTH>
+__global__ __launch_bounds__(64 * WAVES) void f8mm_few(F8MmParams Q) {
+  const MmParams& P = Q.mm;
+  __shared__ __align__(16) float sums[WAVES][32 * 32];  // runs of four in an order of their row's own: no bank conflicts
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves = (int)blockDim.x / 64;
+  const int per_xcd = (P.nblocks + 7) / 8, id = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
+  if (id >= P.nblocks || (int)(blockIdx.x / 8) >= per_xcd) return;
+  const int m0 = id % P.tm * 32, n0 = id / P.tm * 32;
+  // a thread's run of eight results and what the epilogue reads for it
+  const int m = m0 + (int)threadIdx.x / 4, n = n0 + (int)threadIdx.x % 4 * 8;
+  const bool mine = threadIdx.x < 128 && m < P.M && n < P.N;
+  Ahead<T, KIND, false> ahead;
+  float bias[8] = {};
+  if (mine) {
+    if constexpr (KIND != kWgrad) ahead.load(P, m, n);
+    if (KIND == kFwd && P.bias) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bias[e] = n + e < P.N ? to_f32(static_cast<const T*>(P.bias)[n + e]) : 0.f;
+    }
+  }
+  // rows past the end are the last one's: their results are not stored
+  const int rm = min(m0 + (lane & 31), P.M - 1), rn = min(n0 + (lane & 31), P.N - 1);
+  const char* const a = static_cast<const char*>(P.a) + (long long)rm * P.lda + 32 * half;
+  const char* const b = static_cast<const char*>(P.b) + (long long)rn * P.ldb + 32 * half;
+  const uint8_t *const ea = Q.ea + rm, *const eb = Q.eb + rn;
+  u32x4 fm[DEPTH][2][2], fn[DEPTH][2][1][2];
+  uint32_t sm[DEPTH], sn[DEPTH][1];
+  auto load = [&](auto dc, int s) __attribute__((always_inline)) {
+    constexpr int d = decltype(dc)::value;
+    s = min(s, P.steps - 1);  // (no branch: loads are waited for one by one)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const long long at = (long long)s * kF8Group + 64 * h + 16 * j;
+        fm[d][h][j] = *reinterpret_cast<const u32x4*>(a + at);
+        fn[d][h][0][j] = *reinterpret_cast<const u32x4*>(b + at);
+      }
+    sm[d] = ea[s * Q.lea];
+    sn[d][0] = eb[s * Q.leb];
+  };
+  f32x16 acc[1];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[0][e] = 0.f;
+  wave::static_for<DEPTH>([&](auto d) __attribute__((always_inline)) { load(d, wave + waves * decltype(d)::value); });
+  // (steps past the end are multiplied as zeros: a branch would take their loads with it, and wait there)
+  auto multiply = [&](auto dc, int s) __attribute__((always_inline)) {
+    constexpr int d = decltype(dc)::value;
+    const uint32_t in = s < P.steps ? ~0u : 0u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        fm[d][h][j] &= in;
+        fn[d][h][0][j] &= in;
+      }
+      auto nothing = [](auto) {};
+      if constexpr (sizeof(T) == 4)
+        wide_products<ATYPE>(fn[d][h], fm[d][h], sn[d], sm[d], acc, nothing);
+      else
+        f8_products<ATYPE>(fn[d][h], fm[d][h], sn[d], sm[d], acc, nothing);
+    }
+  };
+  int s0 = wave;
+  for (; s0 + waves * DEPTH < P.steps; s0 += waves * DEPTH)
+    wave::static_for<DEPTH>([&](auto dc) __attribute__((always_inline)) {
+      const int s = s0 + waves * decltype(dc)::value;
+      multiply(dc, s);
+      load(dc, s + waves * DEPTH);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  wave::static_for<DEPTH>([&](auto dc) __attribute__((always_inline)) { multiply(dc, s0 + waves * decltype(dc)::value); });
+  float* const to = &sums[wave][(lane & 31) * 32];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const float v[4] = {acc[0][4 * g], acc[0][4 * g + 1], acc[0][4 * g + 2], acc[0][4 * g + 3]};
+    __builtin_memcpy(__builtin_assume_aligned(to + 4 * ((2 * g + half) ^ (lane & 7)), 16), v, 16);
+  }
+  __syncthreads();
+  if (!mine) return;
+  float v[8] = {};
+  for (int w = 0; w < waves; ++w) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int row = (int)threadIdx.x / 4, run = (int)threadIdx.x % 4 * 2 + j;
+      float k[4];
+      __builtin_memcpy(k, __builtin_assume_aligned(&sums[w][row * 32 + 4 * (run ^ (row & 7))], 16), 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * j + e] += k[e];
+    }
+  }
+  if constexpr (KIND == kWgrad) {
+    put<T, false>(static_cast<T*>(P.out) + (long long)m * P.N + n, P.N - n, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += bias[e];
+    finish<T, KIND, false>(P, m, n, ahead, v);
+  }
+}
+
+template <typename T, int KIND, int ATYPE>
+hipError_t launch_f8_few(const F8Plan& pl, hipStream_t stream) {
+  const int steps = pl.p.mm.steps, waves = steps < 2 ? 2 : (steps <= 16 ? steps : 8);  // (two have the epilogue's threads)
+  const dim3 grid((unsigned)((pl.p.mm.nblocks + 7) / 8 * 8)), threads((unsigned)(64 * waves));
+  if (steps <= 8)
+    hipLaunchKernelGGL((f8mm_few<T, KIND, ATYPE, 8, 1>), grid, threads, 0, stream, pl.p);
+  else if (steps <= 16)
+    hipLaunchKernelGGL((f8mm_few<T, KIND, ATYPE, 16, 1>), grid, threads, 0, stream, pl.p);
+  else
+    hipLaunchKernelGGL((f8mm_few<T, KIND, ATYPE, 8, 2>), grid, threads, 0, stream, pl.p);
+  return hipGetLastError();
+}
+
 template <typename T, int KIND, int SHAPE>
 hipError_t launch_f8_type(const F8Plan& pl, hipStream_t stream) {
   return pl.atype == kE4M3 ? launch_f8_shape<T, KIND, SHAPE, kE4M3>(pl, stream)
@@ -432,6 +552,8 @@ hipError_t launch_f8_kind(const F8Plan& pl, hipStream_t stream) {
       if constexpr (sizeof(T) == 2 && KIND != kWgrad) return launch_f8_type<T, KIND, kF8_256x256>(pl, stream);
       return hipErrorInvalidValue;  // (no plan has it)
     case kF8_64x64: return launch_f8_type<T, KIND, kF8_64x64>(pl, stream);
+    case kF8_32x32:
+      return pl.atype == kE4M3 ? launch_f8_few<T, KIND, kE4M3>(pl, stream) : launch_f8_few<T, KIND, kE5M2>(pl, stream);
     default: return hipErrorInvalidValue;
   }
 }

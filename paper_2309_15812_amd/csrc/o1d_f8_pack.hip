@@ -247,7 +247,7 @@ struct F8Cost {
   double alone, shared, ends;
   int resident;
 };
-constexpr F8Cost kF8Costs[3][kF8ShapeCount] = {
+constexpr F8Cost kF8Costs[3][kF8_32x32] = {
     {{0., 0., 0., 0}, {0.9, 0.88, 2.0, 2}, {0.4, 0.37, 0.6, 4}},            // float32 results
     {{1.4, 1.98, 5.3, 1}, {0.52, 0.565, 1.7, 2}, {0.27, 0.225, 0.55, 4}},   // bfloat16
     {{0., 0., 0., 0}, {0.68, 0.43, 1.7, 2}, {0.45, 0.19, 0.55, 4}}};    // bfloat16 weight gradients, whose rows are far apart
@@ -259,6 +259,11 @@ double f8_time(const F8Cost& c, long long groups, long long steps) {
   };
   const long long slots = 256ll * c.resident, rest = groups % slots;
   return (double)(groups / slots) * round(c.resident) + (rest ? round(cdiv(rest, 256)) : 0.);
+}
+
+// Tiles of 32 x 32: a step's reads, of the rows that there are.
+double f8_few_time(int M, int N, long long tiles, int steps) {
+  return (double)cdiv(tiles, 256) * (0.28 + steps * 0.25 * ((M < 32 ? M : 32) + (N < 32 ? N : 32)) / 64.);
 }
 
 }  // namespace
@@ -278,7 +283,8 @@ F8Plan plan_f8(int kind, int M, int N, int K, int esize) {
       const long long per = cdiv(p.steps, pieces), n = cdiv(p.steps, per);
       // (the pieces' sum: a launch, and each piece's results through memory)
       const double sum = n > 1 ? 3.5 + (double)n * M * N * 8 / 9.0e6 : 0.;
-      const double t = f8_time(kF8Costs[esize == 4 ? 0 : (kind == kWgrad ? 2 : 1)][s], tm * tn * n, per) + sum;
+      const double t = s == kF8_32x32 ? f8_few_time(M, N, tm * tn, p.steps)
+                                      : f8_time(kF8Costs[esize == 4 ? 0 : (kind == kWgrad ? 2 : 1)][s], tm * tn * n, per) + sum;
       if (best < 0. || t < best) {
         best = t;
         pl.shape = s;
@@ -287,7 +293,7 @@ F8Plan plan_f8(int kind, int M, int N, int K, int esize) {
         p.per = (int)per;
         p.nsplit = (int)n;
       }
-      if (kind != kWgrad) break;
+      if (kind != kWgrad || s == kF8_32x32) break;
     }
   }
   p.nblocks = p.tm * p.tn * p.nsplit;

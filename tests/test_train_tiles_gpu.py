@@ -25,9 +25,10 @@ def test_group_norm(N, P, C, G, dt):
     gn.test_backward(N, P, C, G, dt)
 
 
-# (rows, summed features, features): tiles of 128 x 128 and, for bfloat16 results, 256 x 256, of 1, 2, 3 and more steps of 128,
-# whole ones and ones that end inside
-PRODUCTS = [(700, 16, 3000), (2048, 128, 2048), (1500, 300, 2000), (2048, 640, 2048), (3001, 100, 5003), (4096, 128, 4096), (4096, 384, 4096),
+# (rows, summed features, features): few tiles of 32 x 32 in each of their kernels, tiles of 64 x 64, 128 x 128 and, for
+# bfloat16 results, 256 x 256, of 1, 2, 3 and more steps of 128, whole ones and ones that end inside
+PRODUCTS = [(100, 1500, 40), (128, 1500, 128), (128, 2300, 128), (33, 2700, 65), (5, 5671, 568), (300, 16, 1000), (512, 16, 1024),
+            (300, 300, 1000), (1001, 768, 777), (640, 700, 1024), (700, 16, 3000), (2048, 128, 2048), (1500, 300, 2000), (2048, 640, 2048), (3001, 100, 5003), (4096, 128, 4096), (4096, 384, 4096),
             (3001, 1500, 5003), (8192, 250, 2048)]
 
 
@@ -58,10 +59,11 @@ def test_products(M, K, N, dt, fmt):
     near(ops.f8_linear_bwd_input(px, pw, dtype=dt), g, e + u(dt) * (g.abs() + e), "dx of none")
 
 
-# (rows, summed, features): both tiles in one piece and in several
+# (rows, summed, features): the tiles, in one piece and in several
 @pytest.mark.parametrize("dt", DTYPES)
 @pytest.mark.parametrize("O,M,I", [(3001, 100, 5003), (2048, 128, 2048), (700, 4100, 1500), (129, 20000, 512), (512, 9000, 1024), (128, 1500, 128),
-                                   (1344, 292, 181), (331, 18238, 458)])
+                                   (1344, 292, 181), (331, 18238, 458), (300, 16, 1000), (512, 16, 1024), (1, 9000, 16), (128, 2300, 128),
+                                   (128, 2300, 256), (130, 1500, 70), (400, 2200, 500), (1, 2300, 1)])
 def test_weight_gradients(O, M, I, dt):
     dyt, xt = ops.pack_f8(randn(O, M, seed=50), "e5m2"), ops.pack_f8(randn(I, M, seed=51))
     D, X = f8.value(dyt), f8.value(xt)
