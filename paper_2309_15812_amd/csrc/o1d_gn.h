@@ -16,6 +16,7 @@ struct GnParams {
   void* out;                // y or dx
   float *mean, *rstd;       // N x G: written by the forward, read by the backward
   float* part;              // partial results (below)
+  void *dw, *db;
   int gb, bundles;          // groups of a workgroup's channels, and how many such pieces
   int chunks, rows;         // not held: pieces of a sample's pixels, and their rows (the last may have fewer)
 };
@@ -30,20 +31,20 @@ struct GnPlan {
   int gb, bundles, chunks, rows;
 };
 constexpr int kGnMostChannels = 1024;  // of a group
-constexpr int kGnMostChunks = 512;     // of a sample (every workgroup joins what they leave)
+constexpr int kGnMostChunks = 512;     // of a sample
 // Threads of the larger workgroups and most runs of a held sample: in bfloat16 the backward unpacks its
 // registers twice and needs 256 of them per thread.
 constexpr int gn_big(bool backward, int esize) { return backward && esize == 2 ? 512 : 1024; }
 constexpr int gn_most_runs(bool backward, int esize) { return backward ? (esize == 2 ? 6 : 8) : 10; }
 GnPlan plan_gn(bool backward, int N, int P, int C, int G, int esize);
 
-// Floats of workspace: the forward's, not held: (mean, sum of squares) of each sample, chunk and
-// group.  The backward's: dw and db of each sample and chunk (2 C each), then, not held, the two sums
-// over each group.
+// Floats of workspace: the forward's, not held: (mean, sum of squares) of each sample, group and
+// chunk.  The backward's: dw and db of each sample and chunk (2 C each), then, not held, the two sums
+// over each group of each chunk, a group's chunks side by side, and of the sample.
 inline long long gn_parts(const GnPlan& pl, int N) { return (long long)N * (pl.held ? 1 : pl.chunks); }
 inline long long gn_fwd_floats(const GnPlan& pl, int N, int G) { return pl.held ? 0 : gn_parts(pl, N) * G * 2; }
 inline long long gn_bwd_floats(const GnPlan& pl, int N, int C, int G) {
-  return gn_parts(pl, N) * (2ll * C + (pl.held ? 0 : 2ll * G));
+  return gn_parts(pl, N) * (2ll * C + (pl.held ? 0 : 2ll * G)) + (pl.held ? 0 : 2ll * N * G);
 }
 
 hipError_t launch_gn_fwd_f32(const GnPlan& pl, const GnParams& p, hipStream_t stream);

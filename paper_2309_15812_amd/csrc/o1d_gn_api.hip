@@ -135,8 +135,9 @@ o1d_status_t o1d_gn_bwd(const void* x, long long ldx, const void* dy, long long 
   p.mean = const_cast<float*>(mean);
   p.rstd = const_cast<float*>(rstd);
   p.part = static_cast<float*>(workspace);
-  O1D_TRY(hip_status(fn, dtype == O1D_F32 ? rows::launch_gn_bwd_f32(pl, p, s) : rows::launch_gn_bwd_bf16(pl, p, s)));
-  return hip_status(fn, rows::launch_col_sum((Dtype)dtype, p.part, (int)rows::gn_parts(pl, N), 2ll * C, C, dw, db, s));
+  p.dw = dw;
+  p.db = db;
+  return hip_status(fn, dtype == O1D_F32 ? rows::launch_gn_bwd_f32(pl, p, s) : rows::launch_gn_bwd_bf16(pl, p, s));
 }
 
 }  // extern "C"

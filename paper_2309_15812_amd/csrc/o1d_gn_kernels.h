@@ -14,8 +14,8 @@
 // Measured: forward of 64 x 3136 x 96 bfloat16 in 32 groups 25 us, 3.1 TB/s: 28 vector instructions for each value (two passes
 // over registers, silu, bfloat16 both ways) keep the vector units 68% busy; with a select in place of each uniform branch,
 // sums by LDS and weights applied after rstd 28.6 us.  Backward of 64 x 784 x 192 float32 36 us, 3.2 TB/s, and 4 us for the sums;
-// 46 us with the library's exponential and quotient in the activation.  Backward of 3 x 12707 x 203 bfloat16 (rows at odd addresses)
-// in two passes 18 us each, held by the 2-byte loads of runs that straddle 16-byte pieces.
+// 46 us with the library's exponential and quotient in the activation.  Backward of 3 x 12707 x 203 bfloat16 in
+// two passes 18 and 15 us, and 4 between them.
 //
 // A thread has one 16-byte run of a row's channels in every row that it takes, so its weights
 // and statistics stay in registers.  A bundle's last run starts early enough to be whole;
@@ -358,58 +358,78 @@ __global__ __launch_bounds__(kGnThreads) void gn_stats(GnParams P) {
     v[e] = fmaf(d * d, count, sq[e]);
   }
   group_sums<T, kGnThreads>(P, at, v, L, L.group[1]);
-  float* part = P.part + ((long long)ch.sample * P.chunks + ch.chunk) * P.G * 2;
   for (int g = threadIdx.x; g < at.groups; g += kGnThreads) {
-    part[2 * (at.g0 + g)] = L.group[0][g] / n;
-    part[2 * (at.g0 + g) + 1] = L.group[1][g];
+    float* part = P.part + (((long long)ch.sample * P.G + at.g0 + g) * P.chunks + ch.chunk) * 2;
+    part[0] = L.group[0][g] / n;
+    part[1] = L.group[1][g];
   }
 }
 
-// The chunks' statistics joined by every workgroup, a wave for a group, and the chunk's results.
+// What the chunks of a sample's group left, 64 chunks to a lane's register.
+constexpr int kGnLeft = kGnMostChunks / 64;
+__device__ __forceinline__ void left_of(const float* of, int chunks, float (&a)[kGnLeft], float (&b)[kGnLeft]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int k = 0; k < kGnLeft; ++k) {
+    const int q = lane + 64 * k;
+    a[k] = q < chunks ? of[2 * q] : 0.f;
+    b[k] = q < chunks ? of[2 * q + 1] : 0.f;
+  }
+}
+
+// The chunks' statistics joined, a wave for a sample's group.  (A launch of its own: joined by every workgroup of gn_apply, a
+// wave group after group, 1 x 37872 x 144 in 48 groups backward took 20 us longer.)
+__global__ __launch_bounds__(kGnThreads) void gn_join(GnParams P) {
+  const long long id = (long long)blockIdx.x * (kGnThreads / 64) + (threadIdx.x >> 6);
+  if (id >= (long long)P.N * P.G) return;
+  const int lane = threadIdx.x & 63;
+  float m[kGnLeft], sq[kGnLeft], s = 0.f, all = 0.f;
+  left_of(P.part + id * P.chunks * 2, P.chunks, m, sq);
+  auto count = [&](int k) __attribute__((always_inline)) {  // (none behind the last chunk)
+    const int from = min(P.P, (lane + 64 * k) * P.rows);
+    return (float)(min(P.P - from, P.rows)) * (float)P.D;
+  };
+  const float total = (float)P.P * (float)P.D;
+#pragma unroll
+  for (int k = 0; k < kGnLeft; ++k) s = fmaf(count(k), m[k], s);
+  const float mean = wave_sum(s) / total;
+#pragma unroll
+  for (int k = 0; k < kGnLeft; ++k) {
+    const float d = m[k] - mean, n = count(k);
+    all += n > 0.f ? fmaf(d * d, n, sq[k]) : 0.f;
+  }
+  const float rstd = 1.f / sqrtf(wave_sum(all) / total + P.eps);
+  if (lane == 0) {
+    P.mean[id] = mean;
+    P.rstd[id] = rstd;
+  }
+}
+
+// The chunk's results.
 template <typename T>
 __global__ __launch_bounds__(kGnThreads) void gn_apply(GnParams P) {
   constexpr int V = kRun<T>, B = kGnBatch / 2;
-  __shared__ float mean_of[kGnMostChannels], rstd_of[kGnMostChannels];
   const GnChunk ch = chunk_of(P);
   GnAt<T, kGnThreads> at;
   at.place(P, ch.sample, ch.bundle);
-  const int lane = threadIdx.x & 63;
-  const float* part = P.part + (long long)ch.sample * P.chunks * P.G * 2;
-  const float total = (float)P.P * (float)P.D;
-  for (int g = threadIdx.x >> 6; g < at.groups; g += kGnThreads / 64) {
-    const float* of = part + (at.g0 + g) * 2;
-    auto count = [&](int q) __attribute__((always_inline)) { return (float)(min(P.P, (q + 1) * P.rows) - q * P.rows) * (float)P.D; };
-    float s = 0.f, sq = 0.f;
-    for (int q = lane; q < P.chunks; q += 64) s = fmaf(count(q), of[(long long)q * P.G * 2], s);
-    const float mean = wave_sum(s) / total;
-    for (int q = lane; q < P.chunks; q += 64) {
-      const float d = of[(long long)q * P.G * 2] - mean;
-      sq += fmaf(d * d, count(q), of[(long long)q * P.G * 2 + 1]);
-    }
-    const float rstd = 1.f / sqrtf(wave_sum(sq) / total + P.eps);
-    if (lane == 0) {
-      mean_of[g] = mean;
-      rstd_of[g] = rstd;
-      if (ch.chunk == 0) {
-        P.mean[(long long)ch.sample * P.G + at.g0 + g] = mean;
-        P.rstd[(long long)ch.sample * P.G + at.g0 + g] = rstd;
-      }
-    }
-  }
-  __syncthreads();
+  int r = ch.r0 + at.slot;
+  uint32_t raw[B][4];
+  auto load = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < B; ++k) at.load(row_of<T>(P.x, P, ch.sample, min(r + k * at.slots, ch.r1 - 1), P.ldx), raw[k]);
+  };
+  load();
   if (!at.active) return;
   float w[V], b[V], mean[V];
   at.vector(P.w, w);
   at.vector(P.b, b);
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    mean[e] = mean_of[at.group(P, e)];
-    w[e] *= rstd_of[at.group(P, e)];
+    const long long g = (long long)ch.sample * P.G + at.g0 + at.group(P, e);
+    mean[e] = P.mean[g];
+    w[e] *= P.rstd[g];
   }
-  for (int r = ch.r0 + at.slot; r < ch.r1; r += B * at.slots) {
-    uint32_t raw[B][4];
-#pragma unroll
-    for (int k = 0; k < B; ++k) at.load(row_of<T>(P.x, P, ch.sample, min(r + k * at.slots, ch.r1 - 1), P.ldx), raw[k]);
+  for (;;) {
 #pragma unroll
     for (int k = 0; k < B; ++k) {
       if (r + k * at.slots >= ch.r1) break;
@@ -420,6 +440,9 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply(GnParams P) {
       gn_values<sizeof(T) == 2>(v, P.act);
       at.store(const_cast<T*>(row_of<T>(P.out, P, ch.sample, r + k * at.slots, P.ldy)), v);
     }
+    r += B * at.slots;
+    if (r >= ch.r1) break;
+    load();
   }
 }
 
@@ -554,6 +577,9 @@ __global__ __launch_bounds__(kGnThreads) void gn_bwd_sums(GnParams P) {
   const GnChunk ch = chunk_of(P);
   GnAt<T, kGnThreads> at;
   at.place(P, ch.sample, ch.bundle);
+  GnRows<T, B> rows;
+  int r = ch.r0 + at.slot;
+  rows.load(P, at, ch, r);
   float w[V], b[V], mean[V], rstd[V], dw[V] = {}, db[V] = {};
   at.vector(P.w, w);
   at.vector(P.b, b);
@@ -563,9 +589,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_bwd_sums(GnParams P) {
     mean[e] = P.mean[g];
     rstd[e] = P.rstd[g];
   }
-  for (int r = ch.r0 + at.slot; r < ch.r1; r += B * at.slots) {
-    GnRows<T, B> rows;
-    rows.load(P, at, ch, r);
+  for (;;) {
 #pragma unroll
     for (int k = 0; k < B; ++k) {
       if (r + k * at.slots >= ch.r1) break;
@@ -579,41 +603,81 @@ __global__ __launch_bounds__(kGnThreads) void gn_bwd_sums(GnParams P) {
         db[e] += g[e];
       }
     }
+    r += B * at.slots;
+    if (r >= ch.r1) break;
+    rows.load(P, at, ch, r);
   }
   const long long piece = (long long)ch.sample * P.chunks + ch.chunk;
   gn_bwd_join<T, kGnThreads>(P, at, dw, db, L, P.part + piece * 2 * P.C);
-  float* part = P.part + (long long)P.N * P.chunks * 2 * P.C + piece * P.G * 2;
   for (int g = threadIdx.x; g < at.groups; g += kGnThreads) {
-    part[2 * (at.g0 + g)] = L.group[0][g];
-    part[2 * (at.g0 + g) + 1] = L.group[1][g];
+    float* part = P.part + (long long)P.N * P.chunks * 2 * P.C + (((long long)ch.sample * P.G + at.g0 + g) * P.chunks + ch.chunk) * 2;
+    part[0] = L.group[0][g];
+    part[1] = L.group[1][g];
+  }
+}
+
+// dw and db of all pieces, 32 columns x 32 slices of the pieces in a workgroup, each in order, and in the
+// workgroups after those the groups' sums, a wave for a sample's group.
+template <typename T>
+__global__ __launch_bounds__(1024) void gn_bwd_close(GnParams P) {
+  constexpr int kCols = 32, kSlices = 32, kBatch = 8;
+  __shared__ float red[kSlices][kCols + 1];
+  const int blocks = (2 * P.C + kCols - 1) / kCols;
+  if ((int)blockIdx.x >= blocks) {
+    const long long id = (long long)((int)blockIdx.x - blocks) * 16 + (threadIdx.x >> 6), groups = (long long)P.N * P.G;
+    if (id >= groups) return;
+    float* const of = P.part + (long long)P.N * P.chunks * 2 * P.C;
+    float g[kGnLeft], gx[kGnLeft], s = 0.f, sx = 0.f;
+    left_of(of + id * P.chunks * 2, P.chunks, g, gx);
+#pragma unroll
+    for (int k = 0; k < kGnLeft; ++k) {
+      s += g[k];
+      sx += gx[k];
+    }
+    s = wave_sum(s);
+    sx = wave_sum(sx);
+    const float inv = 1.f / ((float)P.P * (float)P.D);
+    if ((threadIdx.x & 63) == 0) {
+      float* const to = of + (groups * P.chunks + id) * 2;
+      to[0] = s * inv;
+      to[1] = sx * inv;
+    }
+    return;
+  }
+  const int col = threadIdx.x % kCols, slice = threadIdx.x / kCols, c = blockIdx.x * kCols + col, parts = P.N * P.chunks;
+  float s = 0.f;
+  if (c < 2 * P.C) {
+    for (int j0 = slice; j0 < parts; j0 += kSlices * kBatch) {
+      float v[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int j = j0 + u * kSlices;
+        v[u] = j < parts ? P.part[(long long)j * 2 * P.C + c] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) s += v[u];
+    }
+  }
+  red[slice][col] = s;
+  __syncthreads();
+  if (slice == 0 && c < 2 * P.C) {
+    float t = 0.f;
+#pragma unroll
+    for (int k = 0; k < kSlices; ++k) t += red[k][col];
+    static_cast<T*>(c < P.C ? P.dw : P.db)[c < P.C ? c : c - P.C] = from_f32<T>(t);
   }
 }
 
 template <typename T>
 __global__ __launch_bounds__(kGnThreads) void gn_bwd_apply(GnParams P) {
   constexpr int V = kRun<T>, B = kGnBatch / 2;
-  __shared__ float s_of[kGnMostChannels], sx_of[kGnMostChannels];
   const GnChunk ch = chunk_of(P);
   GnAt<T, kGnThreads> at;
   at.place(P, ch.sample, ch.bundle);
-  const int lane = threadIdx.x & 63;
-  const float inv = 1.f / ((float)P.P * (float)P.D);
-  const float* part = P.part + (long long)P.N * P.chunks * 2 * P.C + (long long)ch.sample * P.chunks * P.G * 2;
-  for (int g = threadIdx.x >> 6; g < at.groups; g += kGnThreads / 64) {
-    const float* of = part + (at.g0 + g) * 2;
-    float s = 0.f, sx = 0.f;
-    for (int q = lane; q < P.chunks; q += 64) {
-      s += of[(long long)q * P.G * 2];
-      sx += of[(long long)q * P.G * 2 + 1];
-    }
-    s = wave_sum(s);
-    sx = wave_sum(sx);
-    if (lane == 0) {
-      s_of[g] = s * inv;
-      sx_of[g] = sx * inv;
-    }
-  }
-  __syncthreads();
+  GnRows<T, B> rows;
+  int r = ch.r0 + at.slot;
+  rows.load(P, at, ch, r);
+  const float* const sums = P.part + ((long long)P.N * P.chunks * (P.C + P.G) + (long long)ch.sample * P.G + at.g0) * 2;
   if (!at.active) return;
   float w[V], b[V], mean[V], rstd[V], s[V], sx[V];
   at.vector(P.w, w);
@@ -623,12 +687,10 @@ __global__ __launch_bounds__(kGnThreads) void gn_bwd_apply(GnParams P) {
     const int i = at.group(P, e);
     mean[e] = P.mean[(long long)ch.sample * P.G + at.g0 + i];
     rstd[e] = P.rstd[(long long)ch.sample * P.G + at.g0 + i];
-    s[e] = s_of[i];
-    sx[e] = sx_of[i];
+    s[e] = sums[2 * i];
+    sx[e] = sums[2 * i + 1];
   }
-  for (int r = ch.r0 + at.slot; r < ch.r1; r += B * at.slots) {
-    GnRows<T, B> rows;
-    rows.load(P, at, ch, r);
+  for (;;) {
 #pragma unroll
     for (int k = 0; k < B; ++k) {
       if (r + k * at.slots >= ch.r1) break;
@@ -640,6 +702,9 @@ __global__ __launch_bounds__(kGnThreads) void gn_bwd_apply(GnParams P) {
       for (int e = 0; e < V; ++e) x[e] = rstd[e] * (fmaf(g[e], w[e], -s[e]) - x[e] * sx[e]);
       at.store(const_cast<T*>(row_of<T>(P.out, P, ch.sample, r + k * at.slots, P.ldy)), x);
     }
+    r += B * at.slots;
+    if (r >= ch.r1) break;
+    rows.load(P, at, ch, r);
   }
 }
 
@@ -680,7 +745,10 @@ hipError_t gn_fwd_t(const GnPlan& pl, const GnParams& p, hipStream_t stream) {
     return done ? hipGetLastError() : hipErrorInvalidValue;
   }
   hipLaunchKernelGGL((gn_stats<T>), dim3(gn_pieces(p)), dim3(kGnThreads), 0, stream, p);
-  const hipError_t e = hipGetLastError();
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(gn_join, dim3((unsigned)cdiv((long long)p.N * p.G, kGnThreads / 64)), dim3(kGnThreads), 0, stream, p);
+  e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((gn_apply<T>), dim3(gn_pieces(p)), dim3(kGnThreads), 0, stream, p);
   return hipGetLastError();
@@ -693,10 +761,14 @@ hipError_t gn_bwd_t(const GnPlan& pl, const GnParams& p, hipStream_t stream) {
       constexpr int TH = decltype(threads)::value, R = decltype(runs)::value;
       hipLaunchKernelGGL((gn_bwd_held<T, TH, R>), dim3(gn_units(p)), dim3(TH), 0, stream, p);
     });
-    return done ? hipGetLastError() : hipErrorInvalidValue;
+    const hipError_t e = done ? hipGetLastError() : hipErrorInvalidValue;
+    return e != hipSuccess ? e : launch_col_sum(sizeof(T) == 4 ? Dtype::F32 : Dtype::BF16, p.part, p.N, 2ll * p.C, p.C, p.dw, p.db, stream);
   }
   hipLaunchKernelGGL((gn_bwd_sums<T>), dim3(gn_pieces(p)), dim3(kGnThreads), 0, stream, p);
-  const hipError_t e = hipGetLastError();
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((gn_bwd_close<T>), dim3((unsigned)(cdiv(2ll * p.C, 32) + cdiv((long long)p.N * p.G, 16))), dim3(1024), 0, stream, p);
+  e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((gn_bwd_apply<T>), dim3(gn_pieces(p)), dim3(kGnThreads), 0, stream, p);
   return hipGetLastError();

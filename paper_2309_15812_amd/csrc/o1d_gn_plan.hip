@@ -41,10 +41,10 @@ GnPlan plan_gn(bool backward, int N, int P, int C, int G, int esize) {
   pl.gb = (int)cdiv(G, pl.bundles);
   pl.bundles = (int)cdiv(G, pl.gb);
   const int rows = 256 / (int)cdiv((long long)pl.gb * D, V);  // at a time
-  // (three or four of a CU, all there at once: backward of 3 x 12707 x 203 bfloat16 with 384, 768 and 1536 pieces 45, 39
-  // and 50 us)
-  long long chunks = cdiv(backward ? 768 : 1024, (long long)N * pl.bundles);
-  const long long least = cdiv(P, 4ll * (rows > 0 ? rows : 1));
+  // (three of a CU, all there at once: 3 x 12707 x 203 bfloat16 in 384, 768 and 1536 pieces forward 31, 28 and 33 us, backward
+  // 44, 38 and 46; at least two rows of a thread: 2 x 4880 x 6 backward with four 18 us, with two 16)
+  long long chunks = cdiv(768, (long long)N * pl.bundles);
+  const long long least = cdiv(P, 2ll * (rows > 0 ? rows : 1));
   if (chunks > least) chunks = least;
   if (chunks > kGnMostChunks) chunks = kGnMostChunks;
   if (chunks < 1) chunks = 1;
