@@ -22,11 +22,13 @@ GnPlan plan_gn(bool backward, int N, int P, int C, int G, int esize) {
       const long long rows = threads / run, need = cdiv(P, rows);
       const int runs = need <= 2 ? 2 : (int)cdiv(need, 2) * 2;
       if (runs > gn_most_runs(backward, esize)) continue;
-      // time: what a CU moves, at the rate it has, and the two reductions
+      // time in us: what a CU moves, at the rate that it has among the others, and the two reductions, which workgroups of 256
+      // threads on a CU share
       const double bytes = (double)P * CB * esize, piece = CB * esize;
-      const double groups = (double)N * real, rounds = (double)cdiv((long long)groups, 256);
-      const double per_cu = groups >= 256 ? 20e3 : 50e3;  // bytes per us
-      const double t = rounds * (bytes / per_cu * (piece < 64 ? 64 / piece : 1.) + (threads == 256 ? 1.5 : 3.));
+      const long long groups = (long long)N * real, rounds = cdiv(groups, 256);
+      const double per_cu = groups >= 256 ? 20e3 : (groups > 102 ? 5.12e6 / groups : 50e3);  // bytes per us
+      const double sums = threads == 256 ? 1.5 * cdiv(groups, backward ? 512 : 1024) : 3. * rounds;
+      const double t = rounds * (bytes / per_cu * (piece < 64 ? 64 / piece : 1.)) + sums + 0.05 * runs;
       if (cost >= 0. && t >= cost) continue;
       cost = t;
       best = {true, threads, runs, gb, real, 1, P};
