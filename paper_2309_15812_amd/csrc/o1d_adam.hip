@@ -16,8 +16,8 @@
 // float32 values, 8-bit states).  A thread has eight values, 16 threads a scale; a workgroup
 // finds the tensor of each piece of 2048 values among those in its arguments.
 //
-// Measured, the parameters of 15 blocks (11.8 million values in 105 tensors): float32 67 us, 4.95 TB/s, and 20 us for the norm; in
-// bfloat16 with 8-bit states 46 us, 4.6 TB/s.
+// Measured, the parameters of 15 blocks (11.8 million values in 105 tensors): float32 66 us, 5.1 TB/s, and 19 us for the norm; in
+// bfloat16 with 8-bit states 47 us, 4.6 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "o1d_adam.h"
@@ -40,15 +40,33 @@ struct AdamList {
 };
 static_assert(sizeof(AdamList) + sizeof(AdamState) + sizeof(AdamHyper) + 4 <= 4096, "a kernel's arguments");
 
-// The tensor of a piece: the last that starts at or before it.  Arguments lie in host memory: a
-// workgroup searches them once (448 bytes in a row; 32 bytes apart the step took 1.6 times the time) and then goes on from there.
-__device__ __forceinline__ int tensor_of(const AdamList& L, int piece) {
+// A list's tensors in LDS.  Arguments lie in host memory, a microsecond away: a workgroup reads all of them at once, whatever
+// their number, and not one that depends on another (searched there, a step of 7 tensors took 12.3 us, so 11.5).
+struct AdamTable {
+  int first[kAdamMost], at[kAdamMost];
+  void* p[kAdamMost];
+  const void* g[kAdamMost];
+  long long n[kAdamMost];
+};
+__device__ __forceinline__ void fill(const AdamList& L, AdamTable& T) {
+  const int i = threadIdx.x;
+  if (i < kAdamMost) {
+    T.first[i] = L.first[i];
+    T.at[i] = L.at[i];
+    T.p[i] = L.p[i];
+    T.g[i] = L.g[i];
+    T.n[i] = L.n[i];
+  }
+  __syncthreads();
+}
+// The tensor of a piece: the last that starts at or before it.
+__device__ __forceinline__ int tensor_of(const AdamTable& T, int count, int piece) {
   const int lane = threadIdx.x & 63;
   int n = 0;
 #pragma unroll
   for (int k = 0; k < (kAdamMost + 63) / 64; ++k) {
     const int i = lane + 64 * k;
-    n += __popcll(__ballot(i < L.count && L.first[i < L.count ? i : 0] <= piece));
+    n += __popcll(__ballot(i < count && T.first[min(i, kAdamMost - 1)] <= piece));
   }
   return __builtin_amdgcn_readfirstlane(n) - 1;
 }
@@ -125,7 +143,9 @@ template <typename TP, typename TG, bool HELD8, bool MASTER>
 __global__ __launch_bounds__(kAdamThreads) void adam(AdamList L, AdamState S, AdamHyper H, int counts) {
 #pragma clang fp contract(off)
   __shared__ Coefs coefs;
-  int piece = blockIdx.x * L.per, k = tensor_of(L, piece);
+  __shared__ AdamTable table;
+  fill(L, table);
+  int piece = blockIdx.x * L.per, k = tensor_of(table, L.count, piece);
   const int end = min(L.pieces, piece + L.per);
   struct Place {
     TP* p;
@@ -134,14 +154,14 @@ __global__ __launch_bounds__(kAdamThreads) void adam(AdamList L, AdamState S, Ad
     bool in;
   };
   auto place = [&]() __attribute__((always_inline)) {
-    while (k + 1 < L.count && L.first[k + 1] <= piece) ++k;
+    while (k + 1 < L.count && table.first[k + 1] <= piece) ++k;
     Place q;
-    const long long n = L.n[k];
-    q.i = (long long)(piece - L.first[k]) * kAdamPiece + threadIdx.x * kAdamRun;
-    q.p = static_cast<TP*>(L.p[k]) + q.i;
-    q.g = static_cast<const TG*>(L.g[k]) + q.i;
+    const long long n = table.n[k];
+    q.i = (long long)(piece - table.first[k]) * kAdamPiece + threadIdx.x * kAdamRun;
+    q.p = static_cast<TP*>(table.p[k]) + q.i;
+    q.g = static_cast<const TG*>(table.g[k]) + q.i;
     q.left = n - q.i;
-    q.at = (long long)L.at[k] * kAdamGroup + q.i;
+    q.at = (long long)table.at[k] * kAdamGroup + q.i;
     q.in = q.i < (n + kAdamGroup - 1) / kAdamGroup * kAdamGroup;  // (the same for 16 threads, a group)
     return q;
   };
@@ -253,21 +273,23 @@ template <typename TG>
 __global__ __launch_bounds__(kNormThreads) void squares(AdamList L, double* part, int add, int ends, int parts, int* arrived,
                                                         float* norm) {
   __shared__ int last;
+  __shared__ AdamTable table;
+  fill(L, table);
   double s = 0.;
   const int end = min(L.pieces, ((int)blockIdx.x + 1) * L.per);
   int piece = min((int)blockIdx.x * L.per + __builtin_amdgcn_readfirstlane(threadIdx.x / kAdamThreads), end - 1);
   const bool any = piece == (int)blockIdx.x * L.per + (int)(threadIdx.x / kAdamThreads);
-  int t = tensor_of(L, piece);
+  int t = tensor_of(table, L.count, piece);
   constexpr int B = 2;  // pieces at a time
   for (; any && piece < end; piece += B * kNormSide) {
     float g[B][kAdamRun];
 #pragma unroll
     for (int k = 0; k < B; ++k) {
       const int at = piece + k * kNormSide;
-      while (t + 1 < L.count && L.first[t + 1] <= min(at, end - 1)) ++t;
-      const long long i = (long long)(at - L.first[t]) * kAdamPiece + threadIdx.x % kAdamThreads * kAdamRun;
-      const long long left = at < end ? L.n[t] - i : 0;
-      load8(static_cast<const TG*>(L.g[t]) + (left > 0 ? i : 0), left, g[k]);
+      while (t + 1 < L.count && table.first[t + 1] <= min(at, end - 1)) ++t;
+      const long long i = (long long)(at - table.first[t]) * kAdamPiece + threadIdx.x % kAdamThreads * kAdamRun;
+      const long long left = at < end ? table.n[t] - i : 0;
+      load8(static_cast<const TG*>(table.g[t]) + (left > 0 ? i : 0), left, g[k]);
     }
 #pragma unroll
     for (int k = 0; k < B; ++k)
