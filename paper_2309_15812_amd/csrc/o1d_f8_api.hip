@@ -61,6 +61,7 @@ o1d_status_t o1d_pack_scaled(const void* x, long long ldx, o1d_scaled_t type, un
   hipStream_t s = static_cast<hipStream_t>(stream);
   O1D_TRY(check_elem_aligned(fn, sums, "the sums", es));
   if (M == 0) return sums ? hip_status(fn, o1d::launch_zero((Dtype)dtype, sums, C, s)) : ok();
+  if (M > (1 << 30) - 64) return fail(O1D_ERR_UNSUPPORTED, "%s: M=%d rows exceed the grid", fn, M);
   O1D_TRY(check_null(fn, {x}));
   if (!q && !e && !qt && !et) return fail(O1D_ERR_INVALID, "%s: no operand is asked for", fn);
   if (q || e) O1D_TRY(check_packed(fn, "the operand", q, e));

@@ -18,7 +18,8 @@ o1d_status_t check_gn(const char* fn, int N, int P, int C, int groups, o1d_dtype
 
 o1d_status_t check_pieces(const char* fn, const rows::GnPlan& pl, int N) {
   const long long n = (pl.held ? rows::cdiv(N, 8) * 8 : (long long)N * pl.chunks) * pl.bundles;
-  return n > 0x7fffffff ? fail(O1D_ERR_UNSUPPORTED, "%s: %lld workgroups exceed the grid", fn, n) : O1D_OK;
+  // (a grid has fewer than 2^32 threads)
+  return n * (pl.held ? pl.threads : 256) > 0xffffffffll ? fail(O1D_ERR_UNSUPPORTED, "%s: %lld workgroups exceed the grid", fn, n) : O1D_OK;
 }
 
 rows::GnParams gn_params(const rows::GnPlan& pl, int N, int P, int C, int groups, o1d_act_t act) {

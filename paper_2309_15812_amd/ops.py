@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -740,7 +741,7 @@ def gn_fwd(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor, groups: int, eps: 
            ) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(y, mean, rstd): act of the group norm of x (N, ..., C) over a sample's pixels and the C / groups channels of a group;
     mean and rstd (N, groups) float32 are for gn_bwd."""
-    a = _act(act)
+    a, groups = _act(act), operator.index(groups)
     if out is None and workspace is None:
         made = _train().gn_fwd(x, w, b, groups, eps, a)
         if made is not None:
@@ -1101,7 +1102,7 @@ class AdamState:
 def adamw(params, grads, state: AdamState, lr: float | torch.Tensor = 1e-3, betas: tuple[float, float] = (0.9, 0.999),
           eps: float = 1e-8, weight_decay: float = 0.01, max_norm: float | None = None,
           workspace: torch.Tensor | None = None) -> torch.Tensor | None:
-    """One AdamW step over all params (of one type, contiguous) in place, given their grads (of one type; None leaves a
+    """One AdamW step over all params (of one type, contiguous, each once) in place, given their grads (of one type; None leaves a
     parameter and its states as they are).  lr may be a float32 tensor of one value on the GPU.  max_norm limits the norm of all
     gradients, which is returned; where it is not finite, nothing changes."""
     if max_norm is not None and not max_norm > 0:

@@ -80,4 +80,4 @@ class AdamW:
             made.append(ops.AdamState(t["sizes"], *(None if t[n] is None else t[n].detach().to(device, copy=True)
                                                     for n in ("m", "v", "step", "ms", "vs", "master"))))
         for g, new, state in zip(self.groups, held["groups"], made):
-            g.update({k: v for k, v in new.items() if k != "state"}, state=state)
+            g.update({k: v.to(state.m.device) if isinstance(v, torch.Tensor) else v for k, v in new.items() if k != "state"}, state=state)

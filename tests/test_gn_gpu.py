@@ -196,3 +196,6 @@ def test_given_outputs_and_images():
                 lambda: ops.gn_bwd(x, y, mean[:1], rstd[:1], w, b), lambda: ops.gn_bwd(x.double(), y, mean, rstd, w, b)):
         with pytest.raises((ValueError, TypeError)):
             bad()
+    for groups in (4.0, "4", None):
+        with pytest.raises(TypeError):
+            ops.gn_fwd(x, w, b, groups)
