@@ -157,8 +157,9 @@ struct GnAt {
 template <typename T, int THREADS>
 struct GnLds {
   float each[THREADS * kRun<T>];
-  float some[kGnMostChannels];
-  float group[2][kGnMostChannels];
+  static constexpr int kMost = THREADS * kRun<T> < kGnMostChannels ? THREADS * kRun<T> : kGnMostChannels;
+  float some[kMost];
+  float group[2][kMost];
 };
 
 // Column sums of the threads' v in `some`, as J rows of CB; returns J.
@@ -721,12 +722,16 @@ bool with_gn(const GnPlan& pl, F&& f) {
         if constexpr (decltype(threads)::value != 512) { f(threads, integral_constant<int, 2>{}); return true; }
         return false;
       case 4: f(threads, integral_constant<int, 4>{}); return true;
+    }
+    if constexpr (decltype(threads)::value == 64) return false;
+    else switch (pl.runs) {
       case 6: f(threads, integral_constant<int, 6>{}); return true;
       case 8: if constexpr (kMost >= 8) { f(threads, integral_constant<int, 8>{}); return true; } return false;
       case 10: if constexpr (kMost >= 10) { f(threads, integral_constant<int, 10>{}); return true; } return false;
       default: return false;
     }
   };
+  if (pl.threads == 64) return runs(integral_constant<int, 64>{});
   if (pl.threads == 256) return runs(integral_constant<int, 256>{});
   if (pl.threads == kBig) return runs(integral_constant<int, kBig>{});
   return false;
