@@ -117,7 +117,7 @@ __device__ __forceinline__ void to8(const float (&v)[kAdamRun], uint8_t* p, floa
   most = max(most, (uint32_t)__builtin_amdgcn_mov_dpp((int)most, 0x140, 0xF, 0xF, true));
   // (below that, 448 / amax leaves float32 and a zero's product with it is NaN)
   const float amax = __uint_as_float(most), top = amax < 448 * 0x1p-126f ? 448 * 0x1p-126f : amax;
-  const float inv = most ? 448.f / top : 0.f;
+  const float inv = most ? 448.f * (1.f / top) : 0.f;  // (the reciprocal rounded first, as in the formula's usual evaluation)
   float u[kAdamRun];
 #pragma unroll
   for (int e = 0; e < kAdamRun; ++e) {
