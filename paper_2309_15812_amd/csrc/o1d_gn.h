@@ -36,6 +36,10 @@ constexpr int kGnMostChunks = 512;     // of a sample
 // registers twice and needs 256 of them per thread.
 constexpr int gn_big(bool backward, int esize) { return backward && esize == 2 ? 512 : 1024; }
 constexpr int gn_most_runs(bool backward, int esize) { return backward ? (esize == 2 ? 6 : 8) : 10; }
+// The runs (even) that a workgroup's threads may have.  (Two of 512 threads are five of 256 at most.)
+constexpr bool gn_takes(bool backward, int esize, int threads, int runs) {
+  return runs <= (threads == 64 ? 4 : gn_most_runs(backward, esize)) && !(threads == 512 && runs == 2);
+}
 GnPlan plan_gn(bool backward, int N, int P, int C, int G, int esize);
 
 // Floats of workspace: the forward's, not held: (mean, sum of squares) of each sample, group and

@@ -715,26 +715,27 @@ __global__ __launch_bounds__(kGnThreads) void gn_bwd_apply(GnParams P) {
 template <bool BACKWARD, int ESIZE, typename F>
 bool with_gn(const GnPlan& pl, F&& f) {
   using std::integral_constant;
-  constexpr int kBig = gn_big(BACKWARD, ESIZE), kMost = gn_most_runs(BACKWARD, ESIZE);
-  auto runs = [&](auto threads) {
-    switch (pl.runs) {
-      case 2:  // (two runs of 512 threads are at most five of 256, which the plan prefers)
-        if constexpr (decltype(threads)::value != 512) { f(threads, integral_constant<int, 2>{}); return true; }
-        return false;
-      case 4: f(threads, integral_constant<int, 4>{}); return true;
-    }
-    if constexpr (decltype(threads)::value == 64) return false;
-    else switch (pl.runs) {
-      case 6: f(threads, integral_constant<int, 6>{}); return true;
-      case 8: if constexpr (kMost >= 8) { f(threads, integral_constant<int, 8>{}); return true; } return false;
-      case 10: if constexpr (kMost >= 10) { f(threads, integral_constant<int, 10>{}); return true; } return false;
-      default: return false;
-    }
+  constexpr int kBig = gn_big(BACKWARD, ESIZE);
+  bool done = false;
+  auto with = [&](auto threads) {
+    auto runs = [&](auto r) {
+      constexpr int TH = decltype(threads)::value, R = decltype(r)::value;
+      if constexpr (gn_takes(BACKWARD, ESIZE, TH, R)) {
+        if (pl.threads != TH || pl.runs != R) return;
+        f(threads, r);
+        done = true;
+      }
+    };
+    runs(integral_constant<int, 2>{});
+    runs(integral_constant<int, 4>{});
+    runs(integral_constant<int, 6>{});
+    runs(integral_constant<int, 8>{});
+    runs(integral_constant<int, 10>{});
   };
-  if (pl.threads == 64) return runs(integral_constant<int, 64>{});
-  if (pl.threads == 256) return runs(integral_constant<int, 256>{});
-  if (pl.threads == kBig) return runs(integral_constant<int, kBig>{});
-  return false;
+  with(integral_constant<int, 64>{});
+  with(integral_constant<int, 256>{});
+  with(integral_constant<int, kBig>{});
+  return done;
 }
 
 inline unsigned gn_units(const GnParams& p) { return (unsigned)(cdiv(p.N, 8) * 8 * p.bundles); }

@@ -21,15 +21,16 @@ GnPlan plan_gn(bool backward, int N, int P, int C, int G, int esize) {
       if (run > threads) continue;
       const long long rows = threads / run, need = cdiv(P, rows);
       const int runs = need <= 2 ? 2 : (int)cdiv(need, 2) * 2;
-      if (runs > (threads == 64 ? 4 : gn_most_runs(backward, esize))) continue;
+      if (!gn_takes(backward, esize, threads, runs)) continue;
       // time in us: what a CU moves, at the rate that it has among the others, and the two reductions, which small workgroups
-      // on a CU have at the same time (65536 samples of 1 x 64 bfloat16 in workgroups of 64 threads 125 us, in two passes 580)
+      // on a CU have at the same time (65536 samples of 1 x 64 bfloat16 in workgroups of 64 threads 125 us, in two passes 580);
+      // rows of fewer channels than a run are loaded one by one (6 x 183 x 7 bfloat16 in two runs 7 us, in four 10)
       const double bytes = (double)P * CB * esize, piece = CB * esize;
       const long long groups = (long long)N * real, rounds = cdiv(groups, 256);
       const double per_cu = groups >= 256 ? 20e3 : (groups > 102 ? 5.12e6 / groups : 50e3);  // bytes per us
       const double sums = threads == 64 ? 1.2 * cdiv(groups, backward ? 2048 : 4096)
                                         : (threads == 256 ? 1.5 * cdiv(groups, backward ? 512 : 1024) : 3. * rounds);
-      const double t = rounds * (bytes / per_cu * (piece < 64 ? 64 / piece : 1.)) + sums + 0.05 * runs;
+      const double t = rounds * (bytes / per_cu * (piece < 64 ? 64 / piece : 1.)) + sums + (C < V ? 0.8 : 0.05) * runs;
       if (cost >= 0. && t >= cost) continue;
       cost = t;
       best = {true, threads, runs, gb, real, 1, P};

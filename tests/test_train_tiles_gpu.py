@@ -16,7 +16,7 @@ HELD = [(1, 196, 24, 3), (1, 1500, 6, 2), (1, 196, 64, 1), (1, 400, 203, 7), (1,
         (1, 400, 64, 1), (1, 784, 203, 7), (1, 400, 6, 2), (64, 30, 203, 7), (1, 400, 33, 33), (64, 49, 203, 7), (1, 784, 6, 2),
         (1, 196, 203, 7), (1, 1500, 192, 4), (64, 784, 203, 7), (1, 1500, 203, 7), (1, 1500, 33, 33), (1, 49, 1024, 1),
         (1, 784, 24, 3), (1, 784, 192, 4), (64, 400, 203, 7), (1, 14, 560, 1), (1, 21, 720, 1), (1, 3136, 6, 2), (1, 3136, 203, 7),
-        (1, 1053, 58, 2), (1, 2161, 1, 1)]
+        (1, 1053, 58, 2), (1, 2161, 1, 1), (1, 1156, 5, 1)]
 
 
 @pytest.mark.parametrize("dt", DTYPES)
