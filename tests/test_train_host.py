@@ -78,7 +78,7 @@ REFUSED = [
     (pack, dict(q=None, e=None, qt=None, et=None), INVALID), (pack, dict(qt=None, et=None), INVALID), (pack, dict(q=ODD), INVALID),
     (pack, dict(ws=None), WORKSPACE), (pack, dict(n=10), WORKSPACE), (pack, dict(q=at(0)), INVALID), (pack, dict(qt=at(1)), INVALID),
     (pack, dict(sums=at(4)), INVALID), (pack, dict(sums=ODD), INVALID), (pack, dict(C=(1 << 20) + 1, ldx=1 << 20), UNSUPPORTED),
-    (pack, dict(M=1 << 30, C=1, ldx=1), UNSUPPORTED), (gn_fwd, dict(N=1 << 25, P=1, C=8, G=1, ldx=8, ldy=8,
+    (pack, dict(M=1 << 30, C=1, ldx=1), UNSUPPORTED), (gn_fwd, dict(N=1 << 27, P=1, C=8, G=1, ldx=8, ldy=8,
      **{k: ctypes.c_void_p(1 << (42 + i)) for i, k in enumerate(("x", "y", "mean", "rstd", "ws"))}, n=1 << 40), UNSUPPORTED),
     (fwd, dict(M=-1), INVALID), (fwd, dict(I=0), INVALID), (fwd, dict(O=0), INVALID), (fwd, dict(type=-1), INVALID), (fwd, dict(act=5), INVALID),
     (fwd, dict(ldy=39), INVALID), (fwd, dict(ldres=39), INVALID), (fwd, dict(ldpre=39), INVALID), (fwd, dict(xq=None), INVALID),
