@@ -32,6 +32,16 @@ struct GnPlan {
 };
 constexpr int kGnMostChannels = 1024;  // of a group
 constexpr int kGnMostChunks = 512;     // of a sample
+constexpr int kGnThreads = 256, kGnBatch = 8;  // in chunks: threads of a workgroup, most rows that a thread takes at a time
+// A row of a sample in chunks.  A thread's next rows are worked out before they are compared with the chunk's end, up to
+// kGnThreads kGnBatch = 2048 behind it; an int has room for 1024 behind the longest sample, and kept to that
+// only by how the plan divides one (the furthest row was 2^31 - 364).
+using GnRow = uint32_t;
+// The k-th of a thread's next rows from r on, `slots` apart, or the chunk's last one.
+__host__ __device__ __forceinline__ GnRow gn_row(GnRow r, int k, int slots, GnRow end) {
+  const GnRow at = r + (GnRow)(k * slots);
+  return at < end ? at : end - 1;
+}
 // Threads of the larger workgroups and most runs of a held sample: in bfloat16 the backward unpacks its
 // registers twice and needs 256 of them per thread.
 constexpr int gn_big(bool backward, int esize) { return backward && esize == 2 ? 512 : 1024; }

@@ -212,7 +212,7 @@ __device__ __forceinline__ void again(uint32_t (&w)[RUNS][4]) {
 }
 
 template <typename T>
-__device__ __forceinline__ const T* row_of(const void* p, const GnParams& P, int n, int r, long long ld) {
+__device__ __forceinline__ const T* row_of(const void* p, const GnParams& P, int n, GnRow r, long long ld) {
   return static_cast<const T*>(p) + ((long long)n * P.P + r) * ld;
 }
 
@@ -287,11 +287,11 @@ __global__ __launch_bounds__(THREADS) void gn_fwd_held(GnParams P) {
 
 // ---- samples in chunks
 
-constexpr int kGnThreads = 256, kGnBatch = 8;
 static_assert(kGnThreads * kRun<float> >= kGnMostChannels, "a run of a row for each thread");
 
 struct GnChunk {
-  int chunk, bundle, sample, r0, r1;
+  int chunk, bundle, sample;
+  GnRow r0, r1;
 };
 __device__ __forceinline__ GnChunk chunk_of(const GnParams& P) {
   GnChunk c;
@@ -299,8 +299,8 @@ __device__ __forceinline__ GnChunk chunk_of(const GnParams& P) {
   c.bundle = id % P.bundles;
   c.chunk = id / P.bundles % P.chunks;
   c.sample = id / P.bundles / P.chunks;
-  c.r0 = c.chunk * P.rows;
-  c.r1 = min(P.P, c.r0 + P.rows);
+  c.r0 = (GnRow)c.chunk * (GnRow)P.rows;
+  c.r1 = min((GnRow)P.P, c.r0 + (GnRow)P.rows);
   return c;
 }
 
@@ -314,11 +314,11 @@ __global__ __launch_bounds__(kGnThreads) void gn_stats(GnParams P) {
   GnAt<T, kGnThreads> at;
   at.place(P, ch.sample, ch.bundle);
   float mean[V] = {}, sq[V] = {}, count = 0.f;
-  for (int r = ch.r0 + at.slot; r < ch.r1; r += B * at.slots) {
+  for (GnRow r = ch.r0 + at.slot; r < ch.r1; r += B * at.slots) {
     uint32_t raw[B][4];
 #pragma unroll
-    for (int k = 0; k < B; ++k) at.load(row_of<T>(P.x, P, ch.sample, min(r + k * at.slots, ch.r1 - 1), P.ldx), raw[k]);
-    const int left = min(B, (ch.r1 - r + at.slots - 1) / at.slots);
+    for (int k = 0; k < B; ++k) at.load(row_of<T>(P.x, P, ch.sample, gn_row(r, k, at.slots, ch.r1), P.ldx), raw[k]);
+    const int left = min(B, ((int)(ch.r1 - r) + at.slots - 1) / at.slots);
     float s[V] = {}, v[V];
 #pragma unroll
     for (int k = 0; k < B; ++k) {
@@ -387,8 +387,8 @@ __global__ __launch_bounds__(kGnThreads) void gn_join(GnParams P) {
   float m[kGnLeft], sq[kGnLeft], s = 0.f, all = 0.f;
   left_of(P.part + id * P.chunks * 2, P.chunks, m, sq);
   auto count = [&](int k) __attribute__((always_inline)) {  // (none behind the last chunk)
-    const int from = min(P.P, (lane + 64 * k) * P.rows);
-    return (float)(min(P.P - from, P.rows)) * (float)P.D;
+    const int q = lane + 64 * k;
+    return q < P.chunks ? (float)min(P.P - q * P.rows, P.rows) * (float)P.D : 0.f;
   };
   const float total = (float)P.P * (float)P.D;
 #pragma unroll
@@ -413,11 +413,11 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply(GnParams P) {
   const GnChunk ch = chunk_of(P);
   GnAt<T, kGnThreads> at;
   at.place(P, ch.sample, ch.bundle);
-  int r = ch.r0 + at.slot;
+  GnRow r = ch.r0 + at.slot;
   uint32_t raw[B][4];
   auto load = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < B; ++k) at.load(row_of<T>(P.x, P, ch.sample, min(r + k * at.slots, ch.r1 - 1), P.ldx), raw[k]);
+    for (int k = 0; k < B; ++k) at.load(row_of<T>(P.x, P, ch.sample, gn_row(r, k, at.slots, ch.r1), P.ldx), raw[k]);
   };
   load();
   if (!at.active) return;
@@ -561,10 +561,10 @@ __global__ __launch_bounds__(THREADS) void gn_bwd_held(GnParams P) {
 template <typename T, int B>
 struct GnRows {
   uint32_t x[B][4], g[B][4];
-  __device__ __forceinline__ void load(const GnParams& P, const GnAt<T, kGnThreads>& at, const GnChunk& ch, int r) {
+  __device__ __forceinline__ void load(const GnParams& P, const GnAt<T, kGnThreads>& at, const GnChunk& ch, GnRow r) {
 #pragma unroll
     for (int k = 0; k < B; ++k) {
-      const int row = min(r + k * at.slots, ch.r1 - 1);
+      const GnRow row = gn_row(r, k, at.slots, ch.r1);
       at.load(row_of<T>(P.x, P, ch.sample, row, P.ldx), x[k]);
       at.load(row_of<T>(P.dy, P, ch.sample, row, P.ldd), g[k]);
     }
@@ -579,7 +579,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_bwd_sums(GnParams P) {
   GnAt<T, kGnThreads> at;
   at.place(P, ch.sample, ch.bundle);
   GnRows<T, B> rows;
-  int r = ch.r0 + at.slot;
+  GnRow r = ch.r0 + at.slot;
   rows.load(P, at, ch, r);
   float w[V], b[V], mean[V], rstd[V], dw[V] = {}, db[V] = {};
   at.vector(P.w, w);
@@ -676,7 +676,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_bwd_apply(GnParams P) {
   GnAt<T, kGnThreads> at;
   at.place(P, ch.sample, ch.bundle);
   GnRows<T, B> rows;
-  int r = ch.r0 + at.slot;
+  GnRow r = ch.r0 + at.slot;
   rows.load(P, at, ch, r);
   const float* const sums = P.part + ((long long)P.N * P.chunks * (P.C + P.G) + (long long)ch.sample * P.G + at.g0) * 2;
   if (!at.active) return;
