@@ -50,6 +50,15 @@ constexpr int gn_most_runs(bool backward, int esize) { return backward ? (esize 
 constexpr bool gn_takes(bool backward, int esize, int threads, int runs) {
   return runs <= (threads == 64 ? 4 : gn_most_runs(backward, esize)) && !(threads == 512 && runs == 2);
 }
+// Between the passes a wave joins a sample's group, and the groups behind the grid's last one in turn: all of them would
+// be more than the fewer than 2^32 threads that a grid has (65536 samples of 1024 groups are 2^32).
+constexpr int kGnMostJoins = 1 << 16;  // workgroups
+constexpr int kGnCloseWaves = 16, kGnCloseCols = 32;  // backward: waves of one, and columns of a gradients' sum in one
+inline unsigned gn_join_blocks(int N, int G, int waves) {
+  const long long blocks = cdiv((long long)N * G, waves);
+  return (unsigned)(blocks < kGnMostJoins ? blocks : kGnMostJoins);
+}
+inline int gn_close_columns(int C) { return (int)cdiv(2ll * C, kGnCloseCols); }  // workgroups of the gradients' sums, before those
 GnPlan plan_gn(bool backward, int N, int P, int C, int G, int esize);
 
 // Floats of workspace: the forward's, not held: (mean, sum of squares) of each sample, group and

@@ -381,28 +381,30 @@ __device__ __forceinline__ void left_of(const float* of, int chunks, float (&a)[
 // The chunks' statistics joined, a wave for a sample's group.  (A launch of its own: joined by every workgroup of gn_apply, a
 // wave group after group, 1 x 37872 x 144 in 48 groups backward took 20 us longer.)
 __global__ __launch_bounds__(kGnThreads) void gn_join(GnParams P) {
-  const long long id = (long long)blockIdx.x * (kGnThreads / 64) + (threadIdx.x >> 6);
-  if (id >= (long long)P.N * P.G) return;
+  constexpr int kWaves = kGnThreads / 64;
   const int lane = threadIdx.x & 63;
-  float m[kGnLeft], sq[kGnLeft], s = 0.f, all = 0.f;
-  left_of(P.part + id * P.chunks * 2, P.chunks, m, sq);
-  auto count = [&](int k) __attribute__((always_inline)) {  // (none behind the last chunk)
-    const int q = lane + 64 * k;
-    return q < P.chunks ? (float)min(P.P - q * P.rows, P.rows) * (float)P.D : 0.f;
-  };
   const float total = (float)P.P * (float)P.D;
+  const long long groups = (long long)P.N * P.G;
+  for (long long id = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6); id < groups; id += (long long)gridDim.x * kWaves) {
+    float m[kGnLeft], sq[kGnLeft], s = 0.f, all = 0.f;
+    left_of(P.part + id * P.chunks * 2, P.chunks, m, sq);
+    auto count = [&](int k) __attribute__((always_inline)) {  // (none behind the last chunk)
+      const int q = lane + 64 * k;
+      return q < P.chunks ? (float)min(P.P - q * P.rows, P.rows) * (float)P.D : 0.f;
+    };
 #pragma unroll
-  for (int k = 0; k < kGnLeft; ++k) s = fmaf(count(k), m[k], s);
-  const float mean = wave_sum(s) / total;
+    for (int k = 0; k < kGnLeft; ++k) s = fmaf(count(k), m[k], s);
+    const float mean = wave_sum(s) / total;
 #pragma unroll
-  for (int k = 0; k < kGnLeft; ++k) {
-    const float d = m[k] - mean, n = count(k);
-    all += n > 0.f ? fmaf(d * d, n, sq[k]) : 0.f;
-  }
-  const float rstd = 1.f / sqrtf(wave_sum(all) / total + P.eps);
-  if (lane == 0) {
-    P.mean[id] = mean;
-    P.rstd[id] = rstd;
+    for (int k = 0; k < kGnLeft; ++k) {
+      const float d = m[k] - mean, n = count(k);
+      all += n > 0.f ? fmaf(d * d, n, sq[k]) : 0.f;
+    }
+    const float rstd = 1.f / sqrtf(wave_sum(all) / total + P.eps);
+    if (lane == 0) {
+      P.mean[id] = mean;
+      P.rstd[id] = rstd;
+    }
   }
 }
 
@@ -621,27 +623,30 @@ __global__ __launch_bounds__(kGnThreads) void gn_bwd_sums(GnParams P) {
 // workgroups after those the groups' sums, a wave for a sample's group.
 template <typename T>
 __global__ __launch_bounds__(1024) void gn_bwd_close(GnParams P) {
-  constexpr int kCols = 32, kSlices = 32, kBatch = 8;
+  constexpr int kCols = kGnCloseCols, kSlices = 32, kBatch = 8;
+  static_assert(kCols * kSlices == 64 * kGnCloseWaves, "a workgroup of either kind");
   __shared__ float red[kSlices][kCols + 1];
   const int blocks = (2 * P.C + kCols - 1) / kCols;
   if ((int)blockIdx.x >= blocks) {
-    const long long id = (long long)((int)blockIdx.x - blocks) * 16 + (threadIdx.x >> 6), groups = (long long)P.N * P.G;
-    if (id >= groups) return;
+    const long long groups = (long long)P.N * P.G;
     float* const of = P.part + (long long)P.N * P.chunks * 2 * P.C;
-    float g[kGnLeft], gx[kGnLeft], s = 0.f, sx = 0.f;
-    left_of(of + id * P.chunks * 2, P.chunks, g, gx);
-#pragma unroll
-    for (int k = 0; k < kGnLeft; ++k) {
-      s += g[k];
-      sx += gx[k];
-    }
-    s = wave_sum(s);
-    sx = wave_sum(sx);
     const float inv = 1.f / ((float)P.P * (float)P.D);
-    if ((threadIdx.x & 63) == 0) {
-      float* const to = of + (groups * P.chunks + id) * 2;
-      to[0] = s * inv;
-      to[1] = sx * inv;
+    long long id = (long long)((int)blockIdx.x - blocks) * kGnCloseWaves + (threadIdx.x >> 6);
+    for (; id < groups; id += (long long)((int)gridDim.x - blocks) * kGnCloseWaves) {
+      float g[kGnLeft], gx[kGnLeft], s = 0.f, sx = 0.f;
+      left_of(of + id * P.chunks * 2, P.chunks, g, gx);
+#pragma unroll
+      for (int k = 0; k < kGnLeft; ++k) {
+        s += g[k];
+        sx += gx[k];
+      }
+      s = wave_sum(s);
+      sx = wave_sum(sx);
+      if ((threadIdx.x & 63) == 0) {
+        float* const to = of + (groups * P.chunks + id) * 2;
+        to[0] = s * inv;
+        to[1] = sx * inv;
+      }
     }
     return;
   }
@@ -753,7 +758,7 @@ hipError_t gn_fwd_t(const GnPlan& pl, const GnParams& p, hipStream_t stream) {
   hipLaunchKernelGGL((gn_stats<T>), dim3(gn_pieces(p)), dim3(kGnThreads), 0, stream, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(gn_join, dim3((unsigned)cdiv((long long)p.N * p.G, kGnThreads / 64)), dim3(kGnThreads), 0, stream, p);
+  hipLaunchKernelGGL(gn_join, dim3(gn_join_blocks(p.N, p.G, kGnThreads / 64)), dim3(kGnThreads), 0, stream, p);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((gn_apply<T>), dim3(gn_pieces(p)), dim3(kGnThreads), 0, stream, p);
@@ -773,7 +778,7 @@ hipError_t gn_bwd_t(const GnPlan& pl, const GnParams& p, hipStream_t stream) {
   hipLaunchKernelGGL((gn_bwd_sums<T>), dim3(gn_pieces(p)), dim3(kGnThreads), 0, stream, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((gn_bwd_close<T>), dim3((unsigned)(cdiv(2ll * p.C, 32) + cdiv((long long)p.N * p.G, 16))), dim3(1024), 0, stream, p);
+  hipLaunchKernelGGL((gn_bwd_close<T>), dim3(gn_close_columns(p.C) + gn_join_blocks(p.N, p.G, kGnCloseWaves)), dim3(64 * kGnCloseWaves), 0, stream, p);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((gn_bwd_apply<T>), dim3(gn_pieces(p)), dim3(kGnThreads), 0, stream, p);

@@ -72,6 +72,32 @@ int main() {
 }
 """
 
+GRIDS = HEAD + r"""
+// All samples' groups are joined whatever their number, by grids of fewer than 2^32 threads.
+int main() {
+  long long most = 0;
+  const int sizes[][3] = {{65536, 2048, 1024}, {65536, 7168, 1024}, {1, 1, 1}, {300, 64, 2}, {1 << 17, 512, 512}, {1 << 16, 1024, 1024},
+                          {(1 << 16) + 1, 1024, 1024}, {0x7fffffff - 1024, 1 << 20, 1 << 20}, {1 << 20, 1 << 10, 1 << 10}, {3, 203, 7}};
+  for (auto& s : sizes) {
+    const long long N = s[0], C = s[1], G = s[2], groups = N * G;
+    const long long join = gn_join_blocks((int)N, (int)G, kGnThreads / 64), close = gn_join_blocks((int)N, (int)G, kGnCloseWaves);
+    const long long columns = gn_close_columns((int)C);
+    if (join < 1 || close < 1 || join * kGnThreads >= 1ll << 32 || (columns + close) * 64 * kGnCloseWaves >= 1ll << 32 ||
+        columns * kGnCloseCols < 2 * C) {
+      printf("%lld samples of %lld groups: %lld and %lld + %lld workgroups\n", N, G, join, columns, close);
+      return 1;
+    }
+    // (a grid that is not cut has a wave for each group)
+    if ((join < kGnMostJoins && join * (kGnThreads / 64) < groups) || (close < kGnMostJoins && close * kGnCloseWaves < groups)) {
+      printf("%lld samples of %lld groups: %lld and %lld workgroups leave groups out\n", N, G, join, close);
+      return 1;
+    }
+    most = join > most ? join : most;
+  }
+  return most == kGnMostJoins ? 0 : 1;
+}
+"""
+
 
 @pytest.fixture(scope="module")
 def compile_run(tmp_path_factory):
@@ -88,4 +114,9 @@ def compile_run(tmp_path_factory):
 
 def test_rows_of_a_chunk_stay_in_it(compile_run):
     r = compile_run(ROWS)
+    assert r.returncode == 0, r.stdout
+
+
+def test_grids_between_the_passes(compile_run):
+    r = compile_run(GRIDS)
     assert r.returncode == 0, r.stdout
