@@ -271,6 +271,7 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!s[0] || !s[1] || !s[2] || !s[0]->is_cuda()) return none();
   const auto device = s[0]->device();
   c10::SmallVector<o1d_adamw_tensor_t, 128> list;
+  c10::SmallVector<const at::Tensor*, 128> written;
   std::optional<o1d_dtype_t> pdt, gdt;
   int64_t start = 0;
   for (Py_ssize_t i = 0; i < count; ++i) {
@@ -288,6 +289,7 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
       if (!u || (gdt && *gdt != *u)) return none();
       gdt = u;
       list.push_back({p->data_ptr(), g->data_ptr(), size, start});
+      written.push_back(p);
     }
     start += up(size, kGroup);
   }
@@ -315,6 +317,9 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
                    ws.data_ptr(), (size_t)ws.numel(), stream);
   });
   if (st) return none();
+  // (a backward that was recorded before the step refuses what it kept of them)
+  for (const at::Tensor* p : written)
+    if (!p->is_inference()) p->unsafeGetTensorImpl()->bump_version();
   if (norm.defined()) return wrap(norm);
   Py_RETURN_TRUE;
   END_HANDLE_TH_ERRORS

@@ -1102,8 +1102,8 @@ class AdamState:
 def adamw(params, grads, state: AdamState, lr: float | torch.Tensor = 1e-3, betas: tuple[float, float] = (0.9, 0.999),
           eps: float = 1e-8, weight_decay: float = 0.01, max_norm: float | None = None,
           workspace: torch.Tensor | None = None) -> torch.Tensor | None:
-    """One AdamW step over all params (of one type, contiguous, each once) in place, given their grads (of one type; None leaves a
-    parameter and its states as they are).  lr may be a float32 tensor of one value on the GPU.  max_norm limits the norm of all
+    """One AdamW step over all params (of one type, contiguous, each once) in place, as autograd's versions of them tell, given their
+    grads (of one type; None leaves a parameter and its states as they are).  lr may be a float32 tensor of one value on the GPU.  max_norm limits the norm of all
     gradients, which is returned; where it is not finite, nothing changes."""
     if max_norm is not None and not max_norm > 0:
         raise ValueError(f"max_norm must be positive, got {max_norm}")
@@ -1117,7 +1117,7 @@ def adamw(params, grads, state: AdamState, lr: float | torch.Tensor = 1e-3, beta
         raise ValueError(f"{len(params)} parameters and {len(grads)} gradients for the states of {len(state.sizes)}")
     device, pdt, gdt = state.m.device, None, None
     table = (_lib.AdamTensor * max(1, len(params)))()
-    count = 0
+    count, written = 0, []
     for p, g, n, at in zip(params, grads, state.sizes, state.starts):
         if p.numel() != n or p.device != device or not p.is_contiguous() or (pdt is not None and p.dtype is not pdt):
             raise ValueError(f"parameters must be contiguous tensors of one type on {device} with the states' sizes, got "
@@ -1131,6 +1131,8 @@ def adamw(params, grads, state: AdamState, lr: float | torch.Tensor = 1e-3, beta
         gdt = g.dtype
         table[count] = _lib.AdamTensor(p.data_ptr(), g.data_ptr(), n, at)
         count += 1
+        if not p.is_inference():
+            written.append(p)
     for t in (pdt, gdt):
         if t is not None and t not in _DT:
             raise TypeError(f"unsupported dtype {t}; use float32 or bfloat16")
@@ -1148,4 +1150,5 @@ def adamw(params, grads, state: AdamState, lr: float | torch.Tensor = 1e-3, beta
     workspace, nbytes = _scratch(workspace, state.step, int(_lib.lib().o1d_adamw_workspace_bytes(max_norm or 0.0)))
     _run("o1d_adamw", state.step, ctypes.addressof(table), count, _DT[pdt] if pdt else 0, _DT[gdt] if gdt else 0,
          ctypes.addressof(s), ctypes.addressof(o), None if norm is None else norm.data_ptr(), workspace.data_ptr(), nbytes)
+    torch.autograd.graph.increment_version(written)
     return norm
