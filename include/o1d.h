@@ -351,7 +351,8 @@ size_t o1d_scaled_linear_bwd_weight_workspace_bytes(int M, int I, int O, o1d_dty
  * of 128; behind its end the states' values up to the next multiple of 128 are set to zeros.  state_bits 32: m and v
  * are float32.  8: m and the root of v are e4m3 (a positive root at least the type's smallest value), with a scale
  * m_scale, v_scale for each 128 values: the largest / 448, at least 2^-126, or 0 for zeros.  master (or NULL): the parameters in float32, from which p is rounded;
- * without it p itself is read.  The states are 16-byte aligned.
+ * without it p itself is read.  follow (not 0, with master): where p is not its master rounded, it was written since the
+ * last step, and its value is taken for the master's.  The states are 16-byte aligned.
  * step: two device integers, the steps taken (read and counted up) and 0.  lr_at: the learning rate in device memory, or NULL for
  * lr.  max_norm > 0 limits the norm of all gradients to it; the norm is then written to `norm`, and where it is not finite
  * nothing else changes.  max_norm 0: no limit, norm is not written and may be NULL.
@@ -371,6 +372,7 @@ typedef struct {
 typedef struct {
   double lr, beta1, beta2, eps, weight_decay, max_norm;
   const float* lr_at;
+  int follow;
 } o1d_adamw_options_t;
 o1d_status_t o1d_adamw(const o1d_adamw_tensor_t* tensors, int count, o1d_dtype_t param_dtype, o1d_dtype_t grad_dtype,
                        const o1d_adamw_state_t* state, const o1d_adamw_options_t* options, float* norm, void* workspace,

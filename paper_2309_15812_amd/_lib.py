@@ -35,7 +35,8 @@ class AdamState(ctypes.Structure):
 
 
 class AdamOptions(ctypes.Structure):
-    _fields_ = [("lr", _d), ("beta1", _d), ("beta2", _d), ("eps", _d), ("weight_decay", _d), ("max_norm", _d), ("lr_at", _vp)]
+    _fields_ = [("lr", _d), ("beta1", _d), ("beta2", _d), ("eps", _d), ("weight_decay", _d), ("max_norm", _d), ("lr_at", _vp),
+                ("follow", _i)]
 
 
 SIGNATURES = {

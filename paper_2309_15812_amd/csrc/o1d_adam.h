@@ -29,6 +29,7 @@ struct AdamHyper {
   const float* lr_at;     // (or NULL) device value of the learning rate
   const float* norm;      // (or NULL) the gradients' norm, to be limited to max_norm
   float max_norm;
+  bool follow;            // with masters: parameters that were written since are read
 };
 
 constexpr int kAdamMost = 112;  // tensors of a launch (what its arguments hold)

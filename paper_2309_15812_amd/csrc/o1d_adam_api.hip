@@ -134,6 +134,7 @@ o1d_status_t o1d_adamw(const o1d_adamw_tensor_t* tensors, int count, o1d_dtype_t
   h.lr_at = H.lr_at;
   h.norm = clip ? norm : nullptr;
   h.max_norm = (float)H.max_norm;
+  h.follow = H.follow != 0;
   return hip_status(fn, rows::launch_adam(pdt, gdt, list.data(), (int)list.size(), st, h, s));
 }
 

@@ -257,11 +257,11 @@ PyObject* adam_starts(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// (params, grads, sizes, (m, v, step, ms, vs, master), lr, beta1, beta2, eps, weight_decay, max_norm or 0.) -> the
+// (params, grads, sizes, (m, v, step, ms, vs, master), lr, beta1, beta2, eps, weight_decay, max_norm or 0., follow) -> the
 // gradients' norm, or True
 PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (n != 10 || !PyList_Check(a[0]) || !PyList_Check(a[1]) || !PyList_Check(a[2]) || !PyTuple_Check(a[3]) ||
+  if (n != 11 || !PyList_Check(a[0]) || !PyList_Check(a[1]) || !PyList_Check(a[2]) || !PyTuple_Check(a[3]) ||
       PyTuple_GET_SIZE(a[3]) != 6)
     return none();
   const Py_ssize_t count = PyList_GET_SIZE(a[0]);
@@ -307,7 +307,7 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
   auto data = [](const at::Tensor* t) { return t ? t->data_ptr() : nullptr; };
   const o1d_adamw_state_t state{data(s[0]), data(s[1]), (float*)data(s[3]), (float*)data(s[4]), (float*)data(s[5]),
                                 (int*)data(s[2]), s[3] ? 8 : 32};
-  const o1d_adamw_options_t options{h[0], h[1], h[2], h[3], h[4], h[5], (const float*)data(lr)};
+  const o1d_adamw_options_t options{h[0], h[1], h[2], h[3], h[4], h[5], (const float*)data(lr), a[10] == Py_True};
   at::Tensor norm, ws = space(p_adamw_bytes(h[5]), *s[0]);
   if (h[5] > 0.) norm = empty({}, *s[0], at::kFloat);
   const c10::DeviceGuard guard(device);

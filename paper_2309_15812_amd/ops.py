@@ -1101,16 +1101,17 @@ class AdamState:
 
 def adamw(params, grads, state: AdamState, lr: float | torch.Tensor = 1e-3, betas: tuple[float, float] = (0.9, 0.999),
           eps: float = 1e-8, weight_decay: float = 0.01, max_norm: float | None = None,
-          workspace: torch.Tensor | None = None) -> torch.Tensor | None:
+          workspace: torch.Tensor | None = None, follow: bool = False) -> torch.Tensor | None:
     """One AdamW step over all params (of one type, contiguous, each once) in place, as autograd's versions of them tell, given their
     grads (of one type; None leaves a parameter and its states as they are).  lr may be a float32 tensor of one value on the GPU.  max_norm limits the norm of all
-    gradients, which is returned; where it is not finite, nothing changes."""
+    gradients, which is returned; where it is not finite, nothing changes.  With masters the parameters are only written;
+    follow=True reads them too, and takes the values of those that are not their masters rounded: somebody wrote them."""
     if max_norm is not None and not max_norm > 0:
         raise ValueError(f"max_norm must be positive, got {max_norm}")
     params, grads = list(params), list(grads)
     if workspace is None:
         made = _train().adamw(params, grads, state.sizes, (state.m, state.v, state.step, state.ms, state.vs, state.master), lr,
-                              betas[0], betas[1], eps, weight_decay, max_norm or 0.0)
+                              betas[0], betas[1], eps, weight_decay, max_norm or 0.0, bool(follow))
         if made is not None:
             return None if max_norm is None else made
     if len(params) != len(state.sizes) or len(grads) != len(params):
@@ -1145,7 +1146,7 @@ def adamw(params, grads, state: AdamState, lr: float | torch.Tensor = 1e-3, beta
                        None if state.vs is None else state.vs.data_ptr(),
                        None if state.master is None else state.master.data_ptr(), state.step.data_ptr(),
                        32 if state.ms is None else 8)
-    o = _lib.AdamOptions(lr, betas[0], betas[1], eps, weight_decay, max_norm or 0.0, lr_at)
+    o = _lib.AdamOptions(lr, betas[0], betas[1], eps, weight_decay, max_norm or 0.0, lr_at, bool(follow))
     norm = state.step.new_empty((), dtype=torch.float32) if max_norm is not None else None
     workspace, nbytes = _scratch(workspace, state.step, int(_lib.lib().o1d_adamw_workspace_bytes(max_norm or 0.0)))
     _run("o1d_adamw", state.step, ctypes.addressof(table), count, _DT[pdt] if pdt else 0, _DT[gdt] if gdt else 0,

@@ -16,7 +16,8 @@ from . import ops
 
 class AdamW:
     """params: tensors, or dicts {"params": tensors} with an lr, betas, eps or weight_decay of their own.  master: keep the
-    parameters in float32 beside them (None: those in bfloat16).  max_norm is of all gradients together, and is for parameters of one
+    parameters in float32 beside them (None: those in bfloat16); a parameter that was written since the last step (a loaded
+    checkpoint) is no longer its master rounded, and goes on from what was written.  max_norm is of all gradients together, and is for parameters of one
     set and type."""
 
     def __init__(self, params, lr: float | torch.Tensor = 1e-3, betas: tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
@@ -50,7 +51,7 @@ class AdamW:
         norm = None
         for g in self.groups:
             norm = ops.adamw(g["params"], [None if p.grad is None else p.grad.contiguous() for p in g["params"]], g["state"], g["lr"], g["betas"], g["eps"],
-                             g["weight_decay"], self.max_norm)
+                             g["weight_decay"], self.max_norm, follow=True)
         return norm
 
     def zero_grad(self) -> None:
@@ -69,7 +70,8 @@ class AdamW:
                             "state": {n: getattr(g["state"], n) for n in names}} for g in self.groups]}
 
     def load_state_dict(self, held: dict) -> None:
-        """Takes over copies of the states, which have to be of these parameters' sizes, and the options."""
+        """Takes over copies of the states, which have to be of these parameters' sizes, and the options.  The parameters are loaded by
+        themselves, before or after: those that are not their masters rounded go on from their own values."""
         if len(held["groups"]) != len(self.groups):
             raise ValueError(f"{len(held['groups'])} sets of states for {len(self.groups)} of parameters")
         made = []

@@ -47,3 +47,103 @@ def test_inference_tensors_have_no_version():
         was = p.clone()
         ops.adamw([p], [g], state, lr=1e-2, weight_decay=0.0, **kw)
         assert bool(((was - p - 1e-2 * g.sign()).abs() <= 1e-5).all())
+
+
+# ---- parameters that were written since the last step
+
+def steps_of(opt, seed):
+    for g in opt.groups:
+        for i, p in enumerate(g["params"]):
+            p.grad = randn(p.numel(), seed=seed + i, dt=p.dtype).view(p.shape)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_written_parameters_go_on_from_what_was_written(bits):
+    sizes = [(33, 7), (4100,), (1,), (130,)]
+    ps = [torch.nn.Parameter(randn(*s, seed=i, dt=BF16)) for i, s in enumerate(sizes)]
+    opt = optim.AdamW(ps, lr=1e-2, bits=bits)
+    state = opt.groups[0]["state"]
+    for k in range(3):
+        steps_of(opt, 10 + 5 * k)
+        opt.step()
+    opt.groups[0].update(lr=0.0, weight_decay=0.0)  # (a step changes nothing by itself)
+    kept = state.master.clone()
+    opt.step()
+    assert torch.equal(state.master, kept)  # the masters' bits below bfloat16 stay
+    assert any(not torch.equal(kept[at:at + n], p.detach().float().view(-1)) for p, n, at in zip(ps, state.sizes, state.starts))
+    new = [randn(p.numel(), seed=40 + i, dt=BF16).view(p.shape) for i, p in enumerate(ps)]
+    with torch.no_grad():
+        ps[0].copy_(new[0])
+        ps[1][7:9].copy_(new[1][7:9])
+    ps[2].data.copy_(new[2])  # (autograd's versions know nothing of this one)
+    now = [p.detach().clone() for p in ps]
+    opt.step()
+    for i, (p, n, at) in enumerate(zip(ps, state.sizes, state.starts)):
+        assert torch.equal(p, now[i])
+        changed = now[i].view(-1) != kept[at:at + n].to(BF16)
+        want = torch.where(changed, now[i].float().view(-1), kept[at:at + n])
+        assert torch.equal(state.master[at:at + n], want)
+
+
+def test_a_loaded_model_is_trained_on():
+    # a checkpoint of the parameters alone, loaded into a block that has made steps
+    runs = []
+    for seed in (1, 2):
+        torch.manual_seed(seed)
+        block = OrientedBlock8(24, 3, groups=4).to(DEV).to(BF16)
+        runs.append((block, optim.AdamW(block.parameters(), lr=1e-3, weight_decay=0.0)))
+    x = randn(2, 6, 5, 24, seed=3, dt=BF16)
+    (block, opt), (other, _) = runs
+    for _ in range(2):
+        opt.zero_grad()
+        block(x).float().square().mean().backward()
+        opt.step()
+    block.load_state_dict(other.state_dict())
+    opt.zero_grad()
+    block(x).float().square().mean().backward()
+    opt.step()
+    for a, b in zip(block.parameters(), other.parameters()):
+        # (after three gradients m is a mean of them and v nearly one of their squares: a step is at most sqrt(3) times the rate)
+        assert bool(((a.float() - b.float()).abs() <= 2e-3 + 2.0 ** -8 * b.float().abs()).all())
+
+
+def test_parameters_written_between_replays():
+    ps = [torch.nn.Parameter(randn(300, seed=1, dt=BF16))]
+    opt = optim.AdamW(ps, lr=1e-2, bits=8)
+    ps[0].grad = randn(300, seed=2, dt=BF16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        opt.step()
+    torch.cuda.current_stream().wait_stream(side)
+    opt.groups[0].update(lr=0.0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step()
+    for k in range(3):
+        new = randn(300, seed=10 + k, dt=BF16)
+        with torch.no_grad():
+            ps[0].copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(ps[0], new) and torch.equal(opt.groups[0]["state"].master[:300], new.float())
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("dt,gdt", [(BF16, BF16), (BF16, F32), (F32, F32), (F32, BF16)])
+def test_following_changes_nothing_where_nobody_wrote(dt, gdt, bits):
+    runs = [[randn(n, seed=n, dt=dt) for n in (1, 127, 129, 5000)] for _ in range(3)]
+    states = [ops.AdamState.zeros(ps, bits=bits, master=True) for ps in runs]
+    ws = torch.empty(512, dtype=torch.uint8, device=DEV)
+    for k in range(4):
+        gs = [randn(p.numel(), seed=20 * k + i, dt=gdt) for i, p in enumerate(runs[0])]
+        for ps, state, kw in zip(runs, states, ({}, {"follow": True}, {"follow": True, "workspace": ws})):
+            ops.adamw(ps, gs, state, lr=1e-2, **kw)
+    for ps, state in zip(runs[1:], states[1:]):
+        for a, b in zip((*runs[0], states[0].master, states[0].m.view(torch.uint8)), (*ps, state.master, state.m.view(torch.uint8))):
+            assert torch.equal(a, b)
+    # one that does not follow keeps to its masters, as it says
+    held = states[0].master[:1].clone()
+    runs[0][0].fill_(7.0)
+    ops.adamw(runs[0], gs, states[0], lr=0.0, weight_decay=0.0)
+    assert torch.equal(runs[0][0], held.to(dt)) and torch.equal(states[0].master[:1], held)
