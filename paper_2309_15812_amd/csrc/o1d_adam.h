@@ -32,6 +32,17 @@ struct AdamHyper {
   bool follow;            // with masters: parameters that were written since are read
 };
 
+// The count of steps that a call finds in device memory, where no check of the host's sees it: one that no
+// call has left is read as the nearest that one may have.
+__host__ __device__ inline int steps_taken(int found) { return found < 0 ? 0 : (found < 0x7ffffffe ? found : 0x7ffffffe); }
+// b^t for t >= 0, by squaring: at most 31 times whatever t is.
+__host__ __device__ inline double power(double b, int t) {
+  double r = 1.;
+  for (uint32_t k = (uint32_t)t; k; k >>= 1, b *= b)
+    if (k & 1) r *= b;
+  return r;
+}
+
 constexpr int kAdamMost = 112;  // tensors of a launch (what its arguments hold)
 // Tensors 0 .. count - 1 of a call; the call's last launch counts the step.
 hipError_t launch_adam(Dtype pdt, Dtype gdt, const AdamTensor* t, int count, const AdamState& s, const AdamHyper& h,

@@ -93,14 +93,6 @@ __device__ __forceinline__ void store8(T* p, long long left, const float (&v)[kA
   }
 }
 
-// b^t for whole t, by squaring.
-__device__ __forceinline__ double power(double b, int t) {
-  double r = 1.;
-  for (; t; t >>= 1, b *= b)
-    if (t & 1) r *= b;
-  return r;
-}
-
 // Eight e4m3 values times their scale, and back: the scale is the largest of 16 lanes' values / 448.
 __device__ __forceinline__ void from8(uint2 w, float scale, float (&v)[kAdamRun]) {
 #pragma unroll
@@ -194,7 +186,7 @@ __global__ __launch_bounds__(kAdamThreads) void adam(AdamList L, AdamState S, Ad
   Place q = place();
   load(q);
   if (threadIdx.x == 0) {
-    const int t = S.step[0] + 1;
+    const int t = steps_taken(S.step[0]) + 1;
     Coefs c;
     c.factor = 1.f;
     c.go = 1;
@@ -249,7 +241,7 @@ __global__ __launch_bounds__(kAdamThreads) void adam(AdamList L, AdamState S, Ad
   if (counts && threadIdx.x == 0) {
     if (atomicAdd(&S.step[1], 1) == (int)gridDim.x - 1) {
       S.step[1] = 0;
-      if (c.go) S.step[0] += 1;
+      if (c.go) S.step[0] = steps_taken(S.step[0]) + 1;
     }
   }
 }

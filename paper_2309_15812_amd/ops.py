@@ -1047,7 +1047,8 @@ class F8LinearFunction(torch.autograd.Function):
 class AdamState:
     """The states of AdamW for tensors of `sizes` values, flat: tensor i's part starts at `starts[i]`, the sum of the sizes
     before it, each rounded up to 128.  m and v are float32, or float8_e4m3fn (v its root) with float32 scales ms and vs for
-    each 128 values; master (or None) the parameters in float32; step int32 (2,), the steps taken and 0."""
+    each 128 values; master (or None) the parameters in float32; step int32 (2,), the steps taken and 0 (a negative count is
+    read as none)."""
 
     __slots__ = ("sizes", "starts", "m", "v", "step", "ms", "vs", "master")
 

@@ -79,6 +79,9 @@ class AdamW:
             device, t = g["state"].m.device, new["state"]
             if list(t["sizes"]) != g["state"].sizes or (t["master"] is None) != (g["state"].master is None):
                 raise ValueError(f"the states are of other parameters: {t['sizes']}")
+            steps = t["step"].tolist()
+            if len(steps) != 2 or steps[0] < 0 or steps[1] != 0:
+                raise ValueError(f"step must be the steps taken and 0, got {steps}")
             made.append(ops.AdamState(t["sizes"], *(None if t[n] is None else t[n].detach().to(device, copy=True)
                                                     for n in ("m", "v", "step", "ms", "vs", "master"))))
         for g, new, state in zip(self.groups, held["groups"], made):

@@ -147,3 +147,14 @@ def test_following_changes_nothing_where_nobody_wrote(dt, gdt, bits):
     runs[0][0].fill_(7.0)
     ops.adamw(runs[0], gs, states[0], lr=0.0, weight_decay=0.0)
     assert torch.equal(runs[0][0], held.to(dt)) and torch.equal(states[0].master[:1], held)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_negative_count_is_read_as_none(bits):
+    runs = [[randn(300, seed=1)] for _ in range(2)]
+    states = [ops.AdamState.zeros(ps, bits=bits) for ps in runs]
+    states[1].step[0] = -3
+    for _ in range(2):
+        for ps, state in zip(runs, states):
+            ops.adamw(ps, [randn(300, seed=2)], state, lr=1e-2, max_norm=1.0)
+    assert torch.equal(runs[0][0], runs[1][0]) and states[1].step.tolist() == states[0].step.tolist() == [2, 0]
