@@ -1016,6 +1016,7 @@ class F8LinearFunction(torch.autograd.Function):
                             None if residual is None else residual.reshape(-1, w.shape[0]).contiguous(), save, x.dtype)
         y, pre = (out, None) if save is None else out
         ctx.act, ctx.grad, ctx.bias, ctx.shape, ctx.dtype = act, grad, b is not None and wants[2], x.shape, x.dtype
+        ctx.dtype_w = w.dtype  # (a float32 weight's gradient is not rounded to the input's type)
         ctx.residual = None if residual is None else residual.shape
         ctx.cols = (x.numel() // x.shape[-1], w.shape)
         ctx.save_for_backward(pre, *(k for t in (xt, wt) for k in ((t.q, t.e) if t is not None else (None, None))))
@@ -1034,11 +1035,11 @@ class F8LinearFunction(torch.autograd.Function):
             gx = f8_linear_bwd_input(pack_f8(dh, ctx.grad), F8.of(wq, we, O), dtype=ctx.dtype).view(ctx.shape)
         if wants[1] or ctx.bias:
             if M == 0:
-                gw, gb = (dh.new_zeros((O, I)) if wants[1] else None), (dh.new_zeros((O,)) if ctx.bias else None)
+                gw, gb = (dh.new_zeros((O, I), dtype=ctx.dtype_w) if wants[1] else None), (dh.new_zeros((O,)) if ctx.bias else None)
             else:
                 dyt, gb = pack_f8(dh, ctx.grad, along="rows", sums=True)
                 gb = gb if ctx.bias else None
-                gw = f8_linear_bwd_weight(dyt, F8.of(xq, xe, M), dtype=ctx.dtype) if wants[1] else None
+                gw = f8_linear_bwd_weight(dyt, F8.of(xq, xe, M), dtype=ctx.dtype_w) if wants[1] else None
         return gx, gw, gb, None, (gy.reshape(ctx.residual) if wants[4] else None), None
 
 

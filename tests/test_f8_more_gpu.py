@@ -1,0 +1,28 @@
+"""Products of 8-bit operands: weights of another type than the input, calls with odd arguments.  Bounds as in test_f8_gpu.py."""
+import math
+
+import pytest
+import torch
+
+from paper_2309_15812_amd import ops
+from test_f8_gpu import E, value
+from test_rows_gpu import ACTS, BF16, DEV, DTYPES, F32, near, randn, u
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_a_float32_weight_of_bfloat16_inputs_keeps_its_gradient(act):
+    x, w = randn(150, 70, seed=1, dt=BF16), randn(45, 70, seed=2, std=0.1).requires_grad_(True)
+    dy = randn(150, 45, seed=3, dt=BF16)
+    ops.F8LinearFunction.apply(x, w, None, act).backward(dy)
+    assert w.grad.dtype is F32
+    pre = ops.f8_linear_fwd(ops.pack_f8(x), ops.pack_f8(w.detach()), act=act, save="pre")[1]
+    dh = dy if act == "none" else ops.act_bwd(pre, dy, act)
+    D, X = value(ops.pack_f8(dh, "e5m2", along="rows")), value(ops.pack_f8(x, along="rows"))
+    want, mag = D @ X.t(), D.abs() @ X.abs().t()
+    e = (150 + 16) * E * mag
+    near(w.grad, want, e + u(F32) * (want.abs() + e), "dw")
+    w.grad = None
+    ops.F8LinearFunction.apply(x[:0], w).sum().backward()
+    assert w.grad.dtype is F32 and not w.grad.any()
