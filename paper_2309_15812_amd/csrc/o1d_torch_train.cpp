@@ -25,6 +25,13 @@ decltype(&o1d_adamw_workspace_bytes) p_adamw_bytes;
 constexpr int64_t kGroup = 128;
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
+// A whole number, or -1 where it is none of C's: the checked path says what is wrong.
+long number(PyObject* o) {
+  const long k = PyLong_AsLong(o);
+  if (k == -1) PyErr_Clear();
+  return k;
+}
+
 // Samples of rows: (N, ..., C).
 bool samples_of(PyObject* o, Rows& r, int& N, int& P) {
   if (!rows_of(o, r) || r.t->dim() < 2 || r.t->size(0) > INT32_MAX) return false;
@@ -40,7 +47,7 @@ PyObject* gn_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int N, P;
   if (n != 6 || !samples_of(a[0], x, N, P)) return none();
   const at::Tensor *w = vector(a[1], x, x.C), *b = vector(a[2], x, x.C);
-  const long G = PyLong_AsLong(a[3]), act = PyLong_AsLong(a[5]);
+  const long G = number(a[3]), act = number(a[5]);
   const double eps = PyFloat_Check(a[4]) ? PyFloat_AS_DOUBLE(a[4]) : -1.;
   if (!w || !b || G < 1 || G > x.C || x.C % G || eps < 0.) return none();
   at::Tensor y = empty_rows(x, x.C), mean = empty({N, G}, *x.t, at::kFloat), rstd = empty({N, G}, *x.t, at::kFloat);
@@ -99,7 +106,7 @@ struct Packed {
 bool packed_of(PyObject* q, PyObject* e, PyObject* cols, Packed& p) {
   p.q = tensor(q);
   p.e = tensor(e);
-  const long K = PyLong_AsLong(cols);
+  const long K = number(cols);
   if (!p.q || !p.e || K < 1 || K > INT32_MAX || !p.q->is_cuda() || p.q->dim() != 2 || p.q->size(0) < 1 ||
       p.q->size(0) > INT32_MAX)
     return false;

@@ -823,6 +823,7 @@ class F8:
     __slots__ = ("q", "e", "cols")
 
     def __init__(self, q: torch.Tensor, e: torch.Tensor, cols: int):
+        cols = operator.index(cols)
         groups = -(-cols // _lib.SCALED_GROUP)
         if cols < 1 or q.dim() != 2 or q.dtype not in _F8_OF or q.shape[1] != groups * _lib.SCALED_GROUP \
                 or not q.is_contiguous():

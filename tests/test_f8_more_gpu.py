@@ -26,3 +26,18 @@ def test_a_float32_weight_of_bfloat16_inputs_keeps_its_gradient(act):
     w.grad = None
     ops.F8LinearFunction.apply(x[:0], w).sum().backward()
     assert w.grad.dtype is F32 and not w.grad.any()
+
+
+def test_numbers_that_are_none_of_cs():
+    x, w = randn(2, 9, 24, seed=10), randn(24, seed=11)
+    for groups in (2 ** 31, 2 ** 40, 2 ** 63, 2 ** 70, -2 ** 70):
+        with pytest.raises(ValueError):
+            ops.gn_fwd(x, w, w, groups)
+    p = ops.pack_f8(randn(6, 40, seed=12))
+    for cols in (40.0, "40", None):
+        with pytest.raises(TypeError):
+            ops.F8(p.q, p.e, cols)
+    for cols in (2 ** 40, 2 ** 70, 0, -40):
+        with pytest.raises(ValueError):
+            ops.F8(p.q, p.e, cols)
+    assert torch.equal(ops.f8_linear_fwd(ops.F8(p.q, p.e, torch.tensor(40)), p), ops.f8_linear_fwd(p, p))
