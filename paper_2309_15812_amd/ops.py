@@ -883,7 +883,7 @@ def pack_f8(x: torch.Tensor, fmt: str = "e4m3", along: str = "features", sums: b
     if sums and along == "features":
         raise ValueError("sums come with along='rows' or 'both'")
     if workspace is None:
-        made = _train().pack(x, _lib.SCALED[fmt], _ALONG[along], sums)
+        made = _train().pack(x, _lib.SCALED[fmt], _ALONG[along], bool(sums))
         if made is not None:
             C = x.shape[-1]
             if along == "features":

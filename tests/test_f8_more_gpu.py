@@ -41,3 +41,15 @@ def test_numbers_that_are_none_of_cs():
         with pytest.raises(ValueError):
             ops.F8(p.q, p.e, cols)
     assert torch.equal(ops.f8_linear_fwd(ops.F8(p.q, p.e, torch.tensor(40)), p), ops.f8_linear_fwd(p, p))
+
+
+def test_sums_asked_for_by_any_true_value():
+    x = randn(200, 40, seed=13)
+    for along, parts in (("rows", 2), ("both", 3)):
+        want = ops.pack_f8(x, along=along, sums=True)
+        for sums in (1, "yes", torch.tensor(True)):
+            got = ops.pack_f8(x, along=along, sums=sums)
+            assert len(got) == parts and torch.equal(got[-1], want[-1])
+        for sums in (0, None, torch.tensor(False)):
+            got = ops.pack_f8(x, along=along, sums=sums)
+            assert isinstance(got, ops.F8) if along == "rows" else len(got) == 2
