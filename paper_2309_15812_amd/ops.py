@@ -858,7 +858,10 @@ class F8:
 
     def float(self) -> torch.Tensor:
         """What it stands for, in float32 (by torch: for looking at, not for computing with)."""
-        scale = torch.exp2(self.e[:, :self.rows].float() - 127).t().repeat_interleave(_lib.SCALED_GROUP, 1)
+        e = self.e[:, :self.rows].to(torch.int32)
+        # (a float32's exponent field is the same number; 0 stands for 2^-127, which has a fraction's bit instead, 255 for NaN)
+        bits = torch.where(e == 0, 1 << 22, torch.where(e == 255, 0x7fc00000, e << 23))
+        scale = bits.to(torch.int32).view(torch.float32).t().repeat_interleave(_lib.SCALED_GROUP, 1)
         return (self.q.float() * scale)[:, :self.cols]
 
 

@@ -53,3 +53,19 @@ def test_sums_asked_for_by_any_true_value():
         for sums in (0, None, torch.tensor(False)):
             got = ops.pack_f8(x, along=along, sums=sums)
             assert isinstance(got, ops.F8) if along == "rows" else len(got) == 2
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_what_an_operand_stands_for(fmt):
+    # every exponent, 0 and 255 among them
+    p = ops.pack_f8(randn(256, 200, seed=14), fmt)
+    p.e[0], p.e[1] = torch.arange(256, device=DEV), torch.arange(255, -1, -1, device=DEV)
+    q = p.q[:, :200].double()
+    scale = (2.0 ** (p.e[:, :256].double() - 127)).t().repeat_interleave(128, 1)[:, :200]
+    want = torch.where(p.e[:, :256].t().repeat_interleave(128, 1)[:, :200] == 255, math.nan, q * scale)
+    near(p.float(), want.float().double(), 0 * want.nan_to_num(0), fmt)  # (powers of two: rounded only below 2^-126)
+    y = ops.f8_linear_fwd(p, ops.pack_f8(randn(9, 200, seed=15)), dtype=F32)
+    top = p.e[:, :256].amax(0)
+    assert torch.isnan(y[top == 255]).all()
+    # (200 products of at most 57344 and 8 times 2^(228 - 127) stay in float32; larger scales may leave it)
+    assert torch.isfinite(y[top <= 228]).all()
