@@ -22,6 +22,8 @@ class AdamW:
 
     def __init__(self, params, lr: float | torch.Tensor = 1e-3, betas: tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 0.01, bits: int = 32, master: bool | None = None, max_norm: float | None = None):
+        if isinstance(params, torch.Tensor):
+            raise TypeError("params are tensors or dicts of them, not one tensor (whose rows would be taken)")
         params = list(params)
         sets = params if params and isinstance(params[0], dict) else [{"params": params}]
         defaults = {"lr": lr, "betas": betas, "eps": eps, "weight_decay": weight_decay}
@@ -31,7 +33,9 @@ class AdamW:
             if unknown:
                 raise ValueError(f"unknown options {sorted(unknown)}")
             kinds: dict = {}
-            for p in given["params"]:
+            for p in [given["params"]] if isinstance(given["params"], torch.Tensor) else given["params"]:
+                if not isinstance(p, torch.Tensor) or not p.is_leaf:  # (no gradient arrives at a tensor that was computed)
+                    raise ValueError(f"parameters must be leaf tensors, got {type(p).__name__}")
                 if id(p) in seen:
                     raise ValueError("a parameter is given twice")
                 seen.add(id(p))

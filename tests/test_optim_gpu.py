@@ -158,3 +158,13 @@ def test_a_negative_count_is_read_as_none(bits):
         for ps, state in zip(runs, states):
             ops.adamw(ps, [randn(300, seed=2)], state, lr=1e-2, max_norm=1.0)
     assert torch.equal(runs[0][0], runs[1][0]) and states[1].step.tolist() == states[0].step.tolist() == [2, 0]
+
+
+def test_a_set_of_one_tensor_is_that_tensor():
+    p = torch.nn.Parameter(randn(5, 30, seed=1))
+    p.grad = randn(5, 30, seed=2)
+    was = p.detach().clone()
+    opt = optim.AdamW([{"params": p, "lr": 0.25, "weight_decay": 0.0}])
+    opt.step()
+    assert len(opt.groups[0]["params"]) == 1 and opt.groups[0]["params"][0] is p
+    assert bool(((was - p - 0.25 * p.grad.sign()).abs() <= 1e-5 + 0.25 * 1e-8 / p.grad.abs()).all())

@@ -54,3 +54,12 @@ def test_counts_that_no_step_left_are_not_loaded(steps):
     with pytest.raises(ValueError, match="step must be"):
         opt.load_state_dict({"groups": [{"lr": 0.2, "state": held}]})
     assert opt.groups[0]["lr"] == 0.1
+
+
+def test_parameters_that_no_gradient_reaches():
+    p = torch.nn.Parameter(torch.zeros(3, 4))
+    with pytest.raises(TypeError):
+        optim.AdamW(p)
+    for bad in ([p * 2], [p[0]], list(p), [{"params": [p.t()]}], ["p"], [{"params": "p"}]):
+        with pytest.raises(ValueError, match="leaf"):
+            optim.AdamW(bad)
