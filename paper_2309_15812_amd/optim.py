@@ -73,8 +73,10 @@ class AdamW:
         return {"groups": [{**{k: v for k, v in g.items() if k not in ("params", "state")},
                             "state": {n: getattr(g["state"], n) for n in names}} for g in self.groups]}
 
+    @torch.no_grad()
     def load_state_dict(self, held: dict) -> None:
-        """Takes over copies of the states, which have to be of these parameters' sizes, and the options.  The parameters are loaded by
+        """Takes over copies of the states, which have to be of these parameters' sizes, and the options, where a captured step finds
+        them (but states of other bits, which need a new capture).  The parameters are loaded by
         themselves, before or after: those that are not their masters rounded go on from their own values."""
         if len(held["groups"]) != len(self.groups):
             raise ValueError(f"{len(held['groups'])} sets of states for {len(self.groups)} of parameters")
@@ -88,5 +90,16 @@ class AdamW:
                 raise ValueError(f"step must be the steps taken and 0, got {steps}")
             made.append(ops.AdamState(t["sizes"], *(None if t[n] is None else t[n].detach().to(device, copy=True)
                                                     for n in ("m", "v", "step", "ms", "vs", "master"))))
+        # (into the tensors that there are, where they are of this kind: a captured step reads and writes those)
         for g, new, state in zip(self.groups, held["groups"], made):
-            g.update({k: v.to(state.m.device) if isinstance(v, torch.Tensor) else v for k, v in new.items() if k != "state"}, state=state)
+            for k, v in new.items():
+                if k == "lr" and isinstance(g["lr"], torch.Tensor):
+                    g["lr"].copy_(torch.as_tensor(v, dtype=torch.float32))
+                elif k != "state":
+                    g[k] = v.detach().to(state.m.device, copy=True) if isinstance(v, torch.Tensor) else v
+            if g["state"].m.dtype is not state.m.dtype:
+                g["state"] = state
+                continue
+            for n in ("m", "v", "step", "ms", "vs", "master"):
+                if getattr(state, n) is not None:
+                    getattr(g["state"], n).copy_(getattr(state, n))

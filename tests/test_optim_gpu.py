@@ -168,3 +168,58 @@ def test_a_set_of_one_tensor_is_that_tensor():
     opt.step()
     assert len(opt.groups[0]["params"]) == 1 and opt.groups[0]["params"][0] is p
     assert bool(((was - p - 0.25 * p.grad.sign()).abs() <= 1e-5 + 0.25 * 1e-8 / p.grad.abs()).all())
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_loaded_states_reach_a_captured_step(bits):
+    def fresh(seed):
+        ps = [torch.nn.Parameter(randn(n, seed=seed + n, dt=BF16)) for n in (300, 7)]
+        for p in ps:
+            p.grad = randn(p.numel(), seed=p.numel(), dt=BF16)
+        return ps, optim.AdamW(ps, lr=torch.tensor(1e-2, device=DEV), bits=bits, max_norm=1.0)
+
+    (ps, opt), (qs, other) = fresh(1), fresh(1000)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        opt.step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step()
+    for _ in range(3):
+        other.step()
+    other.groups[0]["lr"].fill_(3e-2)
+    opt.load_state_dict(other.state_dict())
+    with torch.no_grad():
+        for p, q in zip(ps, qs):
+            p.copy_(q)
+    for k in range(3):
+        graph.replay()
+        other.step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(ps, qs))
+        assert opt.groups[0]["state"].step.tolist() == [4 + k, 0]
+        assert torch.equal(opt.groups[0]["state"].master, other.groups[0]["state"].master)
+        torch.randn(1 << 20, device=DEV).sum().item()
+    other.groups[0]["lr"].zero_()  # the two are apart
+    assert float(opt.groups[0]["lr"]) == float(torch.tensor(3e-2))
+
+
+def test_states_of_other_bits_are_taken():
+    p, q = (torch.nn.Parameter(randn(300, seed=1)) for _ in range(2))
+    a, b = optim.AdamW([p], lr=1e-2, bits=8), optim.AdamW([q], lr=torch.tensor(2e-2, device=DEV), bits=32)
+    for t, opt in ((p, a), (q, b)):
+        t.grad = randn(300, seed=2)
+        opt.step()
+    a.load_state_dict(b.state_dict())
+    assert a.groups[0]["state"].m.dtype is F32 and torch.equal(a.groups[0]["state"].v, b.groups[0]["state"].v)
+    b.groups[0]["lr"].zero_()
+    assert float(a.groups[0]["lr"]) == float(torch.tensor(2e-2))
+    with torch.no_grad():
+        p.copy_(q)
+    before = q.detach().clone()
+    a.step(), b.step()
+    assert torch.equal(q, before) and not torch.equal(p, before)
+    b.load_state_dict({"groups": [{**b.state_dict()["groups"][0], "lr": 0.5}]})
+    assert isinstance(b.groups[0]["lr"], torch.Tensor) and float(b.groups[0]["lr"]) == 0.5
