@@ -3,9 +3,10 @@ gradient's sum over the samples adds a 32nd of them one after the other, then 32
 import pytest
 import torch
 
+import test_gn_gpu as gn
 from paper_2309_15812_amd import ops
 from test_gn_gpu import E, EPS, parts, per_channel, run_forward, whole
-from test_rows_gpu import BF16, DEV, F32, near, randn, u
+from test_rows_gpu import BF16, DEV, DTYPES, F32, near, randn, u
 
 pytestmark = pytest.mark.gpu
 
@@ -69,3 +70,11 @@ def test_the_longest_sample():
         h = (v - mu) * rs * W + B
         eh = abs(W) * rs * (em + (chain + 16) * E * ((v - mu).abs() + abs(mu) + v.abs())) + 4 * E * (h.abs() + abs(B))
         near(y[0, at:at + part, 0], h, eh + u(BF16) * (h.abs() + eh), f"pixels from {at}")
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+def test_rows_wider_than_a_workgroup_in_pieces(dt):
+    N, P, C, G = 1, 9529, 1224, 51
+    for act, pad in (("none", 0), ("silu", 13)):
+        run_forward(N, P, C, G, dt, act, pad, pad % 4)
+    gn.test_backward(N, P, C, G, dt)

@@ -1,9 +1,12 @@
 """AdamW as programs use it: between forward and backward passes, after parameters were written, with states of other programs."""
+import os
+
 import pytest
 import torch
 
-from paper_2309_15812_amd import ops, optim
+from paper_2309_15812_amd import build, ops, optim
 from paper_2309_15812_amd.block import OrientedBlock, OrientedBlock8
+from test_adam_gpu import check_step, make
 from test_rows_gpu import BF16, DEV, DTYPES, F32, randn
 
 pytestmark = pytest.mark.gpu
@@ -223,3 +226,15 @@ def test_states_of_other_bits_are_taken():
     assert torch.equal(q, before) and not torch.equal(p, before)
     b.load_state_dict({"groups": [{**b.state_dict()["groups"][0], "lr": 0.5}]})
     assert isinstance(b.groups[0]["lr"], torch.Tensor) and float(b.groups[0]["lr"]) == 0.5
+
+
+@pytest.mark.parametrize("count", [111, 112, 113, 224, 225])
+def test_launches_that_are_full_and_one_more(count):
+    # a launch takes 112 tensors; the norm's later launches add to the first one's parts
+    assert "kAdamMost = 112" in open(os.path.join(build.CSRC, "o1d_adam.h")).read()
+    ps, gs, state = make([(1 + 37 * (i % 60),) for i in range(count)], F32, F32, 8, False)
+    check_step(ps, gs, state, max_norm=1.0)
+    check_step(ps, gs, state, max_norm=1e6)
+    ps, gs, state = make([(1 + 37 * (i % 60),) for i in range(count)], BF16, F32, 32, True)
+    gs[0] = gs[count // 2] = None
+    check_step(ps, gs, state, max_norm=1.0)
