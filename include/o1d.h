@@ -353,11 +353,11 @@ size_t o1d_scaled_linear_bwd_weight_workspace_bytes(int M, int I, int O, o1d_dty
  * m_scale, v_scale for each 128 values: the largest / 448, at least 2^-126, or 0 for zeros.  master (or NULL): the parameters in float32, from which p is rounded;
  * without it p itself is read.  follow (not 0, with master): where p is not its master rounded, it was written since the
  * last step, and its value is taken for the master's.  The states are 16-byte aligned.
- * step: two device integers, the steps taken (read and counted up) and 0.  lr_at: the learning rate in device memory, or NULL for
+ * step: two device integers, the steps taken (read and counted up; below 0: read as 0) and 0.  lr_at: the learning rate in device memory, or NULL for
  * lr.  max_norm > 0 limits the norm of all gradients to it; the norm is then written to `norm`, and where it is not finite
  * nothing else changes.  max_norm 0: no limit, norm is not written and may be NULL.
- * Without max_norm a value that is not finite makes its parameter and states NaN, 8-bit ones with the 128 values of its scale.  A
- * call without values counts no step.  Tensors that are written overlap no other one; gradients may be shared. */
+ * Without max_norm a gradient that is not finite makes its parameter NaN and its states NaN or infinite, 8-bit ones with all 128
+ * values of their scale.  A call without values counts no step.  Tensors that are written overlap no other one; gradients may be shared. */
 typedef struct {
   void* p;
   const void* g;

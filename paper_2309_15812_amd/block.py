@@ -16,7 +16,8 @@ bfloat16 and 40 in float32.
     y = block(x)                                  # x: (N, H, W, 96)
 
 OrientedBlock8 is that block with group norm in the place of layer norm and its two products of 8-bit floating point operands,
-which are also what it keeps for the weights' gradients.
+which are also what it keeps for the weights' gradients.  (At the widths of the paper's network it is slower than OrientedBlock, and
+keeps more than its checkpoints do: 64 x 56 x 56 x 96 a step of 1135 us and 15.1 bytes, against 814 and 20.2, with checkpoints 885 and 6.5.)
 
 `python -m paper_2309_15812_amd.block` fits a small one to a target on the GPU: with and without checkpoints, and one
 in 8 bits with the library's AdamW.

@@ -13,11 +13,11 @@
 // how a compiler joins them.
 //
 // Memory bounds it: 28 bytes per value in float32, 16.1 (bfloat16 parameters and gradients, their
-// float32 values, 8-bit states).  A thread has eight values, 16 threads a scale; a workgroup
+// float32 values, 8-bit states; 18.1 where the parameters are read beside those).  A thread has eight values, 16 threads a scale; a workgroup
 // finds the tensor of each piece of 2048 values among those in its arguments.
 //
-// Measured, the parameters of 15 blocks (11.8 million values in 105 tensors): float32 66 us, 5.1 TB/s, and 19 us for the norm; in
-// bfloat16 with 8-bit states 47 us, 4.6 TB/s.
+// Measured, the parameters of 15 blocks (11.9 million values in 105 tensors): float32 66 us, 5.1 TB/s, and 19 us for the norm; in
+// bfloat16 with 8-bit states 47 us, 4.1 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

@@ -15,7 +15,7 @@ o1d_status_t check_packed(const char* fn, const char* what, const unsigned char*
   return O1D_OK;
 }
 
-// Rows that a weight gradient sums: the offsets of a tile's 256 rows stay below 2^31 bytes.
+// Rows that a weight gradient sums: the offsets of a tile's 128 rows stay below 2^31 bytes.
 constexpr int kMostSummed = 8 * (int)kMaxStride - 1024;
 
 size_t q_bytes(int R, int K) { return (size_t)R * (size_t)rows::f8_ld(K); }

@@ -22,8 +22,9 @@ GnPlan plan_gn(bool backward, int N, int P, int C, int G, int esize) {
       const long long rows = threads / run, need = cdiv(P, rows);
       const int runs = need <= 2 ? 2 : (int)cdiv(need, 2) * 2;
       if (!gn_takes(backward, esize, threads, runs)) continue;
-      // time in us: what a CU moves, at the rate that it has among the others, and the two reductions, which small workgroups
-      // on a CU have at the same time (65536 samples of 1 x 64 bfloat16 in workgroups of 64 threads 125 us, in two passes 580);
+      // A measure of time that orders the held plans, and them against two passes; as a time it is short, by half for one large
+      // workgroup per CU (64 x 3136 x 96 bfloat16 13.5 of 25 us, two passes 18.3): what a CU moves, at the rate that it has among the
+      // others, and the two reductions, which small workgroups on a CU have at the same time (65536 samples of 1 x 64 bfloat16 in workgroups of 64 threads 125 us, in two passes 580);
       // rows of fewer channels than a run are loaded one by one (6 x 183 x 7 bfloat16 in two runs 7 us, in four 10)
       const double bytes = (double)P * CB * esize, piece = CB * esize;
       const long long groups = (long long)N * real, rounds = cdiv(groups, 256);

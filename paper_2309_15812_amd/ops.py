@@ -918,7 +918,8 @@ def pack_f8(x: torch.Tensor, fmt: str = "e4m3", along: str = "features", sums: b
 def f8_linear_fwd(x: F8, w: F8, b: torch.Tensor | None = None, act: str = "none", residual: torch.Tensor | None = None,
                   save: str | None = None, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None):
     """y = act(x w^T + b) + residual of packed x (M, I) and w (O, I), in dtype.  save="pre" returns (y, pre) with the
-    pre-activation."""
+    pre-activation.  In bfloat16 eight products are summed at a time with 13 bits behind the largest's power of two, and those sums
+    in float32; in float32 all sums are, which takes up to twice as long.  (So have the gradients'.)"""
     if save not in (None, "pre"):
         raise ValueError(f"save must be None or 'pre', got {save!r}")
     if dtype not in _DT:

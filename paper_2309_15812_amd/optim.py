@@ -1,11 +1,15 @@
-"""AdamW over all tensors of a model in one or two launches, with states in 32 or 8 bits.
+"""AdamW over all tensors of a model, 112 of them in a launch (in two with max_norm), with states in 32 or 8 bits.
 
     opt = AdamW(block.parameters(), lr=1e-3, bits=8, max_norm=1.0)
     loss.backward()
     opt.step()
 
-The arithmetic is ops.adamw's (include/o1d.h, o1d_adamw): decoupled weight decay, steps counted in device memory, and with max_norm
-the gradients limited to that norm; a step whose norm is not finite changes nothing.
+The arithmetic is ops.adamw's (include/o1d.h, o1d_adamw): decoupled weight decay, steps counted in device memory, one count
+for all tensors of a set and type (one that had no gradient for a while is corrected as the others are), and with max_norm the gradients limited to
+that norm; a step whose norm is not finite changes nothing.
+
+It is no torch.optim.Optimizer: its sets are in `groups`, and a learning rate that changes is a float32 tensor on the GPU or is
+written there.
 """
 from __future__ import annotations
 
