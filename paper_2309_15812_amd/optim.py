@@ -89,6 +89,8 @@ class AdamW:
             device, t = g["state"].m.device, new["state"]
             if list(t["sizes"]) != g["state"].sizes or (t["master"] is None) != (g["state"].master is None):
                 raise ValueError(f"the states are of other parameters: {t['sizes']}")
+            if isinstance(new.get("lr"), torch.Tensor) and new["lr"].numel() != 1:
+                raise ValueError(f"lr must be one value, got {tuple(new['lr'].shape)}")
             steps = t["step"].tolist()
             if len(steps) != 2 or steps[0] < 0 or steps[1] != 0:
                 raise ValueError(f"step must be the steps taken and 0, got {steps}")
@@ -98,7 +100,7 @@ class AdamW:
         for g, new, state in zip(self.groups, held["groups"], made):
             for k, v in new.items():
                 if k == "lr" and isinstance(g["lr"], torch.Tensor):
-                    g["lr"].copy_(torch.as_tensor(v, dtype=torch.float32))
+                    g["lr"].copy_(torch.as_tensor(v, dtype=torch.float32).reshape(g["lr"].shape))
                 elif k != "state":
                     g[k] = v.detach().to(state.m.device, copy=True) if isinstance(v, torch.Tensor) else v
             if g["state"].m.dtype is not state.m.dtype:

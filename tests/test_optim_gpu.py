@@ -238,3 +238,19 @@ def test_launches_that_are_full_and_one_more(count):
     ps, gs, state = make([(1 + 37 * (i % 60),) for i in range(count)], BF16, F32, 32, True)
     gs[0] = gs[count // 2] = None
     check_step(ps, gs, state, max_norm=1.0)
+
+
+@pytest.mark.parametrize("ours,theirs", [((), (1,)), ((1,), ()), ((1, 1), (1,))])
+def test_loaded_rates_of_other_shapes(ours, theirs):
+    opts = []
+    for shape, rate in ((ours, 0.1), (theirs, 0.3)):
+        p = torch.nn.Parameter(randn(10, seed=1))
+        opts.append(optim.AdamW([p], lr=torch.full(shape, rate, device=DEV)))
+    kept = opts[0].groups[0]["lr"]
+    opts[0].load_state_dict(opts[1].state_dict())
+    assert opts[0].groups[0]["lr"] is kept and float(kept) == float(torch.tensor(0.3))
+    held = opts[1].state_dict()
+    held["groups"][0]["lr"] = torch.zeros(2, device=DEV)
+    with pytest.raises(ValueError):
+        opts[0].load_state_dict(held)
+    assert float(kept) == float(torch.tensor(0.3))
